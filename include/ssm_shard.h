@@ -61,6 +61,7 @@ extern "C" {
 /* Bits of the workspace status word, set by kernels that met bad device metadata. */
 #define SSM_STATUS_BAD_SLOT 1
 #define SSM_STATUS_BAD_SEQLENS 2
+#define SSM_STATUS_BAD_PAGE 4
 
 /* Storage dtype of activations and act-typed weights. */
 typedef enum ssm_dtype { SSM_F32 = 0, SSM_BF16 = 1 } ssm_dtype_t;
@@ -402,6 +403,116 @@ int ssm_stack_decode_step(const ssm_stack_desc_t* desc, const ssm_shard_weights_
                           const float* const* norm_w, const float* final_norm_w, const void* x_t, int32_t batch,
                           const int32_t* cache_slot, void* const* conv_pools, float* const* ssm_pools,
                           int32_t num_slots, void* out, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------- paged attention cache and attention
+ * Section II-A and Section IV-E: a hybrid stack interleaves the mixers with attention layers,
+ * which tensor parallelism splits by heads: a rank owns q_heads query heads and the kv_heads
+ * key/value heads they read (query head h reads kv head h / (q_heads / kv_heads)), between a
+ * column-split [q | k | v] projection and a row-split output projection (ssm_gemm_nt and the
+ * residual-boundary exchange, as for the mixer). These operators are what lies between the two.
+ *
+ * Cache: the keys and values of a sequence's tokens, in pages of page_size tokens that the
+ * sequence's row of a page table names in order, so sequences of any length share one pool and
+ * may share pages that none of them writes any more. k and v are [num_pages][kv_heads][page_size]
+ * [head_dim]; kv_format SSM_KV_ACT holds the activation type, the 8-bit formats hold codes with
+ * one float32 scale per token and head (k_scale, v_scale [num_pages][kv_heads][page_size]):
+ *   SSM_KV_FP8_E4M3: OCP FP8 E4M3 of x * (448 / max|row|), scale max|row| / 448;
+ *   SSM_KV_INT8: round-half-even of x * (127 / max|row|), scale max|row| / 127,
+ * over a row of head_dim values (rows whose largest magnitude is below 1e-30 are stored as zeros;
+ * values must be finite). A pool may be larger than 4 GiB.
+ *
+ * Requirements: kv_heads divides q_heads, q_heads at most 128; head_dim a multiple of 16 up to
+ * 256; page_size a power of two from 16 to 4096; max_pages * page_size at most 2^30; scale finite
+ * and positive; window >= 0. Row strides (ld_*) are in elements, multiples of 8, at least the
+ * row's width. Both activation types go with every cache format. */
+typedef enum ssm_kv_format { SSM_KV_ACT = 0, SSM_KV_FP8_E4M3 = 1, SSM_KV_INT8 = 2 } ssm_kv_format_t;
+typedef struct ssm_attn_desc {
+    int32_t q_heads;    /* query heads of this shard                              */
+    int32_t kv_heads;   /* key/value heads of this shard                          */
+    int32_t head_dim;
+    int32_t page_size;  /* tokens per page                                        */
+    int32_t kv_format;  /* ssm_kv_format_t                                        */
+    int32_t act_dtype;  /* ssm_dtype_t                                            */
+    int32_t window;     /* 0: a token sees all before it; w: the last w, itself included */
+    float scale;        /* of the scores, 1 / sqrt(head_dim) as a rule            */
+} ssm_attn_desc_t;
+typedef struct ssm_kv_pool {
+    void* k;
+    void* v;
+    float* k_scale;     /* null for SSM_KV_ACT */
+    float* v_scale;
+    int32_t num_pages;
+} ssm_kv_pool_t;
+/* The sequences of one call (device int32 arrays):
+ *   cu_seqlens [nseq+1]: sequence i's tokens of this call are packed rows [cu[i], cu[i+1]); null:
+ *     one row per sequence (a decode step)
+ *   kv_len [nseq]: cached tokens of the sequence, this call's included, so that row r of a
+ *     sequence with m rows is its token kv_len - m + r
+ *   page_table [nseq][max_pages]: token p is on page page_table[i][p / page_size]
+ * With cu_seqlens null a kv_len of 0 marks a row without a token (a batch padded to a fixed
+ * size): nothing is cached or read for it, its attention output is zero. Packed rows behind the
+ * last sequence are left as they were in every output. Lengths that do not fit the call (negative,
+ * kv_len below the sequence's rows or above max_pages * page_size, rows outside the call) leave
+ * the sequence's work out and set SSM_STATUS_BAD_SEQLENS; a page index outside the pool leaves
+ * that page's tokens out (neither written nor read nor attended) and sets SSM_STATUS_BAD_PAGE. */
+typedef struct ssm_kv_meta {
+    const int32_t* cu_seqlens;
+    const int32_t* kv_len;
+    const int32_t* page_table;
+    int32_t nseq;
+    int32_t max_pages;
+} ssm_kv_meta_t;
+/* What ssm_kv_append applies to every query and key head before they are used.
+ *   q_norm_w, k_norm_w [head_dim] float32 (null: none): x / sqrt(mean(x^2) + norm_eps) * w
+ *   turns [rot_dim / 2] (null when rot_dim is 0): the rotation of pair i by the token's position,
+ *     in turns per token as 64-bit fixed point (ssm_rope_turns), exact at any position
+ *   rot_dim: the leading values that rotate, a multiple of 8 up to head_dim, or 0
+ *   interleaved: 1 pairs (2i, 2i+1), 0 pairs (i, i + rot_dim / 2) */
+typedef struct ssm_qk_transform {
+    const float* q_norm_w;
+    const float* k_norm_w;
+    const uint64_t* turns;
+    float norm_eps;
+    int32_t rot_dim;
+    int32_t interleaved;
+} ssm_qk_transform_t;
+int ssm_attn_check_desc(const ssm_attn_desc_t* desc);
+/* Host only: radians per token (finite doubles, as base^(-2i/rot_dim)) to turns per token * 2^64. */
+int ssm_rope_turns(const double* radians, int32_t n, uint64_t* turns);
+/* Host-side check of HOST copies of the metadata (cu_seqlens may be null, then T == nseq): lengths
+ * as above (SSM_E_SEQLENS); every page that holds a sequence's tokens inside the pool, and no page
+ * that this call writes named by two sequences (SSM_E_SLOT). */
+int ssm_kv_check_meta_host(const ssm_attn_desc_t* desc, const int32_t* cu_seqlens, const int32_t* kv_len,
+                           const int32_t* page_table, int32_t nseq, int32_t max_pages, int64_t T,
+                           int32_t num_pages);
+/* One workspace serves all four operators for calls of up to max_tokens rows and max_seqs
+ * sequences; ssm_kv_append and ssm_kv_read use its status word only. Initialise it and read its
+ * status as for the mixer's; calls that share it must not overlap in time. */
+int ssm_attn_workspace_bytes(const ssm_attn_desc_t* desc, int64_t max_tokens, int32_t max_seqs, size_t* bytes);
+
+/* qkv [T][ld_qkv] act, columns [q heads | k heads | v heads] of head_dim each. Queries and keys are
+ * transformed (float32, one rounding at the end), k and v written to the cache, q to q_out [T][ld_q]
+ * act, which may be qkv itself with the same stride. tr null: no norm and no rotation. */
+int ssm_kv_append(const ssm_attn_desc_t* desc, const ssm_qk_transform_t* tr, const void* qkv, int64_t ld_qkv,
+                  int64_t T, const ssm_kv_meta_t* meta, const ssm_kv_pool_t* pool, void* q_out, int64_t ld_q,
+                  void* ws, size_t ws_bytes, hipStream_t stream);
+/* The cached tokens of the call's rows back as packed rows k_out, v_out [T][ld] act, columns
+ * [kv heads] of head_dim: codes times scales, rounded to the activation type. */
+int ssm_kv_read(const ssm_attn_desc_t* desc, int64_t T, const ssm_kv_meta_t* meta, const ssm_kv_pool_t* pool,
+                void* k_out, int64_t ld_k, void* v_out, int64_t ld_v, void* ws, size_t ws_bytes, hipStream_t stream);
+/* Causal attention of packed prompt chunks: q, out [T][ld] act, columns [q heads] of head_dim. Row r of
+ * a sequence attends to the cached tokens up to its own (and inside the window); they are read from the
+ * cache, the call's own among them, so ssm_kv_append comes first. out is not q. Scores and the softmax are float32;
+ * with bf16 activations the probabilities are rounded to bf16 for their product with v. A value of v that
+ * is not finite may reach rows before its token; what pages hold behind a sequence's last token never does. */
+int ssm_attn_prefill(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, int64_t T, const ssm_kv_meta_t* meta,
+                     const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
+                     hipStream_t stream);
+/* The same for one new token per sequence: q, out [nseq][ld]; meta->cu_seqlens is not read. The work is
+ * split over the sequences' lengths and joined, in an order that follows from the lengths alone. */
+int ssm_attn_decode(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, const ssm_kv_meta_t* meta,
+                    const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
+                    hipStream_t stream);
 
 /* ------------------------------------------------------------ measurement
  * Per-kernel device time, for benchmarks and profiles only. While enabled, every kernel

@@ -24,7 +24,7 @@ SSM_F32, SSM_BF16 = 0, 1
 SSM_OK = 0
 ERRORS = {-1: "SSM_E_INVAL", -2: "SSM_E_ALIGN", -3: "SSM_E_WORKSPACE", -4: "SSM_E_SLOT",
           -5: "SSM_E_SEQLENS", -6: "SSM_E_HIP"}
-SSM_STATUS_BAD_SLOT, SSM_STATUS_BAD_SEQLENS = 1, 2
+SSM_STATUS_BAD_SLOT, SSM_STATUS_BAD_SEQLENS, SSM_STATUS_BAD_PAGE = 1, 2, 4
 SSM_E_INVAL, SSM_E_ALIGN, SSM_E_WORKSPACE = -1, -2, -3
 SSM_NOALLOC_SCRATCH_BYTES = 32 << 20   # the static scratch of ssm_shard_decode_step_noalloc
 
@@ -65,6 +65,25 @@ class Desc2(ctypes.Structure):
 class Weights2(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "in_proj_w", "conv_w", "conv_b", "out_proj_w", "dt_bias", "A_log", "D", "norm_w")]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "q_heads", "kv_heads", "head_dim", "page_size", "kv_format", "act_dtype", "window")] + [("scale", ctypes.c_float)]
+
+
+class KvPoolC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [("num_pages", ctypes.c_int32)]
+
+
+class KvMetaC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cu_seqlens", "kv_len", "page_table")] + [
+        ("nseq", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class QkTransformC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q_norm_w", "k_norm_w", "turns")] + [
+        ("norm_eps", ctypes.c_float), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -112,6 +131,14 @@ _SIGS = {
     "ssm_stack_decode_workspace_bytes": ([_P, _I32, _P], _I32),
     "ssm_stack_prefill": ([_P, _P, _P, _P, _P, _I64, _P, _P, _P, _I32, _P, _P, _SZ, _P], _I32),
     "ssm_stack_decode_step": ([_P, _P, _P, _P, _P, _I32, _P, _P, _P, _I32, _P, _P, _SZ, _P], _I32),
+    "ssm_attn_check_desc": ([_P], _I32),
+    "ssm_rope_turns": ([_P, _I32, _P], _I32),
+    "ssm_kv_check_meta_host": ([_P, _P, _P, _P, _I32, _I32, _I64, _I32], _I32),
+    "ssm_attn_workspace_bytes": ([_P, _I64, _I32, _P], _I32),
+    "ssm_kv_append": ([_P, _P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
+    "ssm_kv_read": ([_P, _I64, _P, _P, _P, _I64, _P, _I64, _P, _SZ, _P], _I32),
+    "ssm_attn_prefill": ([_P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
+    "ssm_attn_decode": ([_P, _P, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
     "ssm_timing_enable": ([_I32, ctypes.c_char_p], _I32),
     "ssm_timing_collect": ([_P, _I32, _P], _I32),
 }
@@ -358,7 +385,7 @@ class BoundCall:
 
 def bind(name: str, *args, **kw) -> BoundCall:
     """bind("ssm_shard_decode_stage1", desc, weights, x_t, ...) -> a callable issuing that call.
-    Available for the prefill, decode and reduce entry points."""
+    Available for the prefill, decode, reduce, layer and attention entry points."""
     a, keep = _MARSHAL[name](*args, **kw)
     tensors = tuple(v for v in list(args) + list(kw.values()) if isinstance(v, torch.Tensor))
     return BoundCall(name, a, keep + tensors)
@@ -678,3 +705,176 @@ def ssm_stack_prefill(sd, sw, x, meta, pools, out, ws, stream=None):
 
 def ssm_stack_decode_step(sd, sw, x_t, cache_slot, pools, out, ws, stream=None):
     _call("ssm_stack_decode_step", sd, sw, x_t, cache_slot, pools, out, ws, stream)
+
+
+# ------------------------------------------------------------------ paged attention cache
+SSM_KV = {"act": 0, "fp8": 1, "int8": 2}
+_KV_TORCH = {"fp8": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def make_attn_desc(q_heads: int, kv_heads: int, head_dim: int, page_size: int, kv_format: str = "act", act: str = "bf16",
+                   scale: Optional[float] = None, window: int = 0) -> AttnDesc:
+    d = AttnDesc(q_heads, kv_heads, head_dim, page_size, SSM_KV[kv_format], SSM_BF16 if act == "bf16" else SSM_F32, window,
+                 head_dim ** -0.5 if scale is None else scale)
+    _check(lib().ssm_attn_check_desc(ctypes.byref(d)))
+    return d
+
+
+def _attn_act(ad: AttnDesc):
+    return torch.bfloat16 if ad.act_dtype == SSM_BF16 else torch.float32
+
+
+def _kv_dtype(ad: AttnDesc):
+    return {0: _attn_act(ad), 1: torch.float8_e4m3fn, 2: torch.int8}[ad.kv_format]
+
+
+def _same_device(*tensors):
+    """The calls go to the current device's stream: every tensor has to be there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{dev}")
+
+
+class KvPool:
+    """The pages of one attention layer's cache: k and v [pages][kv_heads][page_size][head_dim] of the
+    cache's type (activation type, float8_e4m3fn or int8), scales [pages][kv_heads][page_size] float32
+    with the 8-bit formats. Keeps the tensors it is given."""
+
+    def __init__(self, ad: AttnDesc, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        pages = k.shape[0]
+        for t, what in ((k, "k"), (v, "v")):
+            if tuple(t.shape) != (pages, ad.kv_heads, ad.page_size, ad.head_dim) or t.dtype != _kv_dtype(ad):
+                raise ValueError(f"{what}: {_kv_dtype(ad)} [pages][{ad.kv_heads}][{ad.page_size}][{ad.head_dim}] expected, "
+                                 f"got {t.dtype} {tuple(t.shape)}")
+        if (ad.kv_format != 0) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("the 8-bit formats have scales, the activation type none")
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is not None and (tuple(t.shape) != (pages, ad.kv_heads, ad.page_size) or t.dtype != torch.float32):
+                raise ValueError(f"{what}: float32 [pages][{ad.kv_heads}][{ad.page_size}] expected")
+        self.k, self.v, self.k_scale, self.v_scale, self.num_pages = k, v, k_scale, v_scale, pages
+        self.c = KvPoolC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), pages)
+
+
+def empty_kv_pool(ad: AttnDesc, num_pages: int, device="cuda") -> KvPool:
+    shape = (num_pages, ad.kv_heads, ad.page_size, ad.head_dim)
+    k, v = (torch.empty(shape, dtype=_kv_dtype(ad), device=device) for _ in range(2))
+    ks, vs = (torch.empty(shape[:3], dtype=torch.float32, device=device) if ad.kv_format else None for _ in range(2))
+    return KvPool(ad, k, v, ks, vs)
+
+
+class KvMeta:
+    """Device-resident sequences of one call (int32), validated from their host copy. cu_seqlens None: one
+    row per sequence. A program that goes on token by token advances kv_len in place (`meta.kv_len += 1`)
+    and keeps to the pages of page_table."""
+
+    def __init__(self, ad: AttnDesc, cu_seqlens, kv_len, page_table, num_pages: int, device="cuda"):
+        def host(x):
+            return np.ascontiguousarray(x.cpu().numpy() if isinstance(x, torch.Tensor) else x, np.int32)
+        cu = None if cu_seqlens is None else host(cu_seqlens)
+        kl = host(kv_len)
+        self.nseq = int(kl.shape[0])
+        pt = host(page_table).reshape(self.nseq, -1) if self.nseq else np.zeros((0, 1), np.int32)
+        if cu is not None and cu.shape != (self.nseq + 1,):
+            raise ValueError(f"cu_seqlens: {self.nseq + 1} entries expected, got {cu.shape}")
+        self.max_pages = int(pt.shape[1])
+        self.T = self.nseq if cu is None else int(cu[-1])
+        _check(lib().ssm_kv_check_meta_host(ctypes.byref(ad), None if cu is None else cu.ctypes.data, kl.ctypes.data,
+                                            pt.ctypes.data, self.nseq, self.max_pages, self.T, int(num_pages)))
+        self.host = (cu, kl, pt)
+        self.cu = None if cu is None else torch.from_numpy(cu).to(device)
+        self.kv_len = torch.from_numpy(kl).to(device)
+        self.page_table = torch.from_numpy(pt).to(device)
+        self.c = KvMetaC(None if cu is None else self.cu.data_ptr(), self.kv_len.data_ptr(), self.page_table.data_ptr(),
+                         self.nseq, self.max_pages)
+
+
+def rope_turns(inv_freq, device="cuda") -> torch.Tensor:
+    """Radians per token of every rotated pair -> the device table of QkTransform (int64 holding the 64-bit
+    turns per token)."""
+    f = np.ascontiguousarray(inv_freq.cpu().numpy() if isinstance(inv_freq, torch.Tensor) else inv_freq, np.float64)
+    out = np.zeros(f.shape, np.uint64)
+    _check(lib().ssm_rope_turns(f.ctypes.data, f.size, out.ctypes.data))
+    return torch.from_numpy(out.view(np.int64)).to(device)
+
+
+class QkTransform:
+    """Norm weights (float32 [head_dim], None: none) and rotation (inv_freq: radians per token of each pair,
+    empty or None: none) that ssm_kv_append applies."""
+
+    def __init__(self, ad: AttnDesc, q_norm_w=None, k_norm_w=None, eps: float = 1e-5, inv_freq=None, interleaved: bool = False,
+                 device="cuda"):
+        for w in (q_norm_w, k_norm_w):
+            if w is not None and (tuple(w.shape) != (ad.head_dim,) or w.dtype != torch.float32):
+                raise ValueError(f"norm weight: float32 [{ad.head_dim}] expected")
+        rot = 0 if inv_freq is None else 2 * len(inv_freq)
+        self.turns = rope_turns(inv_freq, device) if rot else None
+        self.q_norm_w, self.k_norm_w = q_norm_w, k_norm_w
+        self.c = QkTransformC(_ptr(q_norm_w), _ptr(k_norm_w), _ptr(self.turns), float(eps), rot, 1 if interleaved else 0)
+
+
+def attn_workspace_bytes(ad: AttnDesc, max_tokens: int, max_seqs: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().ssm_attn_workspace_bytes(ctypes.byref(ad), max_tokens, max_seqs, ctypes.byref(n)))
+    return n.value
+
+
+def _attn_rows(ad: AttnDesc, t: torch.Tensor, rows: int, heads: int, what: str):
+    """(pointer, row stride) of a [rows][heads * head_dim] tensor of the activation type with unit column stride."""
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] != heads * ad.head_dim or t.dtype != _attn_act(ad):
+        raise ValueError(f"{what}: {_attn_act(ad)} [{rows}][{heads * ad.head_dim}] expected, got {t.dtype} {tuple(t.shape)}")
+    if t.shape[0] and t.stride(1) != 1:
+        raise ValueError(f"{what}: unit column stride expected")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def _m_ssm_kv_append(ad, tr: Optional[QkTransform], qkv, meta: KvMeta, pool: KvPool, q_out, ws, stream=None):
+    _same_device(qkv, q_out, ws, pool.k, meta.kv_len)
+    p, ld = _attn_rows(ad, qkv, meta.T, ad.q_heads + 2 * ad.kv_heads, "qkv")
+    q, ldq = _attn_rows(ad, q_out, meta.T, ad.q_heads, "q_out")
+    return (ctypes.byref(ad), ctypes.byref(tr.c) if tr is not None else None, p, ld, meta.T, ctypes.byref(meta.c),
+            ctypes.byref(pool.c), q, ldq, _ptr(ws), ws.numel(), _stream(stream)), (ad, tr, meta, pool)
+
+
+def _m_ssm_kv_read(ad, meta: KvMeta, pool: KvPool, k_out, v_out, ws, stream=None):
+    _same_device(k_out, v_out, ws, pool.k, meta.kv_len)
+    k, ldk = _attn_rows(ad, k_out, meta.T, ad.kv_heads, "k_out")
+    v, ldv = _attn_rows(ad, v_out, meta.T, ad.kv_heads, "v_out")
+    return (ctypes.byref(ad), meta.T, ctypes.byref(meta.c), ctypes.byref(pool.c), k, ldk, v, ldv, _ptr(ws), ws.numel(),
+            _stream(stream)), (ad, meta, pool)
+
+
+def _m_ssm_attn_prefill(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None):
+    _same_device(q, out, ws, pool.k, meta.kv_len)
+    p, ld = _attn_rows(ad, q, meta.T, ad.q_heads, "q")
+    o, ldo = _attn_rows(ad, out, meta.T, ad.q_heads, "out")
+    return (ctypes.byref(ad), p, ld, meta.T, ctypes.byref(meta.c), ctypes.byref(pool.c), o, ldo, _ptr(ws), ws.numel(),
+            _stream(stream)), (ad, meta, pool)
+
+
+def _m_ssm_attn_decode(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None):
+    _same_device(q, out, ws, pool.k, meta.kv_len)
+    p, ld = _attn_rows(ad, q, meta.nseq, ad.q_heads, "q")
+    o, ldo = _attn_rows(ad, out, meta.nseq, ad.q_heads, "out")
+    return (ctypes.byref(ad), p, ld, ctypes.byref(meta.c), ctypes.byref(pool.c), o, ldo, _ptr(ws), ws.numel(),
+            _stream(stream)), (ad, meta, pool)
+
+
+_MARSHAL.update({name[3:]: fn for name, fn in list(globals().items()) if name.startswith(("_m_ssm_kv", "_m_ssm_attn"))})
+
+
+def ssm_kv_append(ad, tr, qkv, meta, pool, q_out, ws, stream=None):
+    _call("ssm_kv_append", ad, tr, qkv, meta, pool, q_out, ws, stream)
+
+
+def ssm_kv_read(ad, meta, pool, k_out, v_out, ws, stream=None):
+    _call("ssm_kv_read", ad, meta, pool, k_out, v_out, ws, stream)
+
+
+def ssm_attn_prefill(ad, q, meta, pool, out, ws, stream=None):
+    _call("ssm_attn_prefill", ad, q, meta, pool, out, ws, stream)
+
+
+def ssm_attn_decode(ad, q, meta, pool, out, ws, stream=None):
+    _call("ssm_attn_decode", ad, q, meta, pool, out, ws, stream)

@@ -8,6 +8,7 @@
 // Decode: the same with one token per sequence and the single-step kernels.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -1446,6 +1447,218 @@ int ssm_stack_decode_step(const ssm_stack_desc_t* sd, const ssm_shard_weights_t*
                   launch_residual_rmsnorm(B.resid, false, one_part(B.y), bf, B.resid, last ? final_w : norm_w[l + 1],
                                           eps, last ? out : B.normed, bf, Bsz, dm, s));
     }
+    return SSM_OK;
+}
+
+}  // extern "C"
+
+// ================================================================ paged attention cache
+namespace {
+
+constexpr int64_t kMaxKvTokens = 1ll << 30;   // tokens per sequence: positions and units stay in 32 bits
+
+int check_attn_desc(const ssm_attn_desc_t* d) {
+    if (!d) return fail(SSM_E_INVAL, "desc is null");
+    SSM_TRY(check_dtype(d->act_dtype, "act"));
+    if (d->kv_format != SSM_KV_ACT && d->kv_format != SSM_KV_FP8_E4M3 && d->kv_format != SSM_KV_INT8)
+        return fail(SSM_E_INVAL, "kv_format %d", d->kv_format);
+    if (d->q_heads < 1 || d->q_heads > 128 || d->kv_heads < 1 || d->q_heads % d->kv_heads)
+        return fail(SSM_E_INVAL, "q_heads %d (1..128) must be a multiple of kv_heads %d", d->q_heads, d->kv_heads);
+    if (d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16)
+        return fail(SSM_E_INVAL, "head_dim %d must be a multiple of 16 up to 256", d->head_dim);
+    if (d->page_size < 16 || d->page_size > 4096 || (d->page_size & (d->page_size - 1)))
+        return fail(SSM_E_INVAL, "page_size %d must be a power of two from 16 to 4096", d->page_size);
+    if (d->window < 0) return fail(SSM_E_INVAL, "window %d", d->window);
+    if (!(d->scale > 0.0f) || !(d->scale < HUGE_VALF)) return fail(SSM_E_INVAL, "scale must be finite and positive");
+    return SSM_OK;
+}
+
+int check_kv_meta(const ssm_attn_desc_t* d, const ssm_kv_meta_t* m, int64_t T, bool per_row) {
+    if (!m) return fail(SSM_E_INVAL, "meta is null");
+    if (T < 0 || T > INT32_MAX) return fail(SSM_E_INVAL, "token count %lld", (long long)T);
+    if (m->nseq < 0) return fail(SSM_E_INVAL, "nseq %d", m->nseq);
+    if (m->nseq == 0) return T == 0 ? SSM_OK : fail(SSM_E_SEQLENS, "T = %lld tokens but no sequences", (long long)T);
+    if (!m->kv_len || !m->page_table) return fail(SSM_E_INVAL, "meta arrays must be non-null");
+    if (m->max_pages < 1 || (int64_t)m->max_pages * d->page_size > kMaxKvTokens)
+        return fail(SSM_E_INVAL, "max_pages %d: 1 to 2^30 / page_size", m->max_pages);
+    if ((per_row || !m->cu_seqlens) && T != m->nseq)
+        return fail(SSM_E_SEQLENS, "T = %lld rows for %d sequences of one row", (long long)T, m->nseq);
+    return SSM_OK;
+}
+
+int check_kv_pool(const ssm_attn_desc_t* d, const ssm_kv_pool_t* p) {
+    if (!p) return fail(SSM_E_INVAL, "pool is null");
+    if (p->num_pages < 1) return fail(SSM_E_INVAL, "num_pages %d", p->num_pages);
+    SSM_TRY(check_ptr(p->k, "pool.k"));
+    SSM_TRY(check_ptr(p->v, "pool.v"));
+    if (d->kv_format != SSM_KV_ACT) {
+        SSM_TRY(check_ptr(p->k_scale, "pool.k_scale"));
+        SSM_TRY(check_ptr(p->v_scale, "pool.v_scale"));
+    }
+    return SSM_OK;
+}
+
+int check_rows(const void* p, int64_t ld, int64_t width, const char* name) {
+    SSM_TRY(check_ptr(p, name));
+    if (ld < width) return fail(SSM_E_INVAL, "%s: row stride %lld below the row's %lld values", name, (long long)ld, (long long)width);
+    if (ld % 8) return fail(SSM_E_ALIGN, "%s: row stride %lld is not a multiple of 8", name, (long long)ld);
+    return SSM_OK;
+}
+
+KvArgs kv_args(const ssm_attn_desc_t* d, int64_t T, const ssm_kv_meta_t* m, const ssm_kv_pool_t* p, void* ws, bool per_row) {
+    KvArgs a{};
+    a.cu = per_row ? nullptr : m->cu_seqlens;
+    a.kv_len = m->kv_len; a.table = m->page_table;
+    a.k = p->k; a.v = p->v; a.ks = p->k_scale; a.vs = p->v_scale;
+    a.status = (int32_t*)ws;
+    a.T = T; a.nseq = m->nseq; a.max_pages = m->max_pages; a.num_pages = p->num_pages;
+    a.page_log2 = __builtin_ctz((unsigned)d->page_size);
+    a.Hq = d->q_heads; a.Hkv = d->kv_heads; a.D = d->head_dim; a.fmt = d->kv_format;
+    a.window = d->window; a.scale = d->scale;
+    return a;
+}
+
+int check_attend(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, void* out, int64_t ld_o) {
+    const int64_t width = (int64_t)d->q_heads * d->head_dim;
+    SSM_TRY(check_rows(q, ld_q, width, "q"));
+    SSM_TRY(check_rows(out, ld_o, width, "out"));
+    if (q == out) return fail(SSM_E_INVAL, "out must not be q");
+    return SSM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ssm_attn_check_desc(const ssm_attn_desc_t* d) { return check_attn_desc(d); }
+
+int ssm_rope_turns(const double* radians, int32_t n, uint64_t* turns) {
+    if (n < 0) return fail(SSM_E_INVAL, "n %d", n);
+    if (n == 0) return SSM_OK;
+    if (!radians || !turns) return fail(SSM_E_INVAL, "radians or turns is null");
+    for (int32_t i = 0; i < n; ++i) {
+        if (!std::isfinite(radians[i])) return fail(SSM_E_INVAL, "radians[%d] is not finite", i);
+        // the fraction of a turn, to the 64 bits of the long double's significand
+        long double f = (long double)radians[i] / 6.283185307179586476925286766559L;
+        f -= std::floor(f);
+        const long double x = std::floor(f * 18446744073709551616.0L + 0.5L);
+        turns[i] = x >= 18446744073709551616.0L ? 0 : (uint64_t)x;
+    }
+    return SSM_OK;
+}
+
+int ssm_kv_check_meta_host(const ssm_attn_desc_t* d, const int32_t* cu, const int32_t* kv_len, const int32_t* table,
+                           int32_t nseq, int32_t max_pages, int64_t T, int32_t num_pages) {
+    SSM_TRY(check_attn_desc(d));
+    if (num_pages < 1) return fail(SSM_E_INVAL, "num_pages %d", num_pages);
+    const ssm_kv_meta_t m{cu, kv_len, table, nseq, max_pages};
+    SSM_TRY(check_kv_meta(d, &m, T, false));
+    if (nseq == 0) return SSM_OK;
+    if (cu && cu[0] != 0) return fail(SSM_E_SEQLENS, "cu_seqlens[0] = %d", cu[0]);
+    for (int32_t i = 0; cu && i < nseq; ++i)
+        if (cu[i + 1] < cu[i]) return fail(SSM_E_SEQLENS, "cu_seqlens[%d] = %d < %d", i + 1, cu[i + 1], cu[i]);
+    if (cu && cu[nseq] != T) return fail(SSM_E_SEQLENS, "cu_seqlens[%d] = %d, T = %lld", nseq, cu[nseq], (long long)T);
+    std::vector<int32_t> named(num_pages, -1);   // the first sequence that names a page
+    std::vector<char> written(num_pages, 0);     // whether a sequence writes it
+    for (int32_t i = 0; i < nseq; ++i) {
+        const int64_t n = kv_len[i], rows = cu ? cu[i + 1] - cu[i] : (n > 0 ? 1 : 0);
+        if (n < rows || n > (int64_t)max_pages * d->page_size)
+            return fail(SSM_E_SEQLENS, "kv_len[%d] = %lld with %lld rows and %d pages", i, (long long)n, (long long)rows, max_pages);
+        const int64_t first = (n - rows) / d->page_size, end = (n + d->page_size - 1) / d->page_size;
+        for (int64_t p = 0; p < end; ++p) {
+            const int32_t pg = table[(int64_t)i * max_pages + p];
+            if (pg < 0 || pg >= num_pages) return fail(SSM_E_SLOT, "page_table[%d][%lld] = %d of %d pages", i, (long long)p, pg, num_pages);
+            const bool writes = rows > 0 && p >= first;
+            if (named[pg] >= 0 && (writes || written[pg]))
+                return fail(SSM_E_SLOT, "page %d is written by this call and named twice (sequences %d and %d)", pg, named[pg], i);
+            if (named[pg] < 0) named[pg] = i;
+            if (writes) written[pg] = 1;
+        }
+    }
+    return SSM_OK;
+}
+
+int ssm_attn_workspace_bytes(const ssm_attn_desc_t* d, int64_t max_tokens, int32_t max_seqs, size_t* bytes) {
+    SSM_TRY(check_attn_desc(d));
+    if (!bytes || max_tokens < 0 || max_tokens > INT32_MAX || max_seqs < 0) return fail(SSM_E_INVAL, "bad size query");
+    *bytes = kWsHeader + std::max(attn_prefill_scratch_bytes(d->act_dtype == SSM_BF16, d->q_heads, d->kv_heads, d->head_dim,
+                                                             max_tokens, max_seqs),
+                                  attn_decode_scratch_bytes(d->head_dim, max_seqs));
+    return SSM_OK;
+}
+
+int ssm_kv_append(const ssm_attn_desc_t* d, const ssm_qk_transform_t* tr, const void* qkv, int64_t ld_qkv, int64_t T,
+                  const ssm_kv_meta_t* m, const ssm_kv_pool_t* pool, void* q_out, int64_t ld_q, void* ws, size_t ws_bytes,
+                  hipStream_t s) {
+    SSM_TRY(check_attn_desc(d));
+    SSM_TRY(check_kv_meta(d, m, T, false));
+    SSM_TRY(check_kv_pool(d, pool));
+    SSM_TRY(check_ws(ws, ws_bytes, kWsHeader));
+    KvAppendArgs a{};
+    if (tr) {
+        if (tr->rot_dim < 0 || tr->rot_dim % 8 || tr->rot_dim > d->head_dim)
+            return fail(SSM_E_INVAL, "rot_dim %d must be a multiple of 8 up to head_dim %d", tr->rot_dim, d->head_dim);
+        if (tr->interleaved != 0 && tr->interleaved != 1) return fail(SSM_E_INVAL, "interleaved %d", tr->interleaved);
+        if (tr->rot_dim > 0) SSM_TRY(check_ptr(tr->turns, "turns"));
+        if (tr->q_norm_w) SSM_TRY(check_ptr(tr->q_norm_w, "q_norm_w"));
+        if (tr->k_norm_w) SSM_TRY(check_ptr(tr->k_norm_w, "k_norm_w"));
+        if ((tr->q_norm_w || tr->k_norm_w) && !(tr->norm_eps >= 0.0f)) return fail(SSM_E_INVAL, "norm_eps must be >= 0");
+        a.q_w = tr->q_norm_w; a.k_w = tr->k_norm_w; a.eps = tr->norm_eps;
+        a.turns = tr->turns; a.rot = tr->rot_dim; a.inter = tr->interleaved;
+    }
+    if (T == 0) return SSM_OK;
+    SSM_TRY(check_rows(qkv, ld_qkv, (int64_t)(d->q_heads + 2 * d->kv_heads) * d->head_dim, "qkv"));
+    SSM_TRY(check_rows(q_out, ld_q, (int64_t)d->q_heads * d->head_dim, "q_out"));
+    if (qkv == q_out && ld_q != ld_qkv) return fail(SSM_E_INVAL, "q_out in place of qkv needs the same row stride");
+    a.kv = kv_args(d, T, m, pool, ws, false);
+    a.qkv = qkv; a.ld = ld_qkv; a.q = q_out; a.ld_q = ld_q;
+    SSM_TIMED("kv.append", s, launch_kv_append(a, d->act_dtype == SSM_BF16, s));
+    return SSM_OK;
+}
+
+int ssm_kv_read(const ssm_attn_desc_t* d, int64_t T, const ssm_kv_meta_t* m, const ssm_kv_pool_t* pool, void* k_out,
+                int64_t ld_k, void* v_out, int64_t ld_v, void* ws, size_t ws_bytes, hipStream_t s) {
+    SSM_TRY(check_attn_desc(d));
+    SSM_TRY(check_kv_meta(d, m, T, false));
+    SSM_TRY(check_kv_pool(d, pool));
+    SSM_TRY(check_ws(ws, ws_bytes, kWsHeader));
+    if (T == 0) return SSM_OK;
+    const int64_t width = (int64_t)d->kv_heads * d->head_dim;
+    SSM_TRY(check_rows(k_out, ld_k, width, "k_out"));
+    SSM_TRY(check_rows(v_out, ld_v, width, "v_out"));
+    SSM_TIMED("kv.read", s, launch_kv_read(kv_args(d, T, m, pool, ws, false), k_out, ld_k, v_out, ld_v, d->act_dtype == SSM_BF16, s));
+    return SSM_OK;
+}
+
+int ssm_attn_prefill(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, int64_t T, const ssm_kv_meta_t* m,
+                     const ssm_kv_pool_t* pool, void* out, int64_t ld_o, void* ws, size_t ws_bytes, hipStream_t s) {
+    SSM_TRY(check_attn_desc(d));
+    SSM_TRY(check_kv_meta(d, m, T, false));
+    SSM_TRY(check_kv_pool(d, pool));
+    const bool bf = d->act_dtype == SSM_BF16;
+    SSM_TRY(check_ws(ws, ws_bytes, kWsHeader + attn_prefill_scratch_bytes(bf, d->q_heads, d->kv_heads, d->head_dim, T, m->nseq)));
+    if (T == 0) return SSM_OK;
+    SSM_TRY(check_attend(d, q, ld_q, out, ld_o));
+    AttnArgs a{};
+    a.kv = kv_args(d, T, m, pool, ws, false);
+    a.q = q; a.ld_q = ld_q; a.o = out; a.ld_o = ld_o; a.scratch = (char*)ws + kWsHeader;
+    SSM_TRY_HIP(launch_attn_prefill(a, bf, s), "attn.prefill");
+    return SSM_OK;
+}
+
+int ssm_attn_decode(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, const ssm_kv_meta_t* m,
+                    const ssm_kv_pool_t* pool, void* out, int64_t ld_o, void* ws, size_t ws_bytes, hipStream_t s) {
+    SSM_TRY(check_attn_desc(d));
+    if (!m) return fail(SSM_E_INVAL, "meta is null");
+    SSM_TRY(check_kv_meta(d, m, m->nseq, true));
+    SSM_TRY(check_kv_pool(d, pool));
+    SSM_TRY(check_ws(ws, ws_bytes, kWsHeader + attn_decode_scratch_bytes(d->head_dim, m->nseq)));
+    if (m->nseq == 0) return SSM_OK;
+    SSM_TRY(check_attend(d, q, ld_q, out, ld_o));
+    AttnArgs a{};
+    a.kv = kv_args(d, m->nseq, m, pool, ws, true);
+    a.q = q; a.ld_q = ld_q; a.o = out; a.ld_o = ld_o; a.scratch = (char*)ws + kWsHeader;
+    SSM_TRY_HIP(launch_attn_decode(a, d->act_dtype == SSM_BF16, s), "attn.decode");
     return SSM_OK;
 }
 

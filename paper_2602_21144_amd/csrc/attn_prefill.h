@@ -1,0 +1,64 @@
+// Causal attention of packed prompt chunks over the paged cache.
+//
+// The g = q_heads / kv_heads query heads of a kv head are stacked on the tokens: row r of a sequence's
+// m g rows is token r / g, head r % g. A tile is kTileRows of these rows; a wave holds 32 of them as the
+// columns of its products, in registers from first to last:
+//   S^T = K Q^T    on 32x32 tiles; a lane holds 16 scores of one query per 32 tokens
+//   O^T = V^T P^T  the lane's scores are this product's operand as they stand: entries 8 s .. 8 s + 7 are
+//                  tokens 16 s + 4 half + {0 .. 3} and 16 s + 8 + 4 half + {0 .. 3}, which over both lane
+//                  halves are the 16 tokens of one K-step once; v comes from LDS in that order, by the
+//                  transposing 64-bit LDS reads (bf16) or one value per lane (float32).
+// So the softmax needs one exchange between lanes per step (the maximum of the two halves), and the
+// rescale of O is one factor per lane. K and V steps of TOK tokens go through LDS, shared by the four
+// waves, in two buffers: the next step's loads are in flight while the present one is computed.
+//
+// Work: the plan kernel lists (tile, range of tokens) items so that no item is longer than a share of
+// the whole work (kTarget items of equal length); tiles behind a long cache are cut into several items
+// whose partial results (m, l and the unnormalised o, float32) a third kernel joins in order. Items are
+// listed longest first, and the workgroups of one item's kv heads are neighbours.
+#pragma once
+#include "kv.h"
+
+namespace ssm {
+
+constexpr int kTileRows = 128;
+constexpr int kStep = 64;          // the plan counts tokens in steps of this many
+constexpr int kTarget = 512;       // items of the whole work: two workgroups for each of 256 compute units
+constexpr int kMinSteps = 8;       // no item is cut shorter than this
+
+struct AttnItem { int32_t seq, row0, k0, k1, part, pad[3]; };   // part -1: the item is the whole tile
+struct AttnJoin { int32_t seq, row0, part, pieces; };
+struct AttnPlan {
+    int32_t* count;      // [0] items, [1] joins
+    int32_t* prefix;     // [nseq + 1] tiles before each sequence
+    AttnItem* items;
+    AttnJoin* joins;
+    float* parts;        // [Hkv][max_parts][kTileRows (DP + 2)]
+    int max_tiles, max_items, max_joins, max_parts;
+    size_t total;
+};
+// sizes for up to T rows of nseq sequences
+inline AttnPlan attn_plan(int Hq, int Hkv, int DP, int64_t T, int nseq, char* base) {
+    AttnPlan p{};
+    const int64_t tiles = (T * (Hq / Hkv) + kTileRows - 1) / kTileRows + nseq;
+    // cut tiles have more steps than a share of the work: their number and their items' are bounded by it
+    const int64_t share = (kTarget + Hkv - 1) / Hkv + 1;
+    p.max_tiles = (int)tiles;
+    p.max_items = (int)(tiles + share);
+    p.max_joins = (int)(tiles < share ? tiles : share);
+    p.max_parts = (int)(2 * share);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { char* q = base ? base + off : nullptr; off += align256(bytes); return q; };
+    p.count = (int32_t*)take(16);
+    p.prefix = (int32_t*)take((size_t)(nseq + 1) * 4);
+    p.items = (AttnItem*)take((size_t)p.max_items * sizeof(AttnItem));
+    p.joins = (AttnJoin*)take((size_t)p.max_joins * sizeof(AttnJoin));
+    p.parts = (float*)take((size_t)Hkv * p.max_parts * kTileRows * (DP + 2) * 4);
+    p.total = off;
+    return p;
+}
+
+template <typename T, int FMT, int DP>
+hipError_t launch_attn_prefill_tile(const AttnArgs& p, const AttnPlan& pl, hipStream_t s);
+
+}  // namespace ssm

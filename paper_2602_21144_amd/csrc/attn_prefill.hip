@@ -1,0 +1,176 @@
+// Attention of prompt chunks: the plan of the work, and the choice of the padded width.
+#include "attn_prefill.h"
+
+namespace ssm {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kBins = 32;
+
+// The steps of one tile: tokens [k0, k1) that its rows see
+struct TileRange { int k0, k1, steps; };
+__device__ __forceinline__ TileRange tile_range(const KvArgs& a, const KvSeq& s, int g, int row0) {
+    const int rows = s.m * g, last = min(row0 + kTileRows, rows) - 1;
+    const int before = s.n - s.m, lo = before + row0 / g;
+    TileRange r;
+    r.k1 = before + last / g + 1;
+    r.k0 = a.window > 0 && lo >= a.window ? (lo - a.window + 1) & ~(kStep - 1) : 0;
+    r.steps = (r.k1 - r.k0 + kStep - 1) / kStep;
+    return r;
+}
+
+// One workgroup: tiles of every sequence, the length that no item exceeds, and the items in bins of
+// falling length. Places inside a bin come from LDS atomics: they settle which item runs first and
+// where partial results lie, never what is added to what.
+__global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnPlan p) {
+    __shared__ int s_wave[kPlanThreads / 64];
+    __shared__ int s_bin[kBins], s_part, s_join;
+    __shared__ unsigned long long s_steps;
+    const int tid = threadIdx.x, lane = tid & 63, g = a.Hq / a.Hkv;
+    kv_check_seqs(a, tid, kPlanThreads);
+    if (tid < kBins) s_bin[tid] = 0;
+    if (tid == 0) {
+        s_steps = 0;
+        s_part = s_join = 0;
+    }
+    const int per = (a.nseq + kPlanThreads - 1) / kPlanThreads;
+    auto tiles_of = [&](int i) {
+        const KvSeq s = kv_seq(a, i);
+        return s.ok ? (int)(((int64_t)s.m * g + kTileRows - 1) / kTileRows) : 0;
+    };
+    int sum = 0;
+    for (int k = 0; k < per; ++k)
+        if (tid * per + k < a.nseq) sum += tiles_of(tid * per + k);
+    int incl = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int o = __shfl_up(incl, off, 64);
+        if (lane >= off) incl += o;
+    }
+    if (lane == 63) s_wave[tid >> 6] = incl;
+    __syncthreads();
+    int at = incl - sum, total = 0;
+    for (int k = 0; k < kPlanThreads / 64; ++k) {
+        if (k < (tid >> 6)) at += s_wave[k];
+        total += s_wave[k];
+    }
+    for (int k = 0; k < per; ++k) {
+        const int i = tid * per + k;
+        if (i < a.nseq) {
+            p.prefix[i] = at;
+            at += tiles_of(i);
+        }
+    }
+    if (total > p.max_tiles) {   // sequences that overlap hold more rows than the call has
+        if (tid == 0) atomicOr(a.status, SSM_STATUS_BAD_SEQLENS);
+        total = p.max_tiles;
+    }
+    __syncthreads();
+    auto seq_of = [&](int t) {   // the last sequence whose tiles begin at or before t
+        int i = 0, e = a.nseq;
+        while (e - i > 1) {
+            const int mid = (i + e) >> 1;
+            if (p.prefix[mid] <= t) i = mid;
+            else e = mid;
+        }
+        return i;
+    };
+    unsigned long long steps = 0;
+    for (int t = tid; t < total; t += kPlanThreads) {
+        const int i = seq_of(t);
+        steps += tile_range(a, kv_seq(a, i), g, (t - p.prefix[i]) * kTileRows).steps;
+    }
+    atomicAdd(&s_steps, steps);
+    __syncthreads();
+    const unsigned long long share = (s_steps * a.Hkv + kTarget - 1) / kTarget;
+    const int most = share < kMinSteps ? kMinSteps : (int)share;   // steps of the longest item
+    auto cut = [&](const TileRange& r, int& pieces, int& len) {
+        pieces = r.steps > most ? (r.steps + most - 1) / most : 1;
+        len = (r.steps + pieces - 1) / pieces;
+        if (pieces > 1) pieces = (r.steps + len - 1) / len;
+    };
+    auto bin_of = [&](int len) { return kBins - 1 - (int)((int64_t)len * kBins / (most + 1)); };
+    for (int t = tid; t < total; t += kPlanThreads) {
+        const int i = seq_of(t);
+        int pieces, len;
+        cut(tile_range(a, kv_seq(a, i), g, (t - p.prefix[i]) * kTileRows), pieces, len);
+        atomicAdd(&s_bin[bin_of(len)], pieces);
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int n = 0;
+        for (int k = 0; k < kBins; ++k) {
+            const int c = s_bin[k];
+            s_bin[k] = n;
+            n += c;
+        }
+        p.count[0] = n;
+    }
+    __syncthreads();
+    for (int t = tid; t < total; t += kPlanThreads) {
+        const int i = seq_of(t), row0 = (t - p.prefix[i]) * kTileRows;
+        const TileRange r = tile_range(a, kv_seq(a, i), g, row0);
+        int pieces, len;
+        cut(r, pieces, len);
+        const int pos = atomicAdd(&s_bin[bin_of(len)], pieces);
+        int part = -1;
+        if (pieces > 1) {
+            part = atomicAdd(&s_part, pieces);
+            p.joins[atomicAdd(&s_join, 1)] = AttnJoin{i, row0, part, pieces};
+        }
+        for (int k = 0; k < pieces; ++k) {
+            const int k0 = r.k0 + k * len * kStep;
+            p.items[pos + k] = AttnItem{i, row0, k0, min(r.k1, k0 + len * kStep), pieces > 1 ? part + k : -1, {0, 0, 0}};
+        }
+    }
+    __syncthreads();
+    if (tid == 0) p.count[1] = s_join;
+}
+
+// The width that a head's values are padded to in the products. Float32, whose rate is a sixteenth of
+// bf16's, has three.
+int padded_dim(bool bf16_act, int D) {
+    if (bf16_act) return D <= 64 ? 64 : (D + 31) / 32 * 32;
+    return D <= 64 ? 64 : D <= 128 ? 128 : 256;
+}
+
+template <typename T, int FMT> hipError_t prefill_dim(const AttnArgs& p, const AttnPlan& pl, int dp, hipStream_t s) {
+    if constexpr (sizeof(T) == 2) {
+        switch (dp) {
+            case 96: return launch_attn_prefill_tile<T, FMT, 96>(p, pl, s);
+            case 160: return launch_attn_prefill_tile<T, FMT, 160>(p, pl, s);
+            case 192: return launch_attn_prefill_tile<T, FMT, 192>(p, pl, s);
+            case 224: return launch_attn_prefill_tile<T, FMT, 224>(p, pl, s);
+        }
+    }
+    switch (dp) {
+        case 64: return launch_attn_prefill_tile<T, FMT, 64>(p, pl, s);
+        case 128: return launch_attn_prefill_tile<T, FMT, 128>(p, pl, s);
+        default: return launch_attn_prefill_tile<T, FMT, 256>(p, pl, s);
+    }
+}
+template <typename T> hipError_t prefill_fmt(const AttnArgs& p, const AttnPlan& pl, int dp, hipStream_t s) {
+    switch (p.kv.fmt) {
+        case SSM_KV_ACT: return prefill_dim<T, SSM_KV_ACT>(p, pl, dp, s);
+        case SSM_KV_FP8_E4M3: return prefill_dim<T, SSM_KV_FP8_E4M3>(p, pl, dp, s);
+        default: return prefill_dim<T, SSM_KV_INT8>(p, pl, dp, s);
+    }
+}
+
+}  // namespace
+
+size_t attn_prefill_scratch_bytes(bool bf16_act, int Hq, int Hkv, int D, int64_t T, int nseq) {
+    return T > 0 ? attn_plan(Hq, Hkv, padded_dim(bf16_act, D), T, nseq, nullptr).total : 0;
+}
+hipError_t launch_attn_prefill(const AttnArgs& p, bool bf16_act, hipStream_t s) {
+    const KvArgs& a = p.kv;
+    const int dp = padded_dim(bf16_act, a.D);
+    const AttnPlan pl = attn_plan(a.Hq, a.Hkv, dp, a.T, a.nseq, p.scratch);
+    KernelTimer kt("attn.prefill_plan", s);
+    SSM_LAUNCH(attn_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, pl);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return bf16_act ? prefill_fmt<bf16>(p, pl, dp, s) : prefill_fmt<float>(p, pl, dp, s);
+}
+
+}  // namespace ssm

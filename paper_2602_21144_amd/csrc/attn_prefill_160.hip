@@ -1,0 +1,6 @@
+// Attention of prompt chunks: the tiles of heads padded to 160 values.
+#include "attn_prefill_kernel.h"
+
+namespace ssm {
+SSM_ATTN_PREFILL_BF16(160)
+}  // namespace ssm

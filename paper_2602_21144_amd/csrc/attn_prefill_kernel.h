@@ -1,0 +1,357 @@
+// The kernels over the plan of attn_prefill.h: the items, and the join of cut tiles. One source file per
+// padded width instantiates them.
+#pragma once
+#include "attn_prefill.h"
+
+namespace ssm {
+
+// ---------------------------------------------------------------- the main kernel
+template <typename T, int DP> struct PrefillShape {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int TOK = BF ? 64 : 32, MT = TOK / 32, DT = DP / 32;
+    static constexpr int PE = 16 / (int)sizeof(T);        // values per staged piece
+    static constexpr int NP = DP / 32;                     // pieces of k (and of v) per thread and step
+    // row strides in LDS: k rows 16 bytes apart modulo 256 (16 lanes read 16 rows), v rows 64 or 192
+    // bytes (bf16: a half wave reads 4 rows of 64 bytes) or 32 bytes (float32) apart
+    static constexpr int KS = DP + PE;
+    static constexpr int VS = BF ? ((DP * 2) % 256 == 64 || (DP * 2) % 256 == 192 ? DP : DP + 32) : DP + 8;
+};
+
+template <typename T, int FMT, int DP>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 && DP <= 128 ? 2 : 1))
+void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
+    using Sh = PrefillShape<T, DP>;
+    using E = typename KvElem<T, FMT>::type;
+    constexpr bool BF = Sh::BF;
+    constexpr int TOK = Sh::TOK, MT = Sh::MT, DT = Sh::DT, PE = Sh::PE, NP = Sh::NP, KS = Sh::KS, VS = Sh::VS;
+    constexpr int GW = PE * (int)sizeof(E) / 4;            // 32-bit words of a piece in the cache
+    __shared__ __align__(16) T s_k[2][TOK * KS];
+    __shared__ __align__(16) T s_v[2][TOK * VS];
+    __shared__ __align__(16) float s_ks[2][FMT == SSM_KV_ACT ? 4 : TOK], s_vs[2][FMT == SSM_KV_ACT ? 4 : TOK];
+    __shared__ int s_bad;
+
+    const KvArgs& a = p.kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+    const int it = (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
+    if (it >= plan.count[0]) return;
+    const AttnItem item = plan.items[it];
+    const KvSeq sq = kv_seq(a, item.seq);
+    const int g = a.Hq / a.Hkv, n = sq.n, before = sq.n - sq.m;
+    const int32_t* table = a.table + (int64_t)item.seq * a.max_pages;
+
+    if (tid == 0) s_bad = 0;
+    if (a.D < DP) {   // dims between D and DP are zero in k and v: q is zero there too
+        for (int i = tid; i < 2 * TOK * KS * (int)sizeof(T) / 4; i += 256) ((uint32_t*)&s_k[0][0])[i] = 0u;
+        for (int i = tid; i < 2 * TOK * VS * (int)sizeof(T) / 4; i += 256) ((uint32_t*)&s_v[0][0])[i] = 0u;
+    }
+    __syncthreads();
+    // pages that the table does not name: their tokens are masked one by one (below)
+    for (int i = (item.k0 >> a.page_log2) + tid; i <= ((min(item.k1, n) - 1) >> a.page_log2); i += 256) {
+        const int pg = table[i];
+        if (pg < 0 || pg >= a.num_pages) {
+            s_bad = 1;
+            atomicOr(a.status, SSM_STATUS_BAD_PAGE);
+        }
+    }
+
+    // this lane's query
+    const int row = item.row0 + wave * 32 + col;
+    const bool on = row < sq.m * g;
+    const int tok = (on ? row : item.row0) / g, hq = head * g + (on ? row : item.row0) % g;
+    const int pos = on ? before + tok : -1;
+    const int row_w = item.row0 + wave * 32;              // the wave's first and last position
+    const bool wave_on = row_w < sq.m * g;
+    const int pos_lo = before + (wave_on ? row_w : item.row0) / g;
+    const int pos_hi = before + min(row_w + 31, sq.m * g - 1) / g;
+    constexpr int QN = BF ? DP / 16 : DP / 8;              // q operands: 8 values per lane per 16 dims, 4 per 8
+    T q[QN][BF ? 8 : 4];
+    {
+        const T* qp = (const T*)p.q + (int64_t)(sq.lo + tok) * p.ld_q + (int64_t)hq * a.D;
+#pragma unroll
+        for (int s = 0; s < QN; ++s) {
+            const int d = BF ? s * 16 + half * 8 : s * 8 + half * 4;
+            if (on && d < a.D) {
+                load16(qp + d, q[s]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < (BF ? 8 : 4); ++e) q[s][e] = from_f32<T>(0.0f);
+            }
+        }
+    }
+
+    // staging: piece i of a step is token i / (DP / PE), values (i % (DP / PE)) PE ..
+    uint32_t rk[NP][GW], rv[NP][GW];
+    float rks = 0.0f, rvs = 0.0f;
+    auto fetch = [&](int tb) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int pc = tid + 256 * i, t = pc / (DP / PE), d = (pc % (DP / PE)) * PE, j = tb + t;
+#pragma unroll
+            for (int w = 0; w < GW; ++w) rk[i][w] = rv[i][w] = 0u;
+            if (j < n && d < a.D) {
+                const int pg = table[j >> a.page_log2];
+                if (pg >= 0 && pg < a.num_pages) {
+                    const int64_t o = kv_pool_row(a, pg, head, j) * a.D + d;
+                    __builtin_memcpy(rk[i], __builtin_assume_aligned((const E*)a.k + o, 4 * GW), 4 * GW);
+                    __builtin_memcpy(rv[i], __builtin_assume_aligned((const E*)a.v + o, 4 * GW), 4 * GW);
+                }
+            }
+        }
+        if constexpr (FMT != SSM_KV_ACT) {
+            rks = rvs = 0.0f;
+            if (tid < TOK && tb + tid < n) {
+                const int pg = table[(tb + tid) >> a.page_log2];
+                if (pg >= 0 && pg < a.num_pages) {
+                    const int64_t r = kv_pool_row(a, pg, head, tb + tid);
+                    rks = a.ks[r];
+                    rvs = a.vs[r];
+                }
+            }
+        }
+    };
+    auto stage = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int pc = tid + 256 * i, t = pc / (DP / PE), d = (pc % (DP / PE)) * PE;
+            if (d >= a.D) continue;
+            u32x4 k, v;
+            if constexpr (FMT == SSM_KV_ACT) {
+                k = u32x4{rk[i][0], rk[i][1], rk[i][2], rk[i][3]};
+                v = u32x4{rv[i][0], rv[i][1], rv[i][2], rv[i][3]};
+            } else if constexpr (BF) {   // codes are exact in bf16; their scales wait for the scores
+                const u32x2 k0 = kv_decode4_bf16<FMT>(rk[i][0]), k1 = kv_decode4_bf16<FMT>(rk[i][GW - 1]);
+                const u32x2 v0 = kv_decode4_bf16<FMT>(rv[i][0]), v1 = kv_decode4_bf16<FMT>(rv[i][GW - 1]);
+                k = u32x4{k0[0], k0[1], k1[0], k1[1]};
+                v = u32x4{v0[0], v0[1], v1[0], v1[1]};
+            } else {
+                float x[4], y[4];
+                kv_decode4<FMT>(rk[i][0], x);
+                kv_decode4<FMT>(rv[i][0], y);
+                __builtin_memcpy(&k, x, 16);
+                __builtin_memcpy(&v, y, 16);
+            }
+            *(u32x4*)&s_k[b][t * KS + d] = k;
+            *(u32x4*)&s_v[b][t * VS + d] = v;
+        }
+        if constexpr (FMT != SSM_KV_ACT) {
+            if (tid < TOK) {
+                s_ks[b][tid] = rks;
+                s_vs[b][tid] = rvs;
+            }
+        }
+    };
+
+    const float c2 = a.scale * kLog2e;
+    float m = -3.0e38f, l = 0.0f;   // finite, so that differences are numbers before any token is seen
+    f32x16 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+
+    fetch(item.k0);
+    stage(0);
+    __syncthreads();
+    const bool bad = s_bad != 0;
+    int b = 0;
+    for (int tb = item.k0; tb < item.k1; tb += TOK, b ^= 1) {
+        const bool more = tb + TOK < item.k1;
+        if (more) fetch(tb + TOK);
+        const bool seen = wave_on && tb <= pos_hi && (a.window <= 0 || tb + TOK - 1 > pos_lo - a.window);
+        if (seen) {
+            f32x16 s[MT];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < QN; ++k)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    if constexpr (BF) {
+                        const bf16x8 kf = *(const bf16x8*)&s_k[b][(t * 32 + col) * KS + k * 16 + half * 8];
+                        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, q[k]), s[t], 0, 0, 0);
+                    } else {
+                        const f32x4 kf = *(const f32x4*)&s_k[b][(t * 32 + col) * KS + k * 8 + half * 4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q[k][e], s[t], 0, 0, 0);
+                    }
+                }
+            if constexpr (FMT != SSM_KV_ACT) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const f32x4 sc = *(const f32x4*)&s_ks[b][t * 32 + 8 * w + 4 * half];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[t][4 * w + e] *= sc[e];
+                    }
+            }
+            const bool edge = tb + TOK - 1 > pos_lo || (a.window > 0 && tb <= pos_hi - a.window);
+            if (edge || bad) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = tb + t * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+                        bool see = j <= pos && (a.window <= 0 || j > pos - a.window);
+                        if (bad && see) {
+                            const int pg = table[j >> a.page_log2];
+                            see = pg >= 0 && pg < a.num_pages;
+                        }
+                        s[t][r] = see ? s[t][r] : -__builtin_inff();
+                    }
+            }
+            float mx = s[0][0];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float mn = fmaxf(m, mx * c2);
+            if (__any(mn > m)) {
+                const float al = fast_exp2(m - mn);
+                l *= al;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= al;
+                m = mn;
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[t][r] = fast_exp2(__builtin_fmaf(s[t][r], c2, -mn));
+                    l += s[t][r];
+                }
+            if constexpr (FMT != SSM_KV_ACT) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const f32x4 sc = *(const f32x4*)&s_vs[b][t * 32 + 8 * w + 4 * half];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[t][4 * w + e] *= sc[e];
+                    }
+            }
+            if constexpr (BF) {
+                // the probabilities enter the product in bf16, half a step (2^-9) off each, as v itself
+                // is stored; the sum l is of the unrounded ones
+#pragma unroll
+                for (int ks = 0; ks < TOK / 16; ++ks) {
+                    bf16x8 pf;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pf[e] = (bf16)s[ks >> 1][8 * (ks & 1) + e];
+                    const T* vp = &s_v[b][(16 * ks + 4 * half + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4];
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        typedef short s16x4 __attribute__((ext_vector_type(4)));
+                        typedef __attribute__((address_space(3))) s16x4* lds4;
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp + t * 32));
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp + 8 * VS + t * 32));
+                        const auto vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[t], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const T* vp = &s_v[b][(8 * (r >> 2) + 4 * half + (r & 3)) * VS + col];
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[t * 32], s[0][r], o[t], 0, 0, 0);
+                }
+            }
+        }
+        if (more) stage(b ^ 1);
+        __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    if (item.part < 0) {
+        if (!on) return;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;   // nothing visible: zeros
+        T* out = (T*)p.o + (int64_t)(sq.lo + tok) * p.ld_o + (int64_t)hq * a.D;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int d = t * 32 + 8 * w + 4 * half;
+                if (d < a.D) {
+                    T y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(o[t][4 * w + e] * inv);
+                    __builtin_memcpy(__builtin_assume_aligned(out + d, 4 * sizeof(T)), y, sizeof y);
+                }
+            }
+    } else if (wave_on) {
+        float* part = plan.parts + ((int64_t)head * plan.max_parts + item.part) * kTileRows * (DP + 2);
+        const int r0 = wave * 32 + col;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+                *(float4*)(part + (int64_t)r0 * DP + t * 32 + 8 * w + 4 * half) =
+                    make_float4(o[t][4 * w], o[t][4 * w + 1], o[t][4 * w + 2], o[t][4 * w + 3]);
+        if (half == 0) {
+            part[kTileRows * DP + r0] = m;
+            part[kTileRows * (DP + 1) + r0] = l;
+        }
+    }
+}
+
+// 16 rows of a cut tile per workgroup: the partial results of its items, in order
+template <typename T, int DP> __global__ __launch_bounds__(256) void attn_prefill_join_kernel(AttnArgs p, AttnPlan plan) {
+    const KvArgs& a = p.kv;
+    const int ji = (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
+    if (ji >= plan.count[1]) return;
+    const AttnJoin jn = plan.joins[ji];
+    const KvSeq sq = kv_seq(a, jn.seq);
+    const int g = a.Hq / a.Hkv;
+    const float* part = plan.parts + ((int64_t)head * plan.max_parts + jn.part) * kTileRows * (DP + 2);
+    const int64_t stride = (int64_t)kTileRows * (DP + 2);
+    const int d4 = a.D / 4;
+    for (int k = threadIdx.x; k < 16 * d4; k += 256) {
+        const int r = (int)blockIdx.y * 16 + k / d4, d = (k % d4) * 4, row = jn.row0 + r;
+        if (row >= sq.m * g) continue;
+        float M = -3.0e38f;
+        for (int v = 0; v < jn.pieces; ++v) M = fmaxf(M, part[v * stride + kTileRows * DP + r]);
+        float o[4] = {0, 0, 0, 0}, ls = 0.0f;
+        for (int v = 0; v < jn.pieces; ++v) {
+            const float* s = part + v * stride;
+            const float f = fast_exp2(s[kTileRows * DP + r] - M);
+            const float4 x = *(const float4*)(s + (int64_t)r * DP + d);
+            ls += f * s[kTileRows * (DP + 1) + r];
+            o[0] += f * x.x; o[1] += f * x.y; o[2] += f * x.z; o[3] += f * x.w;
+        }
+        const float inv = ls > 0.0f ? 1.0f / ls : 0.0f;
+        T y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(o[e] * inv);
+        T* out = (T*)p.o + (int64_t)(sq.lo + row / g) * p.ld_o + (int64_t)(head * g + row % g) * a.D + d;
+        __builtin_memcpy(__builtin_assume_aligned(out, 4 * sizeof(T)), y, sizeof y);
+    }
+}
+
+template <typename T, int FMT, int DP>
+hipError_t launch_attn_prefill_tile(const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
+    KernelTimer kt("attn.prefill", s);
+    SSM_LAUNCH((attn_prefill_kernel<T, FMT, DP>), dim3((unsigned)pl.max_items * p.kv.Hkv), dim3(256), 0, s, p, pl);
+    hipError_t e = hipGetLastError();
+    const int64_t longest = (int64_t)p.kv.max_pages << p.kv.page_log2;
+    if (e != hipSuccess || longest <= kMinSteps * kStep) return e;   // no tile is ever cut
+    KernelTimer kj("attn.prefill_join", s);
+    SSM_LAUNCH((attn_prefill_join_kernel<T, DP>), dim3((unsigned)pl.max_joins * p.kv.Hkv, kTileRows / 16), dim3(256), 0, s, p, pl);
+    return hipGetLastError();
+}
+
+// the instances of one padded width, one file each
+#define SSM_ATTN_PREFILL_BF16(DP)                                                                             \
+    template hipError_t launch_attn_prefill_tile<bf16, SSM_KV_ACT, DP>(const AttnArgs&, const AttnPlan&, hipStream_t);      \
+    template hipError_t launch_attn_prefill_tile<bf16, SSM_KV_FP8_E4M3, DP>(const AttnArgs&, const AttnPlan&, hipStream_t); \
+    template hipError_t launch_attn_prefill_tile<bf16, SSM_KV_INT8, DP>(const AttnArgs&, const AttnPlan&, hipStream_t);
+#define SSM_ATTN_PREFILL_F32(DP)                                                                              \
+    template hipError_t launch_attn_prefill_tile<float, SSM_KV_ACT, DP>(const AttnArgs&, const AttnPlan&, hipStream_t);      \
+    template hipError_t launch_attn_prefill_tile<float, SSM_KV_FP8_E4M3, DP>(const AttnArgs&, const AttnPlan&, hipStream_t); \
+    template hipError_t launch_attn_prefill_tile<float, SSM_KV_INT8, DP>(const AttnArgs&, const AttnPlan&, hipStream_t);
+
+}  // namespace ssm

@@ -393,4 +393,40 @@ hipError_t launch_residual_rmsnorm_slices(float* resid, const float* parts, int 
                                           int64_t T, int d, hipStream_t s);
 hipError_t launch_bcdt_rms(float* x, int64_t T, int R, int N, int64_t ld, float eps, hipStream_t s);
 
+// ---------------------------------------------------------------- paged attention cache
+// The token-indexed cache of an attention layer and one call's sequences in it (ssm_kv_pool_t,
+// ssm_kv_meta_t). A page holds [kv_heads][page_size][head_dim] of k and of v; page_size is a power
+// of two of at least 16, so 16 consecutive tokens that start at a multiple of 16 share a page.
+struct KvArgs {
+    const int32_t* cu;       // [nseq + 1]; null: one token per sequence
+    const int32_t* kv_len;   // [nseq] cached tokens, this call's included
+    const int32_t* table;    // [nseq][max_pages]
+    void* k; void* v; float* ks; float* vs;
+    int32_t* status;
+    int64_t T;               // packed rows of the call
+    int nseq, max_pages, num_pages, page_log2;
+    int Hq, Hkv, D, fmt;     // fmt: SSM_KV_*
+    int window;              // 0: none
+    float scale;
+};
+struct KvAppendArgs {
+    KvArgs kv;
+    const void* qkv; int64_t ld;   // columns [q heads | k heads | v heads]
+    void* q; int64_t ld_q;
+    const float* q_w; const float* k_w; float eps;
+    const uint64_t* turns; int rot, inter;
+};
+hipError_t launch_kv_append(const KvAppendArgs& a, bool bf16_act, hipStream_t s);
+hipError_t launch_kv_read(const KvArgs& a, void* k, int64_t ld_k, void* v, int64_t ld_v, bool bf16_act, hipStream_t s);
+struct AttnArgs {
+    KvArgs kv;
+    const void* q; int64_t ld_q;
+    void* o; int64_t ld_o;
+    char* scratch;                 // the plan and the partial results (attn_*_scratch_bytes)
+};
+size_t attn_decode_scratch_bytes(int D, int64_t batch);
+hipError_t launch_attn_decode(const AttnArgs& a, bool bf16_act, hipStream_t s);
+size_t attn_prefill_scratch_bytes(bool bf16_act, int Hq, int Hkv, int D, int64_t T, int nseq);
+hipError_t launch_attn_prefill(const AttnArgs& a, bool bf16_act, hipStream_t s);
+
 }  // namespace ssm
