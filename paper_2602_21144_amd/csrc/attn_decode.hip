@@ -490,31 +490,14 @@ __global__ __launch_bounds__(256) void attn_decode_join_kernel(AttnArgs p, int w
     const int64_t rb = pl.base + (int64_t)row * nt, re = rb + nt;
     if (u == rb || prev > rb) return;
     const int head = row / rt, q0 = (row % rt) * kRows;
-    const int nq = g - q0 < kRows ? g - q0 : kRows, d4 = a.D / 4;
+    const int nq = g - q0 < kRows ? g - q0 : kRows;
     int last = w;   // the last workgroup with a part of the row
     while (last + 1 < pl.runs.cut && pl.runs.begin(last + 1) < re) ++last;
-    const int64_t stride = part_floats(DP);
     const float* part = (const float*)p.scratch;
-    for (int k = tid; k < nq * d4; k += 256) {
-        const int r = k / d4, d = (k % d4) * 4;
-        auto slot = [&](int v) { return part + (2 * (int64_t)v + (v == w - 1 ? 1 : 0)) * stride; };
-        float M = kNoMax;
-        for (int v = w - 1; v <= last; ++v) M = fmaxf(M, slot(v)[kRows * DP + r]);
-        float o[4] = {0, 0, 0, 0}, ls = 0.0f;
-        for (int v = w - 1; v <= last; ++v) {
-            const float* s = slot(v);
-            const float f = fast_exp2(s[kRows * DP + r] - M);
-            const float4 x = *(const float4*)(s + r * DP + d);
-            ls += f * s[kRows * DP + kRows + r];
-            o[0] += f * x.x; o[1] += f * x.y; o[2] += f * x.z; o[3] += f * x.w;
-        }
-        const float inv = ls > 0.0f ? 1.0f / ls : 0.0f;
-        T y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(o[e] * inv);
-        T* out = (T*)p.o + (int64_t)pl.seq * p.ld_o + (int64_t)(head * g + q0 + r) * a.D + d;
-        __builtin_memcpy(__builtin_assume_aligned(out, 4 * sizeof(T)), y, sizeof y);
-    }
+    auto slot = [&](int v) { return part + (2 * (int64_t)(w - 1) + (v == 0 ? 1 : 2 * v)) * part_floats(DP); };
+    for (int r = tid >> 6; r < nq; r += 4)
+        join_row<T>(last - w + 2, slot, r * DP, kRows * DP + r, kRows * DP + kRows + r, a.D,
+                    (T*)p.o + (int64_t)pl.seq * p.ld_o + (int64_t)(head * g + q0 + r) * a.D);
 }
 
 int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }

@@ -24,6 +24,7 @@ __device__ __forceinline__ TileRange tile_range(const KvArgs& a, const KvSeq& s,
 // where partial results lie, never what is added to what.
 __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnPlan p) {
     __shared__ int s_wave[kPlanThreads / 64];
+    __shared__ int32_t s_prefix[kPlanThreads];
     __shared__ int s_bin[kBins], s_part, s_join;
     __shared__ unsigned long long s_steps;
     const int tid = threadIdx.x, lane = tid & 63, g = a.Hq / a.Hkv;
@@ -54,10 +55,12 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         if (k < (tid >> 6)) at += s_wave[k];
         total += s_wave[k];
     }
+    // the tiles before every sequence: in LDS where they fit
+    int32_t* prefix = a.nseq <= kPlanThreads ? s_prefix : p.prefix;
     for (int k = 0; k < per; ++k) {
         const int i = tid * per + k;
         if (i < a.nseq) {
-            p.prefix[i] = at;
+            prefix[i] = at;
             at += tiles_of(i);
         }
     }
@@ -66,21 +69,29 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         total = p.max_tiles;
     }
     __syncthreads();
-    auto seq_of = [&](int t) {   // the last sequence whose tiles begin at or before t
+    struct Tile { int seq, row0; TileRange r; };
+    auto tile = [&](int t) {   // its sequence is the last one whose tiles begin at or before t
         int i = 0, e = a.nseq;
         while (e - i > 1) {
             const int mid = (i + e) >> 1;
-            if (p.prefix[mid] <= t) i = mid;
+            if (prefix[mid] <= t) i = mid;
             else e = mid;
         }
-        return i;
+        const int row0 = (t - prefix[i]) * kTileRows;
+        return Tile{i, row0, tile_range(a, kv_seq(a, i), g, row0)};
+    };
+    // a thread keeps its first tile over the three passes
+    Tile first{};
+    if (tid < total) first = tile(tid);
+    auto each = [&](auto f) {
+        if (tid < total) f(first);
+        for (int t = tid + kPlanThreads; t < total; t += kPlanThreads) f(tile(t));
     };
     unsigned long long steps = 0;
-    for (int t = tid; t < total; t += kPlanThreads) {
-        const int i = seq_of(t);
-        steps += tile_range(a, kv_seq(a, i), g, (t - p.prefix[i]) * kTileRows).steps;
-    }
-    atomicAdd(&s_steps, steps);
+    each([&](const Tile& x) { steps += x.r.steps; });
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) steps += __shfl_xor(steps, off, 64);
+    if (lane == 0 && steps) atomicAdd(&s_steps, steps);
     __syncthreads();
     const unsigned long long share = (s_steps * a.Hkv + kTarget - 1) / kTarget;
     const int most = share < kMinSteps ? kMinSteps : (int)share;   // steps of the longest item
@@ -89,40 +100,39 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         len = (r.steps + pieces - 1) / pieces;
         if (pieces > 1) pieces = (r.steps + len - 1) / len;
     };
-    auto bin_of = [&](int len) { return kBins - 1 - (int)((int64_t)len * kBins / (most + 1)); };
-    for (int t = tid; t < total; t += kPlanThreads) {
-        const int i = seq_of(t);
+    auto bin_of = [&](int len) { return kBins - 1 - (int)((uint32_t)len * kBins / (uint32_t)(most + 1)); };
+    each([&](const Tile& x) {
         int pieces, len;
-        cut(tile_range(a, kv_seq(a, i), g, (t - p.prefix[i]) * kTileRows), pieces, len);
+        cut(x.r, pieces, len);
         atomicAdd(&s_bin[bin_of(len)], pieces);
-    }
+    });
     __syncthreads();
-    if (tid == 0) {
-        int n = 0;
-        for (int k = 0; k < kBins; ++k) {
-            const int c = s_bin[k];
-            s_bin[k] = n;
-            n += c;
+    if (tid < 64) {
+        const int c = tid < kBins ? s_bin[tid] : 0;
+        int n = c;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int o = __shfl_up(n, off, 64);
+            if (lane >= off) n += o;
         }
-        p.count[0] = n;
+        if (tid < kBins) s_bin[tid] = n - c;
+        if (tid == 63) p.count[0] = n;
     }
     __syncthreads();
-    for (int t = tid; t < total; t += kPlanThreads) {
-        const int i = seq_of(t), row0 = (t - p.prefix[i]) * kTileRows;
-        const TileRange r = tile_range(a, kv_seq(a, i), g, row0);
+    each([&](const Tile& x) {
         int pieces, len;
-        cut(r, pieces, len);
+        cut(x.r, pieces, len);
         const int pos = atomicAdd(&s_bin[bin_of(len)], pieces);
         int part = -1;
         if (pieces > 1) {
             part = atomicAdd(&s_part, pieces);
-            p.joins[atomicAdd(&s_join, 1)] = AttnJoin{i, row0, part, pieces};
+            p.joins[atomicAdd(&s_join, 1)] = AttnJoin{x.seq, x.row0, part, pieces};
         }
         for (int k = 0; k < pieces; ++k) {
-            const int k0 = r.k0 + k * len * kStep;
-            p.items[pos + k] = AttnItem{i, row0, k0, min(r.k1, k0 + len * kStep), pieces > 1 ? part + k : -1, {0, 0, 0}};
+            const int k0 = x.r.k0 + k * len * kStep;
+            p.items[pos + k] = AttnItem{x.seq, x.row0, k0, min(x.r.k1, k0 + len * kStep), pieces > 1 ? part + k : -1, {0, 0, 0}};
         }
-    }
+    });
     __syncthreads();
     if (tid == 0) p.count[1] = s_join;
 }

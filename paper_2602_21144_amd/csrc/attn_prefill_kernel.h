@@ -17,6 +17,8 @@ template <typename T, int DP> struct PrefillShape {
     static constexpr int VS = BF ? ((DP * 2) % 256 == 64 || (DP * 2) % 256 == 192 ? DP : DP + 32) : DP + 8;
 };
 
+constexpr float kLag = 8.0f;
+
 template <typename T, int FMT, int DP>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 && DP <= 128 ? 2 : 1))
 void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
@@ -40,10 +42,6 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     const int32_t* table = a.table + (int64_t)item.seq * a.max_pages;
 
     if (tid == 0) s_bad = 0;
-    if (a.D < DP) {   // dims between D and DP are zero in k and v: q is zero there too
-        for (int i = tid; i < 2 * TOK * KS * (int)sizeof(T) / 4; i += 256) ((uint32_t*)&s_k[0][0])[i] = 0u;
-        for (int i = tid; i < 2 * TOK * VS * (int)sizeof(T) / 4; i += 256) ((uint32_t*)&s_v[0][0])[i] = 0u;
-    }
     __syncthreads();
     // pages that the table does not name: their tokens are masked one by one (below)
     for (int i = (item.k0 >> a.page_log2) + tid; i <= ((min(item.k1, n) - 1) >> a.page_log2); i += 256) {
@@ -79,41 +77,60 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         }
     }
 
-    // staging: piece i of a step is token i / (DP / PE), values (i % (DP / PE)) PE ..
+    // Staging: wave w brings the step's tokens of one block of 16 (two waves share a block of a float32
+    // step), which lie on one page, through a buffer resource that ends behind the sequence's last
+    // token: what is not there reads as zero, and a lane's offsets never change. The block's page is
+    // looked up one step before its loads are issued.
+    constexpr int PR = DP / PE;                            // pieces per row
+    const int blk = BF ? wave : wave >> 1;                 // the wave's block of the step
+    uint32_t off[NP];                                      // byte offset of piece i in its block
+    int at_k[NP], at_v[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int pc = ((BF ? 0 : (wave & 1) * NP) + i) * 64 + lane, t = pc / PR, d = (pc % PR) * PE;
+        off[i] = d < a.D ? (uint32_t)((t * a.D + d) * (int)sizeof(E)) : kOffOutOfRange;
+        at_k[i] = (16 * blk + t) * KS + d;
+        at_v[i] = (16 * blk + t) * VS + d;
+    }
     uint32_t rk[NP][GW], rv[NP][GW];
-    float rks = 0.0f, rvs = 0.0f;
-    auto fetch = [&](int tb) {
+    uint32_t rks = 0, rvs = 0;
+    auto page_at = [&](int tb) {                           // the table entry of the wave's block, if there is one
+        const int j = tb + 16 * blk;
+        return j < n ? table[j >> a.page_log2] : -1;
+    };
+    auto fetch = [&](int tb, int page) {
+        const int pg = __builtin_amdgcn_readfirstlane(page), j = tb + 16 * blk;
+        const bool there = pg >= 0 && pg < a.num_pages;
+        const int tokens = there ? min(n - j, 16) : 0;     // pg -1 where n <= j
+        const int64_t r = there ? kv_pool_row(a, pg, head, j) : 0;
+        const uint32_t bytes = (uint32_t)(tokens * a.D * (int)sizeof(E));
+        const auto k_src = buffer_rsrc((const E*)a.k + r * a.D, bytes), v_src = buffer_rsrc((const E*)a.v + r * a.D, bytes);
+        auto load = [&](__amdgpu_buffer_rsrc_t src, uint32_t o, uint32_t (&x)[GW]) {
+            if constexpr (GW == 4) {
+                const u32x4 w = buffer_load16(src, o);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int pc = tid + 256 * i, t = pc / (DP / PE), d = (pc % (DP / PE)) * PE, j = tb + t;
+                for (int e = 0; e < 4; ++e) x[e] = w[e];
+            } else if constexpr (GW == 2) {
+                const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(src, (int)o, 0, 0);
+                x[0] = w[0];
+                x[1] = w[1];
+            } else {
+                x[0] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)o, 0, 0);
+            }
+        };
 #pragma unroll
-            for (int w = 0; w < GW; ++w) rk[i][w] = rv[i][w] = 0u;
-            if (j < n && d < a.D) {
-                const int pg = table[j >> a.page_log2];
-                if (pg >= 0 && pg < a.num_pages) {
-                    const int64_t o = kv_pool_row(a, pg, head, j) * a.D + d;
-                    __builtin_memcpy(rk[i], __builtin_assume_aligned((const E*)a.k + o, 4 * GW), 4 * GW);
-                    __builtin_memcpy(rv[i], __builtin_assume_aligned((const E*)a.v + o, 4 * GW), 4 * GW);
-                }
-            }
-        }
-        if constexpr (FMT != SSM_KV_ACT) {
-            rks = rvs = 0.0f;
-            if (tid < TOK && tb + tid < n) {
-                const int pg = table[(tb + tid) >> a.page_log2];
-                if (pg >= 0 && pg < a.num_pages) {
-                    const int64_t r = kv_pool_row(a, pg, head, tb + tid);
-                    rks = a.ks[r];
-                    rvs = a.vs[r];
-                }
-            }
+        for (int i = 0; i < NP; ++i) load(k_src, off[i], rk[i]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) load(v_src, off[i], rv[i]);
+        if constexpr (FMT != SSM_KV_ACT) {                 // lanes 0 .. 15 bring the block's scales
+            const uint32_t so = lane < 16 ? 4 * lane : kOffOutOfRange;
+            rks = __builtin_amdgcn_raw_buffer_load_b32(buffer_rsrc(a.ks + r, 4 * tokens), (int)so, 0, 0);
+            rvs = __builtin_amdgcn_raw_buffer_load_b32(buffer_rsrc(a.vs + r, 4 * tokens), (int)so, 0, 0);
         }
     };
     auto stage = [&](int b) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int pc = tid + 256 * i, t = pc / (DP / PE), d = (pc % (DP / PE)) * PE;
-            if (d >= a.D) continue;
             u32x4 k, v;
             if constexpr (FMT == SSM_KV_ACT) {
                 k = u32x4{rk[i][0], rk[i][1], rk[i][2], rk[i][3]};
@@ -130,13 +147,13 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                 __builtin_memcpy(&k, x, 16);
                 __builtin_memcpy(&v, y, 16);
             }
-            *(u32x4*)&s_k[b][t * KS + d] = k;
-            *(u32x4*)&s_v[b][t * VS + d] = v;
+            *(u32x4*)&s_k[b][at_k[i]] = k;
+            *(u32x4*)&s_v[b][at_v[i]] = v;
         }
         if constexpr (FMT != SSM_KV_ACT) {
-            if (tid < TOK) {
-                s_ks[b][tid] = rks;
-                s_vs[b][tid] = rvs;
+            if (lane < 16) {
+                s_ks[b][16 * blk + lane] = __builtin_bit_cast(float, rks);
+                s_vs[b][16 * blk + lane] = __builtin_bit_cast(float, rvs);
             }
         }
     };
@@ -149,14 +166,18 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
 
-    fetch(item.k0);
+    fetch(item.k0, page_at(item.k0));
+    int page = page_at(item.k0 + TOK);
     stage(0);
     __syncthreads();
     const bool bad = s_bad != 0;
     int b = 0;
     for (int tb = item.k0; tb < item.k1; tb += TOK, b ^= 1) {
         const bool more = tb + TOK < item.k1;
-        if (more) fetch(tb + TOK);
+        if (more) {
+            fetch(tb + TOK, page);
+            page = page_at(tb + 2 * TOK);
+        }
         const bool seen = wave_on && tb <= pos_hi && (a.window <= 0 || tb + TOK - 1 > pos_lo - a.window);
         if (seen) {
             f32x16 s[MT];
@@ -210,7 +231,9 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                 for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             const float mn = fmaxf(m, mx * c2);
-            if (__any(mn > m)) {
+            // The sums are kept relative to m, which need not be the maximum itself: it follows once the
+            // maximum is kLag powers of two above it (then no p is above 2^kLag, and no digit is lost)
+            if (__any(mn > m + kLag)) {
                 const float al = fast_exp2(m - mn);
                 l *= al;
 #pragma unroll
@@ -221,7 +244,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[t][r] = fast_exp2(__builtin_fmaf(s[t][r], c2, -mn));
+                    s[t][r] = fast_exp2(__builtin_fmaf(s[t][r], c2, -m));
                     l += s[t][r];
                 }
             if constexpr (FMT != SSM_KV_ACT) {
@@ -299,37 +322,19 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     }
 }
 
-// 16 rows of a cut tile per workgroup: the partial results of its items, in order
+// Four rows of a cut tile per workgroup, one to a wave: the partial results of its items, in order
 template <typename T, int DP> __global__ __launch_bounds__(256) void attn_prefill_join_kernel(AttnArgs p, AttnPlan plan) {
     const KvArgs& a = p.kv;
     const int ji = (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
     if (ji >= plan.count[1]) return;
     const AttnJoin jn = plan.joins[ji];
     const KvSeq sq = kv_seq(a, jn.seq);
-    const int g = a.Hq / a.Hkv;
-    const float* part = plan.parts + ((int64_t)head * plan.max_parts + jn.part) * kTileRows * (DP + 2);
-    const int64_t stride = (int64_t)kTileRows * (DP + 2);
-    const int d4 = a.D / 4;
-    for (int k = threadIdx.x; k < 16 * d4; k += 256) {
-        const int r = (int)blockIdx.y * 16 + k / d4, d = (k % d4) * 4, row = jn.row0 + r;
-        if (row >= sq.m * g) continue;
-        float M = -3.0e38f;
-        for (int v = 0; v < jn.pieces; ++v) M = fmaxf(M, part[v * stride + kTileRows * DP + r]);
-        float o[4] = {0, 0, 0, 0}, ls = 0.0f;
-        for (int v = 0; v < jn.pieces; ++v) {
-            const float* s = part + v * stride;
-            const float f = fast_exp2(s[kTileRows * DP + r] - M);
-            const float4 x = *(const float4*)(s + (int64_t)r * DP + d);
-            ls += f * s[kTileRows * (DP + 1) + r];
-            o[0] += f * x.x; o[1] += f * x.y; o[2] += f * x.z; o[3] += f * x.w;
-        }
-        const float inv = ls > 0.0f ? 1.0f / ls : 0.0f;
-        T y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(o[e] * inv);
-        T* out = (T*)p.o + (int64_t)(sq.lo + row / g) * p.ld_o + (int64_t)(head * g + row % g) * a.D + d;
-        __builtin_memcpy(__builtin_assume_aligned(out, 4 * sizeof(T)), y, sizeof y);
-    }
+    const int g = a.Hq / a.Hkv, r = (int)blockIdx.y * 4 + (threadIdx.x >> 6), row = jn.row0 + r;
+    if (row >= sq.m * g) return;
+    constexpr int64_t stride = (int64_t)kTileRows * (DP + 2);
+    const float* part = plan.parts + ((int64_t)head * plan.max_parts + jn.part) * stride;
+    join_row<T>(jn.pieces, [&](int v) { return part + v * stride; }, (int64_t)r * DP, kTileRows * DP + r,
+                kTileRows * (DP + 1) + r, a.D, (T*)p.o + (int64_t)(sq.lo + row / g) * p.ld_o + (int64_t)(head * g + row % g) * a.D);
 }
 
 template <typename T, int FMT, int DP>
@@ -340,7 +345,7 @@ hipError_t launch_attn_prefill_tile(const AttnArgs& p, const AttnPlan& pl, hipSt
     const int64_t longest = (int64_t)p.kv.max_pages << p.kv.page_log2;
     if (e != hipSuccess || longest <= kMinSteps * kStep) return e;   // no tile is ever cut
     KernelTimer kj("attn.prefill_join", s);
-    SSM_LAUNCH((attn_prefill_join_kernel<T, DP>), dim3((unsigned)pl.max_joins * p.kv.Hkv, kTileRows / 16), dim3(256), 0, s, p, pl);
+    SSM_LAUNCH((attn_prefill_join_kernel<T, DP>), dim3((unsigned)pl.max_joins * p.kv.Hkv, kTileRows / 4), dim3(256), 0, s, p, pl);
     return hipGetLastError();
 }
 
