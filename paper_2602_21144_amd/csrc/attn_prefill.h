@@ -1,7 +1,7 @@
 // Causal attention of packed prompt chunks over the paged cache.
 //
 // The g = q_heads / kv_heads query heads of a kv head are stacked on the tokens: row r of a sequence's
-// m g rows is token r / g, head r % g. A tile is kTileRows of these rows; a wave holds 32 of them as the
+// m g rows is token r / g, head r % g. A tile is tile_rows() of these rows; a wave holds 32 of them as the
 // columns of its products, in registers from first to last:
 //   S^T = K Q^T    on 32x32 tiles; a lane holds 16 scores of one query per 32 tokens
 //   O^T = V^T P^T  the lane's scores are this product's operand as they stand: entries 8 s .. 8 s + 7 are
@@ -9,7 +9,7 @@
 //                  halves are the 16 tokens of one K-step once; v comes from LDS in that order, by the
 //                  transposing 64-bit LDS reads (bf16) or one value per lane (float32).
 // So the softmax needs one exchange between lanes per step (the maximum of the two halves), and the
-// rescale of O is one factor per lane. K and V steps of TOK tokens go through LDS, shared by the four
+// rescale of O is one factor per lane. K and V steps of TOK tokens go through LDS, shared by the
 // waves, in two buffers: the next step's loads are in flight while the present one is computed.
 //
 // Work: the plan kernel lists (tile, range of tokens) items so that no item is longer than a share of
@@ -21,7 +21,8 @@
 
 namespace ssm {
 
-constexpr int kTileRows = 128;
+// rows of a tile: 32 for each of 8 waves where two waves per SIMD have registers enough, else of 4
+constexpr int tile_rows(bool bf16_act, int DP) { return bf16_act && DP <= 128 ? 256 : 128; }
 constexpr int kStep = 64;          // the plan counts tokens in steps of this many
 constexpr int kTarget = 512;       // items of the whole work: two workgroups for each of 256 compute units
 constexpr int kMinSteps = 8;       // no item is cut shorter than this
@@ -33,14 +34,15 @@ struct AttnPlan {
     int32_t* prefix;     // [nseq + 1] tiles before each sequence
     AttnItem* items;
     AttnJoin* joins;
-    float* parts;        // [Hkv][max_parts][kTileRows (DP + 2)]
-    int max_tiles, max_items, max_joins, max_parts;
+    float* parts;        // [Hkv][max_parts][rows (DP + 2)]
+    int rows, max_tiles, max_items, max_joins, max_parts;
     size_t total;
 };
 // sizes for up to T rows of nseq sequences
-inline AttnPlan attn_plan(int Hq, int Hkv, int DP, int64_t T, int nseq, char* base) {
+inline AttnPlan attn_plan(bool bf16_act, int Hq, int Hkv, int DP, int64_t T, int nseq, char* base) {
     AttnPlan p{};
-    const int64_t tiles = (T * (Hq / Hkv) + kTileRows - 1) / kTileRows + nseq;
+    p.rows = tile_rows(bf16_act, DP);
+    const int64_t tiles = (T * (Hq / Hkv) + p.rows - 1) / p.rows + nseq;
     // cut tiles have more steps than a share of the work: their number and their items' are bounded by it
     const int64_t share = (kTarget + Hkv - 1) / Hkv + 1;
     p.max_tiles = (int)tiles;
@@ -53,7 +55,7 @@ inline AttnPlan attn_plan(int Hq, int Hkv, int DP, int64_t T, int nseq, char* ba
     p.prefix = (int32_t*)take((size_t)(nseq + 1) * 4);
     p.items = (AttnItem*)take((size_t)p.max_items * sizeof(AttnItem));
     p.joins = (AttnJoin*)take((size_t)p.max_joins * sizeof(AttnJoin));
-    p.parts = (float*)take((size_t)Hkv * p.max_parts * kTileRows * (DP + 2) * 4);
+    p.parts = (float*)take((size_t)Hkv * p.max_parts * p.rows * (DP + 2) * 4);
     p.total = off;
     return p;
 }

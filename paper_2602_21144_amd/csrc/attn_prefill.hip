@@ -9,8 +9,8 @@ constexpr int kBins = 32;
 
 // The steps of one tile: tokens [k0, k1) that its rows see
 struct TileRange { int k0, k1, steps; };
-__device__ __forceinline__ TileRange tile_range(const KvArgs& a, const KvSeq& s, int g, int row0) {
-    const int rows = s.m * g, last = min(row0 + kTileRows, rows) - 1;
+__device__ __forceinline__ TileRange tile_range(const KvArgs& a, const KvSeq& s, int g, int row0, int height) {
+    const int rows = s.m * g, last = min(row0 + height, rows) - 1;
     const int before = s.n - s.m, lo = before + row0 / g;
     TileRange r;
     r.k1 = before + last / g + 1;
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     const int per = (a.nseq + kPlanThreads - 1) / kPlanThreads;
     auto tiles_of = [&](int i) {
         const KvSeq s = kv_seq(a, i);
-        return s.ok ? (int)(((int64_t)s.m * g + kTileRows - 1) / kTileRows) : 0;
+        return s.ok ? (int)(((int64_t)s.m * g + p.rows - 1) / p.rows) : 0;
     };
     int sum = 0;
     for (int k = 0; k < per; ++k)
@@ -77,8 +77,8 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
             if (prefix[mid] <= t) i = mid;
             else e = mid;
         }
-        const int row0 = (t - prefix[i]) * kTileRows;
-        return Tile{i, row0, tile_range(a, kv_seq(a, i), g, row0)};
+        const int row0 = (t - prefix[i]) * p.rows;
+        return Tile{i, row0, tile_range(a, kv_seq(a, i), g, row0, p.rows)};
     };
     // a thread keeps its first tile over the three passes
     Tile first{};
@@ -170,12 +170,12 @@ template <typename T> hipError_t prefill_fmt(const AttnArgs& p, const AttnPlan& 
 }  // namespace
 
 size_t attn_prefill_scratch_bytes(bool bf16_act, int Hq, int Hkv, int D, int64_t T, int nseq) {
-    return T > 0 ? attn_plan(Hq, Hkv, padded_dim(bf16_act, D), T, nseq, nullptr).total : 0;
+    return T > 0 ? attn_plan(bf16_act, Hq, Hkv, padded_dim(bf16_act, D), T, nseq, nullptr).total : 0;
 }
 hipError_t launch_attn_prefill(const AttnArgs& p, bool bf16_act, hipStream_t s) {
     const KvArgs& a = p.kv;
     const int dp = padded_dim(bf16_act, a.D);
-    const AttnPlan pl = attn_plan(a.Hq, a.Hkv, dp, a.T, a.nseq, p.scratch);
+    const AttnPlan pl = attn_plan(bf16_act, a.Hq, a.Hkv, dp, a.T, a.nseq, p.scratch);
     KernelTimer kt("attn.prefill_plan", s);
     SSM_LAUNCH(attn_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, pl);
     const hipError_t e = hipGetLastError();
