@@ -19,6 +19,13 @@ template <typename T, int DP, int WAVES> struct PrefillShape {
 
 constexpr float kLag = 8.0f;
 
+// f over a value of the lane and of its partner in the other half of the wave
+template <typename F> __device__ __forceinline__ float over_halves(float x, F f) {
+    const uint32_t v = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return f(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
 template <typename T, int FMT, int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, (sizeof(T) == 2 && DP <= 128 ? 2 : 1))
 void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
@@ -30,7 +37,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     constexpr int GW = PE * (int)sizeof(E) / 4;            // 32-bit words of a piece in the cache
     __shared__ __align__(16) T s_k[2][TOK * KS];
     __shared__ __align__(16) T s_v[2][TOK * VS];
-    __shared__ __align__(16) float s_ks[2][FMT == SSM_KV_ACT ? 4 : TOK], s_vs[2][FMT == SSM_KV_ACT ? 4 : TOK];
+    __shared__ __align__(16) float s_ks[4][FMT == SSM_KV_ACT ? 4 : TOK], s_vs[4][FMT == SSM_KV_ACT ? 4 : TOK];
     __shared__ int s_bad;
 
     const KvArgs& a = p.kv;
@@ -98,42 +105,59 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     }
     uint32_t rk[NP][GW], rv[SPLIT ? 1 : NP][GW];           // SPLIT: rk holds what the wave brings
     uint32_t rks = 0, rvs = 0;
-    auto page_at = [&](int tb) {                           // the table entry of the wave's block, if there is one
-        const int j = tb + 16 * blk;
-        return j < n ? table[j >> a.page_log2] : -1;
+    auto page_at = [&](int tb) {                           // the table entry of the wave's block
+        return table[max(min(tb + 16 * blk, n - 1), 0) >> a.page_log2];
+    };
+    // a page is page_bytes long, the head's part of it begins at head_bytes (both below 2^30)
+    const uint32_t row_bytes = (uint32_t)(a.D * (int)sizeof(E)), page_mask = (1u << a.page_log2) - 1;
+    const uint32_t head_row = (uint32_t)head << a.page_log2, page_rows = (uint32_t)a.Hkv << a.page_log2;
+    const uint32_t head_bytes = head_row * row_bytes, page_bytes = page_rows * row_bytes;
+    const char* src = (const char*)(brings_v ? a.v : a.k);
+    // where the block's tokens are: the descriptor of what the wave brings
+    __amdgpu_buffer_rsrc_t from, from_v, from_s, from_vs;
+    auto locate = [&](int tb, int page) {
+        const int pg = __builtin_amdgcn_readfirstlane(page), j = tb + 16 * blk;
+        const bool there = (uint32_t)pg < (uint32_t)a.num_pages && j < n;
+        const uint32_t tokens = there ? (uint32_t)min(n - j, 16) : 0u, in_page = (uint32_t)j & page_mask;
+        const uint32_t page_at0 = there ? (uint32_t)pg : 0u;
+        const uint64_t o = (uint64_t)page_at0 * page_bytes + (head_bytes + in_page * row_bytes);
+        from = buffer_rsrc(src + o, tokens * row_bytes);
+        if constexpr (!SPLIT) from_v = buffer_rsrc((const char*)a.v + o, tokens * row_bytes);
+        if constexpr (FMT != SSM_KV_ACT) {
+            const uint64_t r = (uint64_t)page_at0 * page_rows + (head_row + in_page);
+            from_s = buffer_rsrc(a.ks + r, 4 * tokens);
+            from_vs = buffer_rsrc(a.vs + r, 4 * tokens);
+        }
+    };
+    auto load = [&](__amdgpu_buffer_rsrc_t r, uint32_t o, uint32_t (&x)[GW]) {
+        if constexpr (GW == 4) {
+            const u32x4 w = buffer_load16(r, o);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = w[e];
+        } else if constexpr (GW == 2) {
+            const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, (int)o, 0, 0);
+            x[0] = w[0];
+            x[1] = w[1];
+        } else {
+            x[0] = __builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0);
+        }
+    };
+    // Lanes 0 .. 15 of the waves that bring k bring the block's scales, of k and of v: four buffers of them,
+    // by the step, since a softmax half a step behind reads them later than the codes (below)
+    auto load_scales = [&] {
+        const uint32_t so = lane < 16 && !brings_v ? 4 * lane : kOffOutOfRange;
+        rks = __builtin_amdgcn_raw_buffer_load_b32(from_s, (int)so, 0, 0);
+        rvs = __builtin_amdgcn_raw_buffer_load_b32(from_vs, (int)so, 0, 0);
     };
     auto fetch = [&](int tb, int page) {
-        const int pg = __builtin_amdgcn_readfirstlane(page), j = tb + 16 * __builtin_amdgcn_readfirstlane(blk);
-        const bool there = pg >= 0 && pg < a.num_pages;
-        const int tokens = there ? min(n - j, 16) : 0;     // pg -1 where n <= j
-        const int64_t r = there ? kv_pool_row(a, pg, head, j) : 0;
-        const uint32_t bytes = (uint32_t)(tokens * a.D * (int)sizeof(E));
-        const auto k_src = buffer_rsrc((const E*)(brings_v ? a.v : a.k) + r * a.D, bytes);
-        auto load = [&](__amdgpu_buffer_rsrc_t src, uint32_t o, uint32_t (&x)[GW]) {
-            if constexpr (GW == 4) {
-                const u32x4 w = buffer_load16(src, o);
+        locate(tb, page);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = w[e];
-            } else if constexpr (GW == 2) {
-                const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(src, (int)o, 0, 0);
-                x[0] = w[0];
-                x[1] = w[1];
-            } else {
-                x[0] = __builtin_amdgcn_raw_buffer_load_b32(src, (int)o, 0, 0);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < NP; ++i) load(k_src, off[i], rk[i]);
+        for (int i = 0; i < NP; ++i) load(from, off[i], rk[i]);
         if constexpr (!SPLIT) {
-            const auto v_src = buffer_rsrc((const E*)a.v + r * a.D, bytes);
 #pragma unroll
-            for (int i = 0; i < NP; ++i) load(v_src, off[i], rv[i]);
+            for (int i = 0; i < NP; ++i) load(from_v, off[i], rv[i]);
         }
-        if constexpr (FMT != SSM_KV_ACT) {                 // lanes 0 .. 15 bring the block's scales
-            const uint32_t so = lane < 16 ? 4 * lane : kOffOutOfRange;
-            rks = __builtin_amdgcn_raw_buffer_load_b32(buffer_rsrc((brings_v ? a.vs : a.ks) + r, 4 * tokens), (int)so, 0, 0);
-            if constexpr (!SPLIT) rvs = __builtin_amdgcn_raw_buffer_load_b32(buffer_rsrc(a.vs + r, 4 * tokens), (int)so, 0, 0);
-        }
+        if constexpr (FMT != SSM_KV_ACT) load_scales();
     };
     auto piece = [&](const uint32_t (&w)[GW]) {            // 16 bytes of T
         u32x4 x;
@@ -149,19 +173,22 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         }
         return x;
     };
-    auto stage = [&](int b) {
-        T* to = brings_v ? &s_v[b][0] : &s_k[b][0];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            *(u32x4*)(to + at_k[i]) = piece(rk[i]);
-            if constexpr (!SPLIT) *(u32x4*)&s_v[b][at_v[i]] = piece(rv[i]);
-        }
+    auto stage_piece = [&](int b, int i) {
+        *(u32x4*)((brings_v ? &s_v[b][0] : &s_k[b][0]) + at_k[i]) = piece(rk[i]);
+        if constexpr (!SPLIT) *(u32x4*)&s_v[b][at_v[i]] = piece(rv[i]);
+    };
+    auto stage_scales = [&](int step) {
         if constexpr (FMT != SSM_KV_ACT) {
-            if (lane < 16) {
-                (brings_v ? s_vs : s_ks)[b][16 * blk + lane] = __builtin_bit_cast(float, rks);
-                if constexpr (!SPLIT) s_vs[b][16 * blk + lane] = __builtin_bit_cast(float, rvs);
+            if (lane < 16 && !brings_v) {
+                s_ks[step & 3][16 * blk + lane] = __builtin_bit_cast(float, rks);
+                s_vs[step & 3][16 * blk + lane] = __builtin_bit_cast(float, rvs);
             }
         }
+    };
+    auto stage = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) stage_piece(step & 1, i);
+        stage_scales(step);
     };
 
     const float c2 = a.scale * kLog2e;
@@ -214,26 +241,26 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         }
     };
     bool bad = false;
-    auto soften = [&](int tb, int b) {
+    auto soften = [&](int tb, int step) {
         if constexpr (FMT != SSM_KV_ACT) {
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const f32x4 sc = *(const f32x4*)&s_ks[b][t * 32 + 8 * w + 4 * half];
+                    const f32x4 sc = *(const f32x4*)&s_ks[step & 3][t * 32 + 8 * w + 4 * half];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[t][4 * w + e] *= sc[e];
                 }
         }
         const bool edge = tb + TOK - 1 > pos_lo || (a.window > 0 && tb <= pos_hi - a.window);
-        if (edge) {
+        if (edge) {   // the token of s[t][r] is a constant behind tb + 4 half
+            const int last = pos - tb - 4 * half, first = a.window > 0 ? last - a.window : -1;
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int j = tb + t * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    const bool see = j <= pos && (a.window <= 0 || j > pos - a.window);
-                    s[t][r] = see ? s[t][r] : -__builtin_inff();
+                    const int j = t * 32 + 8 * (r >> 2) + (r & 3);
+                    s[t][r] = j <= last && j > first ? s[t][r] : -__builtin_inff();
                 }
         }
         if (bad) {
@@ -251,7 +278,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = over_halves(mx, [](float x, float y) { return fmaxf(x, y); });
         const float mn = fmaxf(m, mx * c2);
         // The sums are kept relative to m, which need not be the maximum itself: it follows once the
         // maximum is kLag powers of two above it (then no p is above 2^kLag, and no digit is lost)
@@ -267,25 +294,36 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[t][r] = fast_exp2(__builtin_fmaf(s[t][r], c2, -m));
-                l += s[t][r];
+                if constexpr (!BF || FMT != SSM_KV_ACT) l += s[t][r];
             }
         if constexpr (FMT != SSM_KV_ACT) {
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const f32x4 sc = *(const f32x4*)&s_vs[b][t * 32 + 8 * w + 4 * half];
+                    const f32x4 sc = *(const f32x4*)&s_vs[step & 3][t * 32 + 8 * w + 4 * half];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[t][4 * w + e] *= sc[e];
                 }
         }
         if constexpr (BF) {
-            // the probabilities enter the product in bf16, half a step (2^-9) off each, as v itself
-            // is stored; the sum l is of the unrounded ones
+            // The probabilities enter the product in bf16, half a step (2^-9) off each, as v itself is
+            // stored. Their sum l is of the rounded ones where no scale of v is in them: two to an
+            // instruction, in float32, and the weights p / l add up to one.
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+            const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
+            float ls[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int ks = 0; ks < TOK / 16; ++ks)
+            for (int ks = 0; ks < TOK / 16; ++ks) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)s[ks >> 1][8 * (ks & 1) + e];
+                if constexpr (FMT == SSM_KV_ACT) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        ls[ks & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[ks][e], pf[ks][e + 1]}, one, ls[ks & 1], false);
+                }
+            }
+            if constexpr (FMT == SSM_KV_ACT) l += ls[0] + ls[1];
         }
     };
     auto values = [&](int b) {
@@ -316,42 +354,98 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     if constexpr (SPLIT) {
         // Two waves share a SIMD, one of each half of the workgroup: while one half is in its products,
         // the other is in its softmax, half a step behind. In phase 2 i the first half has the products
-        // V(i-1) P(i-1) and K(i) Q, the second half softmax i - 1 and the staging of V(i); in phase 2 i + 1
-        // the second half has its products and the first softmax i and the staging of K(i+1). K(i) is
-        // read in phases 2 i and 2 i + 1, V(i) in 2 i + 2 and 2 i + 3, so two buffers of each do.
+        // V(i-1) P(i-1) and K(i) Q and stages K(i+1), the second half has softmax i - 1; in phase 2 i + 1
+        // the second half has the same products and stages V(i), the first half has softmax i. K(i) is
+        // read in phases 2 i and 2 i + 1, V(i) in 2 i + 2 and 2 i + 3, so two buffers of each do. The
+        // scales of step i + 1 come with K(i+1) in phase 2 i and are read in 2 i + 3 and 2 i + 4, when those
+        // of the step behind it are there already: three buffers, taken as four.
+        //
+        // The products of a phase are one run of MFMAs, each fragment read kLead MFMAs ahead of its own
+        // (one wave alone: 69 cycles per MFMA as the compiler orders it, 41 so; the MFMA takes 32). The
+        // run never branches: P is zero where a step is not seen or not there, and its scores are not used.
+        constexpr int kLead = 4, NV = DT * TOK / 16, NK = QN * MT;
         const int steps = (item.k1 - item.k0 + TOK - 1) / TOK;
+        const int lead = brings_v ? 0 : 1;                 // products(i) stages step i + lead
         fetch(item.k0, page_at(item.k0));
         int page = page_at(item.k0 + TOK);
-        auto bring = [&](int i) {                          // step i from registers to LDS, step i + 1 on its way
-            if (i < steps) {
-                stage(i & 1);
-                if (i + 1 < steps) {
-                    fetch(item.k0 + (i + 1) * TOK, page);
-                    page = page_at(item.k0 + (i + 2) * TOK);
-                }
+        for (int i = tid; i < TOK * VS * 2 / 16; i += 64 * WAVES) ((u32x4*)&s_v[1][0])[i] = u32x4{0, 0, 0, 0};   // V(-1)
+#pragma unroll
+        for (int ks = 0; ks < TOK / 16; ++ks)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)0.0f;
+        const T* v_at = &s_v[0][(4 * half + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4];
+        const T* k_at = &s_k[0][col * KS + half * 8];
+        bf16x8 fr[kLead + 1];
+        auto read = [&](int f, int i) {
+            if (f < NK) {
+                fr[f % (kLead + 1)] = *(const bf16x8*)(k_at + (i & 1) * TOK * KS + (f % MT) * 32 * KS + (f / MT) * 16);
+            } else {
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4* lds4;
+                const T* q = v_at + ((i - 1) & 1) * TOK * VS + ((f - NK) / DT) * 16 * VS + ((f - NK) % DT) * 32;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)q);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + 8 * VS));
+                fr[f % (kLead + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
+        auto read_first = [&](int i) {
+#pragma unroll
+            for (int f = 0; f < kLead; ++f) read(f, i);
+        };
         auto products = [&](int i) {
+            constexpr int kStage = NK + 2, kFetch = kStage + NP + 1;
+            static_assert(kFetch + NP + 1 <= NV + NK, "the run is long enough");
             __builtin_amdgcn_s_setprio(1);
-            if (i > 0 && seen(item.k0 + (i - 1) * TOK)) values((i - 1) & 1);
-            if (i < steps && seen(item.k0 + i * TOK)) scores(i & 1);
+#pragma unroll
+            for (int f = 0; f < NV + NK; ++f) {
+                if (f + kLead < NV + NK) read(f + kLead, i);
+                if (f < NK) {
+                    const int t = f % MT;
+                    if (f / MT == 0) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+                    }
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], __builtin_bit_cast(bf16x8, q[f / MT]), s[t], 0, 0, 0);
+                } else {
+                    const int t = (f - NK) % DT;
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], pf[(f - NK) / DT], o[t], 0, 0, 0);
+                }
+                // what the wave brings, one piece to an MFMA
+                if (f >= kStage && f < kStage + NP) stage_piece((i + lead) & 1, f - kStage);
+                if (f == kStage + NP) {
+                    stage_scales(i + lead);
+                    locate(item.k0 + (i + lead + 1) * TOK, page);
+                }
+                if (f >= kFetch && f < kFetch + NP) load(from, off[f - kFetch], rk[f - kFetch]);
+                if (f == kFetch + NP) {
+                    if constexpr (FMT != SSM_KV_ACT) load_scales();
+                    page = page_at(item.k0 + (i + lead + 2) * TOK);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
             __builtin_amdgcn_s_setprio(0);
         };
-        auto softmax = [&](int i) {
-            if (i < steps && seen(item.k0 + i * TOK)) soften(item.k0 + i * TOK, i & 1);
-        };
-        if (!brings_v) bring(0);
+        if (!brings_v) {                                   // K(0); the second half's V(0) waits for its first products
+            stage(0);
+            fetch(item.k0 + TOK, page);
+            page = page_at(item.k0 + 2 * TOK);
+        }
         __syncthreads();
         bad = s_bad != 0;
-        if (brings_v) {
-            bring(0);
-            __syncthreads();
-        }
+        read_first(0);
+        if (brings_v) __syncthreads();
         for (int i = 0; i <= steps; ++i) {
             products(i);
             __syncthreads();
-            bring(i + 1);
-            softmax(i);
+            if (i < steps && seen(item.k0 + i * TOK)) {
+                soften(item.k0 + i * TOK, i);
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < TOK / 16; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)0.0f;
+            }
+            read_first(i + 1);
             if (!brings_v || i < steps) __syncthreads();
         }
     } else {
@@ -360,24 +454,24 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         stage(0);
         __syncthreads();
         bad = s_bad != 0;
-        int b = 0;
-        for (int tb = item.k0; tb < item.k1; tb += TOK, b ^= 1) {
+        int step = 0;
+        for (int tb = item.k0; tb < item.k1; tb += TOK, ++step) {
             const bool more = tb + TOK < item.k1;
             if (more) {
                 fetch(tb + TOK, page);
                 page = page_at(tb + 2 * TOK);
             }
             if (seen(tb)) {
-                scores(b);
-                soften(tb, b);
-                values(b);
+                scores(step & 1);
+                soften(tb, step);
+                values(step & 1);
             }
-            if (more) stage(b ^ 1);
+            if (more) stage(step + 1);
             __syncthreads();
         }
     }
 
-    l += __shfl_xor(l, 32, 64);
+    l = over_halves(l, [](float x, float y) { return x + y; });
     if (item.part < 0) {
         if (!on) return;
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;   // nothing visible: zeros
