@@ -13,7 +13,7 @@
 // waves, in two buffers: the next step's loads are in flight while the present one is computed.
 //
 // Work: the plan kernel lists (tile, range of tokens) items so that no item is longer than a share of
-// the whole work (kTarget items of equal length); tiles behind a long cache are cut into several items
+// the whole work (tile_target() items of equal length); tiles behind a long cache are cut into several items
 // whose partial results (m, l and the unnormalised o, float32) a third kernel joins in order. Items are
 // listed longest first, and the workgroups of one item's kv heads are neighbours.
 #pragma once
@@ -21,30 +21,43 @@
 
 namespace ssm {
 
-// rows of a tile: 32 for each of 8 waves where two waves per SIMD have registers enough, else of 4
-constexpr int tile_rows(bool bf16_act, int DP) { return bf16_act && DP <= 128 ? 256 : 128; }
+// Rows of a tile: 32 for each of 4 waves, or of 8 for heads of 97 to 128 values where the tiles of 256 rows are
+// one for every compute unit and more. Kernel and join, 8 and 4 waves: 32 heads of 128, 8192 tokens 526 and 568
+// us, 4096 tokens 152 and 171; 16 heads of 112, 4096 tokens 104 and 107, three prompts of 2048 tokens in all, one
+// behind 4096, 57 and 43. Heads of 64 values, 16 of them, 6000 tokens: 114 and 108.
+inline int tile_rows(bool bf16_act, int DP, int64_t rows_heads) { return bf16_act && DP == 128 && rows_heads >= 65536 ? 256 : 128; }
 constexpr int kStep = 64;          // the plan counts tokens in steps of this many
-constexpr int kTarget = 512;       // items of the whole work: two workgroups for each of 256 compute units
-constexpr int kMinSteps = 8;       // no item is cut shorter than this
+// Workgroups that run at once: two on a compute unit where their registers allow it
+inline int tile_places(int rows, int DP) { return rows == 128 && DP <= 128 ? 512 : 256; }
+// Items that the whole work is cut into. Float32 is bound by its MFMAs, two workgroups sharing a unit's:
+// what counts is an even load, in short items whose beginnings and ends the other workgroup covers.
+// (2048 rows in three prompts, one behind 4096 tokens: 512 items of at least 8 steps 218 us, 1024 of at least
+// 4 192 us, their join 3 us more; 2048 200 us and 14 us more.)
+inline int tile_target(bool bf16_act, int rows, int DP) { return bf16_act ? tile_places(rows, DP) : 1024; }
+constexpr int tile_min_steps(bool bf16_act) { return bf16_act ? 8 : 4; }   // no item is cut shorter than this
 
-struct AttnItem { int32_t seq, row0, k0, k1, part, pad[3]; };   // part -1: the item is the whole tile
-struct AttnJoin { int32_t seq, row0, part, pieces; };
+// Tokens [k0, k1) for the tile at row0 of a sequence whose rows begin at lo (m tokens, n cached).
+// part: its partial result; -1: the item is the whole tile; -2: no item
+struct AttnItem { int32_t seq, row0, k0, k1, part, lo, m, n; };
+struct AttnJoin { int32_t row0, part, pieces, lo, m, pad[3]; };
 struct AttnPlan {
-    int32_t* count;      // [0] items, [1] joins
+    int32_t* count;      // joins
     int32_t* prefix;     // [nseq + 1] tiles before each sequence
     AttnItem* items;
     AttnJoin* joins;
     float* parts;        // [Hkv][max_parts][rows (DP + 2)]
-    int rows, max_tiles, max_items, max_joins, max_parts;
+    int rows, places, target, max_tiles, max_items, max_joins, max_parts;
     size_t total;
 };
 // sizes for up to T rows of nseq sequences
 inline AttnPlan attn_plan(bool bf16_act, int Hq, int Hkv, int DP, int64_t T, int nseq, char* base) {
     AttnPlan p{};
-    p.rows = tile_rows(bf16_act, DP);
+    p.rows = tile_rows(bf16_act, DP, T * Hq);
     const int64_t tiles = (T * (Hq / Hkv) + p.rows - 1) / p.rows + nseq;
     // cut tiles have more steps than a share of the work: their number and their items' are bounded by it
-    const int64_t share = (kTarget + Hkv - 1) / Hkv + 1;
+    p.places = tile_places(p.rows, DP);
+    p.target = tile_target(bf16_act, p.rows, DP);
+    const int64_t share = (p.target + Hkv - 1) / Hkv + 1;
     p.max_tiles = (int)tiles;
     p.max_items = (int)(tiles + share);
     p.max_joins = (int)(tiles < share ? tiles : share);

@@ -22,10 +22,11 @@ __device__ __forceinline__ TileRange tile_range(const KvArgs& a, const KvSeq& s,
 // One workgroup: tiles of every sequence, the length that no item exceeds, and the items in bins of
 // falling length. Places inside a bin come from LDS atomics: they settle which item runs first and
 // where partial results lie, never what is added to what.
-__global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnPlan p) {
+__global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnPlan p, bool bf16_act) {
     __shared__ int s_wave[kPlanThreads / 64];
     __shared__ int32_t s_prefix[kPlanThreads];
-    __shared__ int s_bin[kBins], s_part, s_join;
+    __shared__ int s_len[512];
+    __shared__ int s_bin[kBins], s_items, s_part, s_join;
     __shared__ unsigned long long s_steps;
     const int tid = threadIdx.x, lane = tid & 63, g = a.Hq / a.Hkv;
     kv_check_seqs(a, tid, kPlanThreads);
@@ -69,7 +70,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         total = p.max_tiles;
     }
     __syncthreads();
-    struct Tile { int seq, row0; TileRange r; };
+    struct Tile { int seq, row0; KvSeq s; TileRange r; };
     auto tile = [&](int t) {   // its sequence is the last one whose tiles begin at or before t
         int i = 0, e = a.nseq;
         while (e - i > 1) {
@@ -78,7 +79,8 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
             else e = mid;
         }
         const int row0 = (t - prefix[i]) * p.rows;
-        return Tile{i, row0, tile_range(a, kv_seq(a, i), g, row0, p.rows)};
+        const KvSeq s = kv_seq(a, i);
+        return Tile{i, row0, s, tile_range(a, s, g, row0, p.rows)};
     };
     // a thread keeps its first tile over the three passes
     Tile first{};
@@ -93,8 +95,27 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     for (int off = 32; off > 0; off >>= 1) steps += __shfl_xor(steps, off, 64);
     if (lane == 0 && steps) atomicAdd(&s_steps, steps);
     __syncthreads();
-    const unsigned long long share = (s_steps * a.Hkv + kTarget - 1) / kTarget;
-    const int most = share < kMinSteps ? kMinSteps : (int)share;   // steps of the longest item
+    const unsigned long long share = (s_steps * a.Hkv + p.target - 1) / p.target;
+    int most = share < (unsigned)tile_min_steps(bf16_act) ? tile_min_steps(bf16_act) : (int)share;   // steps of the longest item
+    // bf16, where a step waits more than it computes: if every tile has a place of its own at once, the cut is
+    // such that every item has (the first of 16 lengths, from an equal share to twice that, at which the items
+    // are no more than the places)
+    if (bf16_act && (int64_t)total * a.Hkv <= p.places) {
+        if (tid < total) s_len[tid] = first.r.steps;
+        __syncthreads();
+        const int len = most + most * (tid >> 6) / 16;
+        int items = 0;
+        for (int t = lane; t < total; t += 64) items += (s_len[t] + len - 1) / len;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) items += __shfl_xor(items, off, 64);
+        if (lane == 0) s_wave[tid >> 6] = (int64_t)items * a.Hkv <= p.places ? len : 2 * most;
+        __syncthreads();
+        for (int k = 0; k < kPlanThreads / 64; ++k)
+            if (s_wave[k] < 2 * most) {
+                most = s_wave[k];
+                break;
+            }
+    }
     auto cut = [&](const TileRange& r, int& pieces, int& len) {
         pieces = r.steps > most ? (r.steps + most - 1) / most : 1;
         len = (r.steps + pieces - 1) / pieces;
@@ -116,9 +137,10 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
             if (lane >= off) n += o;
         }
         if (tid < kBins) s_bin[tid] = n - c;
-        if (tid == 63) p.count[0] = n;
+        if (tid == 63) s_items = n;
     }
     __syncthreads();
+    for (int k = s_items + tid; k < p.max_items; k += kPlanThreads) p.items[k].part = -2;
     each([&](const Tile& x) {
         int pieces, len;
         cut(x.r, pieces, len);
@@ -126,15 +148,15 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         int part = -1;
         if (pieces > 1) {
             part = atomicAdd(&s_part, pieces);
-            p.joins[atomicAdd(&s_join, 1)] = AttnJoin{x.seq, x.row0, part, pieces};
+            p.joins[atomicAdd(&s_join, 1)] = AttnJoin{x.row0, part, pieces, x.s.lo, x.s.m, {0, 0, 0}};
         }
         for (int k = 0; k < pieces; ++k) {
             const int k0 = x.r.k0 + k * len * kStep;
-            p.items[pos + k] = AttnItem{x.seq, x.row0, k0, min(x.r.k1, k0 + len * kStep), pieces > 1 ? part + k : -1, {0, 0, 0}};
+            p.items[pos + k] = AttnItem{x.seq, x.row0, k0, min(x.r.k1, k0 + len * kStep), pieces > 1 ? part + k : -1, x.s.lo, x.s.m, x.s.n};
         }
     });
     __syncthreads();
-    if (tid == 0) p.count[1] = s_join;
+    if (tid == 0) p.count[0] = s_join;
 }
 
 // The width that a head's values are padded to in the products. Float32, whose rate is a sixteenth of
@@ -177,7 +199,7 @@ hipError_t launch_attn_prefill(const AttnArgs& p, bool bf16_act, hipStream_t s) 
     const int dp = padded_dim(bf16_act, a.D);
     const AttnPlan pl = attn_plan(bf16_act, a.Hq, a.Hkv, dp, a.T, a.nseq, p.scratch);
     KernelTimer kt("attn.prefill_plan", s);
-    SSM_LAUNCH(attn_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, pl);
+    SSM_LAUNCH(attn_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, pl, bf16_act);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     return bf16_act ? prefill_fmt<bf16>(p, pl, dp, s) : prefill_fmt<float>(p, pl, dp, s);

@@ -1,6 +1,8 @@
 // The kernels over the plan of attn_prefill.h: the items, and the join of cut tiles. One source file per
 // padded width instantiates them.
 #pragma once
+#include <utility>
+
 #include "attn_prefill.h"
 
 namespace ssm {
@@ -10,7 +12,7 @@ template <typename T, int DP, int WAVES> struct PrefillShape {
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int TOK = BF ? 64 : 32, MT = TOK / 32, DT = DP / 32;
     static constexpr int PE = 16 / (int)sizeof(T);        // values per staged piece
-    static constexpr int NP = DP / 32;                     // pieces of 1 KB per wave and step, of k and of v (8 waves: of one)
+    static constexpr int NP = DP / 32;                     // pieces of 16 bytes per lane, step and source
     // row strides in LDS: k rows 16 bytes apart modulo 256 (16 lanes read 16 rows), v rows 64 or 192
     // bytes (bf16: a half wave reads 4 rows of 64 bytes) or 32 bytes (float32) apart
     static constexpr int KS = DP + PE;
@@ -18,6 +20,13 @@ template <typename T, int DP, int WAVES> struct PrefillShape {
 };
 
 constexpr float kLag = 8.0f;
+
+// f(integral_constant<int, 0>), .., f(integral_constant<int, n - 1>): places in register arrays that are
+// constants from the start
+template <typename F, int... I> __device__ __forceinline__ void static_each(std::integer_sequence<int, I...>, F f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int n, typename F> __device__ __forceinline__ void static_for(F f) { static_each(std::make_integer_sequence<int, n>{}, f); }
 
 // f over a value of the lane and of its partner in the other half of the wave
 template <typename F> __device__ __forceinline__ float over_halves(float x, F f) {
@@ -27,7 +36,7 @@ template <typename F> __device__ __forceinline__ float over_halves(float x, F f)
 }
 
 template <typename T, int FMT, int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (sizeof(T) == 2 && DP <= 128 ? 2 : 1))
+__global__ __launch_bounds__(64 * WAVES, (DP <= 128 ? 2 : 1))
 void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     using Sh = PrefillShape<T, DP, WAVES>;
     using E = typename KvElem<T, FMT>::type;
@@ -43,22 +52,14 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     const KvArgs& a = p.kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
     const int it = (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
-    if (it >= plan.count[0]) return;
     const AttnItem item = plan.items[it];
-    const KvSeq sq = kv_seq(a, item.seq);
+    if (item.part == -2) return;
+    const struct { int lo, m, n; } sq = {item.lo, item.m, item.n};
     const int g = a.Hq / a.Hkv, n = sq.n, before = sq.n - sq.m;
     const int32_t* table = a.table + (int64_t)item.seq * a.max_pages;
 
     if (tid == 0) s_bad = 0;
     __syncthreads();
-    // pages that the table does not name: their tokens are masked one by one (below)
-    for (int i = (item.k0 >> a.page_log2) + tid; i <= ((min(item.k1, n) - 1) >> a.page_log2); i += 64 * WAVES) {
-        const int pg = table[i];
-        if (pg < 0 || pg >= a.num_pages) {
-            s_bad = 1;
-            atomicOr(a.status, SSM_STATUS_BAD_PAGE);
-        }
-    }
 
     // this lane's query
     const int row = item.row0 + wave * 32 + col;
@@ -86,81 +87,82 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     }
 
     // Staging: a wave brings the step's tokens of one block of 16 (two waves share a block of a float32
-    // step; of 8 waves, four bring k and four v), which lie on one page, through a buffer resource that
-    // ends behind the sequence's last token: what is not there reads as zero, and a lane's offsets never
-    // change. The block's page is looked up one step before its loads are issued.
+    // step), which lie on one page, through buffer resources that end behind the sequence's last token:
+    // what is not there reads as zero, and a lane's offsets never change. Of 8 waves four bring k and four
+    // v (one source each), of 4 waves each brings both. k is staged one step ahead of v (below).
+    constexpr bool PINGPONG = WAVES == 8;
+    static_assert(WAVES == 4 || (PINGPONG && BF), "four waves, or eight of bf16");
+    constexpr int NB = PINGPONG ? 1 : 2;                   // sources of a wave: 0 (k, or v in the second half), 1 (v)
     constexpr int PR = DP / PE;                            // pieces per row
-    constexpr bool SPLIT = WAVES == 8;
-    static_assert(WAVES == 4 || (SPLIT && BF), "four waves, or eight of bf16");
     const int blk = BF ? wave & 3 : wave >> 1;             // the wave's block of the step
-    const bool brings_v = SPLIT && __builtin_amdgcn_readfirstlane(wave) >= 4;
+    const bool second = PINGPONG && wave >= 4;             // the half of the workgroup that brings v
     uint32_t off[NP];                                      // byte offset of piece i in its block
-    int at_k[NP], at_v[NP];
+    int at[NB][NP];                                        // its place in a buffer
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int pc = ((BF ? 0 : (wave & 1) * NP) + i) * 64 + lane, t = pc / PR, d = (pc % PR) * PE;
         off[i] = d < a.D ? (uint32_t)((t * a.D + d) * (int)sizeof(E)) : kOffOutOfRange;
-        at_k[i] = (16 * blk + t) * (brings_v ? VS : KS) + d;
-        at_v[i] = (16 * blk + t) * VS + d;
+        at[0][i] = (16 * blk + t) * (second ? VS : KS) + d;
+        if constexpr (NB == 2) at[1][i] = (16 * blk + t) * VS + d;
     }
-    uint32_t rk[NP][GW], rv[SPLIT ? 1 : NP][GW];           // SPLIT: rk holds what the wave brings
-    uint32_t rks = 0, rvs = 0;
-    auto page_at = [&](int tb) {                           // the table entry of the wave's block
-        return table[max(min(tb + 16 * blk, n - 1), 0) >> a.page_log2];
+    uint32_t held[NB][NP][GW];                             // pieces on their way
+    uint32_t held_ks = 0, held_vs = 0;
+    const char* src[NB];
+    src[0] = (const char*)(second ? a.v : a.k);
+    if constexpr (NB == 2) src[1] = (const char*)a.v;
+    __amdgpu_buffer_rsrc_t from[NB], from_ks, from_vs;
+    auto page_at = [&](int step) {                         // the table entry of the wave's block
+        return table[max(min(item.k0 + step * TOK + 16 * blk, n - 1), 0) >> a.page_log2];
     };
     // a page is page_bytes long, the head's part of it begins at head_bytes (both below 2^30)
     const uint32_t row_bytes = (uint32_t)(a.D * (int)sizeof(E)), page_mask = (1u << a.page_log2) - 1;
     const uint32_t head_row = (uint32_t)head << a.page_log2, page_rows = (uint32_t)a.Hkv << a.page_log2;
     const uint32_t head_bytes = head_row * row_bytes, page_bytes = page_rows * row_bytes;
-    const char* src = (const char*)(brings_v ? a.v : a.k);
-    // where the block's tokens are: the descriptor of what the wave brings
-    __amdgpu_buffer_rsrc_t from, from_v, from_s, from_vs;
-    auto locate = [&](int tb, int page) {
-        const int pg = __builtin_amdgcn_readfirstlane(page), j = tb + 16 * blk;
+    auto locate = [&](auto b, int step, int page) {         // where the block's tokens of source b are
+        const int pg = __builtin_amdgcn_readfirstlane(page), j = item.k0 + step * TOK + 16 * blk;
         const bool there = (uint32_t)pg < (uint32_t)a.num_pages && j < n;
         const uint32_t tokens = there ? (uint32_t)min(n - j, 16) : 0u, in_page = (uint32_t)j & page_mask;
-        const uint32_t page_at0 = there ? (uint32_t)pg : 0u;
-        const uint64_t o = (uint64_t)page_at0 * page_bytes + (head_bytes + in_page * row_bytes);
-        from = buffer_rsrc(src + o, tokens * row_bytes);
-        if constexpr (!SPLIT) from_v = buffer_rsrc((const char*)a.v + o, tokens * row_bytes);
+        const uint32_t page0 = there ? (uint32_t)pg : 0u;
+        const uint64_t o = (uint64_t)page0 * page_bytes + (head_bytes + in_page * row_bytes);
+        from[b] = buffer_rsrc(src[b] + o, tokens * row_bytes);
         if constexpr (FMT != SSM_KV_ACT) {
-            const uint64_t r = (uint64_t)page_at0 * page_rows + (head_row + in_page);
-            from_s = buffer_rsrc(a.ks + r, 4 * tokens);
-            from_vs = buffer_rsrc(a.vs + r, 4 * tokens);
+            if constexpr (b == 0) {
+                const uint64_t r = (uint64_t)page0 * page_rows + (head_row + in_page);
+                from_ks = buffer_rsrc(a.ks + r, 4 * tokens);
+                from_vs = buffer_rsrc(a.vs + r, 4 * tokens);
+            }
         }
     };
-    auto load = [&](__amdgpu_buffer_rsrc_t r, uint32_t o, uint32_t (&x)[GW]) {
+    auto load_piece = [&](auto b, auto i) {
+        uint32_t (&x)[GW] = held[b][i];
         if constexpr (GW == 4) {
-            const u32x4 w = buffer_load16(r, o);
+            const u32x4 w = buffer_load16(from[b], off[i]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = w[e];
         } else if constexpr (GW == 2) {
-            const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, (int)o, 0, 0);
+            const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(from[b], (int)off[i], 0, 0);
             x[0] = w[0];
             x[1] = w[1];
         } else {
-            x[0] = __builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0);
+            x[0] = __builtin_amdgcn_raw_buffer_load_b32(from[b], (int)off[i], 0, 0);
         }
     };
-    // Lanes 0 .. 15 of the waves that bring k bring the block's scales, of k and of v: four buffers of them,
-    // by the step, since a softmax half a step behind reads them later than the codes (below)
+    // Lanes 0 .. 15 of the waves that bring k bring the block's scales, of k and of v
     auto load_scales = [&] {
-        const uint32_t so = lane < 16 && !brings_v ? 4 * lane : kOffOutOfRange;
-        rks = __builtin_amdgcn_raw_buffer_load_b32(from_s, (int)so, 0, 0);
-        rvs = __builtin_amdgcn_raw_buffer_load_b32(from_vs, (int)so, 0, 0);
-    };
-    auto fetch = [&](int tb, int page) {
-        locate(tb, page);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) load(from, off[i], rk[i]);
-        if constexpr (!SPLIT) {
-#pragma unroll
-            for (int i = 0; i < NP; ++i) load(from_v, off[i], rv[i]);
+        if constexpr (FMT != SSM_KV_ACT) {
+            const uint32_t so = lane < 16 && !second ? 4 * lane : kOffOutOfRange;
+            held_ks = __builtin_amdgcn_raw_buffer_load_b32(from_ks, (int)so, 0, 0);
+            held_vs = __builtin_amdgcn_raw_buffer_load_b32(from_vs, (int)so, 0, 0);
         }
-        if constexpr (FMT != SSM_KV_ACT) load_scales();
     };
-    auto piece = [&](const uint32_t (&w)[GW]) {            // 16 bytes of T
-        u32x4 x;
+    auto load_all = [&](auto b, int step) {
+        locate(b, step, page_at(step));
+        static_for<NP>([&](auto i) { load_piece(b, i); });
+        if constexpr (b == 0) load_scales();
+    };
+    auto stage_piece = [&](auto b, int step, auto i) {
+        const uint32_t (&w)[GW] = held[b][i];
+        u32x4 x;                                           // 16 bytes of T
         if constexpr (FMT == SSM_KV_ACT) {
             x = u32x4{w[0], w[1], w[2], w[3]};
         } else if constexpr (BF) {   // codes are exact in bf16; their scales wait for the scores
@@ -171,24 +173,32 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             kv_decode4<FMT>(w[0], f);
             __builtin_memcpy(&x, f, 16);
         }
-        return x;
-    };
-    auto stage_piece = [&](int b, int i) {
-        *(u32x4*)((brings_v ? &s_v[b][0] : &s_k[b][0]) + at_k[i]) = piece(rk[i]);
-        if constexpr (!SPLIT) *(u32x4*)&s_v[b][at_v[i]] = piece(rv[i]);
+        *(u32x4*)((b == 1 || second ? &s_v[step & 1][0] : &s_k[step & 1][0]) + at[b][i]) = x;
     };
     auto stage_scales = [&](int step) {
         if constexpr (FMT != SSM_KV_ACT) {
-            if (lane < 16 && !brings_v) {
-                s_ks[step & 3][16 * blk + lane] = __builtin_bit_cast(float, rks);
-                s_vs[step & 3][16 * blk + lane] = __builtin_bit_cast(float, rvs);
+            if (lane < 16 && !second) {
+                s_ks[step & 3][16 * blk + lane] = __builtin_bit_cast(float, held_ks);
+                s_vs[step & 3][16 * blk + lane] = __builtin_bit_cast(float, held_vs);
             }
         }
     };
-    auto stage = [&](int step) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) stage_piece(step & 1, i);
-        stage_scales(step);
+    auto stage_all = [&](auto b, int step) {
+        static_for<NP>([&](auto i) { stage_piece(b, step, i); });
+        if constexpr (b == 0) stage_scales(step);
+    };
+    constexpr std::integral_constant<int, 0> b0{};
+    constexpr std::integral_constant<int, NB - 1> b1{};
+
+    // pages that the table does not name: their tokens are masked one by one (below)
+    auto check_pages = [&] {
+        for (int i = (item.k0 >> a.page_log2) + tid; i <= ((min(item.k1, n) - 1) >> a.page_log2); i += 64 * WAVES) {
+            const int pg = table[i];
+            if (pg < 0 || pg >= a.num_pages) {
+                s_bad = 1;
+                atomicOr(a.status, SSM_STATUS_BAD_PAGE);
+            }
+        }
     };
 
     const float c2 = a.scale * kLog2e;
@@ -204,42 +214,6 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     auto seen = [&](int tb) {
         return wave_on && tb <= pos_hi && (a.window <= 0 || tb + TOK - 1 > pos_lo - a.window);
     };
-    auto scores = [&](int b) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
-        if constexpr (BF) {
-            // fragments kLead ahead of the products that take them
-            constexpr int kLead = 6, N = QN * MT;
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int k = 0; k < QN; ++k)
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    const bf16x8 kf = *(const bf16x8*)&s_k[b][(t * 32 + col) * KS + k * 16 + half * 8];
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, q[k]), s[t], 0, 0, 0);
-                }
-            __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
-#pragma unroll
-            for (int i = 0; i < N - kLead; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x8, kLead, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        } else {
-#pragma unroll
-            for (int k = 0; k < QN; ++k)
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    const f32x4 kf = *(const f32x4*)&s_k[b][(t * 32 + col) * KS + k * 8 + half * 4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q[k][e], s[t], 0, 0, 0);
-                }
-        }
-    };
     bool bad = false;
     auto soften = [&](int tb, int step) {
         if constexpr (FMT != SSM_KV_ACT) {
@@ -250,6 +224,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                     const f32x4 sc = *(const f32x4*)&s_ks[step & 3][t * 32 + 8 * w + 4 * half];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[t][4 * w + e] *= sc[e];
+                    if (w == 3) __builtin_amdgcn_sched_barrier(0);
                 }
         }
         const bool edge = tb + TOK - 1 > pos_lo || (a.window > 0 && tb <= pos_hi - a.window);
@@ -289,6 +264,12 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             for (int t = 0; t < DT; ++t) o[t] *= al;
             m = mn;
         }
+        if constexpr (BF && DP <= 128) {
+            // (an empty statement that has the sums in the same registers on both ways here: without it the
+            // compiler copies four tiles of them in every step, and spills with 8-bit caches)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) asm volatile("" : "+v"(o[t]));
+        }
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -297,6 +278,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                 if constexpr (!BF || FMT != SSM_KV_ACT) l += s[t][r];
             }
         if constexpr (FMT != SSM_KV_ACT) {
+            __builtin_amdgcn_sched_barrier(0);   // (the scales are read when the scores' registers are free)
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -326,58 +308,57 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             if constexpr (FMT == SSM_KV_ACT) l += ls[0] + ls[1];
         }
     };
-    auto values = [&](int b) {
-        if constexpr (BF) {
-#pragma unroll
-            for (int ks = 0; ks < TOK / 16; ++ks) {
-                const T* vp = &s_v[b][(16 * ks + 4 * half + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4];
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    typedef short s16x4 __attribute__((ext_vector_type(4)));
-                    typedef __attribute__((address_space(3))) s16x4* lds4;
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp + t * 32));
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vp + 8 * VS + t * 32));
-                    const auto vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf[ks], o[t], 0, 0, 0);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const T* vp = &s_v[b][(8 * (r >> 2) + 4 * half + (r & 3)) * VS + col];
-#pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[t * 32], s[0][r], o[t], 0, 0, 0);
-            }
-        }
-    };
-
-    if constexpr (SPLIT) {
-        // Two waves share a SIMD, one of each half of the workgroup: while one half is in its products,
-        // the other is in its softmax, half a step behind. In phase 2 i the first half has the products
-        // V(i-1) P(i-1) and K(i) Q and stages K(i+1), the second half has softmax i - 1; in phase 2 i + 1
-        // the second half has the same products and stages V(i), the first half has softmax i. K(i) is
-        // read in phases 2 i and 2 i + 1, V(i) in 2 i + 2 and 2 i + 3, so two buffers of each do. The
-        // scales of step i + 1 come with K(i+1) in phase 2 i and are read in 2 i + 3 and 2 i + 4, when those
-        // of the step behind it are there already: three buffers, taken as four.
+    const int steps = (item.k1 - item.k0 + TOK - 1) / TOK;
+    if constexpr (BF) {
+        // The products of step i are one run of MFMAs, K(i) Q and then V(i-1) P(i-1), each fragment read
+        // from LDS kLead MFMAs ahead of its own (a wave alone: 69 cycles per MFMA as the compiler orders it,
+        // 41 so; the MFMA takes 32). Meanwhile K(i+1) and V(i) go from registers to LDS and the loads of the
+        // step behind them start, one piece to an MFMA. The run never branches: P is zero where a step is
+        // not seen or not there, and its scores are not used.
         //
-        // The products of a phase are one run of MFMAs, each fragment read kLead MFMAs ahead of its own
-        // (one wave alone: 69 cycles per MFMA as the compiler orders it, 41 so; the MFMA takes 32). The
-        // run never branches: P is zero where a step is not seen or not there, and its scores are not used.
-        constexpr int kLead = 4, NV = DT * TOK / 16, NK = QN * MT;
-        const int steps = (item.k1 - item.k0 + TOK - 1) / TOK;
-        const int lead = brings_v ? 0 : 1;                 // products(i) stages step i + lead
-        fetch(item.k0, page_at(item.k0));
-        int page = page_at(item.k0 + TOK);
+        // Eight waves: two share a SIMD, one of each half of the workgroup, and while one half is in its
+        // products the other is in its softmax, half a step behind. In phase 2 i the first half has the
+        // products of step i and stages K(i+1), the second has softmax i - 1; in phase 2 i + 1 the second half
+        // has the products of step i and stages V(i), the first has softmax i. K(i) is read in phases
+        // 2 i - 1 (its first fragments) to 2 i + 1, V(i) in 2 i + 2 and 2 i + 3: two buffers of each do. The
+        // scales of step i + 1 come with K(i+1) in phase 2 i and are read in 2 i + 3 and 2 i + 4, when those of
+        // the step behind it are there already: three buffers, taken as four.
+        // Four waves, where two halves of 8 would not have registers enough or few rows would leave most of
+        // them without work: one barrier per step, and the other workgroup of the compute unit (up to 128
+        // values per head) fills the softmax.
+        constexpr int kLead = 4, NV = DT * TOK / 16, NK = QN * MT, N = NK + NV;
+        constexpr int kSlots = NB * (2 * NP + 1) + 1, kFirst = N - kSlots;
+        static_assert(kFirst >= 0, "the run is long enough for what it brings");
+        const int lead = second ? 0 : 1;                   // source 0 is staged for step i + lead
         for (int i = tid; i < TOK * VS * 2 / 16; i += 64 * WAVES) ((u32x4*)&s_v[1][0])[i] = u32x4{0, 0, 0, 0};   // V(-1)
+        auto no_probabilities = [&] {
 #pragma unroll
-        for (int ks = 0; ks < TOK / 16; ++ks)
+            for (int ks = 0; ks < TOK / 16; ++ks)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)0.0f;
+                for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)0.0f;
+        };
+        no_probabilities();
+        int page[NB];
+        load_all(b0, 0);
+        if constexpr (NB == 2) {
+            load_all(b1, 0);
+            page[1] = page_at(1);
+        }
+        if (!second) {
+            page[0] = page_at(1);
+            stage_all(b0, 0);
+            locate(b0, 1, page[0]);
+            static_for<NP>([&](auto i) { load_piece(b0, i); });
+            load_scales();
+        }
+        page[0] = page_at(1 + lead);
+        check_pages();
+
         const T* v_at = &s_v[0][(4 * half + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4];
         const T* k_at = &s_k[0][col * KS + half * 8];
         bf16x8 fr[kLead + 1];
-        auto read = [&](int f, int i) {
-            if (f < NK) {
+        auto read = [&](auto f, int i) {
+            if constexpr (f < NK) {
                 fr[f % (kLead + 1)] = *(const bf16x8*)(k_at + (i & 1) * TOK * KS + (f % MT) * 32 * KS + (f / MT) * 16);
             } else {
                 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -388,85 +369,112 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                 fr[f % (kLead + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
-        auto read_first = [&](int i) {
-#pragma unroll
-            for (int f = 0; f < kLead; ++f) read(f, i);
+        auto read_first = [&](int i) { static_for<kLead>([&](auto f) { read(f, i); }); };
+        auto bring = [&](auto slot, int i) {               // slot of kSlots: stage, then locate and load by source
+            if constexpr (slot < NB * NP) {
+                constexpr std::integral_constant<int, slot / NP> b{};
+                stage_piece(b, i + (b == 0 ? lead : 0), std::integral_constant<int, slot % NP>{});
+            } else {
+                constexpr int r = slot - NB * NP, x = r % (NP + 1);
+                constexpr std::integral_constant<int, r / (NP + 1)> b{};
+                if constexpr (r == 0) stage_scales(i + lead);
+                if constexpr (b < NB) {
+                    const int step = i + 1 + (b == 0 ? lead : 0);
+                    if constexpr (x == 0) locate(b, step, page[b]);
+                    else load_piece(b, std::integral_constant<int, x - 1>{});
+                    if constexpr (x == NP) page[b] = page_at(step + 1);
+                } else {
+                    load_scales();
+                }
+            }
         };
         auto products = [&](int i) {
-            constexpr int kStage = NK + 2, kFetch = kStage + NP + 1;
-            static_assert(kFetch + NP + 1 <= NV + NK, "the run is long enough");
             __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int f = 0; f < NV + NK; ++f) {
-                if (f + kLead < NV + NK) read(f + kLead, i);
-                if (f < NK) {
-                    const int t = f % MT;
-                    if (f / MT == 0) {
+            static_for<N>([&](auto f) {
+                if constexpr (f + kLead < N) read(std::integral_constant<int, f + kLead>{}, i);
+                if constexpr (f < NK) {
+                    constexpr int t = f % MT;
+                    if constexpr (f / MT == 0) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
                     }
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], __builtin_bit_cast(bf16x8, q[f / MT]), s[t], 0, 0, 0);
                 } else {
-                    const int t = (f - NK) % DT;
+                    constexpr int t = (f - NK) % DT;
                     o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], pf[(f - NK) / DT], o[t], 0, 0, 0);
                 }
-                // what the wave brings, one piece to an MFMA
-                if (f >= kStage && f < kStage + NP) stage_piece((i + lead) & 1, f - kStage);
-                if (f == kStage + NP) {
-                    stage_scales(i + lead);
-                    locate(item.k0 + (i + lead + 1) * TOK, page);
-                }
-                if (f >= kFetch && f < kFetch + NP) load(from, off[f - kFetch], rk[f - kFetch]);
-                if (f == kFetch + NP) {
-                    if constexpr (FMT != SSM_KV_ACT) load_scales();
-                    page = page_at(item.k0 + (i + lead + 2) * TOK);
-                }
+                if constexpr (f >= kFirst) bring(std::integral_constant<int, f - kFirst>{}, i);
                 __builtin_amdgcn_sched_barrier(0);
-            }
+            });
             __builtin_amdgcn_s_setprio(0);
         };
-        if (!brings_v) {                                   // K(0); the second half's V(0) waits for its first products
-            stage(0);
-            fetch(item.k0 + TOK, page);
-            page = page_at(item.k0 + 2 * TOK);
-        }
+        auto softmax = [&](int i) {
+            if (i < steps && seen(item.k0 + i * TOK)) soften(item.k0 + i * TOK, i);
+            else no_probabilities();
+        };
         __syncthreads();
         bad = s_bad != 0;
+        if (!wave_on) {                                    // no rows: what the wave brings, and the barriers
+            if (second) __syncthreads();
+            for (int i = 0; i <= steps; ++i) {
+                static_for<kSlots>([&](auto slot) { bring(slot, i); });
+                __syncthreads();
+                if constexpr (PINGPONG) {
+                    if (!second || i < steps) __syncthreads();
+                }
+            }
+            return;
+        }
         read_first(0);
-        if (brings_v) __syncthreads();
+        if (second) __syncthreads();
         for (int i = 0; i <= steps; ++i) {
             products(i);
-            __syncthreads();
-            if (i < steps && seen(item.k0 + i * TOK)) {
-                soften(item.k0 + i * TOK, i);
+            if constexpr (PINGPONG) __syncthreads();
+            softmax(i);
+            if constexpr (PINGPONG) {
+                read_first(i + 1);
+                if (!second || i < steps) __syncthreads();
             } else {
-#pragma unroll
-                for (int ks = 0; ks < TOK / 16; ++ks)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)0.0f;
+                __syncthreads();
+                read_first(i + 1);
             }
-            read_first(i + 1);
-            if (!brings_v || i < steps) __syncthreads();
         }
     } else {
-        fetch(item.k0, page_at(item.k0));
-        int page = page_at(item.k0 + TOK);
-        stage(0);
+        load_all(b0, 0);
+        load_all(b1, 0);
+        check_pages();
+        stage_all(b0, 0);
+        stage_all(b1, 0);
         __syncthreads();
         bad = s_bad != 0;
-        int step = 0;
-        for (int tb = item.k0; tb < item.k1; tb += TOK, ++step) {
-            const bool more = tb + TOK < item.k1;
-            if (more) {
-                fetch(tb + TOK, page);
-                page = page_at(tb + 2 * TOK);
+        for (int i = 0; i < steps; ++i) {
+            const int tb = item.k0 + i * TOK;
+            if (i + 1 < steps) {
+                load_all(b0, i + 1);
+                load_all(b1, i + 1);
             }
             if (seen(tb)) {
-                scores(step & 1);
-                soften(tb, step);
-                values(step & 1);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < QN; ++k) {
+                    if (k * 8 >= a.D) break;
+                    const f32x4 kf = *(const f32x4*)&s_k[i & 1][col * KS + k * 8 + half * 4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q[k][e], s[0], 0, 0, 0);
+                }
+                soften(tb, i);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const T* vp = &s_v[i & 1][(8 * (r >> 2) + 4 * half + (r & 3)) * VS + col];
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[t * 32], s[0][r], o[t], 0, 0, 0);
+                }
             }
-            if (more) stage(step + 1);
+            if (i + 1 < steps) {
+                stage_all(b0, i + 1);
+                stage_all(b1, i + 1);
+            }
             __syncthreads();
         }
     }
@@ -504,33 +512,43 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     }
 }
 
-// Four rows of a cut tile per workgroup, one to a wave: the partial results of its items, in order
+// The partial results of cut tiles, in order: four rows of a (tile, kv head) per workgroup and turn, one to
+// a wave
+constexpr int kJoinWorkgroups = 2048;
 template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void attn_prefill_join_kernel(AttnArgs p, AttnPlan plan) {
     const KvArgs& a = p.kv;
-    const int ji = (int)blockIdx.x / a.Hkv, head = (int)blockIdx.x % a.Hkv;
-    if (ji >= plan.count[1]) return;
-    const AttnJoin jn = plan.joins[ji];
-    const KvSeq sq = kv_seq(a, jn.seq);
-    const int g = a.Hq / a.Hkv, r = (int)blockIdx.y * 4 + (threadIdx.x >> 6), row = jn.row0 + r;
-    if (row >= sq.m * g) return;
     constexpr int64_t stride = (int64_t)ROWS * (DP + 2);
-    const float* part = plan.parts + ((int64_t)head * plan.max_parts + jn.part) * stride;
-    join_row<T>(jn.pieces, [&](int v) { return part + v * stride; }, (int64_t)r * DP, ROWS * DP + r,
-                ROWS * (DP + 1) + r, a.D, (T*)p.o + (int64_t)(sq.lo + row / g) * p.ld_o + (int64_t)(head * g + row % g) * a.D);
+    constexpr int turns = ROWS / 4;
+    const int g = a.Hq / a.Hkv, total = plan.count[0] * a.Hkv * turns;
+    for (int i = (int)blockIdx.x; i < total; i += (int)gridDim.x) {
+        const int r = (i % turns) * 4 + (threadIdx.x >> 6), head = i / turns % a.Hkv;
+        const AttnJoin jn = plan.joins[i / turns / a.Hkv];
+        const int row = jn.row0 + r;
+        if (row >= jn.m * g) continue;
+        const float* part = plan.parts + ((int64_t)head * plan.max_parts + jn.part) * stride;
+        join_row<T>(jn.pieces, [&](int v) { return part + v * stride; }, (int64_t)r * DP, ROWS * DP + r, ROWS * (DP + 1) + r, a.D,
+                    (T*)p.o + (int64_t)(jn.lo + row / g) * p.ld_o + (int64_t)(head * g + row % g) * a.D);
+    }
 }
 
-template <typename T, int FMT, int DP>
-hipError_t launch_attn_prefill_tile(const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
-    constexpr int WAVES = tile_rows(sizeof(T) == 2, DP) / 32;
+template <typename T, int FMT, int DP, int WAVES> hipError_t launch_attn_prefill_waves(const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
     KernelTimer kt("attn.prefill", s);
     SSM_LAUNCH((attn_prefill_kernel<T, FMT, DP, WAVES>), dim3((unsigned)pl.max_items * p.kv.Hkv), dim3(64 * WAVES), 0, s, p, pl);
     hipError_t e = hipGetLastError();
     const int64_t longest = (int64_t)p.kv.max_pages << p.kv.page_log2;
-    if (e != hipSuccess || longest <= kMinSteps * kStep) return e;   // no tile is ever cut
+    if (e != hipSuccess || longest <= tile_min_steps(sizeof(T) == 2) * kStep) return e;   // no tile is ever cut
     KernelTimer kj("attn.prefill_join", s);
-    SSM_LAUNCH((attn_prefill_join_kernel<T, DP, 32 * WAVES>), dim3((unsigned)pl.max_joins * p.kv.Hkv, 32 * WAVES / 4), dim3(256), 0,
-               s, p, pl);
+    const int64_t most = (int64_t)pl.max_joins * p.kv.Hkv * (8 * WAVES);
+    SSM_LAUNCH((attn_prefill_join_kernel<T, DP, 32 * WAVES>), dim3((unsigned)(most < kJoinWorkgroups ? most : kJoinWorkgroups)), dim3(256),
+               0, s, p, pl);
     return hipGetLastError();
+}
+template <typename T, int FMT, int DP>
+hipError_t launch_attn_prefill_tile(const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
+    if constexpr (sizeof(T) == 2 && DP == 128) {
+        if (pl.rows == 256) return launch_attn_prefill_waves<T, FMT, DP, 8>(p, pl, s);
+    }
+    return launch_attn_prefill_waves<T, FMT, DP, 4>(p, pl, s);
 }
 
 // the instances of one padded width, one file each
