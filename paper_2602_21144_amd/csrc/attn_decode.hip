@@ -109,6 +109,12 @@ __device__ __forceinline__ Place find_run(const KvArgs& a, int rows_per_seq, int
     return Place{runs, uniform((int)sh[4]), uniform(sh[5])};
 }
 
+// workgroups that are resident at once: 256 compute units, 2 each where the registers allow it
+constexpr int kWorkers = 512;
+// The join of a row that is cut: its first query head, how many of them, and the partial results
+struct RowJoin { int32_t seq, q_head, rows, pieces; };
+constexpr size_t kJoinBytes = kWorkers * sizeof(RowJoin);
+
 // The operand layouts per (activation type, cache format): CH values per 16-byte piece of a k row
 template <typename T, int FMT> struct Layout {
     using E = typename KvElem<T, FMT>::type;
@@ -144,22 +150,27 @@ template <int n> __device__ __forceinline__ void load_words(const void* p, uint3
     }
 }
 
-// The loads of the wave's 32 tokens from tb. Tokens past the sequence's last group of eight, and
-// groups whose page the table does not name, are read from a place that exists and masked.
+// The table's entries for the wave's 32 tokens from tb: of the eight tokens whose k rows the lane loads, and
+// of those whose v rows. Tokens past the sequence's last group of eight are read from that group and masked.
+// The entries are fetched a tile ahead of the loads that need them: loads come back in their order, so a
+// wait for an entry fetched later would be a wait for the whole tile before it.
+struct Pages { int k, v; };
+__device__ __forceinline__ Pages tile_pages(const KvArgs& a, const int32_t* table, int n, int tb, int lane) {
+    const int end = (n - 1) & ~7;
+    return Pages{table[min(tb + 8 * ((lane & 15) >> 2), end) >> a.page_log2], table[min(tb + 8 * (lane >> 4), end) >> a.page_log2]};
+}
+// The loads of the wave's 32 tokens from tb. Groups whose page the table does not name are read from a
+// place that exists and masked.
 template <typename T, int FMT, int DP>
-__device__ __forceinline__ void load_tile(const KvArgs& a, Tile<T, FMT, DP>& x, int seq, int head, int n, int lo, int tb,
-                                          int lane) {
+__device__ __forceinline__ void load_tile(const KvArgs& a, Tile<T, FMT, DP>& x, Pages pg, int head, int n, int lo, int tb, int lane) {
     using L = Tile<T, FMT, DP>;
     using E = typename L::E;
     const int quad = lane >> 4, i = lane & 15;
     const int end = (n - 1) & ~7;
     const int gk = min(tb + 8 * (i >> 2), end), gv = min(tb + 8 * quad, end);
-    const int32_t* row = a.table + (int64_t)seq * a.max_pages;
-    int pk = row[gk >> a.page_log2], pv = row[gv >> a.page_log2];
-    const bool named = pv >= 0 && pv < a.num_pages;
+    const bool named = pg.v >= 0 && pg.v < a.num_pages;
     if (!named) atomicOr(a.status, SSM_STATUS_BAD_PAGE);
-    pk = pk >= 0 && pk < a.num_pages ? pk : 0;
-    pv = named ? pv : 0;
+    const int pk = pg.k >= 0 && pg.k < a.num_pages ? pg.k : 0, pv = named ? pg.v : 0;
     const int64_t rk = kv_pool_row(a, pk, head, gk), rv = kv_pool_row(a, pv, head, gv);
     const E* kp = (const E*)a.k + rk * a.D;
     const E* vp = (const E*)a.v + rv * a.D;
@@ -368,11 +379,16 @@ __global__ __launch_bounds__(256, (min_waves<T, DP>())) void attn_decode_kernel(
     if (blockIdx.x == 0) kv_check_seqs(a, tid, 256);
     const int w = (int)blockIdx.x;
     const Place pl = find_run(a, rows, workers, w, sh);
-    if (w >= pl.runs.cut) return;
+    RowJoin join{};
+    RowJoin* joins = (RowJoin*)p.scratch;
+    if (w >= pl.runs.cut) {
+        if (tid == 0) joins[w] = join;
+        return;
+    }
     int64_t u = pl.runs.begin(w);
     const int64_t u1 = pl.runs.begin(w + 1);
     const float c2 = a.scale * kLog2e;
-    float* part = (float*)p.scratch;
+    float* part = (float*)(p.scratch + kJoinBytes);
     int seq = pl.seq;
     int64_t base = pl.base;
     while (u < u1) {
@@ -400,22 +416,27 @@ __global__ __launch_bounds__(256, (min_waves<T, DP>())) void attn_decode_kernel(
         int tb = start + t0 * kUnit + wave * kWaveTok;
         const int te = min(n, start + t1 * kUnit);
         if (tb < te) {
+            const int32_t* table = a.table + (int64_t)seq * a.max_pages;
             Tile<T, FMT, DP> x;
-            load_tile<T, FMT, DP>(a, x, seq, head, n, lo, tb, lane);
+            Pages pg = tile_pages(a, table, n, tb, lane);
+            Pages next = tile_pages(a, table, n, tb + kUnit, lane);
+            load_tile<T, FMT, DP>(a, x, pg, head, n, lo, tb, lane);
             while (true) {
                 const int nb = tb + kUnit;
                 if (nb >= te) {
                     attend_tile<T, FMT, DP>(x, q, acc, c2);
                     break;
                 }
+                pg = next;
+                next = tile_pages(a, table, n, nb + kUnit, lane);
                 if constexpr (loads_ahead<T, FMT, DP>()) {
                     Tile<T, FMT, DP> y;
-                    load_tile<T, FMT, DP>(a, y, seq, head, n, lo, nb, lane);
+                    load_tile<T, FMT, DP>(a, y, pg, head, n, lo, nb, lane);
                     attend_tile<T, FMT, DP>(x, q, acc, c2);
                     x = y;
                 } else {
                     attend_tile<T, FMT, DP>(x, q, acc, c2);
-                    load_tile<T, FMT, DP>(a, x, seq, head, n, lo, nb, lane);
+                    load_tile<T, FMT, DP>(a, x, pg, head, n, lo, nb, lane);
                 }
                 tb = nb;
             }
@@ -469,58 +490,52 @@ __global__ __launch_bounds__(256, (min_waves<T, DP>())) void attn_decode_kernel(
             }
         }
         __syncthreads();
+        if (t0 == 0 && t1 < nt) {   // the row goes on: this workgroup's record says what its join will be
+            const int64_t end = u + nt;
+            int last = w + 1;
+            while (last + 1 < pl.runs.cut && pl.runs.begin(last + 1) < end) ++last;
+            join = RowJoin{seq, head * g + q0, nq, last - w + 1};
+        }
         u += t1 - t0;
     }
+    if (tid == 0) joins[w] = join;
 }
 
-// The rows that the workgroups' runs cut: workgroup w joins the row that holds the run boundary
-// between w - 1 and w, where that is the row's first one.
+// The rows that the workgroups' runs cut, by the records of the workgroups that began them
 template <typename T>
-__global__ __launch_bounds__(256) void attn_decode_join_kernel(AttnArgs p, int workers, int DP) {
-    __shared__ int64_t sh[8];
-    const KvArgs& a = p.kv;
-    const int tid = threadIdx.x;
-    const int g = a.Hq / a.Hkv, rt = (g + kRows - 1) / kRows, rows = a.Hkv * rt;
-    const int w = (int)blockIdx.x + 1;
-    const Place pl = find_run(a, rows, workers, w, sh);
-    if (w >= pl.runs.cut) return;
-    const int64_t u = pl.runs.begin(w), prev = pl.runs.begin(w - 1);
-    const int nt = row_units(a, pl.seq);
-    const int row = (int)((uint32_t)(u - pl.base) / (uint32_t)nt);
-    const int64_t rb = pl.base + (int64_t)row * nt, re = rb + nt;
-    if (u == rb || prev > rb) return;
-    const int head = row / rt, q0 = (row % rt) * kRows;
-    const int nq = g - q0 < kRows ? g - q0 : kRows;
-    int last = w;   // the last workgroup with a part of the row
-    while (last + 1 < pl.runs.cut && pl.runs.begin(last + 1) < re) ++last;
-    const float* part = (const float*)p.scratch;
-    auto slot = [&](int v) { return part + (2 * (int64_t)(w - 1) + (v == 0 ? 1 : 2 * v)) * part_floats(DP); };
-    for (int r = tid >> 6; r < nq; r += 4)
-        join_row<T>(last - w + 2, slot, r * DP, kRows * DP + r, kRows * DP + kRows + r, a.D,
-                    (T*)p.o + (int64_t)pl.seq * p.ld_o + (int64_t)(head * g + q0 + r) * a.D);
+__global__ __launch_bounds__(256) void attn_decode_join_kernel(AttnArgs p, int DP) {
+    const int w = (int)blockIdx.x;
+    const RowJoin jn = ((const RowJoin*)p.scratch)[w];
+    const float* part = (const float*)(p.scratch + kJoinBytes);
+    auto slot = [&](int v) { return part + (2 * (int64_t)w + (v == 0 ? 1 : 2 * v)) * part_floats(DP); };
+    for (int r = (int)blockIdx.y * 4 + (threadIdx.x >> 6); r < jn.rows; r += 4 * (int)gridDim.y)
+        join_row<T, 8>(jn.pieces, slot, r * DP, kRows * DP + r, kRows * DP + kRows + r, p.kv.D,
+                    (T*)p.o + (int64_t)jn.seq * p.ld_o + (int64_t)(jn.q_head + r) * p.kv.D);
 }
 
 int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
-// workgroups that are resident at once: 256 compute units, 2 each where the registers allow it
-constexpr int kWorkers = 512;
 
 template <typename T, int FMT> hipError_t decode_launch(const AttnArgs& p, hipStream_t s) {
     const KvArgs& a = p.kv;
-    const int64_t rows = (int64_t)a.Hkv * ((a.Hq / a.Hkv + kRows - 1) / kRows) * a.nseq;
+    const int g = a.Hq / a.Hkv;
+    const int64_t rows = (int64_t)a.Hkv * ((g + kRows - 1) / kRows) * a.nseq;
     const int64_t longest = a.window > 0 ? a.window + kWaveTok : (int64_t)a.max_pages << a.page_log2;
     const int64_t most = rows * ((longest + kUnit - 1) / kUnit);
     const int workers = (int)(most < kWorkers ? most : kWorkers);
     const dim3 grid((unsigned)workers), block(256);
-    KernelTimer kt("attn.decode", s);
-    switch (padded_dim(a.D)) {
-        case 64: SSM_LAUNCH((attn_decode_kernel<T, FMT, 64>), grid, block, 0, s, p, workers); break;
-        case 128: SSM_LAUNCH((attn_decode_kernel<T, FMT, 128>), grid, block, 0, s, p, workers); break;
-        default: SSM_LAUNCH((attn_decode_kernel<T, FMT, 256>), grid, block, 0, s, p, workers); break;
+    {
+        KernelTimer kt("attn.decode", s);
+        switch (padded_dim(a.D)) {
+            case 64: SSM_LAUNCH((attn_decode_kernel<T, FMT, 64>), grid, block, 0, s, p, workers); break;
+            case 128: SSM_LAUNCH((attn_decode_kernel<T, FMT, 128>), grid, block, 0, s, p, workers); break;
+            default: SSM_LAUNCH((attn_decode_kernel<T, FMT, 256>), grid, block, 0, s, p, workers); break;
+        }
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || longest <= kUnit || workers < 2) return e;   // no row is ever cut
     KernelTimer kj("attn.decode_join", s);
-    SSM_LAUNCH((attn_decode_join_kernel<T>), dim3((unsigned)workers - 1), block, 0, s, p, workers, padded_dim(a.D));
+    SSM_LAUNCH((attn_decode_join_kernel<T>), dim3((unsigned)workers - 1, (unsigned)((g < kRows ? g : kRows) + 3) / 4), block, 0, s, p,
+               padded_dim(a.D));
     return hipGetLastError();
 }
 template <typename T> hipError_t decode_fmt(const AttnArgs& p, hipStream_t s) {
@@ -534,7 +549,7 @@ template <typename T> hipError_t decode_fmt(const AttnArgs& p, hipStream_t s) {
 }  // namespace
 
 size_t attn_decode_scratch_bytes(int D, int64_t batch) {
-    return batch > 0 ? (size_t)kWorkers * 2 * part_floats(padded_dim(D)) * 4 : 0;
+    return batch > 0 ? kJoinBytes + (size_t)kWorkers * 2 * part_floats(padded_dim(D)) * 4 : 0;
 }
 hipError_t launch_attn_decode(const AttnArgs& p, bool bf16_act, hipStream_t s) {
     return bf16_act ? decode_fmt<bf16>(p, s) : decode_fmt<float>(p, s);

@@ -526,7 +526,7 @@ template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void a
         const int row = jn.row0 + r;
         if (row >= jn.m * g) continue;
         const float* part = plan.parts + ((int64_t)head * plan.max_parts + jn.part) * stride;
-        join_row<T>(jn.pieces, [&](int v) { return part + v * stride; }, (int64_t)r * DP, ROWS * DP + r, ROWS * (DP + 1) + r, a.D,
+        join_row<T, 2>(jn.pieces, [&](int v) { return part + v * stride; }, (int64_t)r * DP, ROWS * DP + r, ROWS * (DP + 1) + r, a.D,
                     (T*)p.o + (int64_t)(jn.lo + row / g) * p.ld_o + (int64_t)(head * g + row % g) * a.D);
     }
 }

@@ -117,33 +117,47 @@ template <int FMT> __device__ __forceinline__ u32x2 kv_decode4_bf16(uint32_t w) 
 template <typename T, int FMT> struct KvElem { using type = uint8_t; };
 template <typename T> struct KvElem<T, SSM_KV_ACT> { using type = T; };
 
-// Joins the partial results of one row, in their order: o = sum_v f_v o_v / sum_v f_v l_v with
-// f_v = 2^(m_v - max m). One wave; slot(v) is partial v, which holds the row's D values at o_at and its
-// statistics at m_at and l_at. Lanes take 4 values each; what is left of the wave splits the partials.
-template <typename T, typename F>
+// Joins the partial results of one row: o = sum_v f_v o_v / sum_v f_v l_v with f_v = 2^(m_v - max m). One
+// wave; slot(v) is partial v, which holds the row's D values at o_at and its statistics at m_at and l_at.
+// Lanes take 4 values each; what is left of the wave splits the partials, every lane's share in order and
+// then the shares. The first values are on their way before the statistics are there.
+template <typename T, int kBatch, typename F>
 __device__ __forceinline__ void join_row(int pieces, F slot, int64_t o_at, int64_t m_at, int64_t l_at, int D, T* out) {
     const int lane = threadIdx.x & 63;
     const int lpr = D <= 64 ? 16 : D <= 128 ? 32 : 64, subs = 64 / lpr;
     const int sub = lane / lpr, d = (lane % lpr) * 4;
+    f32x4 x[kBatch];
+    auto fetch = [&](int v0) {   // partials v0 + sub, v0 + sub + subs, ..
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int v = v0 + k * subs + sub;
+            x[k] = f32x4{0, 0, 0, 0};
+            if (v < pieces && d < D) x[k] = *(const f32x4*)(slot(v) + o_at + d);
+        }
+    };
+    fetch(0);
     float M = -3.0e38f;
     for (int v = lane; v < pieces; v += 64) M = fmaxf(M, slot(v)[m_at]);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-    float ls = 0.0f, o[4] = {0, 0, 0, 0};
-    for (int v0 = 0; v0 < pieces; v0 += 64) {
-        float f = 0.0f;
-        if (v0 + lane < pieces) {
-            f = fast_exp2(slot(v0 + lane)[m_at] - M);
-            ls += f * slot(v0 + lane)[l_at];
-        }
-        const int cnt = pieces - v0 < 64 ? pieces - v0 : 64;
-#pragma unroll 4
-        for (int j = 0; j < cnt; j += subs) {
-            const float fv = __shfl(f, (j + sub) & 63, 64);   // 0 past the last partial
-            if (j + sub < cnt && d < D) {
-                const float4 x = *(const float4*)(slot(v0 + j + sub) + o_at + d);
-                o[0] += fv * x.x; o[1] += fv * x.y; o[2] += fv * x.z; o[3] += fv * x.w;
+    float ls = 0.0f, f = 0.0f, o[4] = {0, 0, 0, 0};
+    for (int v0 = 0; v0 < pieces; v0 += kBatch * subs) {
+        if (v0 % 64 == 0) {   // the factors of the next 64 (a batch is at most 32 of them)
+            f = 0.0f;
+            if (v0 + lane < pieces) {
+                f = fast_exp2(slot(v0 + lane)[m_at] - M);
+                ls += f * slot(v0 + lane)[l_at];
             }
+        }
+        f32x4 y[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) y[k] = x[k];
+        if (v0 + kBatch * subs < pieces) fetch(v0 + kBatch * subs);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const float fv = __shfl(f, (v0 + k * subs + sub) & 63, 64);   // 0 past the last partial
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += fv * y[k][e];
         }
     }
 #pragma unroll
