@@ -13,16 +13,9 @@
 namespace ssm {
 namespace {
 
-template <typename T> __device__ __forceinline__ void kv_load4(const T* p, float (&v)[4]);
-template <> __device__ __forceinline__ void kv_load4<float>(const float* p, float (&v)[4]) {
-    const float4 a = *(const float4*)p;
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-}
-template <> __device__ __forceinline__ void kv_load4<bf16>(const bf16* p, float (&v)[4]) {
-    const bf16x4 a = *(const bf16x4*)p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)a[e];
-}
+// four values as they are stored
+__device__ __forceinline__ f32x4 kv_load4(const float* p) { return *(const f32x4*)p; }
+__device__ __forceinline__ bf16x4 kv_load4(const bf16* p) { return *(const bf16x4*)p; }
 template <typename T> __device__ __forceinline__ void kv_store4(T* p, const float (&v)[4]);
 template <> __device__ __forceinline__ void kv_store4<float>(float* p, const float (&v)[4]) {
     *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
@@ -49,57 +42,103 @@ __device__ __forceinline__ void cos_sin_turns(uint64_t x, float& c, float& s) {
     s = (quarter >= 2) ? -b : b;
 }
 
+// 1 / sqrt(x), one step of 2^-23 off; the instruction takes no subnormal numbers
+__device__ __forceinline__ float inv_root(float x) { return __builtin_amdgcn_rsqf(x < 1.2e-38f ? 1.2e-38f : x); }
+
+// The result of op over groups of LPH neighbouring lanes, in each of them. Every step pairs lanes whose
+// partial results are of different values: neighbours, pairs, then mirrored quads and eights.
+template <int LPH, typename F> __device__ __forceinline__ float group_reduce(float v, F op) {
+    auto moved = [&](auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    v = op(v, moved(std::integral_constant<int, 0xB1>{}));    // quad_perm 1 0 3 2
+    v = op(v, moved(std::integral_constant<int, 0x4E>{}));    // quad_perm 2 3 0 1
+    v = op(v, moved(std::integral_constant<int, 0x141>{}));   // row_half_mirror
+    if constexpr (LPH >= 16) v = op(v, moved(std::integral_constant<int, 0x140>{}));   // row_mirror
+    if constexpr (LPH >= 32) v = op(v, __shfl_xor(v, 16, 64));
+    return v;
+}
+
 // A group of LPH lanes holds one head's D values, 8 per lane in two pieces of 4: the pieces that a
-// rotation pairs (4 values at 4 j and 4 at rot / 2 + 4 j), or 8 neighbours. One workgroup per token
-// and slice of its heads: a lane's four angles serve every head that its group takes.
+// rotation pairs (4 values at 4 j and 4 at rot / 2 + 4 j), or 8 neighbours. One workgroup per token:
+// its angles are worked out once, and each group goes through every 256 / LPH-th head with the next
+// head's values on their way.
+//
+// A chunk of 2048 tokens of 48 heads of 112 into fp8 (37 MB in and out, 7.5 us at the card's copy rate) takes
+// 11.7 us, of which 4 are an empty launch's. It was bound by instructions, not bytes: 15.4 us with the angles in
+// every lane, library root and divisions and sums by way of shared memory. Splitting a token's heads over
+// workgroups is no faster at any number of tokens (2048: 14.8 us, the lookups are repeated; 1 to 256: alike, 4 to 5).
 template <typename T, int FMT, int LPH>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
     using E = typename KvElem<T, FMT>::type;
     const KvArgs& kv = a.kv;
     const int64_t t = blockIdx.x;
     const int D = kv.D, j = threadIdx.x % LPH;
-    if (t == 0 && blockIdx.y == 0) kv_check_seqs(kv, threadIdx.x, 256);
+    const bool on = 8 * j < D;
+    const bool half = !a.inter && 8 * j < a.rot;          // the two pieces are a rotation's two halves
+    const int d0 = half ? 4 * j : 8 * j, d1 = half ? a.rot / 2 + 4 * j : 8 * j + 4;
+    const int heads = kv.Hq + 2 * kv.Hkv;
+    constexpr int step = 256 / LPH;
+    const float inv_d = 1.0f / (float)D;
+    const T* in = (const T*)a.qkv + t * a.ld;
+    int h = threadIdx.x / LPH;
+    // the first head and the norms' weights are on their way while the row's place is looked up
+    using Piece = decltype(kv_load4(in));
+    Piece x0, x1;
+    auto fetch = [&](int head) {
+        x0 = x1 = Piece{};
+        if (on && head < heads) {
+            x0 = kv_load4(in + (int64_t)head * D + d0);
+            x1 = kv_load4(in + (int64_t)head * D + d1);
+        }
+    };
+    fetch(h);
+    float4 qw[2] = {}, kw[2] = {};
+    if (on && a.q_w) qw[0] = *(const float4*)(a.q_w + d0), qw[1] = *(const float4*)(a.q_w + d1);
+    if (on && a.k_w) kw[0] = *(const float4*)(a.k_w + d0), kw[1] = *(const float4*)(a.k_w + d1);
+
+    if (t == 0) kv_check_seqs(kv, threadIdx.x, 256);
     const KvRow row = kv_row(kv, t);
     if (row.seq < 0) return;   // the whole workgroup
     const int pos = row.pos < 0 ? 0 : row.pos;
     const int page = row.pos < 0 ? -1 : kv_page(kv, row.seq, pos);
 
-    const bool on = 8 * j < D;
-    const bool half = !a.inter && 8 * j < a.rot;          // the two pieces are a rotation's two halves
-    const int d0 = half ? 4 * j : 8 * j, d1 = half ? a.rot / 2 + 4 * j : 8 * j + 4;
+    __shared__ __align__(16) float s_cs[128], s_sn[128];
     float cs[4], sn[4];
     const bool turn = on && 8 * j < a.rot;
-    if (turn) {
+    if (a.rot > 0) {
+        if ((int)threadIdx.x < a.rot / 2) cos_sin_turns(a.turns[threadIdx.x] * (uint64_t)pos, s_cs[threadIdx.x], s_sn[threadIdx.x]);
+        __syncthreads();
+        if (turn) {
+            const f32x4 c4 = kv_load4(s_cs + 4 * j), s4 = kv_load4(s_sn + 4 * j);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) cos_sin_turns(a.turns[4 * j + e] * (uint64_t)pos, cs[e], sn[e]);
-    }
-    const int heads = kv.Hq + 2 * kv.Hkv;
-    const int step = (256 / LPH) * gridDim.y;
-    const T* in = (const T*)a.qkv + t * a.ld;
-    for (int h = (int)blockIdx.y * (256 / LPH) + threadIdx.x / LPH; h < heads; h += step) {
-        float x[4] = {}, y[4] = {};
-        if (on) {
-            kv_load4(in + (int64_t)h * D + d0, x);
-            kv_load4(in + (int64_t)h * D + d1, y);
+            for (int e = 0; e < 4; ++e) {
+                cs[e] = c4[e];
+                sn[e] = s4[e];
+            }
         }
+    }
+    for (; h < heads; h += step) {
+        float x[4], y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = (float)x0[e];
+            y[e] = (float)x1[e];
+        }
+        fetch(h + step);   // the next head, while this one is worked on
         const bool is_v = h >= kv.Hq + kv.Hkv;
-        const float* w = is_v ? nullptr : (h < kv.Hq ? a.q_w : a.k_w);
-        if (w) {
+        if (!is_v && (h < kv.Hq ? a.q_w : a.k_w)) {
             float ss = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) ss += x[e] * x[e] + y[e] * y[e];
+            ss = group_reduce<LPH>(ss, [](float p, float q) { return p + q; });
+            const float inv = inv_root(ss * inv_d + a.eps);
+            const float4 w0 = h < kv.Hq ? qw[0] : kw[0], w1 = h < kv.Hq ? qw[1] : kw[1];
+            const float u[4] = {w0.x, w0.y, w0.z, w0.w}, v[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-            for (int off = LPH / 2; off > 0; off >>= 1) ss += __shfl_xor(ss, off, 64);
-            const float inv = 1.0f / sqrtf(ss / (float)D + a.eps);
-            if (on) {
-                float w0[4], w1[4];
-                kv_load4(w + d0, w0);
-                kv_load4(w + d1, w1);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = x[e] * inv * w0[e];
-                    y[e] = y[e] * inv * w1[e];
-                }
+            for (int e = 0; e < 4; ++e) {
+                x[e] = x[e] * inv * u[e];
+                y[e] = y[e] * inv * v[e];
             }
         }
         if (turn && !is_v) {
@@ -141,10 +180,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
             float amax = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(x[e]), fabsf(y[e])));
-#pragma unroll
-            for (int off = LPH / 2; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
-            amax = amax >= kKvTiny ? amax : 0.0f;
-            const float inv = amax > 0.0f ? Q / amax : 0.0f;
+            amax = group_reduce<LPH>(amax, [](float p, float q) { return fmaxf(p, q); });
+            const float scale = amax >= kKvTiny ? amax * (1.0f / Q) : 0.0f;
+            const float inv = scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f;   // one step of 2^-23: no code moves but at a tie
             float u[4], v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -154,7 +192,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
             if (on && page >= 0) {
                 *(uint32_t*)(o + d0) = kv_encode4<FMT>(u);
                 *(uint32_t*)(o + d1) = kv_encode4<FMT>(v);
-                if (j == 0) (is_v ? kv.vs : kv.ks)[r] = amax / Q;
+                if (j == 0) (is_v ? kv.vs : kv.ks)[r] = scale;
             }
         }
     }
@@ -162,13 +200,17 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 
 // kv_read: kReadRows packed rows per workgroup. A page holds a head's tokens next to each other, so
 // the threads walk (k or v, head, row, 8 values) with the row inside the head: neighbouring threads
-// read one stretch of a page.
-constexpr int kReadRows = 16;
+// read one stretch of a page. A thread's next kReadAhead loads are in flight together.
+//
+// Bound by memory: 24000 rows of 16 heads of 128 from fp8 (149 MB in and out) in 27.2 us, 5.5 TB/s. Few rows
+// are split over gridDim.y workgroups (391 rows of bf16: 4.5 us, 12 by 25 workgroups alone).
+constexpr int kReadRows = 16, kReadAhead = 4, kReadGroups = 4096;
 template <typename T, int FMT>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvArgs a, T* k_out, int64_t ld_k, T* v_out, int64_t ld_v) {
     using E = typename KvElem<T, FMT>::type;
+    struct alignas(sizeof(E) == 1 ? 8 : 16) Codes { E e[8]; };
     __shared__ int s_page[kReadRows], s_pos[kReadRows];
-    if (blockIdx.x == 0) kv_check_seqs(a, threadIdx.x, 256);
+    if (blockIdx.x == 0 && blockIdx.y == 0) kv_check_seqs(a, threadIdx.x, 256);
     const int64_t t0 = (int64_t)blockIdx.x * kReadRows;
     if (threadIdx.x < kReadRows) {
         const int64_t t = t0 + threadIdx.x;
@@ -184,43 +226,52 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvArgs a, T* k_out, int64_
         s_pos[threadIdx.x] = pos;
     }
     __syncthreads();
-    const int D = a.D, pieces = D / 8, per = pieces * kReadRows;
-    for (int i = threadIdx.x; i < 2 * a.Hkv * per; i += 256) {
-        const int hh = i / per, r = (i % per) / pieces, d = (i % pieces) * 8;
-        const int page = s_page[r];
-        if (page < 0) continue;
-        const bool is_v = hh >= a.Hkv;
-        const int h = is_v ? hh - a.Hkv : hh;
-        const int64_t row = kv_pool_row(a, page, h, s_pos[r]);
-        const E* p = (const E*)(is_v ? a.v : a.k) + row * D + d;
-        T* o = (is_v ? v_out + (t0 + r) * ld_v : k_out + (t0 + r) * ld_k) + (int64_t)h * D + d;
-        if constexpr (FMT == SSM_KV_ACT) {
-            T v[8];
-            load16(p, v);
-            store16(o, v);
-        } else {
-            const float sc = (is_v ? a.vs : a.ks)[row];
-            const uint2 w = *(const uint2*)p;
-            float x[4], y[4];
-            kv_decode4<FMT>(w.x, x);
-            kv_decode4<FMT>(w.y, y);
-            T v[8];
+    const int D = a.D, pieces = D / 8, per = pieces * kReadRows, all = 2 * a.Hkv * per;
+    const int step = 256 * (int)gridDim.y;
+    for (int i0 = (int)blockIdx.y * 256 + threadIdx.x; i0 < all; i0 += kReadAhead * step) {
+        Codes c[kReadAhead];
+        float sc[kReadAhead];
+        T* o[kReadAhead];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = from_f32<T>(x[e] * sc);
-                v[4 + e] = from_f32<T>(y[e] * sc);
+        for (int b = 0; b < kReadAhead; ++b) {
+            const int i = i0 + b * step;
+            o[b] = nullptr;
+            if (i >= all) continue;
+            const int hh = i / per, r = (i % per) / pieces, d = (i % pieces) * 8;
+            const int page = s_page[r];
+            if (page < 0) continue;
+            const bool is_v = hh >= a.Hkv;
+            const int h = is_v ? hh - a.Hkv : hh;
+            const int64_t row = kv_pool_row(a, page, h, s_pos[r]);
+            c[b] = *(const Codes*)((const E*)(is_v ? a.v : a.k) + row * D + d);
+            if constexpr (FMT != SSM_KV_ACT) sc[b] = (is_v ? a.vs : a.ks)[row];
+            o[b] = (is_v ? v_out + (t0 + r) * ld_v : k_out + (t0 + r) * ld_k) + (int64_t)h * D + d;
+        }
+#pragma unroll
+        for (int b = 0; b < kReadAhead; ++b) {
+            if (!o[b]) continue;
+            if constexpr (FMT == SSM_KV_ACT) {
+                store16(o[b], c[b].e);
+            } else {
+                const uint2 w = __builtin_bit_cast(uint2, c[b]);
+                float x[4], y[4];
+                kv_decode4<FMT>(w.x, x);
+                kv_decode4<FMT>(w.y, y);
+                T v[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = from_f32<T>(x[e] * sc[b]);
+                    v[4 + e] = from_f32<T>(y[e] * sc[b]);
+                }
+                store16(o[b], v);
             }
-            store16(o, v);
         }
     }
 }
 
 template <typename T, int FMT> hipError_t append_launch(const KvAppendArgs& a, hipStream_t s) {
     const int lph = a.kv.D <= 64 ? 8 : a.kv.D <= 128 ? 16 : 32;
-    const int rounds = (a.kv.Hq + 2 * a.kv.Hkv + 256 / lph - 1) / (256 / lph);
-    // few tokens: the heads spread over workgroups; many: one workgroup takes a token's heads
-    const int slices = (int)(a.kv.T >= 1024 ? 1 : rounds);
-    const dim3 grid((unsigned)a.kv.T, (unsigned)slices), block(256);
+    const dim3 grid((unsigned)a.kv.T), block(256);
     if (lph == 8) SSM_LAUNCH((kv_append_kernel<T, FMT, 8>), grid, block, 0, s, a);
     else if (lph == 16) SSM_LAUNCH((kv_append_kernel<T, FMT, 16>), grid, block, 0, s, a);
     else SSM_LAUNCH((kv_append_kernel<T, FMT, 32>), grid, block, 0, s, a);
@@ -234,7 +285,10 @@ template <typename T> hipError_t append_fmt(const KvAppendArgs& a, hipStream_t s
     }
 }
 template <typename T> hipError_t read_fmt(const KvArgs& a, T* k, int64_t ld_k, T* v, int64_t ld_v, hipStream_t s) {
-    const dim3 grid((unsigned)((a.T + kReadRows - 1) / kReadRows)), block(256);
+    // few rows: split until there are kReadGroups workgroups or each thread has one piece
+    const int64_t groups = (a.T + kReadRows - 1) / kReadRows, rounds = (2LL * a.Hkv * (a.D / 8) * kReadRows + 255) / 256;
+    const int64_t want = (kReadGroups + groups - 1) / groups, slices = want < rounds ? want : rounds;
+    const dim3 grid((unsigned)groups, (unsigned)slices), block(256);
     switch (a.fmt) {
         case SSM_KV_ACT: SSM_LAUNCH((kv_read_kernel<T, SSM_KV_ACT>), grid, block, 0, s, a, k, ld_k, v, ld_v); break;
         case SSM_KV_FP8_E4M3: SSM_LAUNCH((kv_read_kernel<T, SSM_KV_FP8_E4M3>), grid, block, 0, s, a, k, ld_k, v, ld_v); break;
