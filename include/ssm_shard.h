@@ -503,8 +503,9 @@ int ssm_kv_read(const ssm_attn_desc_t* desc, int64_t T, const ssm_kv_meta_t* met
 /* Causal attention of packed prompt chunks: q, out [T][ld] act, columns [q heads] of head_dim. Row r of
  * a sequence attends to the cached tokens up to its own (and inside the window); they are read from the
  * cache, the call's own among them, so ssm_kv_append comes first. out is not q. Scores and the softmax are float32;
- * with bf16 activations the probabilities are rounded to bf16 for their product with v. A value of v that
- * is not finite may reach rows before its token; what pages hold behind a sequence's last token never does. */
+ * with bf16 activations the probabilities are rounded to bf16 for their product with v, with float32 ones a
+ * product is exact to 2^-23. A value that is not finite (float32: above 3.38e38) makes the rows that see it
+ * NaN, and one of v may reach rows before its token; what pages hold behind a sequence's last token never does. */
 int ssm_attn_prefill(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, int64_t T, const ssm_kv_meta_t* meta,
                      const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
                      hipStream_t stream);

@@ -7,13 +7,13 @@
 //   O^T = V^T P^T  the lane's scores are this product's operand as they stand: entries 8 s .. 8 s + 7 are
 //                  tokens 16 s + 4 half + {0 .. 3} and 16 s + 8 + 4 half + {0 .. 3}, which over both lane
 //                  halves are the 16 tokens of one K-step once; v comes from LDS in that order, by the
-//                  transposing 64-bit LDS reads (bf16) or one value per lane (float32).
+//                  transposing 64-bit LDS reads (one value per lane in float32 above 128 values a head).
 // So the softmax needs one exchange between lanes per step (the maximum of the two halves), and the
 // rescale of O is one factor per lane. K and V steps of TOK tokens go through LDS, shared by the
 // waves, in two buffers: the next step's loads are in flight while the present one is computed.
 //
 // Work: the plan kernel lists (tile, range of tokens) items so that no item is longer than a share of
-// the whole work (tile_target() items of equal length); tiles behind a long cache are cut into several items
+// the whole work (that of one place, tile_places(), or half of it); tiles behind a long cache are cut into several items
 // whose partial results (m, l and the unnormalised o, float32) a third kernel joins in order. Items are
 // listed longest first, and the workgroups of one item's kv heads are neighbours.
 #pragma once
@@ -27,13 +27,8 @@ namespace ssm {
 // behind 4096, 57 and 43. Heads of 64 values, 16 of them, 6000 tokens: 114 and 108.
 inline int tile_rows(bool bf16_act, int DP, int64_t rows_heads) { return bf16_act && DP == 128 && rows_heads >= 65536 ? 256 : 128; }
 constexpr int kStep = 64;          // the plan counts tokens in steps of this many
-// Workgroups that run at once: two on a compute unit where their registers allow it
-inline int tile_places(int rows, int DP) { return rows == 128 && DP <= 128 ? 512 : 256; }
-// Items that the whole work is cut into. Float32 is bound by its MFMAs, two workgroups sharing a unit's:
-// what counts is an even load, in short items whose beginnings and ends the other workgroup covers.
-// (2048 rows in three prompts, one behind 4096 tokens: 512 items of at least 8 steps 218 us, 1024 of at least
-// 4 192 us, their join 3 us more; 2048 200 us and 14 us more.)
-inline int tile_target(bool bf16_act, int rows, int DP) { return bf16_act ? tile_places(rows, DP) : 1024; }
+// Workgroups that run at once: two on a compute unit where their registers and LDS allow it (PrefillShape)
+inline int tile_places(bool bf16_act, int rows, int DP) { return rows == 128 && DP <= (bf16_act ? 128 : 96) ? 512 : 256; }
 constexpr int tile_min_steps(bool bf16_act) { return bf16_act ? 8 : 4; }   // no item is cut shorter than this
 
 // Tokens [k0, k1) for the tile at row0 of a sequence whose rows begin at lo (m tokens, n cached).
@@ -46,7 +41,7 @@ struct AttnPlan {
     AttnItem* items;
     AttnJoin* joins;
     float* parts;        // [Hkv][max_parts][rows (DP + 2)]
-    int rows, places, target, max_tiles, max_items, max_joins, max_parts;
+    int rows, places, max_tiles, max_items, max_joins, max_parts;
     size_t total;
 };
 // sizes for up to T rows of nseq sequences
@@ -55,9 +50,8 @@ inline AttnPlan attn_plan(bool bf16_act, int Hq, int Hkv, int DP, int64_t T, int
     p.rows = tile_rows(bf16_act, DP, T * Hq);
     const int64_t tiles = (T * (Hq / Hkv) + p.rows - 1) / p.rows + nseq;
     // cut tiles have more steps than a share of the work: their number and their items' are bounded by it
-    p.places = tile_places(p.rows, DP);
-    p.target = tile_target(bf16_act, p.rows, DP);
-    const int64_t share = (p.target + Hkv - 1) / Hkv + 1;
+    p.places = tile_places(bf16_act, p.rows, DP);
+    const int64_t share = (p.places * (bf16_act ? 1 : 2) + Hkv - 1) / Hkv + 1;
     p.max_tiles = (int)tiles;
     p.max_items = (int)(tiles + share);
     p.max_joins = (int)(tiles < share ? tiles : share);

@@ -95,26 +95,27 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     for (int off = 32; off > 0; off >>= 1) steps += __shfl_xor(steps, off, 64);
     if (lane == 0 && steps) atomicAdd(&s_steps, steps);
     __syncthreads();
-    const unsigned long long share = (s_steps * a.Hkv + p.target - 1) / p.target;
+    const unsigned long long share = (s_steps * a.Hkv + p.places - 1) / p.places;
     int most = share < (unsigned)tile_min_steps(bf16_act) ? tile_min_steps(bf16_act) : (int)share;   // steps of the longest item
-    // bf16, where a step waits more than it computes: if every tile has a place of its own at once, the cut is
-    // such that every item has (the first of 16 lengths, from an equal share to twice that, at which the items
-    // are no more than the places)
-    if (bf16_act && (int64_t)total * a.Hkv <= p.places) {
+    // If every tile has a place of its own at once, the cut is such that every item has: the first of 16 lengths,
+    // from an equal share to twice that (float32: one and a half times), at which the items are no more than the
+    // places. Float32 is otherwise cut to half a share, in two rounds: its steps are long, and what the rounds add
+    // costs less than places without work (16 heads of 112, 2048 rows: 131 us and 13 for the join, uncut 160 and 4;
+    // three prompts, one behind 4096 tokens: 146 and 10, in one round 140 and 6).
+    if ((int64_t)total * a.Hkv <= p.places) {
         if (tid < total) s_len[tid] = first.r.steps;
         __syncthreads();
-        const int len = most + most * (tid >> 6) / 16;
+        const int c = tid >> 6, len = most + most * c / 16;
         int items = 0;
         for (int t = lane; t < total; t += 64) items += (s_len[t] + len - 1) / len;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) items += __shfl_xor(items, off, 64);
-        if (lane == 0) s_wave[tid >> 6] = (int64_t)items * a.Hkv <= p.places ? len : 2 * most;
+        if (lane == 0) s_wave[c] = (int64_t)items * a.Hkv <= p.places && (bf16_act || c <= 8) ? len : 0;
         __syncthreads();
-        for (int k = 0; k < kPlanThreads / 64; ++k)
-            if (s_wave[k] < 2 * most) {
-                most = s_wave[k];
-                break;
-            }
+        int found = 0;
+        for (int k = kPlanThreads / 64 - 1; k >= 0; --k) found = s_wave[k] ? s_wave[k] : found;
+        if (found) most = found;
+        else if (!bf16_act) most = max(tile_min_steps(bf16_act), (most + 1) / 2);
     }
     auto cut = [&](const TileRange& r, int& pieces, int& len) {
         pieces = r.steps > most ? (r.steps + most - 1) / most : 1;
@@ -159,17 +160,15 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     if (tid == 0) p.count[0] = s_join;
 }
 
-// The width that a head's values are padded to in the products. Float32, whose rate is a sixteenth of
-// bf16's, has three.
+// The width that a head's values are padded to in the products. Float32 has one above 128.
 int padded_dim(bool bf16_act, int D) {
     if (bf16_act) return D <= 64 ? 64 : (D + 31) / 32 * 32;
-    return D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    return D <= 64 ? 64 : D <= 128 ? (D + 31) / 32 * 32 : 256;
 }
 
 template <typename T, int FMT> hipError_t prefill_dim(const AttnArgs& p, const AttnPlan& pl, int dp, hipStream_t s) {
     if constexpr (sizeof(T) == 2) {
         switch (dp) {
-            case 96: return launch_attn_prefill_tile<T, FMT, 96>(p, pl, s);
             case 160: return launch_attn_prefill_tile<T, FMT, 160>(p, pl, s);
             case 192: return launch_attn_prefill_tile<T, FMT, 192>(p, pl, s);
             case 224: return launch_attn_prefill_tile<T, FMT, 224>(p, pl, s);
@@ -177,6 +176,7 @@ template <typename T, int FMT> hipError_t prefill_dim(const AttnArgs& p, const A
     }
     switch (dp) {
         case 64: return launch_attn_prefill_tile<T, FMT, 64>(p, pl, s);
+        case 96: return launch_attn_prefill_tile<T, FMT, 96>(p, pl, s);
         case 128: return launch_attn_prefill_tile<T, FMT, 128>(p, pl, s);
         default: return launch_attn_prefill_tile<T, FMT, 256>(p, pl, s);
     }

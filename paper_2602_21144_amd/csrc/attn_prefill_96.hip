@@ -3,4 +3,5 @@
 
 namespace ssm {
 SSM_ATTN_PREFILL_BF16(96)
+SSM_ATTN_PREFILL_F32(96)
 }  // namespace ssm

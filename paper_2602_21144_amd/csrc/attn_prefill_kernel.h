@@ -8,16 +8,39 @@
 namespace ssm {
 
 // ---------------------------------------------------------------- the main kernel
-template <typename T, int DP, int WAVES> struct PrefillShape {
+// Float32 products on the bf16 matrix cores: a value is the sum of three bf16 (8 bits each, to nearest, the
+// rest going on: the 24 bits of the value), and a product that of the six pairs that count. What is left out, two
+// products of a middle and a low part, is below 2^-23 of |a b|, where the float32 sum of D products is good to
+// D 2^-24; every product of parts is exact and summed in float32. Six MFMAs of 16 values take 192 cycles, the
+// eight float32 ones that they stand for 512 (32 heads of 128, 8192 tokens: 2.7 ms, 4.1 by float32 MFMAs, 201 and
+// 133 TF/s; three prompts of 2048 tokens in all, 16 heads of 112: 151 and 207 us with plan and join). An 8-bit
+// cache's codes are one part, 3 products. Infinite values have no such parts: they give NaN. Wider heads than 128
+// have no room for the parts in LDS and take the float32 MFMAs.
+template <typename T, int FMT, int DP, int WAVES> struct PrefillShape {
     static constexpr bool BF = sizeof(T) == 2;
+    static constexpr bool SPLIT = !BF && DP <= 128;
+    static constexpr int QP = SPLIT ? 3 : 1, KP = SPLIT && FMT == SSM_KV_ACT ? 3 : 1;   // parts of q and p, of k and v
+    using S = std::conditional_t<BF || SPLIT, bf16, float>;                             // what LDS and the products hold
     static constexpr int TOK = BF ? 64 : 32, MT = TOK / 32, DT = DP / 32;
     static constexpr int PE = 16 / (int)sizeof(T);        // values per staged piece
     static constexpr int NP = DP / 32;                     // pieces of 16 bytes per lane, step and source
     // row strides in LDS: k rows 16 bytes apart modulo 256 (16 lanes read 16 rows), v rows 64 or 192
     // bytes (bf16: a half wave reads 4 rows of 64 bytes) or 32 bytes (float32) apart
-    static constexpr int KS = DP + PE;
-    static constexpr int VS = BF ? ((DP * 2) % 256 == 64 || (DP * 2) % 256 == 192 ? DP : DP + 32) : DP + 8;
+    static constexpr int KS = DP + 16 / (int)sizeof(S);
+    static constexpr int VS = sizeof(S) == 2 ? ((DP * 2) % 256 == 64 || (DP * 2) % 256 == 192 ? DP : DP + 32) : DP + 8;
+    // workgroups of a compute unit, by registers and LDS (tile_places; float32 heads of 96, 24 of them, 8192 tokens:
+    // two 1.44 ms, one with registers to spare 1.67)
+    static constexpr int PER_CU = BF ? (DP <= 128 && WAVES == 4 ? 2 : 1) : (DP <= 96 ? 2 : 1);
 };
+// The next part of two values, which are left with what goes on: two bf16 of a word
+__device__ __forceinline__ uint32_t take_part(float (&r)[2]) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{r[0], r[1]}, bf16x2));
+    r[0] -= __builtin_bit_cast(float, w << 16);
+    r[1] -= __builtin_bit_cast(float, w & 0xffff0000u);
+    return w;
+}
 
 constexpr float kLag = 8.0f;
 
@@ -36,16 +59,18 @@ template <typename F> __device__ __forceinline__ float over_halves(float x, F f)
 }
 
 template <typename T, int FMT, int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (DP <= 128 ? 2 : 1))
+__global__ __launch_bounds__(64 * WAVES, (PrefillShape<T, FMT, DP, WAVES>::PER_CU * WAVES / 4))
 void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
-    using Sh = PrefillShape<T, DP, WAVES>;
+    using Sh = PrefillShape<T, FMT, DP, WAVES>;
+    using S = typename Sh::S;
     using E = typename KvElem<T, FMT>::type;
-    constexpr bool BF = Sh::BF;
+    constexpr bool BF = Sh::BF, SPLIT = Sh::SPLIT, RUN = BF || SPLIT;
+    constexpr int PER_CU = Sh::PER_CU, QP = Sh::QP, KP = Sh::KP;
     constexpr int TOK = Sh::TOK, MT = Sh::MT, DT = Sh::DT, PE = Sh::PE, NP = Sh::NP, KS = Sh::KS, VS = Sh::VS;
     constexpr int ROWS = 32 * WAVES;
     constexpr int GW = PE * (int)sizeof(E) / 4;            // 32-bit words of a piece in the cache
-    __shared__ __align__(16) T s_k[2][TOK * KS];
-    __shared__ __align__(16) T s_v[2][TOK * VS];
+    __shared__ __align__(16) S s_k[2][KP * TOK * KS];
+    __shared__ __align__(16) S s_v[2][KP * TOK * VS];
     __shared__ __align__(16) float s_ks[4][FMT == SSM_KV_ACT ? 4 : TOK], s_vs[4][FMT == SSM_KV_ACT ? 4 : TOK];
     __shared__ int s_bad;
 
@@ -70,18 +95,32 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     const bool wave_on = row_w < sq.m * g;
     const int pos_lo = before + (wave_on ? row_w : item.row0) / g;
     const int pos_hi = before + min(row_w + 31, sq.m * g - 1) / g;
-    constexpr int QN = BF ? DP / 16 : DP / 8;              // q operands: 8 values per lane per 16 dims, 4 per 8
-    T q[QN][BF ? 8 : 4];
+    constexpr int QN = RUN ? DP / 16 : DP / 8;             // q operands: 8 values per lane per 16 dims, 4 per 8
+    S q[QN][QP][RUN ? 8 : 4];
     {
         const T* qp = (const T*)p.q + (int64_t)(sq.lo + tok) * p.ld_q + (int64_t)hq * a.D;
 #pragma unroll
         for (int s = 0; s < QN; ++s) {
-            const int d = BF ? s * 16 + half * 8 : s * 8 + half * 4;
+            const int d = RUN ? s * 16 + half * 8 : s * 8 + half * 4;
+            T x[RUN ? 8 : 4];
             if (on && d < a.D) {
-                load16(qp + d, q[s]);
+                load16(qp + d, x);
             } else {
 #pragma unroll
-                for (int e = 0; e < (BF ? 8 : 4); ++e) q[s][e] = from_f32<T>(0.0f);
+                for (int e = 0; e < (RUN ? 8 : 4); ++e) x[e] = from_f32<T>(0.0f);
+            }
+            if constexpr (SPLIT) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    float y[2] = {x[2 * h], x[2 * h + 1]};
+#pragma unroll
+                    for (int k = 0; k < QP; ++k) {
+                        const uint32_t w = take_part(y);
+                        __builtin_memcpy(&q[s][k][2 * h], &w, 4);
+                    }
+                }
+            } else {
+                __builtin_memcpy(q[s][0], x, sizeof x);
             }
         }
     }
@@ -160,8 +199,33 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         static_for<NP>([&](auto i) { load_piece(b, i); });
         if constexpr (b == 0) load_scales();
     };
-    auto stage_piece = [&](auto b, int step, auto i) {
+    constexpr int kTurns = KP == 3 ? 4 : 1;                // that a piece is staged in
+    float rest[2];
+    u32x2 parts[KP];
+    auto stage_piece = [&](auto b, int step, auto i, auto turn) {
         const uint32_t (&w)[GW] = held[b][i];
+        S* to = (b == 1 || second ? &s_v[step & 1][0] : &s_k[step & 1][0]) + at[b][i];
+        if constexpr (SPLIT && FMT == SSM_KV_ACT) {   // four values in 4 turns: a pair's first part, then its others
+            constexpr int pair = turn / 2, at0 = 2 * pair;
+            static_assert(KP == 3 && kTurns == 4);
+            if constexpr (turn % 2 == 0) {
+                rest[0] = __builtin_bit_cast(float, w[at0]);
+                rest[1] = __builtin_bit_cast(float, w[at0 + 1]);
+                parts[0][pair] = take_part(rest);
+            } else {
+                parts[1][pair] = take_part(rest);
+                parts[2][pair] = take_part(rest);
+            }
+            if constexpr (turn == kTurns - 1) {
+#pragma unroll
+                for (int k = 0; k < KP; ++k) *(u32x2*)(to + k * TOK * (b == 1 ? VS : KS)) = parts[k];
+            }
+            return;
+        }
+        if constexpr (SPLIT && FMT != SSM_KV_ACT) {
+            *(u32x2*)to = kv_decode4_bf16<FMT>(w[0]);
+            return;
+        }
         u32x4 x;                                           // 16 bytes of T
         if constexpr (FMT == SSM_KV_ACT) {
             x = u32x4{w[0], w[1], w[2], w[3]};
@@ -173,7 +237,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             kv_decode4<FMT>(w[0], f);
             __builtin_memcpy(&x, f, 16);
         }
-        *(u32x4*)((b == 1 || second ? &s_v[step & 1][0] : &s_k[step & 1][0]) + at[b][i]) = x;
+        *(u32x4*)to = x;
     };
     auto stage_scales = [&](int step) {
         if constexpr (FMT != SSM_KV_ACT) {
@@ -184,7 +248,9 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         }
     };
     auto stage_all = [&](auto b, int step) {
-        static_for<NP>([&](auto i) { stage_piece(b, step, i); });
+        static_for<NP * kTurns>([&](auto i) {
+            stage_piece(b, step, std::integral_constant<int, i / kTurns>{}, std::integral_constant<int, i % kTurns>{});
+        });
         if constexpr (b == 0) stage_scales(step);
     };
     constexpr std::integral_constant<int, 0> b0{};
@@ -210,12 +276,12 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
 
     f32x16 s[MT];                                          // the step's scores, then its probabilities
-    bf16x8 pf[BF ? TOK / 16 : 1];                          // and those as the operand of the product with v
+    bf16x8 pf[QP][RUN ? TOK / 16 : 1];                     // and those as the operand of the product with v
     auto seen = [&](int tb) {
         return wave_on && tb <= pos_hi && (a.window <= 0 || tb + TOK - 1 > pos_lo - a.window);
     };
     bool bad = false;
-    auto soften = [&](int tb, int step) {
+    auto scale_scores = [&](f32x16 (&s)[MT], int step) {
         if constexpr (FMT != SSM_KV_ACT) {
 #pragma unroll
             for (int t = 0; t < MT; ++t)
@@ -227,6 +293,8 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                     if (w == 3) __builtin_amdgcn_sched_barrier(0);
                 }
         }
+    };
+    auto mask_scores = [&](f32x16 (&s)[MT], int tb) {
         const bool edge = tb + TOK - 1 > pos_lo || (a.window > 0 && tb <= pos_hi - a.window);
         if (edge) {   // the token of s[t][r] is a constant behind tb + 4 half
             const int last = pos - tb - 4 * half, first = a.window > 0 ? last - a.window : -1;
@@ -248,28 +316,45 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                     s[t][r] = pg >= 0 && pg < a.num_pages ? s[t][r] : -__builtin_inff();
                 }
         }
-        float mx = s[0][0];
+    };
+    // Empty statements that have the sums in the same registers on both ways of the branch below, a wave that is
+    // alone on its SIMD in the matrix cores' own (the branch then moves them out and back): without them the
+    // compiler copies four tiles of them in every step, and spills with 8-bit caches
+    constexpr bool ALONE = RUN && DP <= 128 && PER_CU * WAVES == 4;
+    auto keep_sums = [&] {
+        if constexpr (RUN && DP <= 128) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+            for (int t = 0; t < DT; ++t) {
+                if constexpr (ALONE) asm volatile("" : "+a"(o[t]));
+                else asm volatile("" : "+v"(o[t]));
+            }
+        }
+    };
+    auto follow_max = [&](float mx) {                      // mx: of the lane's scores
         mx = over_halves(mx, [](float x, float y) { return fmaxf(x, y); });
         const float mn = fmaxf(m, mx * c2);
         // The sums are kept relative to m, which need not be the maximum itself: it follows once the
         // maximum is kLag powers of two above it (then no p is above 2^kLag, and no digit is lost)
+        if constexpr (ALONE) keep_sums();
         if (__any(mn > m + kLag)) {
             const float al = fast_exp2(m - mn);
             l *= al;
 #pragma unroll
             for (int t = 0; t < DT; ++t) o[t] *= al;
+            if constexpr (ALONE) keep_sums();
             m = mn;
         }
-        if constexpr (BF && DP <= 128) {
-            // (an empty statement that has the sums in the same registers on both ways here: without it the
-            // compiler copies four tiles of them in every step, and spills with 8-bit caches)
+        keep_sums();
+    };
+    auto soften = [&](int tb, int step) {
+        scale_scores(s, step);
+        mask_scores(s, tb);
+        float mx = s[0][0];
 #pragma unroll
-            for (int t = 0; t < DT; ++t) asm volatile("" : "+v"(o[t]));
-        }
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+        follow_max(mx);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -298,18 +383,18 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
 #pragma unroll
             for (int ks = 0; ks < TOK / 16; ++ks) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)s[ks >> 1][8 * (ks & 1) + e];
+                for (int e = 0; e < 8; ++e) pf[0][ks][e] = (bf16)s[ks >> 1][8 * (ks & 1) + e];
                 if constexpr (FMT == SSM_KV_ACT) {
 #pragma unroll
                     for (int e = 0; e < 8; e += 2)
-                        ls[ks & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[ks][e], pf[ks][e + 1]}, one, ls[ks & 1], false);
+                        ls[ks & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[0][ks][e], pf[0][ks][e + 1]}, one, ls[ks & 1], false);
                 }
             }
             if constexpr (FMT == SSM_KV_ACT) l += ls[0] + ls[1];
         }
     };
     const int steps = (item.k1 - item.k0 + TOK - 1) / TOK;
-    if constexpr (BF) {
+    if constexpr (RUN) {
         // The products of step i are one run of MFMAs, K(i) Q and then V(i-1) P(i-1), each fragment read
         // from LDS kLead MFMAs ahead of its own (a wave alone: 69 cycles per MFMA as the compiler orders it,
         // 41 so; the MFMA takes 32). Meanwhile K(i+1) and V(i) go from registers to LDS and the loads of the
@@ -326,16 +411,27 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         // Four waves, where two halves of 8 would not have registers enough or few rows would leave most of
         // them without work: one barrier per step, and the other workgroup of the compute unit (up to 128
         // values per head) fills the softmax.
-        constexpr int kLead = 4, NV = DT * TOK / 16, NK = QN * MT, N = NK + NV;
-        constexpr int kSlots = NB * (2 * NP + 1) + 1, kFirst = N - kSlots;
-        static_assert(kFirst >= 0, "the run is long enough for what it brings");
+        //
+        // Float32: the parts of a fragment of k or v one after the other, each for the parts of q or p that it is
+        // paired with. One wave on each SIMD, whose softmax i - 1 is dealt out over the products K(i) Q, in front
+        // of V(i-1) P(i-1) that needs it.
+        constexpr int MF = KP == 3 ? 6 : QP;               // MFMAs of a fragment's parts
+        constexpr int FK = QN * MT * KP, F = FK + DT * (TOK / 16) * KP;   // fragments of k; and of v
+        constexpr int NK = FK / KP * MF, N = F / KP * MF, NV = N - NK;
+        constexpr int kAfter = SPLIT ? MF * 3 / KP : 0;    // MFMAs of the last kLead fragments
+        constexpr int kLead = SPLIT ? 3 : 4, kSlots = NB * (NP * kTurns + NP + 1) + 1, kSoft = 37;
+        static_assert(BF || F % (kLead + 1) == 0, "a step's first fragments follow the last ones");
+        static_assert(BF ? N >= kSlots : NV > kAfter, "the run is long enough for what it brings");
         const int lead = second ? 0 : 1;                   // source 0 is staged for step i + lead
-        for (int i = tid; i < TOK * VS * 2 / 16; i += 64 * WAVES) ((u32x4*)&s_v[1][0])[i] = u32x4{0, 0, 0, 0};   // V(-1)
+        for (int i = tid; i < KP * TOK * VS * 2 / 16; i += 64 * WAVES) ((u32x4*)&s_v[1][0])[i] = u32x4{0, 0, 0, 0};   // V(-1)
+        if constexpr (SPLIT && FMT != SSM_KV_ACT) {
+            if (tid < TOK) s_vs[3][tid] = 0.0f;            // and its scales
+        }
         auto no_probabilities = [&] {
 #pragma unroll
-            for (int ks = 0; ks < TOK / 16; ++ks)
+            for (int k = 0; k < QP; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[ks][e] = (bf16)0.0f;
+                for (int ks = 0; ks < TOK / 16; ++ks) pf[k][ks] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
         };
         no_probabilities();
         int page[NB];
@@ -354,16 +450,19 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         page[0] = page_at(1 + lead);
         check_pages();
 
-        const T* v_at = &s_v[0][(4 * half + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4];
-        const T* k_at = &s_k[0][col * KS + half * 8];
+        const S* v_at = &s_v[0][(4 * half + ((lane & 15) >> 2)) * VS + ((lane >> 4) & 1) * 16 + (lane & 3) * 4];
+        const S* k_at = &s_k[0][col * KS + half * 8];
         bf16x8 fr[kLead + 1];
         auto read = [&](auto f, int i) {
-            if constexpr (f < NK) {
-                fr[f % (kLead + 1)] = *(const bf16x8*)(k_at + (i & 1) * TOK * KS + (f % MT) * 32 * KS + (f / MT) * 16);
+            constexpr int part = f % KP;
+            if constexpr (f < FK) {
+                constexpr int x = f / KP;
+                fr[f % (kLead + 1)] = *(const bf16x8*)(k_at + ((i & 1) * KP + part) * TOK * KS + (x % MT) * 32 * KS + (x / MT) * 16);
             } else {
                 typedef short s16x4 __attribute__((ext_vector_type(4)));
                 typedef __attribute__((address_space(3))) s16x4* lds4;
-                const T* q = v_at + ((i - 1) & 1) * TOK * VS + ((f - NK) / DT) * 16 * VS + ((f - NK) % DT) * 32;
+                constexpr int x = (f - FK) / KP;
+                const S* q = v_at + (((i - 1) & 1) * KP + part) * TOK * VS + (x / DT) * 16 * VS + (x % DT) * 32;
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)q);
                 const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(q + 8 * VS));
                 fr[f % (kLead + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -371,11 +470,12 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         };
         auto read_first = [&](int i) { static_for<kLead>([&](auto f) { read(f, i); }); };
         auto bring = [&](auto slot, int i) {               // slot of kSlots: stage, then locate and load by source
-            if constexpr (slot < NB * NP) {
-                constexpr std::integral_constant<int, slot / NP> b{};
-                stage_piece(b, i + (b == 0 ? lead : 0), std::integral_constant<int, slot % NP>{});
+            if constexpr (slot < NB * NP * kTurns) {
+                constexpr int piece = slot / kTurns;
+                constexpr std::integral_constant<int, piece / NP> b{};
+                stage_piece(b, i + (b == 0 ? lead : 0), std::integral_constant<int, piece % NP>{}, std::integral_constant<int, slot % kTurns>{});
             } else {
-                constexpr int r = slot - NB * NP, x = r % (NP + 1);
+                constexpr int r = slot - NB * NP * kTurns, x = r % (NP + 1);
                 constexpr std::integral_constant<int, r / (NP + 1)> b{};
                 if constexpr (r == 0) stage_scales(i + lead);
                 if constexpr (b < NB) {
@@ -388,25 +488,84 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                 }
             }
         };
-        auto products = [&](int i) {
-            __builtin_amdgcn_s_setprio(1);
-            static_for<N>([&](auto f) {
-                if constexpr (f + kLead < N) read(std::integral_constant<int, f + kLead>{}, i);
-                if constexpr (f < NK) {
-                    constexpr int t = f % MT;
-                    if constexpr (f / MT == 0) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
-                    }
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], __builtin_bit_cast(bf16x8, q[f / MT]), s[t], 0, 0, 0);
+        // A turn of float32's softmax: scales, masks, maximum, then the probabilities by pairs, each value, a first
+        // part and the others in a turn of their own: six instructions fit beside an MFMA
+        f32x4 sc_v;
+        float rest_p[2], top = 0.0f;
+        auto put = [](bf16x8& x, int word, uint32_t v) {
+            u32x4 y = __builtin_bit_cast(u32x4, x);
+            y[word] = v;
+            x = __builtin_bit_cast(bf16x8, y);
+        };
+        auto soften_turn = [&](f32x16 (&s)[MT], auto k, int i) {
+            const int tb = item.k0 + i * TOK;
+            if constexpr (k == 0) {
+                scale_scores(s, i);
+            } else if constexpr (k == 1) {
+                if (i >= 0 && i < steps && seen(tb)) {
+                    mask_scores(s, tb);
                 } else {
-                    constexpr int t = (f - NK) % DT;
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], pf[(f - NK) / DT], o[t], 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[0][r] = -__builtin_inff();
                 }
-                if constexpr (f >= kFirst) bring(std::integral_constant<int, f - kFirst>{}, i);
-                __builtin_amdgcn_sched_barrier(0);
+            } else if constexpr (k == 2 || k == 3) {
+                if constexpr (k == 2) top = s[0][0];
+#pragma unroll
+                for (int r = 8 * (k - 2); r < 8 * (k - 1); ++r) top = fmaxf(top, s[0][r]);
+            } else if constexpr (k == 4) {
+                if constexpr (FMT != SSM_KV_ACT) sc_v = *(const f32x4*)&s_vs[i & 3][4 * half];
+                follow_max(top);
+            } else {
+                constexpr int w = (k - 5) / 4, ks = w / 4, turn = (k - 5) % 4;
+                if constexpr (turn < 2) {
+                    float y = fast_exp2(__builtin_fmaf(s[0][2 * w + turn], c2, -m));
+                    l += y;
+                    if constexpr (FMT != SSM_KV_ACT) y *= sc_v[(2 * w + turn) & 3];
+                    rest_p[turn] = y;
+                    if constexpr (FMT != SSM_KV_ACT && turn == 1 && w % 2 == 1 && w < 7)
+                        sc_v = *(const f32x4*)&s_vs[i & 3][8 * (w / 2 + 1) + 4 * half];
+                } else if constexpr (turn == 2) {
+                    put(pf[0][ks], w % 4, take_part(rest_p));
+                } else {
+                    put(pf[1][ks], w % 4, take_part(rest_p));
+                    put(pf[2][ks], w % 4, take_part(rest_p));
+                }
+            }
+        };
+        // K(i) Q into sk; sp: the scores of step i - 1 (float32)
+        auto products = [&](int i, f32x16 (&sk)[MT], f32x16 (&sp)[MT]) {
+            if constexpr (BF) __builtin_amdgcn_s_setprio(1);
+            static_for<F>([&](auto f) {
+                if constexpr (SPLIT && f + kLead == F) __syncthreads();   // all of the step is read, all of the next one there
+                if constexpr (f + kLead < F) read(std::integral_constant<int, f + kLead>{}, i);
+                else if constexpr (SPLIT) read(std::integral_constant<int, f + kLead - F>{}, i + 1);
+                constexpr int part = f % KP, first = f / KP * MF + (part == 0 ? 0 : part == 1 ? QP : 2 * QP - 1);
+                static_for<(KP == 3 ? QP - part : QP)>([&](auto x) {   // the parts of q or p
+                    constexpr int at = first + x;          // this MFMA's place in the run
+                    if constexpr (f < FK) {
+                        constexpr int t = f / KP % MT;
+                        if constexpr (f / KP / MT == 0 && part == 0 && x == 0) {
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) sk[t][r] = 0.0f;
+                        }
+                        sk[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], __builtin_bit_cast(bf16x8, q[f / KP / MT][x]), sk[t], 0, 0, 0);
+                    } else {
+                        constexpr int t = (f - FK) / KP % DT;
+                        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[f % (kLead + 1)], pf[x][(f - FK) / KP / DT], o[t], 0, 0, 0);
+                    }
+                    if constexpr (SPLIT) {
+                        static_for<kSoft>([&](auto k) {
+                            if constexpr (k * NK / kSoft == at) soften_turn(sp, k, i - 1);
+                        });
+                    }
+                    static_for<kSlots>([&](auto slot) {
+                        if constexpr ((BF ? N - kSlots + slot : NK + slot * (NV - kAfter) / kSlots) == at) bring(slot, i);
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
             });
-            __builtin_amdgcn_s_setprio(0);
+            if constexpr (BF) __builtin_amdgcn_s_setprio(0);
+            if constexpr (ALONE) keep_sums();
         };
         auto softmax = [&](int i) {
             if (i < steps && seen(item.k0 + i * TOK)) soften(item.k0 + i * TOK, i);
@@ -426,17 +585,27 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             return;
         }
         read_first(0);
-        if (second) __syncthreads();
-        for (int i = 0; i <= steps; ++i) {
-            products(i);
-            if constexpr (PINGPONG) __syncthreads();
-            softmax(i);
-            if constexpr (PINGPONG) {
-                read_first(i + 1);
-                if (!second || i < steps) __syncthreads();
-            } else {
-                __syncthreads();
-                read_first(i + 1);
+        if constexpr (SPLIT) {
+            f32x16 next[MT];
+            int i = 0;
+            for (; i < steps; i += 2) {
+                products(i, next, s);
+                products(i + 1, s, next);
+            }
+            if (i == steps) products(i, next, s);
+        } else {
+            if (second) __syncthreads();
+            for (int i = 0; i <= steps; ++i) {
+                products(i, s, s);
+                if constexpr (PINGPONG) __syncthreads();
+                softmax(i);
+                if constexpr (PINGPONG) {
+                    read_first(i + 1);
+                    if (!second || i < steps) __syncthreads();
+                } else {
+                    __syncthreads();
+                    read_first(i + 1);
+                }
             }
         }
     } else {
@@ -461,12 +630,12 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                     if (k * 8 >= a.D) break;
                     const f32x4 kf = *(const f32x4*)&s_k[i & 1][col * KS + k * 8 + half * 4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q[k][e], s[0], 0, 0, 0);
+                    for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], q[k][0][e], s[0], 0, 0, 0);
                 }
                 soften(tb, i);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const T* vp = &s_v[i & 1][(8 * (r >> 2) + 4 * half + (r & 3)) * VS + col];
+                    const S* vp = &s_v[i & 1][(8 * (r >> 2) + 4 * half + (r & 3)) * VS + col];
 #pragma unroll
                     for (int t = 0; t < DT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[t * 32], s[0][r], o[t], 0, 0, 0);
                 }

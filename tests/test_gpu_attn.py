@@ -39,20 +39,25 @@ def _strided(rows, cols, act, pad):
     return buf, buf[:rows, :cols]
 
 
-def _attend_case(heads, page, q_lens, ctx, act, fmt, window=0, seed=0, pad=8, share=0, decode=False, scale=None):
+def _attend_case(heads, page, q_lens, ctx, act, fmt, window=0, seed=0, pad=8, share=0, decode=False, scale=None,
+                 powers=(0, 0)):
     from paper_2602_21144_amd import binding as B
     hq, hkv, D = heads
     rng = np.random.default_rng(seed)
     kv_len = [a + b for a, b in zip(q_lens, ctx)]
     pages = Pages(rng, kv_len, page, share=share)
     (K, V), (kd, vd), (ks, vs) = poisoned_pool(torch, dict(hkv=hkv, d=D), pages, rng, act, fmt)
+    for x, dev, e in ((K, kd, powers[0]), (V, vd, powers[1])):   # exact: powers of two
+        x *= 2.0 ** e
+        if e:
+            dev.mul_(2.0 ** e)
     ad = B.make_attn_desc(hq, hkv, D, page, kv_format=fmt, act=act, window=window, scale=scale)
     pool = B.KvPool(ad, kd, vd, ks, vs)
     T = sum(q_lens)
     cu = None if decode else np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
     meta = B.KvMeta(ad, cu, kv_len, pages.table, pages.num)
     qbuf, q = _strided(T, hq * D, act, pad)
-    q.copy_(torch.from_numpy(rng.standard_normal((T, hq * D)).astype(np.float32)))
+    q.copy_(torch.from_numpy(rng.standard_normal((T, hq * D)).astype(np.float32) * 2.0 ** -powers[0]))
     obuf, out = _strided(T, hq * D, act, pad)
     ws = B.workspace(B.attn_workspace_bytes(ad, T, len(q_lens)))
     (B.ssm_attn_decode if decode else B.ssm_attn_prefill)(ad, q, meta, pool, out, ws)
@@ -290,6 +295,13 @@ def test_rows_behind_the_last_sequence_stay():
     assert B.take_status(ws) == 0
     for t in (q, out, kr, vr):
         assert torch.isnan(t[25:]).all() and torch.isfinite(t[:25]).all()
+
+
+@pytest.mark.parametrize("powers", [(40, -60), (-60, 100), (-100, 0)])
+@pytest.mark.parametrize("decode", [False, True])
+def test_float32_values_of_any_magnitude(powers, decode):
+    """Scores of order one from factors far apart, small and large v: the parts of a value keep its 24 bits."""
+    _attend_case((4, 2, 112), 16, [1, 1] if decode else [70, 33], [300, 20], "f32", "act", decode=decode, seed=15, powers=powers)
 
 
 # ------------------------------------------------------------------- append and read
