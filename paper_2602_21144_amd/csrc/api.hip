@@ -13,6 +13,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1456,6 +1457,10 @@ int ssm_stack_decode_step(const ssm_stack_desc_t* sd, const ssm_shard_weights_t*
 namespace {
 
 constexpr int64_t kMaxKvTokens = 1ll << 30;   // tokens per sequence: positions and units stay in 32 bits
+// A call's rows and sequences: a launch holds below 2^32 threads, the largest one (prompt attention) at most
+// 512 for every (256 rows of query heads, and sequence, by kv heads): 512 (2^22 128 / 256 + 2^15 128 + ..)
+constexpr int64_t kMaxKvRows = 1ll << 22;
+constexpr int32_t kMaxKvSeqs = 1 << 15;
 
 int check_attn_desc(const ssm_attn_desc_t* d) {
     if (!d) return fail(SSM_E_INVAL, "desc is null");
@@ -1475,8 +1480,8 @@ int check_attn_desc(const ssm_attn_desc_t* d) {
 
 int check_kv_meta(const ssm_attn_desc_t* d, const ssm_kv_meta_t* m, int64_t T, bool per_row) {
     if (!m) return fail(SSM_E_INVAL, "meta is null");
-    if (T < 0 || T > INT32_MAX) return fail(SSM_E_INVAL, "token count %lld", (long long)T);
-    if (m->nseq < 0) return fail(SSM_E_INVAL, "nseq %d", m->nseq);
+    if (T < 0 || T > kMaxKvRows) return fail(SSM_E_INVAL, "token count %lld: 0 to 2^22", (long long)T);
+    if (m->nseq < 0 || m->nseq > kMaxKvSeqs) return fail(SSM_E_INVAL, "nseq %d: 0 to 2^15", m->nseq);
     if (m->nseq == 0) return T == 0 ? SSM_OK : fail(SSM_E_SEQLENS, "T = %lld tokens but no sequences", (long long)T);
     if (!m->kv_len || !m->page_table) return fail(SSM_E_INVAL, "meta arrays must be non-null");
     if (m->max_pages < 1 || (int64_t)m->max_pages * d->page_size > kMaxKvTokens)
@@ -1558,8 +1563,14 @@ int ssm_kv_check_meta_host(const ssm_attn_desc_t* d, const int32_t* cu, const in
     for (int32_t i = 0; cu && i < nseq; ++i)
         if (cu[i + 1] < cu[i]) return fail(SSM_E_SEQLENS, "cu_seqlens[%d] = %d < %d", i + 1, cu[i + 1], cu[i]);
     if (cu && cu[nseq] != T) return fail(SSM_E_SEQLENS, "cu_seqlens[%d] = %d, T = %lld", nseq, cu[nseq], (long long)T);
-    std::vector<int32_t> named(num_pages, -1);   // the first sequence that names a page
-    std::vector<char> written(num_pages, 0);     // whether a sequence writes it
+    std::vector<int32_t> named;   // the first sequence that names a page
+    std::vector<char> written;    // whether a sequence writes it
+    try {
+        named.assign(num_pages, -1);
+        written.assign(num_pages, 0);
+    } catch (const std::bad_alloc&) {
+        return fail(SSM_E_INVAL, "no host memory to check %d pages", num_pages);
+    }
     for (int32_t i = 0; i < nseq; ++i) {
         const int64_t n = kv_len[i], rows = cu ? cu[i + 1] - cu[i] : (n > 0 ? 1 : 0);
         if (n < rows || n > (int64_t)max_pages * d->page_size)
@@ -1580,7 +1591,8 @@ int ssm_kv_check_meta_host(const ssm_attn_desc_t* d, const int32_t* cu, const in
 
 int ssm_attn_workspace_bytes(const ssm_attn_desc_t* d, int64_t max_tokens, int32_t max_seqs, size_t* bytes) {
     SSM_TRY(check_attn_desc(d));
-    if (!bytes || max_tokens < 0 || max_tokens > INT32_MAX || max_seqs < 0) return fail(SSM_E_INVAL, "bad size query");
+    if (!bytes || max_tokens < 0 || max_tokens > kMaxKvRows || max_seqs < 0 || max_seqs > kMaxKvSeqs)
+        return fail(SSM_E_INVAL, "bad size query: up to 2^22 rows of 2^15 sequences");
     *bytes = kWsHeader + std::max(attn_prefill_scratch_bytes(d->act_dtype == SSM_BF16, d->q_heads, d->kv_heads, d->head_dim,
                                                              max_tokens, max_seqs),
                                   attn_decode_scratch_bytes(d->head_dim, max_seqs));

@@ -201,6 +201,31 @@ def test_call_refusals(name):
     assert B.lib().ssm_last_error()
 
 
+@pytest.mark.parametrize("name", ALL)
+def test_calls_larger_than_a_launch_are_refused(name):
+    A, I = _Fake.A, B.SSM_E_INVAL
+    assert _call(name, T=(1 << 15) + 1, meta=B.KvMetaC(A, A, A, (1 << 15) + 1, 4)) == I
+    if name != "ssm_attn_decode":
+        assert _call(name, T=(1 << 22) + 1, wsb=1 << 40) == I
+        assert _call(name, T=1 << 31, wsb=1 << 40) == I
+    n = ctypes.c_size_t()
+    size = lambda t, s: _rc("ssm_attn_workspace_bytes", ctypes.byref(_desc(q_heads=128, kv_heads=128)), t, s, ctypes.byref(n))  # noqa: E731
+    assert size((1 << 22) + 1, 1) == I and size(1, (1 << 15) + 1) == I
+    assert size(1 << 22, 1 << 15) == 0 and n.value < 1 << 33
+
+
+def test_host_check_of_a_pool_that_no_memory_describes():
+    import resource
+    used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+    low, high = resource.getrlimit(resource.RLIMIT_AS)
+    resource.setrlimit(resource.RLIMIT_AS, (used + (1 << 30), high))
+    try:
+        assert _host_meta([0, 5], [20], [[0, 1, 2]], num=(1 << 31) - 1) == B.SSM_E_INVAL
+    finally:
+        resource.setrlimit(resource.RLIMIT_AS, (low, high))
+    assert _host_meta([0, 5], [20], [[0, 1, 2]]) == 0
+
+
 def test_append_refusals():
     A = _Fake.A
     tr = lambda **kw: B.QkTransformC(**{**dict(q_norm_w=A, k_norm_w=A, turns=A, norm_eps=1e-5, rot_dim=32, interleaved=0), **kw})  # noqa: E731
