@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     if (lane == 0 && steps) atomicAdd(&s_steps, steps);
     __syncthreads();
     const unsigned long long share = (s_steps * a.Hkv + p.places - 1) / p.places;
-    int most = share < (unsigned)tile_min_steps(bf16_act) ? tile_min_steps(bf16_act) : (int)share;   // steps of the longest item
+    int most = share < (unsigned)p.min_steps ? p.min_steps : (int)share;   // steps of the longest item
     // If every tile has a place of its own at once, the cut is such that every item has: the first of 16 lengths,
     // from an equal share to twice that (float32: one and a half times), at which the items are no more than the
     // places. Float32 is otherwise cut to half a share, in two rounds: its steps are long, and what the rounds add
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         int found = 0;
         for (int k = kPlanThreads / 64 - 1; k >= 0; --k) found = s_wave[k] ? s_wave[k] : found;
         if (found) most = found;
-        else if (!bf16_act) most = max(tile_min_steps(bf16_act), (most + 1) / 2);
+        else if (!bf16_act) most = max(p.min_steps, (most + 1) / 2);
     }
     auto cut = [&](const TileRange& r, int& pieces, int& len) {
         pieces = r.steps > most ? (r.steps + most - 1) / most : 1;

@@ -705,7 +705,7 @@ template <typename T, int FMT, int DP, int WAVES> hipError_t launch_attn_prefill
     SSM_LAUNCH((attn_prefill_kernel<T, FMT, DP, WAVES>), dim3((unsigned)pl.max_items * p.kv.Hkv), dim3(64 * WAVES), 0, s, p, pl);
     hipError_t e = hipGetLastError();
     const int64_t longest = (int64_t)p.kv.max_pages << p.kv.page_log2;
-    if (e != hipSuccess || longest <= tile_min_steps(sizeof(T) == 2) * kStep) return e;   // no tile is ever cut
+    if (e != hipSuccess || longest <= pl.min_steps * kStep) return e;   // no tile is ever cut
     KernelTimer kj("attn.prefill_join", s);
     const int64_t most = (int64_t)pl.max_joins * p.kv.Hkv * (8 * WAVES);
     SSM_LAUNCH((attn_prefill_join_kernel<T, DP, 32 * WAVES>), dim3((unsigned)(most < kJoinWorkgroups ? most : kJoinWorkgroups)), dim3(256),
