@@ -16,6 +16,10 @@
 // the whole work (that of one place, tile_places(), or half of it); tiles behind a long cache are cut into several items
 // whose partial results (m, l and the unnormalised o, float32) a third kernel joins in order. Items are
 // listed longest first, and the workgroups of one item's kv heads are neighbours.
+//
+// Bound by instructions beside the MFMAs: 8192 tokens, 32 heads of 128 in bf16, 509 us, 1.08 PFLOP/s with the matrix
+// cores' pipe 56% busy (a large library product reaches 1.65); three prompts of 2048 tokens in all, one behind 4096,
+// 16 heads of 112: 36 us, the plan and the join 6 and 7; 33 tokens behind 40000 in fp8, 32 heads of 128: 50 us and 13.
 #pragma once
 #include "kv.h"
 
