@@ -756,6 +756,9 @@ class KvPool:
         self.k, self.v, self.k_scale, self.v_scale, self.num_pages = k, v, k_scale, v_scale, pages
         self.c = KvPoolC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), pages)
 
+    def tensors(self):
+        return self.k, self.v, self.k_scale, self.v_scale
+
 
 def empty_kv_pool(ad: AttnDesc, num_pages: int, device="cuda") -> KvPool:
     shape = (num_pages, ad.kv_heads, ad.page_size, ad.head_dim)
@@ -789,6 +792,9 @@ class KvMeta:
         self.c = KvMetaC(None if cu is None else self.cu.data_ptr(), self.kv_len.data_ptr(), self.page_table.data_ptr(),
                          self.nseq, self.max_pages)
 
+    def tensors(self):
+        return self.cu, self.kv_len, self.page_table
+
 
 def rope_turns(inv_freq, device="cuda") -> torch.Tensor:
     """Radians per token of every rotated pair -> the device table of QkTransform (int64 holding the 64-bit
@@ -813,6 +819,9 @@ class QkTransform:
         self.q_norm_w, self.k_norm_w = q_norm_w, k_norm_w
         self.c = QkTransformC(_ptr(q_norm_w), _ptr(k_norm_w), _ptr(self.turns), float(eps), rot, 1 if interleaved else 0)
 
+    def tensors(self):
+        return self.q_norm_w, self.k_norm_w, self.turns
+
 
 def attn_workspace_bytes(ad: AttnDesc, max_tokens: int, max_seqs: int) -> int:
     n = ctypes.c_size_t()
@@ -830,7 +839,7 @@ def _attn_rows(ad: AttnDesc, t: torch.Tensor, rows: int, heads: int, what: str):
 
 
 def _m_ssm_kv_append(ad, tr: Optional[QkTransform], qkv, meta: KvMeta, pool: KvPool, q_out, ws, stream=None):
-    _same_device(qkv, q_out, ws, pool.k, meta.kv_len)
+    _same_device(qkv, q_out, ws, *pool.tensors(), *meta.tensors(), *(tr.tensors() if tr is not None else ()))
     p, ld = _attn_rows(ad, qkv, meta.T, ad.q_heads + 2 * ad.kv_heads, "qkv")
     q, ldq = _attn_rows(ad, q_out, meta.T, ad.q_heads, "q_out")
     return (ctypes.byref(ad), ctypes.byref(tr.c) if tr is not None else None, p, ld, meta.T, ctypes.byref(meta.c),
@@ -838,7 +847,7 @@ def _m_ssm_kv_append(ad, tr: Optional[QkTransform], qkv, meta: KvMeta, pool: KvP
 
 
 def _m_ssm_kv_read(ad, meta: KvMeta, pool: KvPool, k_out, v_out, ws, stream=None):
-    _same_device(k_out, v_out, ws, pool.k, meta.kv_len)
+    _same_device(k_out, v_out, ws, *pool.tensors(), *meta.tensors())
     k, ldk = _attn_rows(ad, k_out, meta.T, ad.kv_heads, "k_out")
     v, ldv = _attn_rows(ad, v_out, meta.T, ad.kv_heads, "v_out")
     return (ctypes.byref(ad), meta.T, ctypes.byref(meta.c), ctypes.byref(pool.c), k, ldk, v, ldv, _ptr(ws), ws.numel(),
@@ -846,7 +855,7 @@ def _m_ssm_kv_read(ad, meta: KvMeta, pool: KvPool, k_out, v_out, ws, stream=None
 
 
 def _m_ssm_attn_prefill(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None):
-    _same_device(q, out, ws, pool.k, meta.kv_len)
+    _same_device(q, out, ws, *pool.tensors(), *meta.tensors())
     p, ld = _attn_rows(ad, q, meta.T, ad.q_heads, "q")
     o, ldo = _attn_rows(ad, out, meta.T, ad.q_heads, "out")
     return (ctypes.byref(ad), p, ld, meta.T, ctypes.byref(meta.c), ctypes.byref(pool.c), o, ldo, _ptr(ws), ws.numel(),
@@ -854,7 +863,7 @@ def _m_ssm_attn_prefill(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None)
 
 
 def _m_ssm_attn_decode(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None):
-    _same_device(q, out, ws, pool.k, meta.kv_len)
+    _same_device(q, out, ws, *pool.tensors(), *meta.tensors())
     p, ld = _attn_rows(ad, q, meta.nseq, ad.q_heads, "q")
     o, ldo = _attn_rows(ad, out, meta.nseq, ad.q_heads, "out")
     return (ctypes.byref(ad), p, ld, ctypes.byref(meta.c), ctypes.byref(pool.c), o, ldo, _ptr(ws), ws.numel(),

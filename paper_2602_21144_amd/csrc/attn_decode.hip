@@ -524,7 +524,8 @@ template <typename T, int FMT> hipError_t decode_launch(const AttnArgs& p, hipSt
     const KvArgs& a = p.kv;
     const int g = a.Hq / a.Hkv;
     const int64_t rows = (int64_t)a.Hkv * ((g + kRows - 1) / kRows) * a.nseq;
-    const int64_t longest = a.window > 0 ? a.window + kWaveTok : (int64_t)a.max_pages << a.page_log2;
+    const int64_t cached = (int64_t)a.max_pages << a.page_log2, seen = (int64_t)a.window + kWaveTok;
+    const int64_t longest = a.window > 0 && seen < cached ? seen : cached;
     const int64_t most = rows * ((longest + kUnit - 1) / kUnit);
     const int workers = (int)(most < kWorkers ? most : kWorkers);
     const dim3 grid((unsigned)workers), block(256);

@@ -152,6 +152,21 @@ def test_scores_of_any_size_and_scale():
     _attend_case((2, 1, 64), 16, [40], [20], "f32", "act", seed=12, scale=1e-4)
 
 
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_prefill_of_many_sequences(act):
+    """More sequences than the plan keeps in shared memory, most of them short or empty."""
+    rng = np.random.default_rng(17)
+    q = [int(x) for x in rng.integers(0, 4, 1500)]
+    _attend_case((2, 1, 16), 16, q, [int(x) for x in rng.integers(0, 40, 1500)], act, "act", seed=17)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_window_wider_than_any_cache(decode):
+    q = [1, 1] if decode else [50, 3]
+    for window in (2 ** 31 - 1, 2 ** 31 - 40):
+        _attend_case((2, 1, 64), 16, q, [3000, 10], "bf16", "act", window=window, decode=decode, seed=18)
+
+
 # ------------------------------------------------------------------- rows and pages that hold nothing
 @pytest.mark.parametrize("act,fmt", [("bf16", "act"), ("f32", "fp8")])
 def test_padded_decode_batch(act, fmt):
@@ -515,6 +530,58 @@ def test_graph_of_decode_steps_follows_kv_len():
     for a, b in zip(outs[0][0], outs[1][0]):
         assert torch.equal(a, b)
     assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][2], outs[1][2])
+
+
+@pytest.mark.parametrize("act,fmt", [("bf16", "fp8"), ("f32", "act")])
+def test_graphs_of_chunks_share_a_workspace(act, fmt):
+    """Two captured chunks (append, attention, read-back), one of a single sequence and one of three, and a
+    captured decode step, in one workspace: replayed in turn on other inputs, each equals its eager calls."""
+    from paper_2602_21144_amd import binding as B
+    rng = np.random.default_rng(43)
+    hq, hkv, D, page = 6, 2, 112, 16
+    ad = B.make_attn_desc(hq, hkv, D, page, kv_format=fmt, act=act)
+    tr = B.QkTransform(ad, None, torch.ones(D, device="cuda"), 1e-5, 10000.0 ** (-np.arange(56) / 56.0))
+    calls = [([150], [1000]), ([3, 40, 1], [0, 17, 700]), (None, [30, 260])]
+    ws = B.workspace(max(B.attn_workspace_bytes(ad, 200, 4), 1))
+    jobs = []
+    for rows, ctx in calls:
+        m = rows or [1] * len(ctx)
+        kv = [a + b for a, b in zip(m, ctx)]
+        pages = Pages(rng, kv, page)
+        _, (kd, vd), (ks, vs) = poisoned_pool(torch, dict(hkv=hkv, d=D), pages, rng, act, fmt)
+        pool = B.KvPool(ad, kd, vd, ks, vs)
+        meta = B.KvMeta(ad, None if rows is None else np.concatenate([[0], np.cumsum(m)]), kv, pages.table, pages.num)
+        T = sum(m)
+        x = torch.randn(T, (hq + 2 * hkv) * D, device="cuda").to(_t(act))
+        q, out, kr, vr = (torch.empty(T, n * D, dtype=_t(act), device="cuda") for n in (hq, hq, hkv, hkv))
+
+        def run(meta=meta, pool=pool, x=x, q=q, out=out, kr=kr, vr=vr, rows=rows):
+            B.ssm_kv_append(ad, tr, x, meta, pool, q, ws)
+            (B.ssm_attn_decode if rows is None else B.ssm_attn_prefill)(ad, q, meta, pool, out, ws)
+            B.ssm_kv_read(ad, meta, pool, kr, vr, ws)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            run()
+            s.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                run()
+        torch.cuda.current_stream().wait_stream(s)
+        jobs.append((run, g, x, (out, kr, vr)))
+    for t in range(3):
+        for run, g, x, outs in jobs:
+            x.normal_()
+            run()
+            torch.cuda.synchronize()
+            want = [o.clone() for o in outs]
+            for o in outs:
+                o.fill_(float("nan"))
+            g.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(want, outs):
+                assert torch.equal(a, b)
+    assert B.take_status(ws) == 0
 
 
 def test_calls_on_two_streams_with_their_own_workspaces():
