@@ -64,15 +64,23 @@ template <int LPH, typename F> __device__ __forceinline__ float group_reduce(flo
 // its angles are worked out once, and each group goes through every 256 / LPH-th head with the next
 // head's values on their way.
 //
-// A chunk of 2048 tokens of 48 heads of 112 into fp8 (37 MB in and out, 7.5 us at the card's copy rate) takes
-// 11.7 us, of which 4 are an empty launch's. It was bound by instructions, not bytes: 15.4 us with the angles in
+// A chunk of 2048 tokens of 48 heads of 112 into fp8 (37 MB in and out, 6 us at 6.2 TB/s) takes
+// 10.6 us, of which 4 are an empty launch's. It was bound by instructions, not bytes: 15.4 us with the angles in
 // every lane, library root and divisions and sums by way of shared memory. Splitting a token's heads over
 // workgroups is no faster at any number of tokens (2048: 14.8 us, the lookups are repeated; 1 to 256: alike, 4 to 5).
+//
+// Workgroups go to the 8 XCDs in turn. Of each 128 an XCD takes 16 neighbouring tokens, so that the parts of a line that
+// they write (rows of 224 bytes or of codes, four bytes of scale) meet in one L2: 4792 tokens of 48 heads of 112 in bf16
+// 31.4 -> 28.6 us, 2048 in fp8 10.9 -> 10.6 (an eighth of all tokens to each XCD: 27.9 and 10.7, but 42.8 for 41.8
+// where rows are whole lines).
+__device__ __forceinline__ int64_t token_of(uint32_t b, int64_t T) {
+    return b < (T & ~(int64_t)127) ? (b & ~127u) + (b & 7) * 16 + ((b >> 3) & 15) : b;
+}
 template <typename T, int FMT, int LPH>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
     using E = typename KvElem<T, FMT>::type;
     const KvArgs& kv = a.kv;
-    const int64_t t = blockIdx.x;
+    const int64_t t = token_of(blockIdx.x, kv.T);
     const int D = kv.D, j = threadIdx.x % LPH;
     const bool on = 8 * j < D;
     const bool half = !a.inter && 8 * j < a.rot;          // the two pieces are a rotation's two halves
@@ -202,7 +210,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 // the threads walk (k or v, head, row, 8 values) with the row inside the head: neighbouring threads
 // read one stretch of a page. A thread's next kReadAhead loads are in flight together.
 //
-// Bound by memory: 24000 rows of 16 heads of 128 from fp8 (149 MB in and out, 30 us at the card's copy rate)
+// Bound by memory: 24000 rows of 16 heads of 128 from fp8 (149 MB in and out, 24 us at 6.2 TB/s)
 // in 25.3 us, 5.9 TB/s. The packed rows are stored past the caches (42.4 us without, where the cache is not
 // there from an earlier call: what is written takes the place of what is to be read). Few rows are split over
 // gridDim.y workgroups (391 rows of bf16: 4.5 us, 12 by 25 workgroups alone).
