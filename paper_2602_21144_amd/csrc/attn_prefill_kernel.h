@@ -682,7 +682,8 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
 }
 
 // The partial results of cut tiles, in order: four rows of a (tile, kv head) per workgroup and turn, one to
-// a wave
+// a wave, two partials on their way (5 partials of 8000 rows, 32 of 1056: 7.7 and 7.1 us; four 9.2 and 6.5, eight
+// 12.3 and 6.5)
 constexpr int kJoinWorkgroups = 2048;
 template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void attn_prefill_join_kernel(AttnArgs p, AttnPlan plan) {
     const KvArgs& a = p.kv;
