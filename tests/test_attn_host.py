@@ -113,6 +113,18 @@ def test_workspace_grows_with_rows_and_sequences():
         assert _rc("ssm_attn_workspace_bytes", d, *args) == B.SSM_E_INVAL
 
 
+@pytest.mark.parametrize("q,kv", [(32, 8), (32, 1), (128, 128), (128, 1), (16, 16), (1, 1)])
+@pytest.mark.parametrize("dim", [96, 112, 128, 160])
+def test_workspace_for_more_rows_serves_fewer(q, kv, dim):
+    """Also where the larger call is cut into taller tiles (65536 rows of query heads)."""
+    for act in (B.SSM_BF16, B.SSM_F32):
+        d = _desc(q_heads=q, kv_heads=kv, head_dim=dim, act_dtype=act)
+        edge = 65536 // q
+        sizes = [B.attn_workspace_bytes(d, t, n) for t in (1, edge // 2, edge - 1, edge, edge + 1, 2 * edge) for n in (1, 40)]
+        for n in (0, 1):
+            assert sizes[n::2] == sorted(sizes[n::2])
+
+
 def _host_meta(cu, kv, table, T=None, num=10, desc=None):
     cu = None if cu is None else np.array(cu, np.int32)
     kv, table = np.array(kv, np.int32), np.array(table, np.int32)
