@@ -1,4 +1,5 @@
 // Attention of prompt chunks: the plan of the work, and the choice of the padded width.
+#include "attn_cut.h"
 #include "attn_prefill.h"
 
 namespace ssm {
@@ -38,23 +39,24 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     const int per = (a.nseq + kPlanThreads - 1) / kPlanThreads;
     auto tiles_of = [&](int i) {
         const KvSeq s = kv_seq(a, i);
-        return s.ok ? (int)(((int64_t)s.m * g + p.rows - 1) / p.rows) : 0;
+        return s.ok ? tiles_of_rows(s.m, g, p.rows) : 0;
     };
     int sum = 0;
     for (int k = 0; k < per; ++k)
-        if (tid * per + k < a.nseq) sum += tiles_of(tid * per + k);
+        if (tid * per + k < a.nseq) sum = add_tiles(sum, tiles_of(tid * per + k));
     int incl = sum;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
         const int o = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += o;
+        if (lane >= off) incl = add_tiles(incl, o);
     }
     if (lane == 63) s_wave[tid >> 6] = incl;
     __syncthreads();
-    int at = incl - sum, total = 0;
+    int at = __shfl_up(incl, 1, 64), total = 0;
+    if (lane == 0) at = 0;
     for (int k = 0; k < kPlanThreads / 64; ++k) {
-        if (k < (tid >> 6)) at += s_wave[k];
-        total += s_wave[k];
+        if (k < (tid >> 6)) at = add_tiles(at, s_wave[k]);
+        total = add_tiles(total, s_wave[k]);
     }
     // the tiles before every sequence: in LDS where they fit
     int32_t* prefix = a.nseq <= kPlanThreads ? s_prefix : p.prefix;
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         const int i = tid * per + k;
         if (i < a.nseq) {
             prefix[i] = at;
-            at += tiles_of(i);
+            at = add_tiles(at, tiles_of(i));
         }
     }
     if (total > p.max_tiles) {   // sequences that overlap hold more rows than the call has
