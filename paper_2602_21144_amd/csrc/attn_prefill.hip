@@ -97,8 +97,7 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     for (int off = 32; off > 0; off >>= 1) steps += __shfl_xor(steps, off, 64);
     if (lane == 0 && steps) atomicAdd(&s_steps, steps);
     __syncthreads();
-    const unsigned long long share = (s_steps * a.Hkv + p.places - 1) / p.places;
-    int most = share < (unsigned)p.min_steps ? p.min_steps : (int)share;   // steps of the longest item
+    int most = longest_item(s_steps, a.Hkv, p.places, p.min_steps);   // steps of the longest item
     // If every tile has a place of its own at once, the cut is such that every item has: the first of 16 lengths,
     // from an equal share to twice that (float32: one and a half times), at which the items are no more than the
     // places. Float32 is otherwise cut to half a share, in two rounds: its steps are long, and what the rounds add
@@ -119,16 +118,9 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
         if (found) most = found;
         else if (!bf16_act) most = max(p.min_steps, (most + 1) / 2);
     }
-    auto cut = [&](const TileRange& r, int& pieces, int& len) {
-        pieces = r.steps > most ? (r.steps + most - 1) / most : 1;
-        len = (r.steps + pieces - 1) / pieces;
-        if (pieces > 1) pieces = (r.steps + len - 1) / len;
-    };
-    auto bin_of = [&](int len) { return kBins - 1 - (int)((uint32_t)len * kBins / (uint32_t)(most + 1)); };
     each([&](const Tile& x) {
-        int pieces, len;
-        cut(x.r, pieces, len);
-        atomicAdd(&s_bin[bin_of(len)], pieces);
+        const TileCut c = cut_tile(x.r.steps, most);
+        atomicAdd(&s_bin[item_bin(c.len, most, kBins)], c.pieces);
     });
     __syncthreads();
     if (tid < 64) {
@@ -145,9 +137,8 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(KvArgs a, AttnP
     __syncthreads();
     for (int k = s_items + tid; k < p.max_items; k += kPlanThreads) p.items[k].part = -2;
     each([&](const Tile& x) {
-        int pieces, len;
-        cut(x.r, pieces, len);
-        const int pos = atomicAdd(&s_bin[bin_of(len)], pieces);
+        const auto [pieces, len] = cut_tile(x.r.steps, most);
+        const int pos = atomicAdd(&s_bin[item_bin(len, most, kBins)], pieces);
         int part = -1;
         if (pieces > 1) {
             part = atomicAdd(&s_part, pieces);
