@@ -743,18 +743,21 @@ class KvPool:
 
     def __init__(self, ad: AttnDesc, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        pages = k.shape[0]
-        for t, what in ((k, "k"), (v, "v")):
-            if tuple(t.shape) != (pages, ad.kv_heads, ad.page_size, ad.head_dim) or t.dtype != _kv_dtype(ad):
+        self.k, self.v, self.k_scale, self.v_scale, self.num_pages = k, v, k_scale, v_scale, k.shape[0]
+        self.check(ad)
+        self.c = KvPoolC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.num_pages)
+
+    def check(self, ad: AttnDesc):
+        """The tensors are pages of `ad`: a call takes their extents from its own descriptor."""
+        for t, what in ((self.k, "k"), (self.v, "v")):
+            if tuple(t.shape) != (self.num_pages, ad.kv_heads, ad.page_size, ad.head_dim) or t.dtype != _kv_dtype(ad):
                 raise ValueError(f"{what}: {_kv_dtype(ad)} [pages][{ad.kv_heads}][{ad.page_size}][{ad.head_dim}] expected, "
                                  f"got {t.dtype} {tuple(t.shape)}")
-        if (ad.kv_format != 0) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+        if (ad.kv_format != 0) != (self.k_scale is not None) or (self.k_scale is None) != (self.v_scale is None):
             raise ValueError("the 8-bit formats have scales, the activation type none")
-        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            if t is not None and (tuple(t.shape) != (pages, ad.kv_heads, ad.page_size) or t.dtype != torch.float32):
+        for t, what in ((self.k_scale, "k_scale"), (self.v_scale, "v_scale")):
+            if t is not None and (tuple(t.shape) != (self.num_pages, ad.kv_heads, ad.page_size) or t.dtype != torch.float32):
                 raise ValueError(f"{what}: float32 [pages][{ad.kv_heads}][{ad.page_size}] expected")
-        self.k, self.v, self.k_scale, self.v_scale, self.num_pages = k, v, k_scale, v_scale, pages
-        self.c = KvPoolC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), pages)
 
     def tensors(self):
         return self.k, self.v, self.k_scale, self.v_scale
@@ -777,7 +780,7 @@ class KvMeta:
             return np.ascontiguousarray(x.cpu().numpy() if isinstance(x, torch.Tensor) else x, np.int32)
         cu = None if cu_seqlens is None else host(cu_seqlens)
         kl = host(kv_len)
-        self.nseq = int(kl.shape[0])
+        self.nseq, self.page_size = int(kl.shape[0]), ad.page_size
         pt = host(page_table).reshape(self.nseq, -1) if self.nseq else np.zeros((0, 1), np.int32)
         if cu is not None and cu.shape != (self.nseq + 1,):
             raise ValueError(f"cu_seqlens: {self.nseq + 1} entries expected, got {cu.shape}")
@@ -811,13 +814,16 @@ class QkTransform:
 
     def __init__(self, ad: AttnDesc, q_norm_w=None, k_norm_w=None, eps: float = 1e-5, inv_freq=None, interleaved: bool = False,
                  device="cuda"):
-        for w in (q_norm_w, k_norm_w):
-            if w is not None and (tuple(w.shape) != (ad.head_dim,) or w.dtype != torch.float32):
-                raise ValueError(f"norm weight: float32 [{ad.head_dim}] expected")
+        self.q_norm_w, self.k_norm_w = q_norm_w, k_norm_w
+        self.check(ad)
         rot = 0 if inv_freq is None else 2 * len(inv_freq)
         self.turns = rope_turns(inv_freq, device) if rot else None
-        self.q_norm_w, self.k_norm_w = q_norm_w, k_norm_w
         self.c = QkTransformC(_ptr(q_norm_w), _ptr(k_norm_w), _ptr(self.turns), float(eps), rot, 1 if interleaved else 0)
+
+    def check(self, ad: AttnDesc):
+        for w in (self.q_norm_w, self.k_norm_w):
+            if w is not None and (tuple(w.shape) != (ad.head_dim,) or w.dtype != torch.float32):
+                raise ValueError(f"norm weight: float32 [{ad.head_dim}] expected")
 
     def tensors(self):
         return self.q_norm_w, self.k_norm_w, self.turns
@@ -838,7 +844,17 @@ def _attn_rows(ad: AttnDesc, t: torch.Tensor, rows: int, heads: int, what: str):
     return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
 
 
+def _fits(ad: AttnDesc, meta: KvMeta, pool: KvPool, tr: Optional[QkTransform] = None):
+    """What was made for another descriptor is refused: the kernels index by the call's."""
+    pool.check(ad)
+    if meta.page_size != ad.page_size:
+        raise ValueError(f"meta is of pages of {meta.page_size} tokens, the descriptor of {ad.page_size}")
+    if tr is not None:
+        tr.check(ad)
+
+
 def _m_ssm_kv_append(ad, tr: Optional[QkTransform], qkv, meta: KvMeta, pool: KvPool, q_out, ws, stream=None):
+    _fits(ad, meta, pool, tr)
     _same_device(qkv, q_out, ws, *pool.tensors(), *meta.tensors(), *(tr.tensors() if tr is not None else ()))
     p, ld = _attn_rows(ad, qkv, meta.T, ad.q_heads + 2 * ad.kv_heads, "qkv")
     q, ldq = _attn_rows(ad, q_out, meta.T, ad.q_heads, "q_out")
@@ -847,6 +863,7 @@ def _m_ssm_kv_append(ad, tr: Optional[QkTransform], qkv, meta: KvMeta, pool: KvP
 
 
 def _m_ssm_kv_read(ad, meta: KvMeta, pool: KvPool, k_out, v_out, ws, stream=None):
+    _fits(ad, meta, pool)
     _same_device(k_out, v_out, ws, *pool.tensors(), *meta.tensors())
     k, ldk = _attn_rows(ad, k_out, meta.T, ad.kv_heads, "k_out")
     v, ldv = _attn_rows(ad, v_out, meta.T, ad.kv_heads, "v_out")
@@ -855,6 +872,7 @@ def _m_ssm_kv_read(ad, meta: KvMeta, pool: KvPool, k_out, v_out, ws, stream=None
 
 
 def _m_ssm_attn_prefill(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None):
+    _fits(ad, meta, pool)
     _same_device(q, out, ws, *pool.tensors(), *meta.tensors())
     p, ld = _attn_rows(ad, q, meta.T, ad.q_heads, "q")
     o, ldo = _attn_rows(ad, out, meta.T, ad.q_heads, "out")
@@ -863,6 +881,7 @@ def _m_ssm_attn_prefill(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None)
 
 
 def _m_ssm_attn_decode(ad, q, meta: KvMeta, pool: KvPool, out, ws, stream=None):
+    _fits(ad, meta, pool)
     _same_device(q, out, ws, *pool.tensors(), *meta.tensors())
     p, ld = _attn_rows(ad, q, meta.nseq, ad.q_heads, "q")
     o, ldo = _attn_rows(ad, out, meta.nseq, ad.q_heads, "out")
