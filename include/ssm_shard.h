@@ -506,7 +506,8 @@ int ssm_kv_read(const ssm_attn_desc_t* desc, int64_t T, const ssm_kv_meta_t* met
  * cache, the call's own among them, so ssm_kv_append comes first. out is not q. Scores and the softmax are float32;
  * with bf16 activations the probabilities are rounded to bf16 for their product with v, with float32 ones a
  * product is exact to 2^-23. A value that is not finite (float32: above 3.38e38) makes the rows that see it
- * NaN, and one of v may reach rows before its token; what pages hold behind a sequence's last token never does. */
+ * NaN, and one of v may reach up to 255 rows (of tokens and query heads) next to them, before its token or past
+ * the window. What pages hold behind a sequence's last token, or in front of what its rows see, never does. */
 int ssm_attn_prefill(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, int64_t T, const ssm_kv_meta_t* meta,
                      const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
                      hipStream_t stream);

@@ -81,6 +81,9 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     if (item.part == -2) return;
     const struct { int lo, m, n; } sq = {item.lo, item.m, item.n};
     const int g = a.Hq / a.Hkv, n = sq.n, before = sq.n - sq.m;
+    // the first token that a row of the tile sees, and the step that the item begins with: not one wholly before it
+    const int front = __builtin_amdgcn_readfirstlane(a.window > 0 ? max(before + item.row0 / g - a.window + 1, 0) : 0);
+    const int k0 = item.k0 + (max(front - item.k0, 0) & ~(TOK - 1));
     const int32_t* table = a.table + (int64_t)item.seq * a.max_pages;
 
     if (tid == 0) s_bad = 0;
@@ -151,14 +154,14 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
     if constexpr (NB == 2) src[1] = (const char*)a.v;
     __amdgpu_buffer_rsrc_t from[NB], from_ks, from_vs;
     auto page_at = [&](int step) {                         // the table entry of the wave's block
-        return table[max(min(item.k0 + step * TOK + 16 * blk, n - 1), 0) >> a.page_log2];
+        return table[max(min(k0 + step * TOK + 16 * blk, n - 1), 0) >> a.page_log2];
     };
     // a page is page_bytes long, the head's part of it begins at head_bytes (both below 2^30)
     const uint32_t row_bytes = (uint32_t)(a.D * (int)sizeof(E)), page_mask = (1u << a.page_log2) - 1;
     const uint32_t head_row = (uint32_t)head << a.page_log2, page_rows = (uint32_t)a.Hkv << a.page_log2;
     const uint32_t head_bytes = head_row * row_bytes, page_bytes = page_rows * row_bytes;
     auto locate = [&](auto b, int step, int page) {         // where the block's tokens of source b are
-        const int pg = __builtin_amdgcn_readfirstlane(page), j = item.k0 + step * TOK + 16 * blk;
+        const int pg = __builtin_amdgcn_readfirstlane(page), j = k0 + step * TOK + 16 * blk;
         const bool there = (uint32_t)pg < (uint32_t)a.num_pages && j < n;
         const uint32_t tokens = there ? (uint32_t)min(n - j, 16) : 0u, in_page = (uint32_t)j & page_mask;
         const uint32_t page0 = there ? (uint32_t)pg : 0u;
@@ -239,6 +242,21 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         }
         *(u32x4*)to = x;
     };
+    // Tokens of step 0 before `front` are seen by no row, and what the cache holds there must not reach the product with
+    // v (0 * infinity): its values and scales become zeros. Scores of such tokens are masked one by one.
+    auto clear_front = [&](auto b) {
+        if (front <= k0) return;
+        const int gone = front - k0 - 16 * blk;            // leading tokens of the wave's block
+        if (b == 1 || second) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int t = (((BF ? 0 : (wave & 1) * NP) + i) * 64 + lane) / PR;
+#pragma unroll
+                for (int e = 0; e < GW; ++e) held[b][i][e] = t < gone ? 0u : held[b][i][e];
+            }
+        }
+        if constexpr (FMT != SSM_KV_ACT && b == 0) held_vs = lane < gone ? 0u : held_vs;
+    };
     auto stage_scales = [&](int step) {
         if constexpr (FMT != SSM_KV_ACT) {
             if (lane < 16 && !second) {
@@ -258,7 +276,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
 
     // pages that the table does not name: their tokens are masked one by one (below)
     auto check_pages = [&] {
-        for (int i = (item.k0 >> a.page_log2) + tid; i <= ((min(item.k1, n) - 1) >> a.page_log2); i += 64 * WAVES) {
+        for (int i = (max(k0, front) >> a.page_log2) + tid; i <= ((min(item.k1, n) - 1) >> a.page_log2); i += 64 * WAVES) {
             const int pg = table[i];
             if (pg < 0 || pg >= a.num_pages) {
                 s_bad = 1;
@@ -393,7 +411,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             if constexpr (FMT == SSM_KV_ACT) l += ls[0] + ls[1];
         }
     };
-    const int steps = (item.k1 - item.k0 + TOK - 1) / TOK;
+    const int steps = (item.k1 - k0 + TOK - 1) / TOK;
     if constexpr (RUN) {
         // The products of step i are one run of MFMAs, K(i) Q and then V(i-1) P(i-1), each fragment read
         // from LDS kLead MFMAs ahead of its own (a wave alone: 69 cycles per MFMA as the compiler orders it,
@@ -436,8 +454,10 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         no_probabilities();
         int page[NB];
         load_all(b0, 0);
+        clear_front(b0);
         if constexpr (NB == 2) {
             load_all(b1, 0);
+            clear_front(b1);
             page[1] = page_at(1);
         }
         if (!second) {
@@ -498,7 +518,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             x = __builtin_bit_cast(bf16x8, y);
         };
         auto soften_turn = [&](f32x16 (&s)[MT], auto k, int i) {
-            const int tb = item.k0 + i * TOK;
+            const int tb = k0 + i * TOK;
             if constexpr (k == 0) {
                 scale_scores(s, i);
             } else if constexpr (k == 1) {
@@ -568,7 +588,7 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
             if constexpr (ALONE) keep_sums();
         };
         auto softmax = [&](int i) {
-            if (i < steps && seen(item.k0 + i * TOK)) soften(item.k0 + i * TOK, i);
+            if (i < steps && seen(k0 + i * TOK)) soften(k0 + i * TOK, i);
             else no_probabilities();
         };
         __syncthreads();
@@ -612,12 +632,20 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
         load_all(b0, 0);
         load_all(b1, 0);
         check_pages();
+        clear_front(b0);
         stage_all(b0, 0);
         stage_all(b1, 0);
+        if (front > k0) {                                  // as clear_front(b1), by what the lane staged
+#pragma unroll 1
+            for (int i = 0; i < NP; ++i) {
+                const int pc = ((wave & 1) * NP + i) * 64 + lane, t = 16 * blk + pc / PR;
+                if (k0 + t < front) *(u32x4*)&s_v[0][t * VS + (pc % PR) * PE] = u32x4{0, 0, 0, 0};
+            }
+        }
         __syncthreads();
         bad = s_bad != 0;
         for (int i = 0; i < steps; ++i) {
-            const int tb = item.k0 + i * TOK;
+            const int tb = k0 + i * TOK;
             if (i + 1 < steps) {
                 load_all(b0, i + 1);
                 load_all(b1, i + 1);

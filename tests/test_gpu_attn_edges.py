@@ -38,3 +38,85 @@ def test_overlapping_sequences_of_many_tiles():
     assert B.take_status(ws) == B.SSM_STATUS_BAD_SEQLENS
     # a window of one token: every row is its own token's v
     assert torch.equal(out.view(T, hq, D), v.view(T, 1, D).expand(T, hq, D))
+
+
+def _t(act):
+    return torch.bfloat16 if act == "bf16" else torch.float32
+
+
+def _f64(t):
+    return t.detach().to("cpu", torch.float64).numpy()
+
+
+def _near(got, want, tol, what):
+    assert np.isfinite(got).all(), f"{what}: {(~np.isfinite(got)).sum()} of {got.size} not finite"
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.max(np.abs(got - want) / tol):.2f} of the bound"
+
+
+def _attend(heads, page, q_lens, ctx, act, fmt, window=0, decode=False, seed=0, slid_out=False, rows=None):
+    """The attention of a call against the oracle at every row, or at about `rows` of each sequence. slid_out: what no row
+    of a sequence sees any more holds NaN values and scales, and pages of such tokens alone are named out of range.
+    Rows behind the last sequence keep what they hold. Returns what it called with."""
+    from paper_2602_21144_amd import binding as B
+    hq, hkv, D = heads
+    rng = np.random.default_rng(seed)
+    kv_len = [a + b for a, b in zip(q_lens, ctx)]
+    pages = Pages(rng, kv_len, page)
+    (K, V), dev, scales = poisoned_pool(torch, dict(hkv=hkv, d=D), pages, rng, act, fmt)
+    ad = B.make_attn_desc(hq, hkv, D, page, kv_format=fmt, act=act, window=window)
+    T = sum(q_lens)
+    meta = B.KvMeta(ad, None if decode else np.concatenate([[0], np.cumsum(q_lens)]), kv_len, pages.table, pages.num)
+    if slid_out:
+        table = pages.table.copy()
+        for i, (m, n) in enumerate(zip(q_lens, kv_len)):
+            first = max(0, n - m - window + 1)
+            at = [pages.where(i, p) for p in range(first)]
+            if at:
+                pg, off = (torch.tensor([int(x[j]) for x in at], device="cuda") for j in range(2))
+                for t, s in zip(dev, scales):
+                    if s is None:
+                        t[pg, :, off] = float("nan")
+                    else:
+                        t.view(torch.uint8)[pg, :, off] = 0x7f
+                        s[pg, :, off] = float("nan")
+            for p in range(first // page):
+                table[i, p] = (-1, pages.num, 2 ** 31 - 1)[p % 3]
+        meta.page_table.copy_(torch.from_numpy(table))
+    pool = B.KvPool(ad, *dev, *scales)
+    q = torch.from_numpy(rng.standard_normal((T, hq * D)).astype(np.float32)).to(_t(act)).cuda()
+    out = torch.full((T + 3, hq * D), float("nan"), dtype=_t(act), device="cuda")
+    ws = B.workspace(B.attn_workspace_bytes(ad, T, len(q_lens)))
+    (B.ssm_attn_decode if decode else B.ssm_attn_prefill)(ad, q, meta, pool, out, ws)
+    assert B.take_status(ws) == 0
+    assert torch.isnan(out[T:]).all(), "written behind the rows"
+    qh, got = _f64(q).reshape(T, hq, D), _f64(out[:T]).reshape(T, hq, D)
+    assert np.isfinite(got).all(), f"{(~np.isfinite(got)).sum()} of {got.size} values are not finite"
+    at = 0
+    for i, (m, n) in enumerate(zip(q_lens, kv_len)):
+        if m == 0:
+            continue
+        sel = np.arange(m) if rows is None or m <= rows else np.unique(np.r_[0, 1, m - 2, m - 1, rng.integers(0, m, rows)])
+        o, ab, big = oa.attend(qh[at + sel], tokens(K, pages, i, n), tokens(V, pages, i, n), n - m + sel, ad.scale, window)
+        _near(got[at + sel], o, attn_tol(o, ab, big, n, D, act, fmt), f"sequence {i}")
+        at += m
+    return B, ad, pool, meta, q, out, ws
+
+
+FORMATS = [("bf16", "act"), ("bf16", "fp8"), ("bf16", "int8"), ("f32", "act"), ("f32", "fp8"), ("f32", "int8")]
+
+
+# ------------------------------------------------------------------- tokens that slid out of the window
+@pytest.mark.parametrize("act,fmt", FORMATS)
+@pytest.mark.parametrize("heads", [(4, 2, 64), (2, 1, 96), (3, 1, 128), (2, 1, 160), (4, 2, 256)])
+def test_prefill_sees_nothing_in_front_of_the_window(act, fmt, heads):
+    """NaN in values, codes and scales of tokens that no row sees, and pages of them given back: the window's first token
+    is at every place of a step of 64 and of a block of 16, and in a later tile and piece."""
+    _attend(heads, 16, [1, 1, 5, 40], [199, 333, 127, 1000], act, fmt, window=50, seed=61, slid_out=True)
+    _attend(heads, 16, [1, 2, 3], [63, 130, 96], act, fmt, window=33, seed=62, slid_out=True)
+
+
+@pytest.mark.parametrize("act,fmt", FORMATS)
+@pytest.mark.parametrize("window", [1, 15, 16, 17, 31, 64, 100])
+def test_prefill_windows_that_begin_anywhere(act, fmt, window):
+    _attend((2, 1, 64), 32, [1, 1, 2, 7], [64 + 13, 128, 200, 97], act, fmt, window=window, seed=63, slid_out=True)
