@@ -174,7 +174,7 @@ __device__ __forceinline__ void load_tile(const KvArgs& a, Tile<T, FMT, DP>& x, 
     const int end = (n - 1) & ~7;
     const int gk = min(tb + 8 * (i >> 2), end), gv = min(tb + 8 * quad, end);
     const bool named = pg.v >= 0 && pg.v < a.num_pages;
-    if (!named) atomicOr(a.status, SSM_STATUS_BAD_PAGE);
+    if (!named && gv + 7 >= lo) atomicOr(a.status, SSM_STATUS_BAD_PAGE);   // a page wholly in front of the window may be gone
     const int pk = pg.k >= 0 && pg.k < a.num_pages ? pg.k : 0, pv = named ? pg.v : 0;
     const int64_t rk = kv_pool_row(a, pk, head, gk), rv = kv_pool_row(a, pv, head, gv);
     const E* kp = (const E*)a.k + rk * a.D;

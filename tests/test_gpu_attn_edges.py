@@ -120,3 +120,22 @@ def test_prefill_sees_nothing_in_front_of_the_window(act, fmt, heads):
 @pytest.mark.parametrize("window", [1, 15, 16, 17, 31, 64, 100])
 def test_prefill_windows_that_begin_anywhere(act, fmt, window):
     _attend((2, 1, 64), 32, [1, 1, 2, 7], [64 + 13, 128, 200, 97], act, fmt, window=window, seed=63, slid_out=True)
+
+
+@pytest.mark.parametrize("act,fmt", FORMATS)
+@pytest.mark.parametrize("window", [1, 16, 17, 33, 50, 100])
+def test_decode_sees_nothing_in_front_of_the_window(act, fmt, window):
+    _attend((4, 2, 64), 16, [1] * 5, [199, 333, 127, 1000, 20], act, fmt, window=window, decode=True, seed=64, slid_out=True)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_page_out_of_the_pool_inside_the_window_is_reported(decode):
+    """The first page with a visible token, of which the window takes the last one."""
+    B, ad, pool, meta, q, out, ws = _attend((4, 2, 64), 16, [1, 1], [199, 333], "bf16", "act", window=40, decode=decode, seed=65)
+    f = B.ssm_attn_decode if decode else B.ssm_attn_prefill
+    for first, want in ((334 - 40 - 1) // 16 - 1, 0), ((334 - 40) // 16, B.SSM_STATUS_BAD_PAGE):
+        keep = meta.page_table[1, first].item()
+        meta.page_table[1, first] = -1
+        f(ad, q, meta, pool, out, ws)
+        assert B.take_status(ws) == want
+        meta.page_table[1, first] = keep
