@@ -449,7 +449,9 @@ typedef struct ssm_kv_pool {
  *     one row per sequence (a decode step)
  *   kv_len [nseq]: cached tokens of the sequence, this call's included, so that row r of a
  *     sequence with m rows is its token kv_len - m + r
- *   page_table [nseq][max_pages]: token p is on page page_table[i][p / page_size]
+ *   page_table [nseq][max_pages]: token p is on page page_table[i][p / page_size]; with a window the entries
+ *     of pages that lie in front of what the sequence's first row sees are not read from (a page that
+ *     slid out may be given to another sequence)
  * With cu_seqlens null a kv_len of 0 marks a row without a token (a batch padded to a fixed
  * size): nothing is cached or read for it, its attention output is zero. Packed rows behind the
  * last sequence are left as they were in every output. Lengths that do not fit the call (negative,
@@ -481,8 +483,8 @@ int ssm_attn_check_desc(const ssm_attn_desc_t* desc);
 /* Host only: radians per token (finite doubles, as base^(-2i/rot_dim)) to turns per token * 2^64. */
 int ssm_rope_turns(const double* radians, int32_t n, uint64_t* turns);
 /* Host-side check of HOST copies of the metadata (cu_seqlens may be null, then T == nseq): lengths
- * as above (SSM_E_SEQLENS); every page that holds a sequence's tokens inside the pool, and no page
- * that this call writes named by two sequences (SSM_E_SLOT). */
+ * as above (SSM_E_SEQLENS); every page that holds tokens which the call's rows see inside the pool, and no
+ * page that this call writes named twice among those (SSM_E_SLOT). */
 int ssm_kv_check_meta_host(const ssm_attn_desc_t* desc, const int32_t* cu_seqlens, const int32_t* kv_len,
                            const int32_t* page_table, int32_t nseq, int32_t max_pages, int64_t T,
                            int32_t num_pages);

@@ -1576,7 +1576,9 @@ int ssm_kv_check_meta_host(const ssm_attn_desc_t* d, const int32_t* cu, const in
         if (n < rows || n > (int64_t)max_pages * d->page_size)
             return fail(SSM_E_SEQLENS, "kv_len[%d] = %lld with %lld rows and %d pages", i, (long long)n, (long long)rows, max_pages);
         const int64_t first = (n - rows) / d->page_size, end = (n + d->page_size - 1) / d->page_size;
-        for (int64_t p = 0; p < end; ++p) {
+        // pages of which none of the rows sees a token may be gone, or another sequence's by now
+        const int64_t seen = d->window > 0 ? std::max<int64_t>(n - rows - d->window + 1, 0) : 0;
+        for (int64_t p = seen / d->page_size; p < end; ++p) {
             const int32_t pg = table[(int64_t)i * max_pages + p];
             if (pg < 0 || pg >= num_pages) return fail(SSM_E_SLOT, "page_table[%d][%lld] = %d of %d pages", i, (long long)p, pg, num_pages);
             const bool writes = rows > 0 && p >= first;

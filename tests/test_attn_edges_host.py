@@ -51,3 +51,40 @@ def test_transform_of_another_descriptor():
     x = torch.zeros(1, 8 * 32, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="norm weight"):
         B._m_ssm_kv_append(ad, tr, x, B.KvMeta(ad, None, [3], [[0]], 3, device="cpu"), _host_pool(ad), x, x)
+
+
+def _meta_rc(cu, kv, table, num, **desc):
+    ad = B.AttnDesc(**{**dict(q_heads=8, kv_heads=2, head_dim=64, page_size=16, kv_format=0, act_dtype=B.SSM_BF16, window=0, scale=0.125),
+                       **desc})
+    cu = None if cu is None else np.array(cu, np.int32)
+    kv, table = np.array(kv, np.int32), np.array(table, np.int32)
+    T = len(kv) if cu is None else int(cu[-1])
+    return B.lib().ssm_kv_check_meta_host(ctypes.byref(ad), None if cu is None else cu.ctypes.data, kv.ctypes.data, table.ctypes.data,
+                                          len(kv), table.shape[1], T, num)
+
+
+def test_host_check_of_pages_that_slid_out_of_the_window():
+    slot = -4
+    # 64 tokens, one row at 63: a window of 16 sees 48 .. 63, page 3 alone
+    assert _meta_rc(None, [64], [[-1, -1, 9, 3]], 4, window=16) == 0
+    assert _meta_rc(None, [64], [[-1, -1, 9, 3]], 4, window=17) == slot       # token 47 is on page 2
+    assert _meta_rc(None, [64], [[-1, -1, 2, 3]], 4, window=17) == 0
+    assert _meta_rc(None, [64], [[-1, -1, 2, 3]], 4) == slot                  # no window: all are seen
+    # ten rows, the first at 54: a window of 16 sees from 39 on
+    assert _meta_rc([0, 10], [64], [[-1, -1, 2, 3]], 4, window=16) == 0
+    assert _meta_rc([0, 10], [64], [[-1, -1, -1, 3]], 4, window=16) == slot
+    # a page that the first sequence gave back is written by the second, in either order
+    assert _meta_rc(None, [64, 5], [[0, 1, 2, 3], [0, 0, 0, 0]], 4, window=20) == 0
+    assert _meta_rc(None, [5, 64], [[0, 0, 0, 0], [0, 1, 2, 3]], 4, window=20) == 0
+    assert _meta_rc(None, [64, 5], [[0, 1, 2, 3], [2, 0, 0, 0]], 4, window=20) == slot
+    # the sequence's own first page again as its last
+    assert _meta_rc(None, [64], [[3, 1, 2, 3]], 4, window=20) == 0 and _meta_rc(None, [64], [[3, 1, 2, 3]], 4) == slot
+    # windows up to the largest, and one that nothing has slid out of
+    assert _meta_rc(None, [64], [[0, 1, 2, 3]], 4, window=2 ** 31 - 1) == 0
+    assert _meta_rc(None, [64], [[-1, 1, 2, 3]], 4, window=2 ** 31 - 1) == slot
+    assert _meta_rc(None, [64], [[-1, 1, 2, 3]], 4, window=49) == slot and _meta_rc(None, [64], [[-1, 1, 2, 3]], 4, window=48) == 0
+    # rows longer than the window: every page that they are on is written
+    assert _meta_rc([0, 60], [64], [[-1, 1, 2, 3]], 4, window=4) == slot
+    # a sequence without rows in the call: what its next one sees
+    assert _meta_rc([0, 0], [64], [[-1, -1, -1, 3]], 4, window=17) == 0
+    assert _meta_rc([0, 0], [64], [[-1, -1, -1, 3]], 4, window=18) == slot

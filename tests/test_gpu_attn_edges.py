@@ -139,3 +139,63 @@ def test_page_out_of_the_pool_inside_the_window_is_reported(decode):
         f(ad, q, meta, pool, out, ws)
         assert B.take_status(ws) == want
         meta.page_table[1, first] = keep
+
+
+@pytest.mark.parametrize("act,fmt", [("bf16", "act"), ("f32", "fp8")])
+def test_pages_that_slid_out_are_used_again(act, fmt):
+    """A pool of seven pages of 16 serves a sequence of 160 tokens with a window of 40, token by token after its prompt, and
+    beside it one that starts on the pages that it gave back."""
+    from paper_2602_21144_amd import binding as B
+    hq, hkv, D, page, W, num = 4, 2, 32, 16, 40, 7
+    rng = np.random.default_rng(66)
+    ad = B.make_attn_desc(hq, hkv, D, page, kv_format=fmt, act=act, window=W)
+    pool = B.empty_kv_pool(ad, num)
+    for t in pool.tensors():
+        if t is not None:
+            t.view(torch.uint8).fill_(0xff)
+    width = (hq + 2 * hkv) * D
+    x = []
+    for n in (160, 20):   # values that every format holds exactly: e4m3 ones of a row whose largest is 448, by 2^-7
+        y = oa.round_e4m3(np.clip(60 * rng.standard_normal((n, hq + 2 * hkv, D)), -448, 448))
+        y[..., 0] = 448
+        x.append(torch.from_numpy((y * 2.0 ** -7).reshape(n, width).astype(np.float32)).to(_t(act)).cuda())
+    q, out = ([torch.empty(t.shape[0], hq * D, dtype=_t(act), device="cuda") for t in x] for _ in range(2))
+    free, table = list(range(num)), np.full((2, 10), -1, np.int32)
+    ws = B.workspace(B.attn_workspace_bytes(ad, 64, 2))
+
+    def call(lens, rows):
+        """`rows` new tokens of each sequence, which has lens[i] of them then."""
+        seqs = [i for i in range(2) if rows[i]]
+        for i in seqs:
+            first = max(0, lens[i] - rows[i] - W + 1) // page
+            for p in range(first):
+                if table[i, p] >= 0:
+                    free.append(int(table[i, p]))
+                    table[i, p] = -1
+            for p in range((lens[i] - rows[i]) // page, -(-lens[i] // page)):
+                if table[i, p] < 0:
+                    table[i, p] = free.pop(0)
+        one = all(rows[i] == 1 for i in seqs)
+        cu = None if one else np.concatenate([[0], np.cumsum([rows[i] for i in seqs])])
+        meta = B.KvMeta(ad, cu, [lens[i] for i in seqs], table[seqs], num)
+        rows_of = lambda t: torch.cat([t[i][lens[i] - rows[i]:lens[i]] for i in seqs])  # noqa: E731
+        qq, oo = (torch.empty(sum(rows), hq * D, dtype=_t(act), device="cuda") for _ in range(2))
+        B.ssm_kv_append(ad, None, rows_of(x), meta, pool, qq, ws)
+        (B.ssm_attn_decode if one else B.ssm_attn_prefill)(ad, qq, meta, pool, oo, ws)
+        at = 0
+        for i in seqs:
+            q[i][lens[i] - rows[i]:lens[i]], out[i][lens[i] - rows[i]:lens[i]] = qq[at:at + rows[i]], oo[at:at + rows[i]]
+            at += rows[i]
+    n = [0, 0]
+    for rows in [(48, 0), (20, 0), (5, 0)] + [(1, 0)] * 27 + [(7, 3)] + [(1, 1)] * 17 + [(36, 0)]:
+        n = [a + b for a, b in zip(n, rows)]
+        call(n, rows)
+    assert n == [160, 20] and B.take_status(ws) == 0
+    for i, m in enumerate(n):
+        _, k, v = oa.append(_f64(x[i]), hq, hkv, range(m), None, None, 0.0, np.zeros(0), False)
+        if fmt != "act":
+            (k, sk), (v, sv) = oa.quantise(k, fmt), oa.quantise(v, fmt)
+            k, v = k * sk[..., None], v * sv[..., None]
+        o, ab, big = oa.attend(_f64(q[i]).reshape(m, hq, D), k, v, range(m), ad.scale, W)
+        got = _f64(out[i]).reshape(m, hq, D)
+        _near(got, o, attn_tol(o, ab, big, m, D, act, fmt), f"sequence {i}")
