@@ -495,17 +495,18 @@ int ssm_attn_workspace_bytes(const ssm_attn_desc_t* desc, int64_t max_tokens, in
 
 /* qkv [T][ld_qkv] act, columns [q heads | k heads | v heads] of head_dim each. Queries and keys are
  * transformed (float32, one rounding at the end), k and v written to the cache, q to q_out [T][ld_q]
- * act, which may be qkv itself with the same stride. tr null: no norm and no rotation. */
+ * act: qkv itself with the same stride, or rows that share nothing with it (other columns of one buffer may be).
+ * tr null: no norm and no rotation. */
 int ssm_kv_append(const ssm_attn_desc_t* desc, const ssm_qk_transform_t* tr, const void* qkv, int64_t ld_qkv,
                   int64_t T, const ssm_kv_meta_t* meta, const ssm_kv_pool_t* pool, void* q_out, int64_t ld_q,
                   void* ws, size_t ws_bytes, hipStream_t stream);
 /* The cached tokens of the call's rows back as packed rows k_out, v_out [T][ld] act, columns
- * [kv heads] of head_dim: codes times scales, rounded to the activation type. */
+ * [kv heads] of head_dim: codes times scales, rounded to the activation type. k_out and v_out share nothing. */
 int ssm_kv_read(const ssm_attn_desc_t* desc, int64_t T, const ssm_kv_meta_t* meta, const ssm_kv_pool_t* pool,
                 void* k_out, int64_t ld_k, void* v_out, int64_t ld_v, void* ws, size_t ws_bytes, hipStream_t stream);
 /* Causal attention of packed prompt chunks: q, out [T][ld] act, columns [q heads] of head_dim. Row r of
  * a sequence attends to the cached tokens up to its own (and inside the window); they are read from the
- * cache, the call's own among them, so ssm_kv_append comes first. out is not q. Scores and the softmax are float32;
+ * cache, the call's own among them, so ssm_kv_append comes first. out shares nothing with q. Scores and the softmax are float32;
  * with bf16 activations the probabilities are rounded to bf16 for their product with v, with float32 ones a
  * product is exact to 2^-23. A value that is not finite (float32: above 3.38e38) makes the rows that see it
  * NaN, and one of v may reach up to 255 rows (of tokens and query heads) next to them, before its token or past

@@ -1510,6 +1510,19 @@ int check_rows(const void* p, int64_t ld, int64_t width, const char* name) {
     return SSM_OK;
 }
 
+int64_t act_bytes(const ssm_attn_desc_t* d) { return d->act_dtype == SSM_BF16 ? 2 : 4; }
+
+// Whether a [T][ld_a] of `wide_a` values a row and b [T][ld_b] of `wide_b` share a value of `size` bytes. Columns
+// of one buffer (equal strides) are told apart; other strides count as sharing where one begins inside the other.
+bool rows_share(const void* a, int64_t ld_a, int64_t wide_a, const void* b, int64_t ld_b, int64_t wide_b, int64_t T, int64_t size) {
+    const __int128 apart = (__int128)(uintptr_t)b - (__int128)(uintptr_t)a;   // strides are any 64-bit number
+    if (apart >= ((__int128)(T - 1) * ld_a + wide_a) * size || -apart >= ((__int128)(T - 1) * ld_b + wide_b) * size) return false;
+    if (T == 1 || ld_a != ld_b) return true;
+    // row j of b begins `in` bytes into row j + rows of a
+    const __int128 pitch = (__int128)ld_a * size, rows = apart >= 0 ? apart / pitch : -((-apart + pitch - 1) / pitch), in = apart - rows * pitch;
+    return (in < wide_a * size && rows > -T && rows < T) || (in + wide_b * size > pitch && rows + 1 > -T && rows + 1 < T);
+}
+
 KvArgs kv_args(const ssm_attn_desc_t* d, int64_t T, const ssm_kv_meta_t* m, const ssm_kv_pool_t* p, void* ws, bool per_row) {
     KvArgs a{};
     a.cu = per_row ? nullptr : m->cu_seqlens;
@@ -1523,11 +1536,11 @@ KvArgs kv_args(const ssm_attn_desc_t* d, int64_t T, const ssm_kv_meta_t* m, cons
     return a;
 }
 
-int check_attend(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, void* out, int64_t ld_o) {
+int check_attend(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, void* out, int64_t ld_o, int64_t T) {
     const int64_t width = (int64_t)d->q_heads * d->head_dim;
     SSM_TRY(check_rows(q, ld_q, width, "q"));
     SSM_TRY(check_rows(out, ld_o, width, "out"));
-    if (q == out) return fail(SSM_E_INVAL, "out must not be q");
+    if (rows_share(q, ld_q, width, out, ld_o, width, T, act_bytes(d))) return fail(SSM_E_INVAL, "out must not overlap q");
     return SSM_OK;
 }
 
@@ -1621,9 +1634,12 @@ int ssm_kv_append(const ssm_attn_desc_t* d, const ssm_qk_transform_t* tr, const 
         a.turns = tr->turns; a.rot = tr->rot_dim; a.inter = tr->interleaved;
     }
     if (T == 0) return SSM_OK;
-    SSM_TRY(check_rows(qkv, ld_qkv, (int64_t)(d->q_heads + 2 * d->kv_heads) * d->head_dim, "qkv"));
-    SSM_TRY(check_rows(q_out, ld_q, (int64_t)d->q_heads * d->head_dim, "q_out"));
+    const int64_t q_wide = (int64_t)d->q_heads * d->head_dim, wide = q_wide + 2LL * d->kv_heads * d->head_dim;
+    SSM_TRY(check_rows(qkv, ld_qkv, wide, "qkv"));
+    SSM_TRY(check_rows(q_out, ld_q, q_wide, "q_out"));
     if (qkv == q_out && ld_q != ld_qkv) return fail(SSM_E_INVAL, "q_out in place of qkv needs the same row stride");
+    if (qkv != q_out && rows_share(qkv, ld_qkv, wide, q_out, ld_q, q_wide, T, act_bytes(d)))
+        return fail(SSM_E_INVAL, "q_out overlaps qkv and is not its first columns");
     a.kv = kv_args(d, T, m, pool, ws, false);
     a.qkv = qkv; a.ld = ld_qkv; a.q = q_out; a.ld_q = ld_q;
     SSM_TIMED("kv.append", s, launch_kv_append(a, d->act_dtype == SSM_BF16, s));
@@ -1640,6 +1656,7 @@ int ssm_kv_read(const ssm_attn_desc_t* d, int64_t T, const ssm_kv_meta_t* m, con
     const int64_t width = (int64_t)d->kv_heads * d->head_dim;
     SSM_TRY(check_rows(k_out, ld_k, width, "k_out"));
     SSM_TRY(check_rows(v_out, ld_v, width, "v_out"));
+    if (rows_share(k_out, ld_k, width, v_out, ld_v, width, T, act_bytes(d))) return fail(SSM_E_INVAL, "v_out overlaps k_out");
     SSM_TIMED("kv.read", s, launch_kv_read(kv_args(d, T, m, pool, ws, false), k_out, ld_k, v_out, ld_v, d->act_dtype == SSM_BF16, s));
     return SSM_OK;
 }
@@ -1652,7 +1669,7 @@ int ssm_attn_prefill(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, int6
     const bool bf = d->act_dtype == SSM_BF16;
     SSM_TRY(check_ws(ws, ws_bytes, kWsHeader + attn_prefill_scratch_bytes(bf, d->q_heads, d->kv_heads, d->head_dim, T, m->nseq)));
     if (T == 0) return SSM_OK;
-    SSM_TRY(check_attend(d, q, ld_q, out, ld_o));
+    SSM_TRY(check_attend(d, q, ld_q, out, ld_o, T));
     AttnArgs a{};
     a.kv = kv_args(d, T, m, pool, ws, false);
     a.q = q; a.ld_q = ld_q; a.o = out; a.ld_o = ld_o; a.scratch = (char*)ws + kWsHeader;
@@ -1668,7 +1685,7 @@ int ssm_attn_decode(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, const
     SSM_TRY(check_kv_pool(d, pool));
     SSM_TRY(check_ws(ws, ws_bytes, kWsHeader + attn_decode_scratch_bytes(d->head_dim, m->nseq)));
     if (m->nseq == 0) return SSM_OK;
-    SSM_TRY(check_attend(d, q, ld_q, out, ld_o));
+    SSM_TRY(check_attend(d, q, ld_q, out, ld_o, m->nseq));
     AttnArgs a{};
     a.kv = kv_args(d, m->nseq, m, pool, ws, true);
     a.q = q; a.ld_q = ld_q; a.o = out; a.ld_o = ld_o; a.scratch = (char*)ws + kWsHeader;

@@ -88,3 +88,44 @@ def test_host_check_of_pages_that_slid_out_of_the_window():
     # a sequence without rows in the call: what its next one sees
     assert _meta_rc([0, 0], [64], [[-1, -1, -1, 3]], 4, window=17) == 0
     assert _meta_rc([0, 0], [64], [[-1, -1, -1, 3]], 4, window=18) == slot
+
+
+A = 0x1000000   # looks like device memory: the refusals come before anything is read
+
+
+def _op(name, x, ldx, o, ldo, T=4, act=B.SSM_BF16):
+    """8 query heads and 2 kv heads of 64: rows of 768 (append), 128 (read) or 512 values into 512, 128 or 512."""
+    d = ctypes.byref(B.AttnDesc(8, 2, 64, 16, 0, act, 0, 0.125))
+    m = ctypes.byref(B.KvMetaC(A, A, A, T, 4))
+    p = ctypes.byref(B.KvPoolC(A, A, None, None, 8))
+    f = getattr(B.lib(), name)
+    ws = (A, 1 << 40, None)
+    if name == "ssm_kv_append":
+        return f(d, None, x, ldx, T, m, p, o, ldo, *ws)
+    if name == "ssm_kv_read":
+        return f(d, T, m, p, x, ldx, o, ldo, *ws)
+    if name == "ssm_attn_prefill":
+        return f(d, x, ldx, T, m, p, o, ldo, *ws)
+    return f(d, x, ldx, m, p, o, ldo, *ws)
+
+
+WIDE = {"ssm_kv_append": (768, 512), "ssm_kv_read": (128, 128), "ssm_attn_prefill": (512, 512), "ssm_attn_decode": (512, 512)}
+
+
+@pytest.mark.parametrize("name", list(WIDE))
+@pytest.mark.parametrize("act,size", [(B.SSM_BF16, 2), (B.SSM_F32, 4)])
+def test_operands_that_share_memory(name, act, size):
+    wx, wo = WIDE[name]
+    ld = wx + wo
+    cases = [(A + 16, wx, wo), (A + 16, ld, ld), (A + (wx - 8) * size, ld, ld), (A - 16, ld, ld), (A - (wo - 8) * size, ld, ld),
+             (A + 2 * ld * size, ld, ld), (A - 3 * ld * size, ld, ld), (A + (3 * ld + wx - 8) * size, ld, ld),
+             (A - (3 * ld + wo - 8) * size, ld, ld), (A + ((wx - 8) + 3 * wx) * size, wx, wo), (A, wx + 8, wo),
+             (A + (ld - 8) * size, ld, ld)]   # the last: its row ends in the next row's beginning
+    if name != "ssm_kv_append":
+        cases.append((A, ld, ld))
+    for o, ldx, ldo in cases:
+        assert _op(name, A, ldx, o, ldo, act=act) == B.SSM_E_INVAL, (hex(o), ldx, ldo)
+        assert b"overlap" in B.lib().ssm_last_error() or o == A
+    # strides that no memory holds
+    assert _op(name, A, 1 << 60, A + 16, 1 << 60, act=act) == B.SSM_E_INVAL
+    assert _op(name, A, ld, A + (wx - 8) * size, ld, T=1, act=act) == B.SSM_E_INVAL
