@@ -237,3 +237,39 @@ def test_operands_as_columns_of_one_buffer(act, fmt, rows):
     assert B.take_status(ws) == 0
     for a, b in zip(*got):
         assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+# ------------------------------------------------------------------- codes
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["fp8", "int8"])
+@pytest.mark.parametrize("size", [2.0 ** -90, 1.0, 2.0 ** 100])
+def test_codes_are_the_stated_float32_ones(act, fmt, size):
+    """Code for code and scale for scale the float32 form of the definition, x * (Q / max) and max / Q with every step
+    rounded to nearest: values of few bits lie on ties wherever Q / max is a power of two."""
+    from paper_2602_21144_amd import binding as B
+    T, hkv, D, page = 2048, 4, 112, 64
+    ad = B.make_attn_desc(4, hkv, D, page, kv_format=fmt, act=act)
+    pages = Pages(np.random.default_rng(68), [T], page)
+    g = torch.Generator().manual_seed(68)
+    x = torch.randn(T, 3 * hkv * D, generator=g).bfloat16().float() * size
+    x.view(T, 3 * hkv, D)[:100, :, 3] = 7 * size          # Q / max is 64 / size with fp8
+    x.view(T, 3 * hkv, D)[100:200, :, 5] = -127 * size     # and 1 / size with int8
+    x = x.to(_t(act))
+    pool, q = B.empty_kv_pool(ad, pages.num), torch.empty(T, hkv * D, dtype=_t(act), device="cuda")
+    meta = B.KvMeta(ad, [0, T], [T], pages.table, pages.num)
+    ws = B.workspace(B.attn_workspace_bytes(ad, T, 1))
+    B.ssm_kv_append(ad, None, x.cuda(), meta, pool, q, ws)
+    assert B.take_status(ws) == 0
+    Q = np.float32(oa.CODE_MAX[fmt])
+    pg, off = (np.array([pages.where(0, p)[i] for p in range(T)]) for i in range(2))
+    for h0, t, s in ((hkv, pool.k, pool.k_scale), (2 * hkv, pool.v, pool.v_scale)):
+        y = x.float().numpy().reshape(T, 3 * hkv, D)[:, h0:h0 + hkv]
+        top = np.abs(y).max(-1)
+        assert np.array_equal(s.cpu().numpy()[pg, :, off], top / Q)
+        z = np.clip(y * (Q / top)[..., None], -Q, Q)
+        got = t.view(torch.uint8).cpu().numpy()[pg, :, off]
+        if fmt == "fp8":
+            want = torch.from_numpy(z).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+        else:
+            want = np.rint(z).astype(np.int8).view(np.uint8)
+        assert np.array_equal(got, want), f"{(got != want).sum()} of {got.size} codes"
