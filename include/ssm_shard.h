@@ -418,8 +418,9 @@ int ssm_stack_decode_step(const ssm_stack_desc_t* desc, const ssm_shard_weights_
  * one float32 scale per token and head (k_scale, v_scale [num_pages][kv_heads][page_size]):
  *   SSM_KV_FP8_E4M3: OCP FP8 E4M3 of x * (448 / max|row|), scale max|row| / 448;
  *   SSM_KV_INT8: round-half-even of x * (127 / max|row|), scale max|row| / 127,
- * over a row of head_dim values (rows whose largest magnitude is below 1e-30 are stored as zeros;
- * values must be finite). A pool may be larger than 4 GiB.
+ * over a row of head_dim values (rows whose largest magnitude is below 1e-30 are stored as zeros; a
+ * row that holds NaN or an infinity gets the scale NaN, and is NaN as a whole when it is read). A pool
+ * may be larger than 4 GiB.
  *
  * Requirements: kv_heads divides q_heads, q_heads at most 128; head_dim a multiple of 16 up to
  * 256; page_size a power of two from 16 to 4096; max_pages * page_size at most 2^30; scale finite

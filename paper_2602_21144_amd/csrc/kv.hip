@@ -201,14 +201,21 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
             }
         } else {
             constexpr float Q = kv_code_max<FMT>();
+            // The largest magnitude, by the order of the bits: infinity lies above all numbers, NaN above that
+            auto larger = [](float p, float q) {
+                return __builtin_bit_cast(float, max(__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q)));
+            };
             float amax = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(x[e]), fabsf(y[e])));
-            amax = group_reduce<LPH>(amax, [](float p, float q) { return fmaxf(p, q); });
+            for (int e = 0; e < 4; ++e) amax = larger(amax, larger(fabsf(x[e]), fabsf(y[e])));
+            amax = group_reduce<LPH>(amax, larger);
+            const bool finite = amax < __builtin_inff();
             // Both quotients are the nearest ones. A row's factor is often a power of two (its largest value 1.75 2^k), and
             // then values of few bits lie on ties, which a factor one step off would send the wrong way.
-            const float scale = amax >= kKvTiny ? row_scale<FMT>(amax) : 0.0f;
-            const float inv = amax >= kKvTiny ? row_factor<FMT>(amax, scale) : 0.0f;
+            // A row with a value that is no number, for which int8 has no code, is lost as a whole: its scale is NaN.
+            const bool held = finite && amax >= kKvTiny;
+            const float scale = held ? row_scale<FMT>(amax) : finite ? 0.0f : __builtin_nanf("");
+            const float inv = held ? row_factor<FMT>(amax, scale) : 0.0f;
             float u[4], v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {

@@ -273,3 +273,60 @@ def test_codes_are_the_stated_float32_ones(act, fmt, size):
         else:
             want = np.rint(z).astype(np.int8).view(np.uint8)
         assert np.array_equal(got, want), f"{(got != want).sum()} of {got.size} codes"
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["act", "fp8", "int8"])
+@pytest.mark.parametrize("heads", [(2, 2, 16), (4, 2, 112), (2, 1, 256)])
+@pytest.mark.parametrize("transform", [False, True])
+def test_values_that_are_no_numbers_stay_visible(act, fmt, heads, transform):
+    """NaN and infinities in rows of k and v: an 8-bit cache holds such a row as NaN, the activation type holds the value;
+    rows beside it are as without it, and single tokens and prompts that see it are NaN."""
+    from paper_2602_21144_amd import binding as B
+    hq, hkv, D = heads
+    T, page, g = 24, 16, hq // hkv
+    ad = B.make_attn_desc(hq, hkv, D, page, kv_format=fmt, act=act)
+    pages = Pages(np.random.default_rng(69), [T], page)
+    w = (hq + 2 * hkv) * D
+    clean = torch.from_numpy(np.random.default_rng(69).standard_normal((T, w)).astype(np.float32)).to(_t(act)).cuda()
+    x = clean.clone()
+    v = x.view(T, hq + 2 * hkv, D)
+    hit = {3: (hq, float("nan")), 7: (hq + hkv, float("nan")), 11: (hq + 2 * hkv - 1, float("inf")), 15: (hq, float("-inf"))}
+    for i, (t, (h, value)) in enumerate(hit.items()):
+        v[t, h, (0, D - 1, D // 2, 5)[i]] = value
+    v[19, hq + hkv, :] = float("nan")
+    tr = None
+    if transform:
+        tr = B.QkTransform(ad, torch.ones(D, device="cuda"), torch.ones(D, device="cuda"), 1e-5, 10000.0 ** (-np.arange(D // 2) * 2.0 / D))
+    ws = B.workspace(B.attn_workspace_bytes(ad, T, 1))
+    meta = B.KvMeta(ad, [0, T], [T], pages.table, pages.num)
+    res = []
+    for rows in (clean, x):
+        pool = B.empty_kv_pool(ad, pages.num)
+        q, k, vv, o = (torch.zeros(T, n * D, dtype=_t(act), device="cuda") for n in (hq, hkv, hkv, hq))
+        B.ssm_kv_append(ad, tr, rows, meta, pool, q, ws)
+        B.ssm_kv_read(ad, meta, pool, k, vv, ws)
+        B.ssm_attn_prefill(ad, q, meta, pool, o, ws)
+        steps = []
+        for n in (3, 4, 7, 8, T):
+            od = torch.zeros(1, hq * D, dtype=_t(act), device="cuda")
+            B.ssm_attn_decode(ad, q[n - 1:n], B.KvMeta(ad, None, [n], pages.table, pages.num), pool, od, ws)
+            steps.append(od)
+        assert B.take_status(ws) == 0
+        res.append((q, k.view(T, hkv, D), vv.view(T, hkv, D), o.view(T, hq, D), torch.cat(steps).view(5, hq, D)))
+    (q0, k0, v0, o0, s0), (q1, k1, v1, o1, s1) = res
+    assert torch.equal(q0, q1)
+    for which, a, b in (("k", k0, k1), ("v", v0, v1)):
+        base = hq if which == "k" else hq + hkv
+        lost = {(t, h - base) for t, (h, _) in hit.items() if base <= h < base + hkv} | ({(19, 0)} if which == "v" else set())
+        for t in range(T):
+            for h in range(hkv):
+                if (t, h) not in lost:
+                    assert torch.equal(a[t, h], b[t, h]), f"{which} of token {t}, head {h}"
+                elif fmt == "act":
+                    assert not torch.isfinite(b[t, h]).all()
+                else:
+                    assert torch.isnan(b[t, h]).all(), f"{which} of token {t}, head {h}"
+    # heads of kv head 0 see token 3's k from row 3 on
+    assert torch.isnan(o1[3:, :g]).all() and torch.isnan(s1[1:, :g]).all()
+    assert torch.equal(s1[0], s0[0])
