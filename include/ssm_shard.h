@@ -423,8 +423,8 @@ int ssm_stack_decode_step(const ssm_stack_desc_t* desc, const ssm_shard_weights_
  * may be larger than 4 GiB.
  *
  * Requirements: kv_heads divides q_heads, q_heads at most 128; head_dim a multiple of 16 up to
- * 256; page_size a power of two from 16 to 4096; max_pages * page_size at most 2^30; scale finite
- * and positive; window >= 0; a call has up to 2^22 rows and 2^15 sequences. Row strides (ld_*) are
+ * 256; page_size a power of two from 16 to 4096; max_pages * page_size at most 2^30; scale
+ * positive, up to 2.3e38; window >= 0; a call has up to 2^22 rows and 2^15 sequences. Row strides (ld_*) are
  * in elements, multiples of 8, at least the row's width. Both activation types go with every cache
  * format. */
 typedef enum ssm_kv_format { SSM_KV_ACT = 0, SSM_KV_FP8_E4M3 = 1, SSM_KV_INT8 = 2 } ssm_kv_format_t;

@@ -1474,7 +1474,8 @@ int check_attn_desc(const ssm_attn_desc_t* d) {
     if (d->page_size < 16 || d->page_size > 4096 || (d->page_size & (d->page_size - 1)))
         return fail(SSM_E_INVAL, "page_size %d must be a power of two from 16 to 4096", d->page_size);
     if (d->window < 0) return fail(SSM_E_INVAL, "window %d", d->window);
-    if (!(d->scale > 0.0f) || !(d->scale < HUGE_VALF)) return fail(SSM_E_INVAL, "scale must be finite and positive");
+    // the kernels take scale log2(e): an infinite one would make scores of 0 NaN
+    if (!(d->scale > 0.0f) || !(d->scale * kLog2e < HUGE_VALF)) return fail(SSM_E_INVAL, "scale must be positive, up to 2.3e38");
     return SSM_OK;
 }
 

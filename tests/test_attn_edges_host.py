@@ -129,3 +129,9 @@ def test_operands_that_share_memory(name, act, size):
     # strides that no memory holds
     assert _op(name, A, 1 << 60, A + 16, 1 << 60, act=act) == B.SSM_E_INVAL
     assert _op(name, A, ld, A + (wx - 8) * size, ld, T=1, act=act) == B.SSM_E_INVAL
+
+
+def test_scales_up_to_the_largest_that_stays_finite():
+    rc = lambda x: B.lib().ssm_attn_check_desc(ctypes.byref(B.AttnDesc(8, 2, 64, 16, 0, B.SSM_BF16, 0, x)))  # noqa: E731
+    assert rc(2.3e38) == 0 and rc(1e-45) == 0
+    assert rc(2.4e38) == B.SSM_E_INVAL and rc(3.4e38) == B.SSM_E_INVAL     # times log2(e): infinite
