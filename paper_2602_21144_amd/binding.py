@@ -777,7 +777,11 @@ class KvMeta:
 
     def __init__(self, ad: AttnDesc, cu_seqlens, kv_len, page_table, num_pages: int, device="cuda"):
         def host(x):
-            return np.ascontiguousarray(x.cpu().numpy() if isinstance(x, torch.Tensor) else x, np.int32)
+            a = np.asarray(x.cpu().numpy() if isinstance(x, torch.Tensor) else x)
+            b = np.ascontiguousarray(a).astype(np.int32)
+            if not np.array_equal(a, b):
+                raise ValueError("metadata: 32-bit whole numbers expected")
+            return b
         cu = None if cu_seqlens is None else host(cu_seqlens)
         kl = host(kv_len)
         self.nseq, self.page_size = int(kl.shape[0]), ad.page_size

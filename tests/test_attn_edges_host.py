@@ -135,3 +135,15 @@ def test_scales_up_to_the_largest_that_stays_finite():
     rc = lambda x: B.lib().ssm_attn_check_desc(ctypes.byref(B.AttnDesc(8, 2, 64, 16, 0, B.SSM_BF16, 0, x)))  # noqa: E731
     assert rc(2.3e38) == 0 and rc(1e-45) == 0
     assert rc(2.4e38) == B.SSM_E_INVAL and rc(3.4e38) == B.SSM_E_INVAL     # times log2(e): infinite
+
+
+def test_metadata_that_32_bits_do_not_hold():
+    ad = B.make_attn_desc(4, 2, 32, 16)
+    big = 1 << 32
+    for cu, kv, table in ((None, [3 + big], [[0]]), (None, [3], [[big]]), ([0, 3 + big], [3], [[0]]), (None, [2.5], [[0]])):
+        for wrap in (np.array, torch.tensor):
+            with pytest.raises(ValueError, match="32-bit"):
+                B.KvMeta(ad, None if cu is None else wrap(cu), wrap(kv), wrap(table), 4, device="cpu")
+    m = B.KvMeta(ad, torch.tensor([0, 3]), torch.tensor([20]), torch.tensor([[0, 2]]), 4, device="cpu")
+    assert m.kv_len.dtype == torch.int32 and m.kv_len.tolist() == [20] and m.T == 3
+    assert B.KvMeta(ad, None, [], [], 4, device="cpu").nseq == 0
