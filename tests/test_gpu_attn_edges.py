@@ -54,9 +54,10 @@ def _near(got, want, tol, what):
     assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.max(np.abs(got - want) / tol):.2f} of the bound"
 
 
-def _attend(heads, page, q_lens, ctx, act, fmt, window=0, decode=False, seed=0, slid_out=False, rows=None):
+def _attend(heads, page, q_lens, ctx, act, fmt, window=0, decode=False, seed=0, slid_out=False, rows=None, gone=None):
     """The attention of a call against the oracle at every row, or at about `rows` of each sequence. slid_out: what no row
-    of a sequence sees any more holds NaN values and scales, and pages of such tokens alone are named out of range.
+    of a sequence sees any more holds NaN values and scales, and pages of such tokens alone are named out of range. gone
+    {sequence: pages}: these are named out of range as well, though rows see them, and their tokens do not exist.
     Rows behind the last sequence keep what they hold. Returns what it called with."""
     from paper_2602_21144_amd import binding as B
     hq, hkv, D = heads
@@ -83,12 +84,14 @@ def _attend(heads, page, q_lens, ctx, act, fmt, window=0, decode=False, seed=0, 
             for p in range(first // page):
                 table[i, p] = (-1, pages.num, 2 ** 31 - 1)[p % 3]
         meta.page_table.copy_(torch.from_numpy(table))
+    for i, ps in (gone or {}).items():
+        meta.page_table[i, ps] = pages.num
     pool = B.KvPool(ad, *dev, *scales)
     q = torch.from_numpy(rng.standard_normal((T, hq * D)).astype(np.float32)).to(_t(act)).cuda()
     out = torch.full((T + 3, hq * D), float("nan"), dtype=_t(act), device="cuda")
     ws = B.workspace(B.attn_workspace_bytes(ad, T, len(q_lens)))
     (B.ssm_attn_decode if decode else B.ssm_attn_prefill)(ad, q, meta, pool, out, ws)
-    assert B.take_status(ws) == 0
+    assert B.take_status(ws) == (B.SSM_STATUS_BAD_PAGE if gone else 0)
     assert torch.isnan(out[T:]).all(), "written behind the rows"
     qh, got = _f64(q).reshape(T, hq, D), _f64(out[:T]).reshape(T, hq, D)
     assert np.isfinite(got).all(), f"{(~np.isfinite(got)).sum()} of {got.size} values are not finite"
@@ -97,7 +100,8 @@ def _attend(heads, page, q_lens, ctx, act, fmt, window=0, decode=False, seed=0, 
         if m == 0:
             continue
         sel = np.arange(m) if rows is None or m <= rows else np.unique(np.r_[0, 1, m - 2, m - 1, rng.integers(0, m, rows)])
-        o, ab, big = oa.attend(qh[at + sel], tokens(K, pages, i, n), tokens(V, pages, i, n), n - m + sel, ad.scale, window)
+        ok = np.array([p // page not in gone.get(i, ()) for p in range(n)]) if gone else None
+        o, ab, big = oa.attend(qh[at + sel], tokens(K, pages, i, n), tokens(V, pages, i, n), n - m + sel, ad.scale, window, ok)
         _near(got[at + sel], o, attn_tol(o, ab, big, n, D, act, fmt), f"sequence {i}")
         at += m
     return B, ad, pool, meta, q, out, ws
@@ -330,3 +334,66 @@ def test_values_that_are_no_numbers_stay_visible(act, fmt, heads, transform):
     # heads of kv head 0 see token 3's k from row 3 on
     assert torch.isnan(o1[3:, :g]).all() and torch.isnan(s1[1:, :g]).all()
     assert torch.equal(s1[0], s0[0])
+
+
+# ------------------------------------------------------------------- forms of larger calls
+# Tiles of 256 rows by eight waves: bf16, heads of 97 to 128 values, 65536 rows of query heads and more
+BF16 = [("bf16", "act"), ("bf16", "fp8"), ("bf16", "int8")]
+
+
+@pytest.mark.parametrize("act,fmt", BF16)
+@pytest.mark.parametrize("window", [0, 100, 700])
+@pytest.mark.parametrize("heads,q,ctx", [
+    ((128, 1, 128), [512], [0]),                        # the first call of this form, one kv head
+    ((128, 1, 128), [1, 300, 0, 211, 5], [0, 900, 40, 0, 2000]),
+    ((64, 8, 112), [1024], [3000]),                     # cut into items and joined
+    ((64, 8, 112), [700, 1, 400], [0, 2500, 1111]),
+    ((16, 16, 112), [2049, 0, 2081], [0, 7, 64]),       # last tiles of 1 and of 33 rows
+    ((24, 8, 128), [2731, 5], [1, 4000]),
+])
+def test_tiles_of_256_rows(act, fmt, window, heads, q, ctx):
+    assert sum(q) * heads[0] >= 65536
+    _attend(heads, 32, q, ctx, act, fmt, window=window, seed=70, slid_out=window > 0, rows=14)
+
+
+@pytest.mark.parametrize("fmt", ["act", "fp8"])
+@pytest.mark.parametrize("rows", [1023, 1024, 1025])
+def test_both_sides_of_the_taller_tiles(fmt, rows):
+    _attend((64, 8, 112), 64, [rows - 40, 40], [100, 1500], "bf16", fmt, seed=71, rows=12)
+
+
+@pytest.mark.parametrize("fmt", ["act", "int8"])
+@pytest.mark.parametrize("window", [0, 500])
+def test_tiles_of_256_rows_without_some_pages(fmt, window):
+    _attend((64, 8, 128), 16, [1100], [300], "bf16", fmt, window=window, seed=72, rows=16, gone={0: [3, 21, 22, 40, 86]})
+
+
+@pytest.mark.parametrize("act,fmt", FORMATS)
+@pytest.mark.parametrize("heads", [(4, 2, 96), (6, 2, 112), (16, 4, 128), (2, 1, 160), (4, 2, 224), (5, 1, 256)])
+def test_few_rows_behind_a_long_cache(act, fmt, heads):
+    """Tiles that are cut into many items, at every padded width: the buffers of a step's scales go round."""
+    for q, ctx in (([1], [4000]), ([33], [3000]), ([5, 3, 1], [2500, 1000, 1700])):
+        _attend(heads, 32, q, ctx, act, fmt, seed=73, rows=10)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+def test_many_pages_a_table_row(decode):
+    """65536 tokens of one kv head, in the smallest pages."""
+    _attend((3, 1, 32), 16, [1] if decode else [3], [65536], "bf16", "fp8", decode=decode, seed=74)
+
+
+# ------------------------------------------------------------------- many tokens appended
+@pytest.mark.parametrize("act,fmt", [("bf16", "act"), ("bf16", "fp8"), ("f32", "act"), ("f32", "int8")])
+@pytest.mark.parametrize("rows,pos0", [((127,), (0,)), ((128,), (5,)), ((129,), (16,)), ((100, 1, 0, 156), (0, 40, 3, 17)),
+                                       ((255, 1), (0, 0)), ((390,), (10,)), ((1500,), (3,))])
+def test_append_of_many_tokens_against_the_oracle(act, fmt, rows, pos0):
+    """Around and past the groups of 128 tokens that are dealt out to the XCDs: every token in its own place."""
+    from test_gpu_attn import _append_case
+    _append_case(act, fmt, (3, 1, 64), 0, False, False, pos0, rows=rows, seed=75)
+    _append_case(act, fmt, (4, 2, 112), 32, True, True, pos0, rows=rows, seed=76, page=64)
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_append_of_many_wide_heads(act):
+    from test_gpu_attn import _append_case
+    _append_case(act, "fp8", (2, 1, 256), 64, False, True, (0, 2), rows=(200, 190), seed=77, page=32)
