@@ -467,7 +467,8 @@ typedef struct ssm_kv_meta {
     int32_t max_pages;
 } ssm_kv_meta_t;
 /* What ssm_kv_append applies to every query and key head before they are used.
- *   q_norm_w, k_norm_w [head_dim] float32 (null: none): x / sqrt(mean(x^2) + norm_eps) * w
+ *   q_norm_w, k_norm_w [head_dim] float32 (null: none): x / sqrt(mean(x^2) + norm_eps) * w, the mean and its sum
+ *     with norm_eps float32 and taken as 1.2e-38 below that (values up to 1e18 in magnitude)
  *   turns [rot_dim / 2] (null when rot_dim is 0): the rotation of pair i by the token's position,
  *     in turns per token as 64-bit fixed point (ssm_rope_turns), exact at any position
  *   rot_dim: the leading values that rotate, a multiple of 8 up to head_dim, or 0
@@ -509,14 +510,18 @@ int ssm_kv_read(const ssm_attn_desc_t* desc, int64_t T, const ssm_kv_meta_t* met
  * a sequence attends to the cached tokens up to its own (and inside the window); they are read from the
  * cache, the call's own among them, so ssm_kv_append comes first. out shares nothing with q. Scores and the softmax are float32;
  * with bf16 activations the probabilities are rounded to bf16 for their product with v, with float32 ones a
- * product is exact to 2^-23. A value that is not finite (float32: above 3.38e38) makes the rows that see it
- * NaN, and one of v may reach up to 255 rows (of tokens and query heads) next to them, before its token or past
- * the window. What pages hold behind a sequence's last token, or in front of what its rows see, never does. */
+ * product is exact to 2^-23 (what is summed for the softmax's denominator is rounded as well where the cache is
+ * bf16, so the weights add up to one; elsewhere it is not). The sums of p v are divided at the end: scaled scores
+ * up to 1e9 in magnitude, and |v| times the visible tokens up to 1e36. A value that is not finite (float32: above
+ * 3.38e38) makes the rows that see it NaN or what the formula gives, and one of v may reach up to 255 rows (of
+ * tokens and query heads) next to them, before its token or past the window. What pages hold behind a sequence's
+ * last token, or in front of what its rows see, never does. */
 int ssm_attn_prefill(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, int64_t T, const ssm_kv_meta_t* meta,
                      const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
                      hipStream_t stream);
 /* The same for one new token per sequence: q, out [nseq][ld]; meta->cu_seqlens is not read. The work is
- * split over the sequences' lengths and joined, in an order that follows from the lengths alone. */
+ * split over the sequences' lengths and joined, in an order that follows from the lengths alone. A value that is
+ * not finite reaches the rows that see it and no others. */
 int ssm_attn_decode(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, const ssm_kv_meta_t* meta,
                     const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
                     hipStream_t stream);

@@ -397,3 +397,40 @@ def test_append_of_many_tokens_against_the_oracle(act, fmt, rows, pos0):
 def test_append_of_many_wide_heads(act):
     from test_gpu_attn import _append_case
     _append_case(act, "fp8", (2, 1, 256), 64, False, True, (0, 2), rows=(200, 190), seed=77, page=32)
+
+
+@pytest.mark.parametrize("act,fmt", FORMATS)
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_as_large_as_stated(act, fmt, decode, sign):
+    """Scaled scores of up to 0.97e9 (and down to that below 0), 1.5e7 apart: every row is the v of its largest score,
+    though a score's float32 product with the exponent's factor is up to 64 off."""
+    from paper_2602_21144_amd import binding as B
+    n, D, page, hq = 64, 96, 16, 2
+    ad = B.make_attn_desc(hq, 1, D, page, kv_format=fmt, act=act, scale=1.8)
+    pool = B.empty_kv_pool(ad, n // page)
+    table = np.arange(n // page)[None]
+    x = torch.zeros(n, hq + 2, D)
+    x[:, :hq, 0] = 2.0 ** 13 * sign
+    x[:, hq, 0] = 2.0 ** 10 * torch.arange(1, n + 1)
+    x[:, hq + 1] = torch.from_numpy(np.random.default_rng(78).choice([0.5, 1.0, 1.5, -1.75], (n, D)).astype(np.float32))
+    x[:, hq + 1, 0] = 1.75                                  # the row's largest: the others are fp8 codes then
+    x = x.view(n, -1).to(_t(act)).cuda()
+    q, out, k, v = (torch.empty(n, w * D, dtype=_t(act), device="cuda") for w in (hq, hq, 1, 1))
+    ws = B.workspace(B.attn_workspace_bytes(ad, n, 1))
+    meta = B.KvMeta(ad, [0, n], [n], table, n // page)
+    B.ssm_kv_append(ad, None, x, meta, pool, q, ws)
+    B.ssm_kv_read(ad, meta, pool, k, v, ws)
+    rows = range(n)
+    if decode:
+        for t in rows:
+            B.ssm_attn_decode(ad, q[t:t + 1], B.KvMeta(ad, None, [t + 1], table, n // page), pool, out[t:t + 1], ws)
+    else:
+        B.ssm_attn_prefill(ad, q, meta, pool, out, ws)
+    assert B.take_status(ws) == 0
+    scores = np.float64(1.8) * 2.0 ** 13 * _f64(k)[:, 0]
+    assert scores.max() < 1e9 and np.diff(scores).min() > 1e6
+    want = np.stack([_f64(v)[t if sign > 0 else 0] for t in rows])[:, None].repeat(hq, 1)
+    # the winner's p rounded once (bf16: 2^-8) and the result (2^-8); float32: product, sum, quotient
+    tol = np.abs(want) * (2.1 * 2.0 ** -8 if act == "bf16" else 8 * 2.0 ** -24)
+    _near(_f64(out).reshape(n, hq, D), want, tol, "the largest score's v")
