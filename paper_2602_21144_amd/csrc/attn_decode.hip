@@ -22,9 +22,9 @@
 // The next tile's loads are issued before the present one is computed. Eight-bit codes become bf16
 // exactly; their scales multiply the scores and the probabilities.
 //
-// Bound by memory: one sequence of 131072 tokens, 8 kv heads of 128 in bf16, 94 us and 7 for the join (5.7 TB/s in the
-// main kernel), 256 sequences of 513 to 1025 tokens, 16 heads of 112, 248 us (5.6), 64 of 200 to 8192 tokens in fp8
-// 111 us (5.1, the decoding beside it). One of 391 tokens in float32 is one chain of loads, 9 us, and the join's 4.
+// Bound by memory: one sequence of 131072 tokens, 8 kv heads of 128 in bf16, 95 us and 7 for the join (5.7 TB/s in the
+// main kernel), 256 sequences of 513 to 1025 tokens, 16 heads of 112, 250 us (5.6), 64 of 200 to 8192 tokens in fp8
+// 111 us (5.1, the decoding beside it). One of 391 tokens in float32 is one chain of loads, 10 us, and the join's 4.
 #include "kv.h"
 
 namespace ssm {
@@ -113,20 +113,18 @@ __device__ __forceinline__ Place find_run(const KvArgs& a, int rows_per_seq, int
     return Place{runs, uniform((int)sh[4]), uniform(sh[5])};
 }
 
-// Workgroups that are resident at once: 256 compute units, 2 each where the registers allow it (768 and 1024: 104
-// and 115 us for one sequence of 131072 tokens with its join, 128 and 116 for the 64 in fp8; 512: 102 and 115)
+// Runs, in all forms: two for each of the 256 compute units, which take two workgroups at once up to 128 values a head
+// (one of float32 rows of 65 to 128 values) and one above. 768, 1024 and 512 of them: 104, 115 and 102 us for one
+// sequence of 131072 tokens with its join, 128, 116 and 115 for the 64 in fp8. 256 and 512 where one workgroup
+// fills a unit: 16 heads of 224, 16 sequences of 1000 to 4000 tokens 112 and 115, 16 of 256 over 2 kv heads, 116
+// sequences 57 and 60 (float32 161 and 161), one of 65536 tokens 52 and 74 (its join has half the partials then);
+// 16 of 112 in float32, 64 sequences 346 and 330, one of 20000 tokens 57 and 64; over fp8 pages 241 and 188.
 constexpr int kWorkers = 512;
 // The join of a row that is cut: its first query head, how many of them, and the partial results
 struct RowJoin { int32_t seq, q_head, rows, pieces; };
 constexpr size_t kJoinBytes = kWorkers * sizeof(RowJoin);
 
-// The operand layouts per (activation type, cache format): CH values per 16-byte piece of a k row
-template <typename T, int FMT> struct Layout {
-    using E = typename KvElem<T, FMT>::type;
-    static constexpr int CH = 16 / (int)sizeof(E);
-};
-
-// raw registers of one 32-token tile
+// Raw registers of one 32-token tile: a k row in 16-byte pieces of CH values
 template <typename T, int FMT, int DP> struct Tile {
     using E = typename KvElem<T, FMT>::type;
     static constexpr int CH = 16 / (int)sizeof(E), NC = DP / (4 * CH), VEC = DP / 16;
@@ -314,8 +312,8 @@ __device__ __forceinline__ void attend_tile(Tile<T, FMT, DP>& x, const Query<T, 
         if constexpr (FMT != SSM_KV_ACT) p[e] *= x.vs[e];
     }
     if constexpr (BF) {
-        // the probabilities enter the product in bf16, half a step (2^-9) off each, as v itself is
-        // stored; the sum l is of the unrounded ones
+        // the probabilities enter the product in bf16, up to half a step (2^-8 of the value) off
+        // each, as v itself is stored; the sum l is of the unrounded ones
         bf16x8 b;
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e] = (bf16)p[e];

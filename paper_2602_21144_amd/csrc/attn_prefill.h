@@ -17,9 +17,10 @@
 // whose partial results (m, l and the unnormalised o, float32) a third kernel joins in order. Items are
 // listed longest first, and the workgroups of one item's kv heads are neighbours.
 //
-// Bound by instructions beside the MFMAs: 8192 tokens, 32 heads of 128 in bf16, 509 us, 1.08 PFLOP/s with the matrix
-// cores' pipe 56% busy (a large library product reaches 1.65); three prompts of 2048 tokens in all, one behind 4096,
-// 16 heads of 112: 36 us, the plan and the join 6 and 7; 33 tokens behind 40000 in fp8, 32 heads of 128: 50 us and 13.
+// Bound by instructions beside the MFMAs: 8192 tokens, 32 heads of 128 in bf16, 524 us a call of many in a row, 1.05
+// PFLOP/s (535 to 641 for the kernel in a trace of ten), with the matrix cores' pipe 56% busy (a large library
+// product reaches 1.65); three prompts of 2048 tokens in all, one behind 4096, 16 heads of 112: 36 us, the plan and
+// the join 7 and 8; 33 tokens behind 40000 in fp8, 32 heads of 128: 52 us, and 16 for those two.
 #pragma once
 #include "kv.h"
 
@@ -33,8 +34,8 @@ inline int tile_rows(bool bf16_act, int DP, int64_t rows_heads) { return bf16_ac
 constexpr int kStep = 64;          // the plan counts tokens in steps of this many
 // Workgroups that run at once: two on a compute unit where their registers and LDS allow it (PrefillShape)
 inline int tile_places(bool bf16_act, int rows, int DP) { return rows == 128 && DP <= (bf16_act ? 128 : 96) ? 512 : 256; }
-// No item is cut shorter than this: what its steps take (1 to 2 us one of bf16, twice that above 128 values a
-// head, 4 to 5 of float32) against the join. Ten sequences of 1 to 7 rows, the longest behind 3059 tokens, 16 heads
+// The least that the longest item's steps are limited to: what steps take (1 to 2 us one of bf16, twice that above 128
+// values a head, 4 to 5 of float32) against the join. A tile above it is cut evenly (9 steps at 8: 5 and 4). Ten sequences of 1 to 7 rows, the longest behind 3059 tokens, 16 heads
 // of 256: 8 steps 37 us, 4 30, 2 29; 8 of 64 fp8, 2745 tokens: 26, 23, 22; eight prompts of 28 to 441 rows, 20 of
 // 80 fp8: 23, 31, 34. Float32, nine calls of up to 2500 rows, mean: 4 steps 26.6 us, 2 25.6, 1 25.9.
 constexpr int tile_min_steps(bool bf16_act, int DP) { return !bf16_act ? 2 : DP <= 128 ? 8 : 4; }

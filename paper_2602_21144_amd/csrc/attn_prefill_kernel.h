@@ -392,8 +392,8 @@ void attn_prefill_kernel(AttnArgs p, AttnPlan plan) {
                 }
         }
         if constexpr (BF) {
-            // The probabilities enter the product in bf16, half a step (2^-9) off each, as v itself is
-            // stored. Their sum l is of the rounded ones where no scale of v is in them: two to an
+            // The probabilities enter the product in bf16, up to half a step (2^-8 of the value)
+            // off each, as v itself is stored. Their sum l is of the rounded ones where no scale of v is in them: two to an
             // instruction, in float32, and the weights p / l add up to one.
             typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
             const bf16x2 one = {(bf16)1.0f, (bf16)1.0f};
