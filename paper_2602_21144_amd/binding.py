@@ -773,7 +773,8 @@ def empty_kv_pool(ad: AttnDesc, num_pages: int, device="cuda") -> KvPool:
 class KvMeta:
     """Device-resident sequences of one call (int32), validated from their host copy. cu_seqlens None: one
     row per sequence. A program that goes on token by token advances kv_len in place (`meta.kv_len += 1`)
-    and keeps to the pages of page_table."""
+    and keeps to the pages of page_table. With a window, entries of pages in front of what the sequence's first
+    row sees may be anything. Pools and descriptors of other shapes are refused by the calls."""
 
     def __init__(self, ad: AttnDesc, cu_seqlens, kv_len, page_table, num_pages: int, device="cuda"):
         def host(x):
