@@ -526,6 +526,99 @@ int ssm_attn_decode(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, co
                     const ssm_kv_pool_t* pool, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
                     hipStream_t stream);
 
+/* ------------------------------------------------------- gated delta rule and its norms
+ * A third recurrent mixer for the stacks of Section II-A and Section IV-E, split by heads with the
+ * same cache and exchange principles (Section IV-A, Section IV-B): a rank owns v_heads value heads
+ * and the qk_heads query/key heads they read (value head h reads head h / (v_heads / qk_heads)),
+ * between a column-split projection with its convolution and a row-split output projection. Per
+ * value head, with the state S (v_dim x qk_dim):
+ *   alpha_t = exp(-exp(A_log_h) softplus(a_t + dt_bias_h)),  beta_t = beta_max sigmoid(b_t)
+ *   u_t = beta_t (v_t - alpha_t S_{t-1} k_t);  S_t = alpha_t S_{t-1} + u_t k_t^T;  o_t = scale S_t q_t
+ * and, where qk_norm is 1, k and q divided by sqrt(sum of their squares + norm_eps) first.
+ * All sums, the decays and the state are float32; o is rounded once, to the activation type.
+ * Requirements: qk_heads divides v_heads, v_heads at most 128; qk_dim a multiple of 16 up to 256,
+ * v_dim a multiple of 16 up to 512; scale finite and positive; norm_eps positive; beta_max in (0, 2];
+ * a call has up to 2^22 rows and 2^15 sequences. The rule is stable for keys of length up to
+ * sqrt(2 / beta): with qk_norm 0 that is the caller's. Squares of q and k have to stay in float32.
+ * State cache: ssm_pool [num_slots][v_heads][v_dim][qk_dim] float32.
+ * A value that is not finite reaches what the formulas say; in prompts also up to 63 rows of its
+ * sequence in front of its own, in the heads that read it. */
+typedef struct ssm_delta_desc {
+    int32_t qk_heads;   /* query/key heads of this shard */
+    int32_t v_heads;    /* value heads of this shard     */
+    int32_t qk_dim;
+    int32_t v_dim;
+    int32_t act_dtype;  /* ssm_dtype_t                   */
+    int32_t qk_norm;    /* 1: q and k are normalised     */
+    float scale;        /* of q, 1 / sqrt(qk_dim) as a rule */
+    float norm_eps;
+    float beta_max;     /* 1, or 2 for negative eigenvalues */
+} ssm_delta_desc_t;
+typedef struct ssm_delta_gates {
+    const float* A_log;     /* [v_heads] */
+    const float* dt_bias;   /* [v_heads] */
+} ssm_delta_gates_t;
+typedef enum ssm_gate_fn { SSM_GATE_IDENTITY = 0, SSM_GATE_SIGMOID = 1, SSM_GATE_SILU = 2, SSM_GATE_TANH = 3 } ssm_gate_fn_t;
+/* The norm of every head of a row and its gate, in float32 with one rounding at the end:
+ *   gate_first 0: x / sqrt(mean(x^2) + eps) * w * gate(z);   1: y / sqrt(mean(y^2) + eps) * w, y = x gate(z)
+ * over the head's values; w [dim], or [heads][dim] with per_head 1; z [T][ld_z] of the rows' type, the
+ * columns as the row's (null: no gate). Squares have to stay in float32. */
+typedef struct ssm_gated_norm {
+    const float* w;
+    const void* z;
+    int64_t ld_z;
+    float eps;            /* > 0 */
+    int32_t per_head;
+    int32_t gate;         /* ssm_gate_fn_t */
+    int32_t gate_first;
+} ssm_gated_norm_t;
+int ssm_delta_check_desc(const ssm_delta_desc_t* desc);
+/* One workspace serves both operators for calls of up to max_tokens rows and max_seqs sequences.
+ * Initialise it and read its status as for the mixer's; calls that share it must not overlap in time. */
+int ssm_delta_workspace_bytes(const ssm_delta_desc_t* desc, int64_t max_tokens, int32_t max_seqs, size_t* bytes);
+/* Packed prompts: qkv [T][ld_qkv] act, columns [q heads | k heads | v heads]; a and b [T][ld_ab] act, v_heads
+ * columns each (any stride of at least v_heads, aligned to their type: columns of the projection); out [T][ld_out]
+ * act, columns [v heads]. ld_qkv and ld_out are multiples of 8. Metadata as for ssm_shard_prefill; the state of
+ * every sequence's slot is written (zeros for an empty fresh one). A slot outside the pool starts its sequence
+ * from zeros and stores nothing; packed rows behind the last sequence are left as they were. out shares nothing
+ * with the inputs. */
+int ssm_delta_prefill(const ssm_delta_desc_t* desc, const ssm_delta_gates_t* gates, const void* qkv, int64_t ld_qkv,
+                      const void* a, const void* b, int64_t ld_ab, int64_t T, const ssm_seq_meta_t* meta,
+                      float* ssm_pool, int32_t num_slots, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
+                      hipStream_t stream);
+/* One token for each of `batch` sequences on ssm_pool[slot] in place (cache_slot [batch] device int32, distinct);
+ * a slot outside the pool gives a row of zeros. norm (null: none): the head norm applied to o before it is
+ * rounded, z [batch][ld_z]. */
+int ssm_delta_decode(const ssm_delta_desc_t* desc, const ssm_delta_gates_t* gates, const void* qkv, int64_t ld_qkv,
+                     const void* a, const void* b, int64_t ld_ab, int32_t batch, const int32_t* cache_slot,
+                     float* ssm_pool, int32_t num_slots, const ssm_gated_norm_t* norm, void* out, int64_t ld_out,
+                     void* ws, size_t ws_bytes, hipStream_t stream);
+/* out [T][ld_out] = the norm above of x [T][ld_x], both of dtype (ssm_dtype_t), `heads` heads of `dim` values a
+ * row. dim is a multiple of 8 up to 2048, heads at most 512, strides multiples of 8, T up to 2^22. out is x itself
+ * with the same stride, or shares nothing with x and z. */
+int ssm_gated_rmsnorm(const void* x, int64_t ld_x, int32_t dtype, int64_t T, int32_t heads, int32_t dim,
+                      const ssm_gated_norm_t* norm, void* out, int64_t ld_out, hipStream_t stream);
+/* What lies between two blocks where the block's output is normed, gated or scaled before it returns to the
+ * residual stream (ssm_residual_rmsnorm with the terms of `block`):
+ *   y = parts[0] + ... + parts[n_parts-1] (float32, in that order);  y = y / sqrt(mean(y^2) + post_eps) * post_w
+ *   residual = base + scale * gate(g) * y;  normed = residual / sqrt(mean(residual^2) + eps) * norm_w
+ *   post_w [d] float32 (null: no norm); g [T][ld_gate] of gate_dtype (null: none), one row for all with ld_gate 0
+ * The other arguments, their limits and errors as for ssm_residual_rmsnorm; ld_gate 0 or a multiple of 8 of at
+ * least d. residual is base itself or shares nothing with the inputs; normed shares nothing with the inputs or
+ * residual. */
+typedef struct ssm_block_out {
+    const float* post_w;
+    const void* gate;
+    int64_t ld_gate;
+    float post_eps;       /* > 0 where post_w is set */
+    float scale;          /* finite */
+    int32_t gate_dtype;   /* ssm_dtype_t */
+    int32_t gate_fn;      /* ssm_gate_fn_t */
+} ssm_block_out_t;
+int ssm_block_rmsnorm(const void* base, int32_t base_dtype, const void* const* parts, int32_t n_parts,
+                      int32_t parts_dtype, const ssm_block_out_t* block, float* residual, const float* norm_w, float eps,
+                      void* normed, int32_t normed_dtype, int64_t T, int32_t d, hipStream_t stream);
+
 /* ------------------------------------------------------------ measurement
  * Per-kernel device time, for benchmarks and profiles only. While enabled, every kernel
  * the library launches from the calling thread is launched with hipExtLaunchKernel and

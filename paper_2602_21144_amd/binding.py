@@ -86,6 +86,25 @@ class QkTransformC(ctypes.Structure):
         ("norm_eps", ctypes.c_float), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
+class DeltaDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("qk_heads", "v_heads", "qk_dim", "v_dim", "act_dtype", "qk_norm")] + [
+        (n, ctypes.c_float) for n in ("scale", "norm_eps", "beta_max")]
+
+
+class DeltaGatesC(ctypes.Structure):
+    _fields_ = [("A_log", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p)]
+
+
+class GatedNormC(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("z", ctypes.c_void_p), ("ld_z", ctypes.c_int64), ("eps", ctypes.c_float),
+                ("per_head", ctypes.c_int32), ("gate", ctypes.c_int32), ("gate_first", ctypes.c_int32)]
+
+
+class BlockOutC(ctypes.Structure):
+    _fields_ = [("post_w", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64), ("post_eps", ctypes.c_float),
+                ("scale", ctypes.c_float), ("gate_dtype", ctypes.c_int32), ("gate_fn", ctypes.c_int32)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 _P, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 
@@ -139,6 +158,12 @@ _SIGS = {
     "ssm_kv_read": ([_P, _I64, _P, _P, _P, _I64, _P, _I64, _P, _SZ, _P], _I32),
     "ssm_attn_prefill": ([_P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
     "ssm_attn_decode": ([_P, _P, _I64, _P, _P, _P, _I64, _P, _SZ, _P], _I32),
+    "ssm_delta_check_desc": ([_P], _I32),
+    "ssm_delta_workspace_bytes": ([_P, _I64, _I32, _P], _I32),
+    "ssm_delta_prefill": ([_P, _P, _P, _I64, _P, _P, _I64, _I64, _P, _P, _I32, _P, _I64, _P, _SZ, _P], _I32),
+    "ssm_delta_decode": ([_P, _P, _P, _I64, _P, _P, _I64, _I32, _P, _P, _I32, _P, _P, _I64, _P, _SZ, _P], _I32),
+    "ssm_gated_rmsnorm": ([_P, _I64, _I32, _I64, _I32, _I32, _P, _P, _I64, _P], _I32),
+    "ssm_block_rmsnorm": ([_P, _I32, _P, _I32, _I32, _P, _P, _P, ctypes.c_float, _P, _I32, _I64, _I32, _P], _I32),
     "ssm_timing_enable": ([_I32, ctypes.c_char_p], _I32),
     "ssm_timing_collect": ([_P, _I32, _P], _I32),
 }
@@ -385,7 +410,7 @@ class BoundCall:
 
 def bind(name: str, *args, **kw) -> BoundCall:
     """bind("ssm_shard_decode_stage1", desc, weights, x_t, ...) -> a callable issuing that call.
-    Available for the prefill, decode, reduce, layer and attention entry points."""
+    Available for the prefill, decode, reduce, layer, attention and delta-rule entry points."""
     a, keep = _MARSHAL[name](*args, **kw)
     tensors = tuple(v for v in list(args) + list(kw.values()) if isinstance(v, torch.Tensor))
     return BoundCall(name, a, keep + tensors)
@@ -911,3 +936,173 @@ def ssm_attn_prefill(ad, q, meta, pool, out, ws, stream=None):
 
 def ssm_attn_decode(ad, q, meta, pool, out, ws, stream=None):
     _call("ssm_attn_decode", ad, q, meta, pool, out, ws, stream)
+
+
+# ------------------------------------------------------------------ gated delta rule and its norms
+SSM_GATE = {"identity": 0, "sigmoid": 1, "silu": 2, "tanh": 3}
+
+
+def make_delta_desc(qk_heads: int, v_heads: int, qk_dim: int, v_dim: int, act: str = "bf16", qk_norm: bool = True,
+                    scale: Optional[float] = None, norm_eps: float = 1e-6, beta_max: float = 1.0) -> DeltaDesc:
+    d = DeltaDesc(qk_heads, v_heads, qk_dim, v_dim, SSM_BF16 if act == "bf16" else SSM_F32, 1 if qk_norm else 0,
+                  (qk_dim ** -0.5 if qk_dim > 0 else 1.0) if scale is None else scale, norm_eps, beta_max)
+    _check(lib().ssm_delta_check_desc(ctypes.byref(d)))
+    return d
+
+
+def delta_workspace_bytes(dd: DeltaDesc, max_tokens: int, max_seqs: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().ssm_delta_workspace_bytes(ctypes.byref(dd), max_tokens, max_seqs, ctypes.byref(n)))
+    return n.value
+
+
+def empty_delta_pool(dd: DeltaDesc, num_slots: int, device="cuda") -> torch.Tensor:
+    return torch.empty(num_slots, dd.v_heads, dd.v_dim, dd.qk_dim, dtype=torch.float32, device=device)
+
+
+def _rows(t: torch.Tensor, rows: int, width: int, dtype, what: str):
+    """(pointer, row stride) of a [rows][width] tensor with unit column stride."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.dtype != dtype:
+        raise ValueError(f"{what}: {dtype} [{rows}][{width}] expected, got {t.dtype} {tuple(t.shape)}")
+    if t.numel() and t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: unit column stride expected")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def _f32(t: torch.Tensor, shape, what: str):
+    if tuple(t.shape) != tuple(shape) or t.dtype != torch.float32:
+        raise ValueError(f"{what}: float32 {list(shape)} expected, got {t.dtype} {tuple(t.shape)}")
+
+
+class DeltaGates:
+    """A_log and dt_bias (float32 [v_heads]) of a gated delta layer."""
+
+    def __init__(self, dd: DeltaDesc, A_log: torch.Tensor, dt_bias: torch.Tensor):
+        self.A_log, self.dt_bias = A_log, dt_bias
+        self.check(dd)
+        self.c = DeltaGatesC(_ptr(A_log), _ptr(dt_bias))
+
+    def check(self, dd: DeltaDesc):
+        _f32(self.A_log, (dd.v_heads,), "A_log")
+        _f32(self.dt_bias, (dd.v_heads,), "dt_bias")
+
+    def tensors(self):
+        return self.A_log, self.dt_bias
+
+
+class GatedNorm:
+    """The norm of every head of `dim` values and its gate: weights w (float32 [dim], or [heads * dim]), gate columns z
+    ([rows][heads * dim] of the rows' type, None: no gate)."""
+
+    def __init__(self, w: torch.Tensor, z: Optional[torch.Tensor], heads: int, dim: int, eps: float = 1e-5, gate: str = "silu",
+                 gate_first: bool = False):
+        self.w, self.z, self.heads, self.dim = w, z, heads, dim
+        per_head = w.numel() != dim
+        _f32(w, (heads * dim if per_head else dim,), "norm weight")
+        p, ld = (None, 0) if z is None else _rows(z, z.shape[0], heads * dim, z.dtype, "z")
+        self.c = GatedNormC(_ptr(w), p, ld, float(eps), 1 if per_head else 0, SSM_GATE[gate], 1 if gate_first else 0)
+
+    def check(self, rows: int, heads: int, dim: int, dtype):
+        if (self.heads, self.dim) != (heads, dim):
+            raise ValueError(f"norm of {self.heads} heads of {self.dim} values, {heads} of {dim} expected")
+        if self.z is not None and (self.z.shape[0] != rows or self.z.dtype != dtype):
+            raise ValueError(f"z: {dtype} [{rows}] expected, got {self.z.dtype} {tuple(self.z.shape)}")
+
+    def tensors(self):
+        return self.w, self.z
+
+
+def _delta_operands(dd: DeltaDesc, gates: DeltaGates, qkv, a, b, rows: int, pool, out, ws):
+    act = torch.bfloat16 if dd.act_dtype == SSM_BF16 else torch.float32
+    gates.check(dd)
+    if pool.dim() != 4:
+        raise ValueError("ssm_pool: [slots][v_heads][v_dim][qk_dim] expected")
+    _f32(pool, (pool.shape[0], dd.v_heads, dd.v_dim, dd.qk_dim), "ssm_pool")
+    _same_device(qkv, a, b, pool, out, ws, *gates.tensors())
+    wide = dd.v_heads * dd.v_dim
+    q, ldq = _rows(qkv, rows, 2 * dd.qk_heads * dd.qk_dim + wide, act, "qkv")
+    pa, lda = _rows(a, rows, dd.v_heads, act, "a")
+    pb, ldb = _rows(b, rows, dd.v_heads, act, "b")
+    if rows > 1 and lda != ldb:
+        raise ValueError("a and b: the same row stride expected")
+    o, ldo = _rows(out, rows, wide, act, "out")
+    return (ctypes.byref(dd), ctypes.byref(gates.c), q, ldq, pa, pb, max(lda, ldb)), (o, ldo, _ptr(ws), ws.numel()), act
+
+
+def _m_ssm_delta_prefill(dd, gates: DeltaGates, qkv, a, b, meta: SeqMeta, ssm_pool, out, ws, stream=None):
+    head, tail, _ = _delta_operands(dd, gates, qkv, a, b, meta.T, ssm_pool, out, ws)
+    _same_device(meta.cu, meta.slot, meta.has_init)
+    return head + (meta.T, ctypes.byref(meta.c), _ptr(ssm_pool), ssm_pool.shape[0]) + tail + (_stream(stream),), (dd, gates, meta)
+
+
+def _m_ssm_delta_decode(dd, gates: DeltaGates, qkv, a, b, cache_slot, ssm_pool, out, ws, norm: Optional[GatedNorm] = None,
+                        stream=None):
+    n = qkv.shape[0]
+    head, tail, act = _delta_operands(dd, gates, qkv, a, b, n, ssm_pool, out, ws)
+    if tuple(cache_slot.shape) != (n,) or cache_slot.dtype != torch.int32:
+        raise ValueError(f"cache_slot: int32 [{n}] expected")
+    _same_device(cache_slot)
+    if norm is not None:
+        norm.check(n, dd.v_heads, dd.v_dim, act)
+        _same_device(*norm.tensors())
+    return head + (n, _ptr(cache_slot), _ptr(ssm_pool), ssm_pool.shape[0], ctypes.byref(norm.c) if norm is not None else None) + (
+        tail + (_stream(stream),)), (dd, gates, norm)
+
+
+def _m_ssm_gated_rmsnorm(x, norm: GatedNorm, out, stream=None):
+    rows, width = x.shape
+    norm.check(rows, norm.heads, norm.dim, x.dtype)
+    _same_device(x, out, *norm.tensors())
+    p, ld = _rows(x, rows, norm.heads * norm.dim, x.dtype, "x")
+    o, ldo = _rows(out, rows, norm.heads * norm.dim, x.dtype, "out")
+    return (p, ld, _dtype_of(x), rows, norm.heads, norm.dim, ctypes.byref(norm.c), o, ldo, _stream(stream)), (norm,)
+
+
+def _m_ssm_block_rmsnorm(base, parts, residual, norm_w, eps, normed, post_w=None, post_eps: Optional[float] = None, gate=None,
+                         gate_fn: str = "identity", scale: float = 1.0, stream=None):
+    """residual <- base + scale * gate_fn(gate) * y, y = sum(parts) (RMSNorm'ed with post_w); normed <- RMSNorm(residual)
+    * norm_w. base, every part, residual and normed are [T][d]; gate [T][d] (rows may be strided) or [1][d] for all."""
+    T, d = base.shape
+    pdt = _dtype_of(parts[0]) if parts else SSM_F32
+    arr = (ctypes.c_void_p * max(len(parts), 1))(*[_ptr(p).value for p in parts])
+    for p in parts:
+        if p.shape != base.shape or _dtype_of(p) != pdt:
+            raise ValueError("parts must match base's shape and share one dtype")
+    for t in (residual, normed):
+        if t.shape != base.shape:
+            raise ValueError(f"residual and normed: {list(base.shape)} expected, got {list(t.shape)}")
+    if residual.dtype != torch.float32:
+        raise ValueError("residual: float32 expected")
+    for w in (norm_w,) if post_w is None else (norm_w, post_w):
+        _f32(w, (d,), "norm weight")
+    _same_device(base, residual, norm_w, normed, post_w, gate, *parts)
+    g, ldg = (None, 0) if gate is None else _rows(gate, gate.shape[0], d, gate.dtype, "gate")
+    if gate is not None and gate.shape[0] != T and gate.shape[0] != 1:
+        raise ValueError(f"gate: [{T}][{d}] or [1][{d}] expected, got {list(gate.shape)}")
+    if gate is not None and gate.shape[0] == 1:
+        ldg = 0
+    block = BlockOutC(_ptr(post_w), g, ldg, float(eps if post_eps is None else post_eps), float(scale),
+                      SSM_F32 if gate is None else _dtype_of(gate), SSM_GATE[gate_fn])
+    return (_ptr(base), _dtype_of(base), arr, len(parts), pdt, ctypes.byref(block), _ptr(residual), _ptr(norm_w), float(eps),
+            _ptr(normed), _dtype_of(normed), T, d, _stream(stream)), (arr, block, list(parts))
+
+
+_MARSHAL.update({name[3:]: fn for name, fn in list(globals().items())
+                 if name.startswith(("_m_ssm_delta", "_m_ssm_gated", "_m_ssm_block"))})
+
+
+def ssm_delta_prefill(dd, gates, qkv, a, b, meta, ssm_pool, out, ws, stream=None):
+    _call("ssm_delta_prefill", dd, gates, qkv, a, b, meta, ssm_pool, out, ws, stream)
+
+
+def ssm_delta_decode(dd, gates, qkv, a, b, cache_slot, ssm_pool, out, ws, norm=None, stream=None):
+    _call("ssm_delta_decode", dd, gates, qkv, a, b, cache_slot, ssm_pool, out, ws, norm, stream)
+
+
+def ssm_gated_rmsnorm(x, norm, out, stream=None):
+    _call("ssm_gated_rmsnorm", x, norm, out, stream)
+
+
+def ssm_block_rmsnorm(base, parts, residual, norm_w, eps, normed, post_w=None, post_eps=None, gate=None, gate_fn="identity",
+                      scale=1.0, stream=None):
+    _call("ssm_block_rmsnorm", base, parts, residual, norm_w, eps, normed, post_w, post_eps, gate, gate_fn, scale, stream)

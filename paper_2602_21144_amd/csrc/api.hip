@@ -1695,3 +1695,211 @@ int ssm_attn_decode(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, const
 }
 
 }  // extern "C"
+
+// ================================================================ gated delta rule and its norms
+namespace {
+
+int64_t dtype_bytes(int32_t t) { return t == SSM_BF16 ? 2 : 4; }
+
+int check_delta_desc(const ssm_delta_desc_t* d) {
+    if (!d) return fail(SSM_E_INVAL, "desc is null");
+    SSM_TRY(check_dtype(d->act_dtype, "act"));
+    if (d->v_heads < 1 || d->v_heads > 128 || d->qk_heads < 1 || d->v_heads % d->qk_heads)
+        return fail(SSM_E_INVAL, "v_heads %d (1..128) must be a multiple of qk_heads %d", d->v_heads, d->qk_heads);
+    if (d->qk_dim < 16 || d->qk_dim > 256 || d->qk_dim % 16)
+        return fail(SSM_E_INVAL, "qk_dim %d must be a multiple of 16 up to 256", d->qk_dim);
+    if (d->v_dim < 16 || d->v_dim > 512 || d->v_dim % 16)
+        return fail(SSM_E_INVAL, "v_dim %d must be a multiple of 16 up to 512", d->v_dim);
+    if (d->qk_norm != 0 && d->qk_norm != 1) return fail(SSM_E_INVAL, "qk_norm %d", d->qk_norm);
+    if (!(d->scale > 0.0f) || !std::isfinite(d->scale)) return fail(SSM_E_INVAL, "scale must be finite and positive");
+    if (!(d->norm_eps > 0.0f) || !std::isfinite(d->norm_eps)) return fail(SSM_E_INVAL, "norm_eps must be finite and positive");
+    if (!(d->beta_max > 0.0f) || !(d->beta_max <= 2.0f)) return fail(SSM_E_INVAL, "beta_max must be in (0, 2]");
+    return SSM_OK;
+}
+
+int check_gated_norm(const ssm_gated_norm_t* n, int64_t width) {
+    SSM_TRY(check_ptr(n->w, "norm.w"));
+    if (!(n->eps > 0.0f) || !std::isfinite(n->eps)) return fail(SSM_E_INVAL, "norm.eps must be finite and positive");
+    if (n->per_head != 0 && n->per_head != 1) return fail(SSM_E_INVAL, "norm.per_head %d", n->per_head);
+    if (n->gate < SSM_GATE_IDENTITY || n->gate > SSM_GATE_TANH) return fail(SSM_E_INVAL, "norm.gate %d", n->gate);
+    if (n->gate_first != 0 && n->gate_first != 1) return fail(SSM_E_INVAL, "norm.gate_first %d", n->gate_first);
+    if (n->z) SSM_TRY(check_rows(n->z, n->ld_z, width, "norm.z"));
+    return SSM_OK;
+}
+
+GatedNormArgs norm_args(const ssm_gated_norm_t* n) {
+    GatedNormArgs a{};
+    if (!n) return a;
+    a.w = n->w; a.z = n->z; a.ld_z = n->ld_z; a.eps = n->eps;
+    a.per_head = n->per_head; a.gate = n->gate; a.gate_first = n->gate_first;
+    return a;
+}
+
+// Whether two ranges of memory share a byte.
+bool share(const void* a, __int128 na, const void* b, __int128 nb) {
+    const __int128 x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + nb && y < x + na;
+}
+
+// The operands that prompts and single tokens have in common; rows 0: nothing is looked at.
+int delta_args(const ssm_delta_desc_t* d, const ssm_delta_gates_t* g, const void* qkv, int64_t ld_qkv, const void* a,
+               const void* b, int64_t ld_ab, int64_t rows, float* pool, int32_t num_slots, void* out, int64_t ld_out,
+               DeltaArgs* o) {
+    if (!g) return fail(SSM_E_INVAL, "gates is null");
+    SSM_TRY(check_ptr(g->A_log, "gates.A_log"));
+    SSM_TRY(check_ptr(g->dt_bias, "gates.dt_bias"));
+    SSM_TRY(check_ptr(pool, "ssm_pool"));
+    if (num_slots < 1) return fail(SSM_E_INVAL, "num_slots %d", num_slots);
+    const int64_t size = dtype_bytes(d->act_dtype), wide = (int64_t)d->v_heads * d->v_dim, in = 2LL * d->qk_heads * d->qk_dim + wide;
+    if (rows > 0) {
+        SSM_TRY(check_rows(qkv, ld_qkv, in, "qkv"));
+        SSM_TRY(check_rows(out, ld_out, wide, "out"));
+        if (!a || !b) return fail(SSM_E_INVAL, "%s is null", a ? "b" : "a");
+        if (((uintptr_t)a | (uintptr_t)b) % size) return fail(SSM_E_ALIGN, "a or b is not aligned to its type");
+        if (ld_ab < d->v_heads) return fail(SSM_E_INVAL, "a, b: row stride %lld below %d heads", (long long)ld_ab, d->v_heads);
+        for (const void* ab : {a, b})
+            if (rows_share(ab, ld_ab, d->v_heads, out, ld_out, wide, rows, size)) return fail(SSM_E_INVAL, "out must not overlap a or b");
+        if (rows_share(qkv, ld_qkv, in, out, ld_out, wide, rows, size)) return fail(SSM_E_INVAL, "out must not overlap qkv");
+        const __int128 states = (__int128)num_slots * d->v_heads * d->v_dim * d->qk_dim * 4;
+        if (share(pool, states, out, ((__int128)(rows - 1) * ld_out + wide) * size) ||
+            share(pool, states, qkv, ((__int128)(rows - 1) * ld_qkv + in) * size))
+            return fail(SSM_E_INVAL, "ssm_pool overlaps qkv or out");
+    }
+    o->qkv = qkv; o->ld = ld_qkv; o->a = a; o->b = b; o->ld_ab = ld_ab; o->A_log = g->A_log; o->dt_bias = g->dt_bias;
+    o->pool = pool; o->S = num_slots; o->out = out; o->ld_out = ld_out; o->T = rows;
+    o->Hk = d->qk_heads; o->Hv = d->v_heads; o->dk = d->qk_dim; o->dv = d->v_dim; o->rep = d->v_heads / d->qk_heads;
+    o->qk_norm = d->qk_norm; o->scale = d->scale; o->eps = d->norm_eps; o->beta_max = d->beta_max;
+    return SSM_OK;
+}
+
+int check_delta_size(int64_t T, int32_t nseq) {
+    if (T < 0 || T > kMaxKvRows) return fail(SSM_E_INVAL, "token count %lld: 0 to 2^22", (long long)T);
+    if (nseq < 0 || nseq > kMaxKvSeqs) return fail(SSM_E_INVAL, "%d sequences: 0 to 2^15", nseq);
+    return SSM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ssm_delta_check_desc(const ssm_delta_desc_t* d) { return check_delta_desc(d); }
+
+int ssm_delta_workspace_bytes(const ssm_delta_desc_t* d, int64_t max_tokens, int32_t max_seqs, size_t* bytes) {
+    SSM_TRY(check_delta_desc(d));
+    SSM_TRY(check_delta_size(max_tokens, max_seqs));
+    if (!bytes) return fail(SSM_E_INVAL, "bytes is null");
+    *bytes = kWsHeader + delta_prefill_scratch_bytes(d->act_dtype == SSM_BF16, d->qk_heads, d->v_heads, d->qk_dim, d->v_dim,
+                                                     max_tokens, max_seqs);
+    return SSM_OK;
+}
+
+int ssm_delta_prefill(const ssm_delta_desc_t* d, const ssm_delta_gates_t* gates, const void* qkv, int64_t ld_qkv,
+                      const void* a, const void* b, int64_t ld_ab, int64_t T, const ssm_seq_meta_t* m, float* ssm_pool,
+                      int32_t num_slots, void* out, int64_t ld_out, void* ws, size_t ws_bytes, hipStream_t s) {
+    SSM_TRY(check_delta_desc(d));
+    SSM_TRY(check_meta(m, T));
+    SSM_TRY(check_delta_size(T, m->nseq));
+    const bool bf = d->act_dtype == SSM_BF16;
+    SSM_TRY(check_ws(ws, ws_bytes, kWsHeader + delta_prefill_scratch_bytes(bf, d->qk_heads, d->v_heads, d->qk_dim, d->v_dim, T, m->nseq)));
+    DeltaArgs p{};
+    SSM_TRY(delta_args(d, gates, qkv, ld_qkv, a, b, ld_ab, T, ssm_pool, num_slots, out, ld_out, &p));
+    p.cu = m->cu_seqlens; p.slot = m->cache_slot; p.has_init = m->has_initial_state; p.nseq = m->nseq;
+    p.status = (int32_t*)ws; p.scratch = (char*)ws + kWsHeader;
+    SSM_TRY_HIP(launch_delta_prefill(p, bf, s), "delta.prefill");
+    return SSM_OK;
+}
+
+int ssm_delta_decode(const ssm_delta_desc_t* d, const ssm_delta_gates_t* gates, const void* qkv, int64_t ld_qkv,
+                     const void* a, const void* b, int64_t ld_ab, int32_t batch, const int32_t* cache_slot, float* ssm_pool,
+                     int32_t num_slots, const ssm_gated_norm_t* norm, void* out, int64_t ld_out, void* ws, size_t ws_bytes,
+                     hipStream_t s) {
+    SSM_TRY(check_delta_desc(d));
+    SSM_TRY(check_delta_size(batch, batch));
+    SSM_TRY(check_ws(ws, ws_bytes, kWsHeader));
+    if (batch > 0 && !cache_slot) return fail(SSM_E_INVAL, "cache_slot is null");
+    DeltaArgs p{};
+    SSM_TRY(delta_args(d, gates, qkv, ld_qkv, a, b, ld_ab, batch, ssm_pool, num_slots, out, ld_out, &p));
+    const int64_t wide = (int64_t)d->v_heads * d->v_dim;
+    if (norm) SSM_TRY(check_gated_norm(norm, wide));
+    if (batch == 0) return SSM_OK;
+    if (norm && norm->z && rows_share(norm->z, norm->ld_z, wide, out, ld_out, wide, batch, dtype_bytes(d->act_dtype)))
+        return fail(SSM_E_INVAL, "out must not overlap norm.z");
+    p.slot = cache_slot; p.nseq = batch; p.status = (int32_t*)ws; p.norm = norm_args(norm);
+    SSM_TRY_HIP(launch_delta_decode(p, d->act_dtype == SSM_BF16, s), "delta.decode");
+    return SSM_OK;
+}
+
+int ssm_gated_rmsnorm(const void* x, int64_t ld_x, int32_t dtype, int64_t T, int32_t heads, int32_t dim,
+                      const ssm_gated_norm_t* norm, void* out, int64_t ld_out, hipStream_t s) {
+    SSM_TRY(check_dtype(dtype, "x"));
+    if (T < 0 || T > kMaxKvRows) return fail(SSM_E_INVAL, "rows %lld: 0 to 2^22", (long long)T);
+    if (heads < 1 || heads > 512) return fail(SSM_E_INVAL, "heads %d: 1 to 512", heads);
+    if (dim < 8 || dim % 8 || dim > gated_rmsnorm_max_dim())
+        return fail(SSM_E_INVAL, "dim %d: a multiple of 8 up to %d", dim, gated_rmsnorm_max_dim());
+    if (!norm) return fail(SSM_E_INVAL, "norm is null");
+    const int64_t width = (int64_t)heads * dim, size = dtype_bytes(dtype);
+    SSM_TRY(check_gated_norm(norm, width));
+    if (T == 0) return SSM_OK;
+    SSM_TRY(check_rows(x, ld_x, width, "x"));
+    SSM_TRY(check_rows(out, ld_out, width, "out"));
+    if (x == out && ld_x != ld_out) return fail(SSM_E_INVAL, "out in place of x needs the same row stride");
+    if ((x != out && rows_share(x, ld_x, width, out, ld_out, width, T, size)) ||
+        (norm->z && rows_share(norm->z, norm->ld_z, width, out, ld_out, width, T, size)))
+        return fail(SSM_E_INVAL, "out overlaps x without being it, or norm.z");
+    SSM_TIMED("layer.gated_rmsnorm", s, launch_gated_rmsnorm(x, ld_x, dtype == SSM_BF16, T, heads, dim, norm_args(norm), out, ld_out, s));
+    return SSM_OK;
+}
+
+int ssm_block_rmsnorm(const void* base, int32_t base_dtype, const void* const* parts, int32_t n_parts, int32_t parts_dtype,
+                      const ssm_block_out_t* block, float* residual, const float* norm_w, float eps, void* normed,
+                      int32_t normed_dtype, int64_t T, int32_t d, hipStream_t s) {
+    SSM_TRY(check_dtype(base_dtype, "base"));
+    SSM_TRY(check_dtype(parts_dtype, "parts"));
+    SSM_TRY(check_dtype(normed_dtype, "normed"));
+    SSM_TRY(check_norm_dim(d));
+    if (T < 0 || T > kMaxKvRows) return fail(SSM_E_INVAL, "rows %lld: 0 to 2^22", (long long)T);
+    if (n_parts < 0 || n_parts > kMaxNormParts) return fail(SSM_E_INVAL, "n_parts %d (0..%d)", n_parts, kMaxNormParts);
+    if (!(eps > 0.0f)) return fail(SSM_E_INVAL, "eps must be positive");
+    if (!block) return fail(SSM_E_INVAL, "block is null");
+    if (block->post_w && !(block->post_eps > 0.0f)) return fail(SSM_E_INVAL, "block.post_eps must be positive");
+    if (!std::isfinite(block->scale)) return fail(SSM_E_INVAL, "block.scale must be finite");
+    if (block->gate_fn < SSM_GATE_IDENTITY || block->gate_fn > SSM_GATE_TANH) return fail(SSM_E_INVAL, "block.gate_fn %d", block->gate_fn);
+    if (block->gate) SSM_TRY(check_dtype(block->gate_dtype, "block.gate"));
+    if (T == 0) return SSM_OK;
+    SSM_TRY(check_ptr(base, "base"));
+    SSM_TRY(check_ptr(residual, "residual"));
+    SSM_TRY(check_ptr(norm_w, "norm_w"));
+    SSM_TRY(check_ptr(normed, "normed"));
+    if (block->post_w) SSM_TRY(check_ptr(block->post_w, "block.post_w"));
+    if (n_parts > 0 && !parts) return fail(SSM_E_INVAL, "parts is null");
+    const __int128 n = (__int128)T * d;
+    const __int128 out_bytes = n * dtype_bytes(normed_dtype);
+    if (share(residual, n * 4, normed, out_bytes)) return fail(SSM_E_INVAL, "normed overlaps residual");
+    auto apart = [&](const void* p, __int128 bytes, const char* what) {
+        if (share(p, bytes, residual, n * 4) || share(p, bytes, normed, out_bytes))
+            return fail(SSM_E_INVAL, "%s overlaps residual or normed", what);
+        return SSM_OK;
+    };
+    if (base != residual || base_dtype != SSM_F32) SSM_TRY(apart(base, n * dtype_bytes(base_dtype), "base"));
+    BlockNormArgs a{};
+    a.parts.n = n_parts;
+    for (int k = 0; k < n_parts; ++k) {
+        SSM_TRY(check_ptr(parts[k], "parts[k]"));
+        SSM_TRY(apart(parts[k], n * dtype_bytes(parts_dtype), "parts[k]"));
+        a.parts.p[k] = parts[k];
+    }
+    if (block->gate) {
+        const int64_t ld = block->ld_gate;
+        if (ld != 0) SSM_TRY(check_rows(block->gate, ld, d, "block.gate"));
+        else SSM_TRY(check_ptr(block->gate, "block.gate"));
+        SSM_TRY(apart(block->gate, ((__int128)(T - 1) * ld + d) * dtype_bytes(block->gate_dtype), "block.gate"));
+    }
+    a.base = base; a.post_w = block->post_w; a.post_eps = block->post_eps; a.scale = block->scale;
+    a.gate = block->gate; a.ld_gate = block->ld_gate; a.gate_fn = block->gate_fn;
+    a.resid = residual; a.w = norm_w; a.eps = eps; a.out = normed; a.d = d;
+    SSM_TIMED("layer.block_rmsnorm", s, launch_block_rmsnorm(a, base_dtype == SSM_BF16, parts_dtype == SSM_BF16,
+                                                             block->gate && block->gate_dtype == SSM_BF16, normed_dtype == SSM_BF16, T, s));
+    return SSM_OK;
+}
+
+}  // extern "C"

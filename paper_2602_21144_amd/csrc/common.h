@@ -429,4 +429,40 @@ hipError_t launch_attn_decode(const AttnArgs& a, bool bf16_act, hipStream_t s);
 size_t attn_prefill_scratch_bytes(bool bf16_act, int Hq, int Hkv, int D, int64_t T, int nseq);
 hipError_t launch_attn_prefill(const AttnArgs& a, bool bf16_act, hipStream_t s);
 
+// ---------------------------------------------------------------- gated delta rule and its norms
+struct GatedNormArgs {
+    const float* w; const void* z; int64_t ld_z;   // w null: no norm (decode); z null: no gate
+    float eps;
+    int per_head, gate, gate_first;                // gate: SSM_GATE_*
+};
+struct DeltaArgs {
+    const void* qkv; int64_t ld;                   // [T][ld], columns [q heads | k heads | v heads]
+    const void* a; const void* b; int64_t ld_ab;   // [T][ld_ab], one column per value head
+    const float* A_log; const float* dt_bias;
+    float* pool; int S;                            // [S][Hv][dv][dk]
+    const int32_t* cu; const int32_t* slot; const int32_t* has_init;
+    int32_t* status;
+    void* out; int64_t ld_out;
+    int64_t T; int nseq;
+    int Hk, Hv, dk, dv, rep;                       // rep: value heads per query/key head
+    int qk_norm; float scale, eps, beta_max;
+    GatedNormArgs norm;                            // decode
+    char* scratch;                                 // prefill (delta_prefill_scratch_bytes)
+};
+size_t delta_prefill_scratch_bytes(bool bf16_act, int Hk, int Hv, int dk, int dv, int64_t T, int nseq);
+hipError_t launch_delta_prefill(const DeltaArgs& a, bool bf16_act, hipStream_t s);
+hipError_t launch_delta_decode(const DeltaArgs& a, bool bf16_act, hipStream_t s);   // nseq sequences
+int gated_rmsnorm_max_dim();
+hipError_t launch_gated_rmsnorm(const void* x, int64_t ld_x, bool bf16_act, int64_t T, int heads, int dim,
+                                const GatedNormArgs& n, void* out, int64_t ld_out, hipStream_t s);
+struct BlockNormArgs {
+    const void* base; NormParts parts;
+    const float* post_w; float post_eps, scale;
+    const void* gate; int64_t ld_gate; int gate_fn;
+    float* resid; const float* w; float eps; void* out;
+    int d;
+};
+hipError_t launch_block_rmsnorm(const BlockNormArgs& a, bool base_bf16, bool parts_bf16, bool gate_bf16, bool out_bf16,
+                                int64_t T, hipStream_t s);
+
 }  // namespace ssm
