@@ -1699,6 +1699,8 @@ int ssm_attn_decode(const ssm_attn_desc_t* d, const void* q, int64_t ld_q, const
 // ================================================================ gated delta rule and its norms
 namespace {
 
+constexpr int64_t kMaxDeltaStride = 1 << 22;
+
 int64_t dtype_bytes(int32_t t) { return t == SSM_BF16 ? 2 : 4; }
 
 int check_delta_desc(const ssm_delta_desc_t* d) {
@@ -1754,6 +1756,8 @@ int delta_args(const ssm_delta_desc_t* d, const ssm_delta_gates_t* g, const void
     if (rows > 0) {
         SSM_TRY(check_rows(qkv, ld_qkv, in, "qkv"));
         SSM_TRY(check_rows(out, ld_out, wide, "out"));
+        // 64 rows of a chunk are one buffer of 32-bit offsets
+        if (ld_qkv > kMaxDeltaStride) return fail(SSM_E_INVAL, "qkv: row stride %lld above 2^22", (long long)ld_qkv);
         if (!a || !b) return fail(SSM_E_INVAL, "%s is null", a ? "b" : "a");
         if (((uintptr_t)a | (uintptr_t)b) % size) return fail(SSM_E_ALIGN, "a or b is not aligned to its type");
         if (ld_ab < d->v_heads) return fail(SSM_E_INVAL, "a, b: row stride %lld below %d heads", (long long)ld_ab, d->v_heads);

@@ -91,31 +91,6 @@ template <int NJ> __device__ __forceinline__ void row_store(const f32x4 (&S)[NJ]
         if (32 * j + 4 * lane8 < dk) *(f32x4*)(row + 32 * j + 4 * lane8) = S[j];
 }
 
-// ---------------------------------------------------------------- prompts
-// One workgroup per (32 rows of a head's state, sequence), token by token.
-template <typename T, int NJ> __global__ __launch_bounds__(256) void delta_prefill_kernel(DeltaArgs p) {
-    const int blocks = (p.dv + 31) / 32, h = blockIdx.x / blocks, i = blockIdx.y;
-    const int r = (blockIdx.x % blocks) * 32 + (threadIdx.x >> 3), lane8 = threadIdx.x & 7;
-    const int lo = p.cu[i], hi = p.cu[i + 1], slot = p.slot[i];
-    const bool bad = lo < 0 || hi < lo || (int64_t)hi > p.T, ok = slot >= 0 && slot < p.S;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && (bad || !ok))
-        atomicOr(p.status, (bad ? SSM_STATUS_BAD_SEQLENS : 0) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
-    if (bad || r >= p.dv) return;   // whole groups of 8 lanes
-    float* row = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + r) * p.dk;
-    f32x4 S[NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) S[j] = f32x4{};
-    if (ok && p.has_init[i]) row_load(S, row, lane8, p.dk);
-    for (int64_t t = lo; t < hi; ++t) {
-        const T* x = (const T*)p.qkv + t * p.ld;
-        Token<T, NJ> tok;
-        tok.load(p, x, t, h, lane8);
-        const float o = row_step(S, tok, to_f32(x[2 * p.Hk * p.dk + h * p.dv + r]));
-        if (lane8 == 0) ((T*)p.out)[t * p.ld_out + h * p.dv + r] = from_f32<T>(o);
-    }
-    if (ok) row_store(S, row, lane8, p.dk);
-}
-
 // ---------------------------------------------------------------- single tokens
 // One workgroup per (head, sequence): 32 rows a pass, NP passes' rows in flight together.
 template <typename T, int NJ, int NP> __global__ __launch_bounds__(256) void delta_decode_kernel(DeltaArgs p) {
@@ -182,13 +157,6 @@ template <typename T, int NJ, int NP> __global__ __launch_bounds__(256) void del
         if (tid + 256 * e < p.dv) out[tid + 256 * e] = from_f32<T>(y[e]);
 }
 
-template <typename T> hipError_t prefill_launch(const DeltaArgs& p, hipStream_t s) {
-    const dim3 grid((unsigned)(p.Hv * ((p.dv + 31) / 32)), (unsigned)p.nseq);
-    if (p.dk <= 64) SSM_LAUNCH((delta_prefill_kernel<T, 2>), grid, dim3(256), 0, s, p);
-    else if (p.dk <= 128) SSM_LAUNCH((delta_prefill_kernel<T, 4>), grid, dim3(256), 0, s, p);
-    else SSM_LAUNCH((delta_prefill_kernel<T, 8>), grid, dim3(256), 0, s, p);
-    return hipGetLastError();
-}
 template <typename T> hipError_t decode_launch(const DeltaArgs& p, hipStream_t s) {
     const dim3 grid((unsigned)p.Hv, (unsigned)p.nseq);
     if (p.dk <= 64) SSM_LAUNCH((delta_decode_kernel<T, 2, 4>), grid, dim3(256), 0, s, p);
@@ -199,13 +167,6 @@ template <typename T> hipError_t decode_launch(const DeltaArgs& p, hipStream_t s
 
 }  // namespace
 
-size_t delta_prefill_scratch_bytes(bool, int, int, int, int, int64_t, int) { return 0; }
-
-hipError_t launch_delta_prefill(const DeltaArgs& p, bool bf16_act, hipStream_t s) {
-    if (p.nseq <= 0) return hipSuccess;
-    KernelTimer kt("delta.prefill", s);
-    return bf16_act ? prefill_launch<bf16>(p, s) : prefill_launch<float>(p, s);
-}
 hipError_t launch_delta_decode(const DeltaArgs& p, bool bf16_act, hipStream_t s) {
     if (p.nseq <= 0) return hipSuccess;
     KernelTimer kt("delta.decode", s);

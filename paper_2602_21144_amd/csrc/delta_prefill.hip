@@ -1,0 +1,681 @@
+// Prompts of the gated delta rule, in chunks of 64 tokens on the matrix cores. Per value head, with the state S
+// (dk x dv here), G the running sum of log alpha in the chunk and kappa k~ = the key's unit vector:
+//   A_ij = beta_i e^(Gi - Gj) k_i . k_j (j < i),  T = (I + A)^-1                         no state in it
+//   R = beta V - beta e^G (K S),  U = T R,  O = e^G (Q S) + (e^(Gi - Gj) q_i . k_j)_{j <= i} U
+//   S <- e^(G_C) S + K^T (e^(G_C - Gj) U)
+// Pass 1 (delta_chunk_kernel) has a workgroup per chunk and value head: T and the masked products of queries
+// and keys. Pass 2 (delta_main_kernel) walks a sequence's chunks with the state in accumulators: columns of S
+// need nothing of each other, so a wave owns 16 of them and talks to no other wave.
+//
+// Operands are f16, sums float32. A row of q or k is scaled by the power of two that takes its largest value to
+// 2^12, which holds bf16 values exactly (down to 2^-26 of the row's largest; smaller ones to 2^-37 of it); float32
+// ones are two f16 values, 22 bits. What is computed (S, R, U) is scaled by column in the same way and
+// split in two where it carries the state on; a product of two splits is three MFMAs, off by 2^-22. Where only an
+// output that will be rounded to bf16 depends on it, the first f16 value alone (2^-11) stands for S, U and the
+// products of queries and keys.
+#include <algorithm>
+
+#include "gate.h"
+
+namespace ssm {
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kC = 64;           // tokens per chunk
+constexpr int kFrags = 6;        // 16 x 32 pieces of a lower triangular 64 x 64 matrix
+constexpr size_t kScalBytes = 2048;   // beta, beta e^G kappa, kappa, kappa e^(G_C - G), c e^G, c 2^20, e^(G_C), each by token
+constexpr int kFindSeqs = 256;   // more sequences are laid out by a launch of its own
+
+// the parts of a stored q, k or product: float32 activations take two f16 values
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+
+// Piece (row tile it, k step s) of a lower triangle: rows 16 it .., columns 32 s ..
+__host__ __device__ constexpr int frag_of(int it, int s) { return it < 2 ? it : 2 * it - 2 + s; }
+// Operand layout of a 16 x 32 piece: lane l holds row l % 16 and, with hh = l / 16, columns 4 hh .. 4 hh + 3 and
+// 16 + 4 hh .. 16 + 4 hh + 3: the order in which two stacked accumulator tiles hold their rows. Pieces of q and k
+// have their rows rotated by 4 hh, so that the transposing reads of k meet every bank once.
+__device__ __forceinline__ int qk_unit(int row, int hh) { return 16 * hh + ((row + 4 * hh) & 15); }
+
+// Sizes of the workspace. Per chunk and q/k head: pieces of k, then of q; per chunk and value head: T (two parts), the
+// products of queries and keys, the tokens' factors.
+constexpr size_t qk_bytes(int NS, int parts) { return (size_t)4 * NS * parts * 1024; }   // k or q
+constexpr size_t v_bytes(int parts) { return (size_t)kFrags * (2 + parts) * 1024 + kScalBytes; }
+
+struct DeltaWs {
+    int32_t* base;     // [nseq] first chunk of every sequence
+    int32_t* count;    // chunks of the call (launch of its own)
+    int2* plan;        // [slots] sequence and chunk (launch of its own)
+    char* qk; char* v;
+    int slots;         // chunks there is room for
+};
+
+struct Args {
+    DeltaArgs d;
+    DeltaWs w;
+};
+
+struct SeqRows {
+    int lo, n;
+    bool ok;
+};
+__device__ __forceinline__ SeqRows seq_rows(const DeltaArgs& p, int i) {
+    const int lo = p.cu[i], hi = p.cu[i + 1];
+    const bool ok = lo >= 0 && hi >= lo && (int64_t)hi <= p.T;
+    return SeqRows{lo, ok ? hi - lo : 0, ok};
+}
+__device__ __forceinline__ int chunks_of(int rows) { return (rows + kC - 1) / kC; }
+
+// exclusive running sum of v over the 256 threads; total: the whole sum
+__device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
+    const int tid = threadIdx.x;
+    int c = v;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int o = __shfl_up(c, off, 64);
+        if ((tid & 63) >= off) c += o;
+    }
+    if ((tid & 63) == 63) lds[tid >> 6] = c;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < (tid >> 6)) before += lds[w];
+    }
+    *total = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    __syncthreads();
+    return before + c - v;
+}
+
+// Lays out the chunks of a call of more than 256 sequences
+__global__ __launch_bounds__(256) void delta_plan_kernel(Args a) {
+    __shared__ int lds[4];
+    int start = 0;
+    for (int i0 = 0; i0 < a.d.nseq; i0 += 256) {
+        const int i = i0 + threadIdx.x;
+        const int n = i < a.d.nseq ? chunks_of(seq_rows(a.d, i).n) : 0;
+        int total;
+        const int at = start + block_scan(n, lds, &total);
+        if (i < a.d.nseq) a.w.base[i] = at;
+        for (int k = 0; k < n && at + k < a.w.slots; ++k) a.w.plan[at + k] = make_int2(i, k);
+        start = min(start + total, 1 << 30);   // sequences that overlap may name any number of rows
+    }
+    if (threadIdx.x == 0) *a.w.count = min(start, a.w.slots);
+}
+
+__device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(127 + e) << 23); }
+// The exponent of m's scale: m pow2(scale_exp(m)) lies in [2^12, 2^13); 0 and what is too small or not finite get one
+// that keeps all factors finite
+__device__ __forceinline__ int scale_exp(float m) {
+    const int e = (int)((__builtin_bit_cast(uint32_t, m) >> 23) & 255u);
+    return 12 + 127 - min(max(e, 40), 230);
+}
+
+template <int N> __device__ __forceinline__ f16x8 pair_f16(const float (&v)[N], int at) {
+    f16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (_Float16)v[at + e];
+    return o;
+}
+
+__device__ __forceinline__ f32x4 mma(const f16x8& a, const f16x8& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma4(float a, float b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------- pass 1
+constexpr int kLdA = kC + 4;   // row stride of the 64 x 64 float32 matrix
+
+// This thread's 8-value pieces of a row of q or k: scaled to f16 parts in operand layout. Returns the sum of squares
+// of the row; e: the exponent of its scale.
+template <typename T, int NS>
+__device__ __forceinline__ float stage_row(const __amdgpu_buffer_rsrc_t& r, uint32_t off, int dk, int row, int c4, char* lds, int* e) {
+    float v[NS][8], ss = 0.0f, m = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int n = 32 * s + 8 * c4;
+        const uint32_t at = n < dk ? off + n * (uint32_t)sizeof(T) : kOffOutOfRange;
+        T x[8];
+        u32x4 raw[sizeof(T) / 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = buffer_load16(r, n < dk ? at + 16 * i : at);
+        __builtin_memcpy(x, raw, sizeof x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[s][k] = to_f32(x[k]);
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            ss = __builtin_fmaf(v[s][k], v[s][k], ss);
+            m = fmaxf(m, fabsf(v[s][k]));
+        }
+    ss += __shfl_xor(ss, 1, 64);
+    ss += __shfl_xor(ss, 2, 64);
+    m = fmaxf(m, __shfl_xor(m, 1, 64));
+    m = fmaxf(m, __shfl_xor(m, 2, 64));
+    *e = scale_exp(m);
+    const float f = pow2(*e);
+    const int it = row >> 4;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = v[s][k] * f;
+#pragma unroll
+        for (int part = 0; part < kParts<T>; ++part) {
+            const f16x8 h = pair_f16(x, 0);
+            // values 0..3 of the piece are (hh, half) = (2 (c4 & 1), c4 / 2), values 4..7 the next hh
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                f16x4 o;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[k] = h[4 * q + k];
+                char* unit = lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(row & 15, 2 * (c4 & 1) + q)) * 16 + (c4 >> 1) * 8;
+                *(f16x4*)unit = o;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] -= (float)h[k];
+        }
+    }
+    return ss;
+}
+
+template <int NS> __device__ __forceinline__ f16x8 qk_piece(const char* lds, int part, int it, int s, int lane) {
+    return *(const f16x8*)(lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(lane & 15, lane >> 4)) * 16);
+}
+
+template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk_kernel(Args a) {
+    constexpr int PA = kParts<T>;
+    __shared__ __attribute__((aligned(16))) char s_k[qk_bytes(NS, PA)], s_q[qk_bytes(NS, PA)];
+    __shared__ __attribute__((aligned(16))) float s_t[kC * kLdA];
+    __shared__ float s_gh[kC], s_gl[kC], s_beta[kC], s_kap[kC], s_c[kC];
+    __shared__ int s_find[8];
+    const DeltaArgs& p = a.d;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, slot = blockIdx.x, h = blockIdx.y;
+    int seq = -1, chunk = 0;
+    if (p.nseq <= kFindSeqs) {
+        int n = 0, total;
+        if (tid < p.nseq) {
+            const SeqRows r = seq_rows(p, tid);
+            n = chunks_of(r.n);
+            if (!r.ok && slot == 0 && h == 0) atomicOr(p.status, SSM_STATUS_BAD_SEQLENS);
+        }
+        if (tid == 0) s_find[4] = -1;
+        const int at = block_scan(n, s_find, &total);
+        if (slot == 0 && h == 0 && tid < p.nseq) a.w.base[tid] = at;
+        if (slot >= at && slot < at + n) {
+            s_find[4] = tid;
+            s_find[5] = slot - at;
+        }
+        __syncthreads();
+        seq = s_find[4];
+        chunk = s_find[5];
+    } else if (slot < *a.w.count) {
+        const int2 pl = a.w.plan[slot];
+        seq = pl.x;
+        chunk = pl.y;
+    }
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    chunk = __builtin_amdgcn_readfirstlane(chunk);
+    if (seq < 0) return;
+    const SeqRows sr = seq_rows(p, seq);
+    const int64_t t0 = (int64_t)__builtin_amdgcn_readfirstlane(sr.lo) + (int64_t)chunk * kC;
+    const int nq = min(__builtin_amdgcn_readfirstlane(sr.n) - chunk * kC, kC);
+    const int hk = h / p.rep;
+
+    // rows of q and k: four threads to a row
+    const __amdgpu_buffer_rsrc_t rx = buffer_rsrc((const T*)p.qkv + t0 * p.ld, (uint32_t)((nq - 1) * p.ld + 2 * p.Hk * p.dk) * sizeof(T));
+    const int row = tid >> 2, c4 = tid & 3;
+    const uint32_t off = row < nq ? (uint32_t)(row * p.ld + hk * p.dk) * (uint32_t)sizeof(T) : kOffOutOfRange;
+    float av = 0.0f, bv = 0.0f;
+    if (tid < nq) {
+        av = to_f32(((const T*)p.a)[(t0 + tid) * p.ld_ab + h]);
+        bv = to_f32(((const T*)p.b)[(t0 + tid) * p.ld_ab + h]);
+    }
+    int eq, ek;
+    const float sq = stage_row<T, NS>(rx, off, row < nq ? p.dk : 0, row, c4, s_q, &eq);
+    const float sk = stage_row<T, NS>(rx, off + (uint32_t)(p.Hk * p.dk) * (uint32_t)sizeof(T), row < nq ? p.dk : 0, row, c4, s_k, &ek);
+    if (c4 == 0) {
+        s_c[row] = p.scale * (p.qk_norm ? 1.0f / sqrtf(fmaxf(sq + p.eps, 1.2e-38f)) : 1.0f) * pow2(-eq);
+        s_kap[row] = (p.qk_norm ? 1.0f / sqrtf(fmaxf(sk + p.eps, 1.2e-38f)) : 1.0f) * pow2(-ek);
+    }
+    if (tid < kC) {
+        // log2 of alpha; below -1000 it is 0 in float32 either way, and the sums of what follows stay exact. The running
+        // sum in 64 bits, kept as two float32 values: what comes after a reset is as exact as without one
+        float g = -fast_exp2(p.A_log[h] * kLog2e) * kLog2e * softplus_f(av + p.dt_bias[h]);
+        g = tid < nq ? (g < -1000.0f ? -1000.0f : g) : 0.0f;
+        double c = (double)g;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const double up = __shfl_up(c, o, 64);
+            if (tid >= o) c += up;
+        }
+        s_gh[tid] = (float)c;
+        s_gl[tid] = (float)(c - (double)(float)c);
+        s_beta[tid] = tid < nq ? p.beta_max * sigmoid_f(bv) : 0.0f;
+    }
+    __syncthreads();
+
+    // wave w: columns i = 16 w + lane % 16 of K K^T and K Q^T, rows j = 16 jt + 4 hh + r
+    const int hh = lane >> 4, i = 16 * wave + (lane & 15);
+    char* vout = a.w.v + ((int64_t)slot * p.Hv + h) * v_bytes(PA);
+    {
+        const float gh = s_gh[i], gl = s_gl[i], bk = s_beta[i] * s_kap[i];
+        float pv[2][4];
+#pragma unroll
+        for (int jt = 0; jt < 4; ++jt) {
+            if (jt > wave && jt % 2 == 0) break;
+            f32x4 kk{}, kq{};
+            if (jt <= wave) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const f16x8 x = qk_piece<NS>(s_k, 0, jt, s, lane), y = qk_piece<NS>(s_k, 0, wave, s, lane),
+                                z = qk_piece<NS>(s_q, 0, wave, s, lane);
+                    kk = mma(x, y, kk);
+                    kq = mma(x, z, kq);
+                    if constexpr (PA == 2) {
+                        const f16x8 xl = qk_piece<NS>(s_k, 1, jt, s, lane);
+                        kk = mma(xl, y, kk);
+                        kq = mma(xl, z, kq);
+                        kk = mma(x, qk_piece<NS>(s_k, 1, wave, s, lane), kk);
+                        kq = mma(x, qk_piece<NS>(s_q, 1, wave, s, lane), kq);
+                    }
+                }
+            }
+            const int j0 = 16 * jt + 4 * hh;
+            const float4 jh = *(const float4*)&s_gh[j0], jl = *(const float4*)&s_gl[j0], jk = *(const float4*)&s_kap[j0];
+            const float jhv[4] = {jh.x, jh.y, jh.z, jh.w}, jlv[4] = {jl.x, jl.y, jl.z, jl.w}, jkv[4] = {jk.x, jk.y, jk.z, jk.w};
+            f32x4 av4;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float ex = fast_exp2((gh - jhv[r]) + (gl - jlv[r]));
+                av4[r] = j0 + r < i ? kk[r] * ex * (bk * jkv[r]) : 0.0f;
+                pv[jt & 1][r] = j0 + r <= i ? kq[r] * ex * pow2(-20) : 0.0f;
+            }
+            if (jt <= wave) *(f32x4*)&s_t[i * kLdA + j0] = av4;
+            if (jt & 1) {
+                float x[8] = {pv[0][0], pv[0][1], pv[0][2], pv[0][3], pv[1][0], pv[1][1], pv[1][2], pv[1][3]};
+#pragma unroll
+                for (int part = 0; part < PA; ++part) {
+                    const f16x8 o = pair_f16(x, 0);
+                    *(f16x8*)(vout + (size_t)((2 + part) * kFrags + frag_of(wave, jt >> 1)) * 1024 + lane * 16) = o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] -= (float)o[e];
+                }
+            }
+        }
+    }
+    // q and k for pass 2, once per q/k head
+    if (h % p.rep == 0) {
+        char* qk = a.w.qk + ((int64_t)slot * p.Hk + hk) * (2 * qk_bytes(NS, PA));
+        for (int u = tid; u < (int)qk_bytes(NS, PA) / 16; u += 256) {
+            *(u32x4*)(qk + u * 16) = *(const u32x4*)(s_k + u * 16);
+            *(u32x4*)(qk + qk_bytes(NS, PA) + u * 16) = *(const u32x4*)(s_q + u * 16);
+        }
+    }
+    // the tokens' factors
+    if (tid < kC) {
+        float* f = (float*)(vout + (size_t)kFrags * (2 + PA) * 1024);
+        const float gh = s_gh[tid], gl = s_gl[tid], ch = s_gh[kC - 1], cl = s_gl[kC - 1];
+        const float eg = fast_exp2(gh + gl), kap = s_kap[tid];
+        f[tid] = s_beta[tid];
+        f[kC + tid] = s_beta[tid] * eg * kap;
+        f[2 * kC + tid] = kap;
+        f[3 * kC + tid] = kap * fast_exp2((ch - gh) + (cl - gl));
+        f[4 * kC + tid] = s_c[tid] * eg;
+        f[5 * kC + tid] = s_c[tid] * pow2(20);
+        f[6 * kC + tid] = fast_exp2(ch + cl);
+    }
+    __syncthreads();
+
+    // T = (I + A)^-1 in place, in float32: the diagonal 16 x 16 blocks by substitution (lane: block and column), then
+    // [T1 0; -T2 A21 T1 T2] for blocks of 16 and of 32
+    if (wave == 0) {
+        const int b0 = 16 * hh, c = lane & 15;
+        float x[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float s = r == c ? 1.0f : 0.0f;
+#pragma unroll
+            for (int j4 = 0; j4 < 16; j4 += 4) {
+                if (j4 >= r) break;
+                const f32x4 m = *(const f32x4*)&s_t[(b0 + r) * kLdA + b0 + j4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j4 + e < r) s = __builtin_fmaf(-m[e], x[j4 + e], s);
+            }
+            x[r] = s;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s_t[(b0 + r) * kLdA + b0 + c] = x[r];
+    }
+    __syncthreads();
+    const int col = lane & 15;
+    // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column
+    auto row4 = [&](int r0, int c0) { return *(const f32x4*)&s_t[(r0 + col) * kLdA + c0 + 4 * hh]; };
+    auto times = [&](f32x4 m, const f32x4& x, f32x4 acc) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc = mma4(m[r], x[r], acc);
+        return acc;
+    };
+    auto col4 = [&](int r0, int c0) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = s_t[(r0 + 4 * hh + r) * kLdA + c0 + col];
+        return v;
+    };
+    auto put = [&](int r0, int c0, const f32x4& v) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s_t[(r0 + 4 * hh + r) * kLdA + c0 + col] = -v[r];
+    };
+    if (wave < 2) {
+        const int c0 = 32 * wave, r0 = c0 + 16;
+        const f32x4 x = times(row4(r0, c0), col4(c0, c0), f32x4{});
+        put(r0, c0, times(row4(r0, r0), x, f32x4{}));
+    }
+    __syncthreads();
+    {
+        const int r2 = wave >> 1, c0 = 16 * (wave & 1);
+        f32x4 x[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x[k] = f32x4{};
+            if ((wave & 1) == 0) x[k] = times(row4(32 + 16 * k, 0), col4(0, c0), x[k]);
+            x[k] = times(row4(32 + 16 * k, 16), col4(16, c0), x[k]);
+        }
+        f32x4 y = times(row4(32 + 16 * r2, 32), x[0], f32x4{});
+        if (r2 == 1) y = times(row4(48, 48), x[1], y);
+        __syncthreads();
+        put(32 + 16 * r2, c0, y);
+    }
+    __syncthreads();
+    for (int f = wave; f < kFrags; f += 4) {
+        const int it = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) & 1;
+        const f32x4 v0 = row4(16 * it, 32 * s);
+        const f32x4 v1 = 2 * s + 1 <= it ? row4(16 * it, 32 * s + 16) : f32x4{};
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = v0[e] * pow2(12);
+            x[4 + e] = v1[e] * pow2(12);
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const f16x8 o = pair_f16(x, 0);
+            *(f16x8*)(vout + (size_t)(part * kFrags + f) * 1024 + lane * 16) = o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] -= (float)o[e];
+        }
+    }
+}
+
+// ---------------------------------------------------------------- pass 2
+// Values of this lane's column: their largest magnitude over the column's four lanes
+__device__ __forceinline__ float column_max(float m) {
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    return fmaxf(m, __shfl_xor(m, 32, 64));
+}
+template <int N> __device__ __forceinline__ float largest(const f32x4 (&v)[N]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(v[t][r]));
+    return m;
+}
+// two stacked tiles, times f, as an operand of two parts
+__device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, float f, f16x8& hi, f16x8& lo) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float a = x0[r] * f, b = x1[r] * f;
+        hi[r] = (_Float16)a;
+        hi[4 + r] = (_Float16)b;
+        lo[r] = (_Float16)(a - (float)hi[r]);
+        lo[4 + r] = (_Float16)(b - (float)hi[4 + r]);
+    }
+}
+
+template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES) void delta_main_kernel(Args a) {
+    constexpr int PA = kParts<T>, NT = 2 * NS;
+    constexpr int kQk = (int)qk_bytes(NS, PA), kV = (int)v_bytes(PA);
+    __shared__ __attribute__((aligned(16))) char s_qk[2 * kQk], s_v[kV];
+    const DeltaArgs& p = a.d;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, hh = lane >> 4;
+    const int blocks = (p.dv + 16 * WAVES - 1) / (16 * WAVES), h = blockIdx.x / blocks, seq = blockIdx.y, hk = h / p.rep;
+    const int c0 = ((int)(blockIdx.x % blocks) * WAVES + wave) * 16;     // this wave's columns
+    const bool on = c0 < p.dv;
+    const SeqRows sr = seq_rows(p, seq);
+    const int slot = p.slot[seq], n = chunks_of(sr.n), base = sr.n > 0 ? a.w.base[seq] : 0;
+    const bool fits = sr.ok && base + n <= a.w.slots, ok = slot >= 0 && slot < p.S;
+    if (blockIdx.x == 0 && tid == 0 && (!fits || !ok))
+        atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
+    if (!fits) return;
+    float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
+    f32x4 S[NT];
+    const bool carry = ok && p.has_init[seq];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        S[t] = f32x4{};
+        if (carry && on && 16 * t < p.dk) S[t] = *(const f32x4*)(state + 16 * t);
+    }
+    float unit = 1.0f;                                 // S times this power of two is the state
+    for (int c = 0; c < n; ++c) {
+        const char* qk = a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk);
+        const char* vs = a.w.v + ((int64_t)(base + c) * p.Hv + h) * kV;
+        __syncthreads();
+        for (int u = tid; u < 2 * kQk / 16; u += 64 * WAVES) *(u32x4*)(s_qk + u * 16) = *(const u32x4*)(qk + u * 16);
+        for (int u = tid; u < kV / 16; u += 64 * WAVES) *(u32x4*)(s_v + u * 16) = *(const u32x4*)(vs + u * 16);
+        const int64_t t0 = (int64_t)sr.lo + (int64_t)c * kC;
+        const int nq = min(sr.n - c * kC, kC);
+        // V of this lane's column, tokens 16 it + 4 hh + r
+        float v[4][4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * it + 4 * hh + r;
+                v[it][r] = on && t < nq ? to_f32(((const T*)p.qkv)[(t0 + t) * p.ld + 2 * p.Hk * p.dk + h * p.dv + c0 + (lane & 15)]) : 0.0f;
+            }
+        __syncthreads();
+        if (!on) continue;
+        const float* fac = (const float*)(s_v + kFrags * (2 + PA) * 1024);
+        auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
+        auto tri = [&](int part, int it, int s) { return *(const f16x8*)(s_v + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16); };
+
+        // K S
+        f16x8 Sh[NS], Sl[NS];
+        const float ms = column_max(largest(S));
+        const int es = scale_exp(ms);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) split2(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
+        const float fs = unit * pow2(-es);
+        f32x4 R[4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            R[it] = f32x4{};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const f16x8 k = qk_piece<NS>(s_qk, 0, it, s, lane);
+                R[it] = mma(k, Sh[s], R[it]);
+                R[it] = mma(k, Sl[s], R[it]);
+                if constexpr (PA == 2) R[it] = mma(qk_piece<NS>(s_qk, 1, it, s, lane), Sh[s], R[it]);
+            }
+            const f32x4 be = tok4(0, it), bk = tok4(1, it);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) R[it][r] = be[r] * v[it][r] - bk[r] * (R[it][r] * fs);
+        }
+        // U = T R
+        const int er = scale_exp(column_max(largest(R)));
+        f16x8 Rh[2], Rl[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) split2(R[2 * s], R[2 * s + 1], pow2(er), Rh[s], Rl[s]);
+        f32x4 U[4], W[4];
+        const float fr = pow2(-er) * pow2(-12);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            f32x4 x{};
+#pragma unroll
+            for (int s = 0; s <= it / 2; ++s) {
+                const f16x8 th = tri(0, it, s), tl = tri(1, it, s);
+                x = mma(th, Rh[s], x);
+                x = mma(th, Rl[s], x);
+                x = mma(tl, Rh[s], x);
+            }
+            const f32x4 ka = tok4(2, it), kw = tok4(3, it);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float u = x[r] * fr;
+                U[it][r] = u * ka[r];
+                W[it][r] = u * kw[r];
+            }
+        }
+        // O = Q S + P U
+        {
+            const int eu = scale_exp(column_max(largest(U)));
+            f16x8 Uh[2], Ul[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) split2(U[2 * s], U[2 * s + 1], pow2(eu), Uh[s], Ul[s]);
+            T* out = (T*)p.out + t0 * p.ld_out + h * p.dv + c0 + (lane & 15);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                f32x4 x{}, y{};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const f16x8 q = qk_piece<NS>(s_qk + kQk, 0, it, s, lane);
+                    x = mma(q, Sh[s], x);
+                    if constexpr (PA == 2) {
+                        x = mma(q, Sl[s], x);
+                        x = mma(qk_piece<NS>(s_qk + kQk, 1, it, s, lane), Sh[s], x);
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s <= it / 2; ++s) {
+                    const f16x8 q = tri(2, it, s);
+                    y = mma(q, Uh[s], y);
+                    if constexpr (PA == 2) {
+                        y = mma(q, Ul[s], y);
+                        y = mma(tri(3, it, s), Uh[s], y);
+                    }
+                }
+                const f32x4 ce = tok4(4, it), cc = tok4(5, it);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int t = 16 * it + 4 * hh + r;
+                    if (t < nq) out[t * p.ld_out] = from_f32<T>(ce[r] * (x[r] * fs) + cc[r] * (y[r] * pow2(-eu)));
+                }
+            }
+        }
+        // S <- decay S + K^T W, in the units of W's scale; a state far above W keeps the scale in range
+        const float decay = fac[6 * kC];
+        const float mw = column_max(largest(W));
+        const int ew = scale_exp(fmaxf(mw, ms * unit * decay * pow2(-10)));
+        f16x8 Wh[2], Wl[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) split2(W[2 * s], W[2 * s + 1], pow2(ew), Wh[s], Wl[s]);
+        const float keep = decay * unit * pow2(ew);
+        unit = pow2(-ew);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] *= keep;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of 16
+                // values of k, transposed as they are read
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+                for (int part = 0; part < PA; ++part) {
+                    s16x4 k2[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const char* at = s_qk + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 +
+                                                 qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
+                        k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+                    }
+                    const f16x8 k = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    S[t] = mma(k, Wh[s], S[t]);
+                    if (part == 0) S[t] = mma(k, Wl[s], S[t]);
+                }
+            }
+        }
+    }
+    if (ok && on) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (16 * t >= p.dk) break;
+            f32x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = S[t][r] * unit;
+            *(f32x4*)(state + 16 * t) = o;
+        }
+    }
+}
+
+// k steps of 32 that the kernels are built for
+int steps_of(int dk) {
+    const int n = (dk + 31) / 32;
+    return n <= 2 ? 2 : n <= 4 ? n : n <= 6 ? 6 : 8;
+}
+
+DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, int nseq, size_t* total) {
+    DeltaWs w{};
+    const int parts = bf16_act ? 1 : 2;
+    w.slots = (int)(T / kC) + nseq;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { char* q = scratch ? scratch + off : nullptr; off += align256(bytes); return q; };
+    w.base = (int32_t*)take((size_t)nseq * 4);
+    w.count = (int32_t*)take(4);
+    w.plan = (int2*)take((size_t)w.slots * 8);
+    w.qk = take((size_t)w.slots * Hk * 2 * qk_bytes(steps_of(dk), parts));
+    w.v = take((size_t)w.slots * Hv * v_bytes(parts));
+    *total = off;
+    return w;
+}
+
+template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream_t s) {
+    constexpr int WAVES = 4;
+    const DeltaArgs& p = a.d;
+    if (p.nseq > kFindSeqs) {
+        KernelTimer kt("delta.plan", s);
+        SSM_LAUNCH(delta_plan_kernel, dim3(1), dim3(256), 0, s, a);
+    }
+    {
+        KernelTimer kt("delta.chunk", s);
+        SSM_LAUNCH((delta_chunk_kernel<T, NS>), dim3((unsigned)a.w.slots, (unsigned)p.Hv), dim3(256), 0, s, a);
+    }
+    const unsigned blocks = (unsigned)((p.dv + 16 * WAVES - 1) / (16 * WAVES));
+    KernelTimer kt("delta.main", s);
+    SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), dim3(p.Hv * blocks, (unsigned)p.nseq), dim3(64 * WAVES), 0, s, a);
+    return hipGetLastError();
+}
+template <typename T> hipError_t prefill_steps(const Args& a, hipStream_t s) {
+    switch (steps_of(a.d.dk)) {
+        case 2: return prefill_launch<T, 2>(a, s);
+        case 3: return prefill_launch<T, 3>(a, s);
+        case 4: return prefill_launch<T, 4>(a, s);
+        case 6: return prefill_launch<T, 6>(a, s);
+        default: return prefill_launch<T, 8>(a, s);
+    }
+}
+
+}  // namespace
+
+size_t delta_prefill_scratch_bytes(bool bf16_act, int Hk, int Hv, int dk, int, int64_t T, int nseq) {
+    size_t total;
+    layout(nullptr, bf16_act, Hk, Hv, dk, T, nseq, &total);
+    return total;
+}
+
+hipError_t launch_delta_prefill(const DeltaArgs& p, bool bf16_act, hipStream_t s) {
+    if (p.nseq <= 0) return hipSuccess;
+    size_t total;
+    const Args a{p, layout(p.scratch, bf16_act, p.Hk, p.Hv, p.dk, p.T, p.nseq, &total)};
+    return bf16_act ? prefill_steps<bf16>(a, s) : prefill_steps<float>(a, s);
+}
+
+}  // namespace ssm

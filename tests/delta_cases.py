@@ -69,12 +69,13 @@ def f64(t):
 
 def out_bound(want, sizes, act):
     """Outputs: one rounding of the value (half a step: 2^-8 of it in bf16, 2^-24 in float32), and in front of it what
-    the sums leave. bf16 prompts round the state (2^-8) and the products of queries and keys (2^-8) to bf16 as operands,
-    all relative to `sizes`; the rest, float32 sums and what stands for float32 operands, stays below a quarter of a
-    2^-8. In float32 nothing is rounded below 2^-23 a product; sums of up to 256 values, and as many steps of the
-    recurrence as a test has between two resets of its errors by the decay, leave some tens of 2^-24: 128 of them."""
+    the sums leave. Prompts of bf16 round the state, or a token's update and the product of its key with the query, to
+    f16 as operands: at most two roundings of 2^-11, relative to `sizes`, which is 2^-10, a quarter of 2^-8; the rest,
+    float32 sums and operands of 22 bits, stays below a twentieth of 2^-8. In float32 operands have 22 bits (a product is
+    off by 2^-21 at most), sums up to 256 values, and the errors of as many steps of the recurrence as a test has between
+    two resets by the decay add up: 128 times 2^-24."""
     half = 2.0 ** -8 if act == "bf16" else 2.0 ** -24
-    return half * np.abs(want) + (2.25 * half if act == "bf16" else 128 * half) * sizes + 1e-30
+    return half * np.abs(want) + (0.3 * half if act == "bf16" else 128 * half) * sizes + 1e-30
 
 
 def state_bound(want, act):

@@ -133,7 +133,7 @@ def _call(kind="prefill", desc=None, rows=100, **kw):
     return _rc("ssm_delta_decode", *head, rows, o["slot"], o["pool"], o["slots"], norm, *tail)
 
 
-BAD = [(dict(qkv=None), -1), (dict(qkv=16 * M + 8), -2), (dict(ld_qkv=508), -1), (dict(ld_qkv=516), -2), (dict(a=None), -1),
+BAD = [(dict(qkv=None), -1), (dict(qkv=16 * M + 8), -2), (dict(ld_qkv=508), -1), (dict(ld_qkv=(1 << 22) + 8), -1), (dict(ld_qkv=516), -2), (dict(a=None), -1),
        (dict(b=None), -1), (dict(a=32 * M + 1), -2), (dict(ld_ab=3), -1), (dict(pool=None), -1), (dict(pool=64 * M + 4), -2),
        (dict(slots=0), -1), (dict(out=None), -1), (dict(out=48 * M + 2), -2), (dict(ld_out=248), -1), (dict(ld_out=260), -2),
        (dict(ws=None), -1), (dict(ws=128 * M + 8), -2), (dict(ws_bytes=255), -3), (dict(A_log=None), -1), (dict(dt_bias=M + 4), -2),
@@ -172,7 +172,7 @@ def test_call_refusals_of_each_kind():
 def test_prefill_workspace_refusal():
     d = _desc()
     need = B.delta_workspace_bytes(d, 100, 2)
-    assert need == 256 or _call(desc=d, ws_bytes=need - 1) == B.SSM_E_WORKSPACE
+    assert _call(desc=d, ws_bytes=need - 1) == B.SSM_E_WORKSPACE
 
 
 def _gated(x=M * 16, ld_x=256, dtype=1, T=10, heads=4, dim=64, norm=(M, M * 32, 256, 1e-5, 0, 2, 0), out=M * 48, ld_out=256):
