@@ -578,7 +578,7 @@ int ssm_delta_check_desc(const ssm_delta_desc_t* desc);
 int ssm_delta_workspace_bytes(const ssm_delta_desc_t* desc, int64_t max_tokens, int32_t max_seqs, size_t* bytes);
 /* Packed prompts: qkv [T][ld_qkv] act, columns [q heads | k heads | v heads]; a and b [T][ld_ab] act, v_heads
  * columns each (any stride of at least v_heads, aligned to their type: columns of the projection); out [T][ld_out]
- * act, columns [v heads]. ld_qkv and ld_out are multiples of 8, ld_qkv at most 2^22. Metadata as for ssm_shard_prefill; the state of
+ * act, columns [v heads]. ld_qkv and ld_out are multiples of 8, at most 2^22. Metadata as for ssm_shard_prefill; the state of
  * every sequence's slot is written (zeros for an empty fresh one). A slot outside the pool starts its sequence
  * from zeros and stores nothing; packed rows behind the last sequence are left as they were. out shares nothing
  * with the inputs. */

@@ -1757,7 +1757,8 @@ int delta_args(const ssm_delta_desc_t* d, const ssm_delta_gates_t* g, const void
         SSM_TRY(check_rows(qkv, ld_qkv, in, "qkv"));
         SSM_TRY(check_rows(out, ld_out, wide, "out"));
         // 64 rows of a chunk are one buffer of 32-bit offsets
-        if (ld_qkv > kMaxDeltaStride) return fail(SSM_E_INVAL, "qkv: row stride %lld above 2^22", (long long)ld_qkv);
+        if (ld_qkv > kMaxDeltaStride || ld_out > kMaxDeltaStride)
+            return fail(SSM_E_INVAL, "qkv, out: row strides %lld, %lld above 2^22", (long long)ld_qkv, (long long)ld_out);
         if (!a || !b) return fail(SSM_E_INVAL, "%s is null", a ? "b" : "a");
         if (((uintptr_t)a | (uintptr_t)b) % size) return fail(SSM_E_ALIGN, "a or b is not aligned to its type");
         if (ld_ab < d->v_heads) return fail(SSM_E_INVAL, "a, b: row stride %lld below %d heads", (long long)ld_ab, d->v_heads);

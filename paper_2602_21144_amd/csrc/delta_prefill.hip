@@ -416,8 +416,11 @@ template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk
 // ---------------------------------------------------------------- pass 2
 // Values of this lane's column: their largest magnitude over the column's four lanes
 __device__ __forceinline__ float column_max(float m) {
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    return fmaxf(m, __shfl_xor(m, 32, 64));
+    const uint32_t v = __builtin_bit_cast(uint32_t, m);
+    const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    const uint32_t w = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])));
+    const auto y = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1]));
 }
 template <int N> __device__ __forceinline__ float largest(const f32x4 (&v)[N]) {
     float m = 0.0f;
@@ -427,33 +430,114 @@ template <int N> __device__ __forceinline__ float largest(const f32x4 (&v)[N]) {
         for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(v[t][r]));
     return m;
 }
-// two stacked tiles, times f, as an operand of two parts
-__device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, float f, f16x8& hi, f16x8& lo) {
+// two stacked tiles, times f (a power of two), as an operand: its first f16 values, and what they leave
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <bool LO> __device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, float f, f16x8& hi, f16x8& lo) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float a = x0[r] * f, b = x1[r] * f;
-        hi[r] = (_Float16)a;
-        hi[4 + r] = (_Float16)b;
-        lo[r] = (_Float16)(a - (float)hi[r]);
-        lo[4 + r] = (_Float16)(b - (float)hi[4 + r]);
+    for (int r = 0; r < 8; r += 2) {
+        const float a = r < 4 ? x0[r] : x1[r - 4], b = r < 4 ? x0[r + 1] : x1[r - 3];
+        const f16x2 h = __builtin_convertvector((f32x2){a * f, b * f}, f16x2);
+        hi[r] = h[0];
+        hi[r + 1] = h[1];
+        if constexpr (LO) {
+            const f16x2 l = __builtin_convertvector((f32x2){__builtin_fmaf(a, f, -(float)h[0]), __builtin_fmaf(b, f, -(float)h[1])}, f16x2);
+            lo[r] = l[0];
+            lo[r + 1] = l[1];
+        }
     }
 }
 
+// What pass 2 holds in LDS: two stages of a chunk's k, masked products and factors, and of its q where they fit
+// (kQStages 2); else one of q (1); else a single stage of everything, waited for in full (0).
+constexpr size_t kLds = 160 * 1024;
+template <typename T, int NS> struct MainLds {
+    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kV = (int)v_bytes(kParts<T>);
+    static constexpr int kQStages = 2 * (2 * kQk + kV) <= (int)kLds ? 2 : 2 * (kQk + kV) + kQk <= (int)kLds ? 1 : 0;
+    static constexpr int kStages = kQStages > 0 ? 2 : 1;
+    static constexpr int kBytes = kStages * (kQk + kV) + (kQStages == 2 ? 2 : 1) * kQk;
+    static_assert(kBytes <= (int)kLds, "pass 2 does not fit into LDS");
+};
+
+// `bytes` (a multiple of 1 KB) from a buffer to LDS, dealt out over the workgroup's waves
+template <int WAVES, int BYTES> __device__ __forceinline__ void dma_pieces(const __amdgpu_buffer_rsrc_t& r, uint32_t from, uint32_t lds, int wave, int lane) {
+    constexpr int N = BYTES / 1024;
+#pragma unroll
+    for (int i = 0; i < (N + WAVES - 1) / WAVES; ++i) {
+        const int j = wave + WAVES * i;
+        if (N % WAVES == 0 || j < N)
+            dma16(r, (uint32_t)lane * 16, from + (uint32_t)j * 1024, __builtin_amdgcn_readfirstlane(lds + (uint32_t)j * 1024));
+    }
+}
+
+// One value of a row of T, zero (and nothing stored) behind the buffer's end
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+    typedef uint32_t type;
+    static __device__ __forceinline__ type load(const __amdgpu_buffer_rsrc_t& r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0); }
+    static __device__ __forceinline__ void store(const __amdgpu_buffer_rsrc_t& r, uint32_t off, float v) {
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, (int)off, 0, 0);
+    }
+    static __device__ __forceinline__ float value(type v) { return __builtin_bit_cast(float, v); }
+};
+template <> struct Raw<bf16> {
+    typedef uint16_t type;
+    static __device__ __forceinline__ type load(const __amdgpu_buffer_rsrc_t& r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b16(r, (int)off, 0, 0); }
+    static __device__ __forceinline__ void store(const __amdgpu_buffer_rsrc_t& r, uint32_t off, float v) {
+        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (bf16)v), r, (int)off, 0, 0);
+    }
+    static __device__ __forceinline__ float value(type v) { return (float)__builtin_bit_cast(bf16, v); }
+};
+
+// While a chunk is computed the next one's pieces and values are on their way, and the stores of its outputs stay out
+// at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'.
 template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES) void delta_main_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
-    constexpr int kQk = (int)qk_bytes(NS, PA), kV = (int)v_bytes(PA);
-    __shared__ __attribute__((aligned(16))) char s_qk[2 * kQk], s_v[kV];
+    using L = MainLds<T, NS>;
+    constexpr int kQk = L::kQk, kV = L::kV;
+    constexpr uint32_t sz = sizeof(T);
+    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
     const DeltaArgs& p = a.d;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, hh = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int blocks = (p.dv + 16 * WAVES - 1) / (16 * WAVES), h = blockIdx.x / blocks, seq = blockIdx.y, hk = h / p.rep;
     const int c0 = ((int)(blockIdx.x % blocks) * WAVES + wave) * 16;     // this wave's columns
     const bool on = c0 < p.dv;
     const SeqRows sr = seq_rows(p, seq);
-    const int slot = p.slot[seq], n = chunks_of(sr.n), base = sr.n > 0 ? a.w.base[seq] : 0;
+    const int lo = __builtin_amdgcn_readfirstlane(sr.lo), rows = __builtin_amdgcn_readfirstlane(sr.n);
+    const int slot = p.slot[seq], n = chunks_of(rows), base = rows > 0 ? __builtin_amdgcn_readfirstlane(a.w.base[seq]) : 0;
     const bool fits = sr.ok && base + n <= a.w.slots, ok = slot >= 0 && slot < p.S;
     if (blockIdx.x == 0 && tid == 0 && (!fits || !ok))
         atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
     if (!fits) return;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
+    // places of a stage: k and the masked products by stage, q behind them
+    auto k_at = [&](int c) { return (L::kStages == 2 ? (c & 1) : 0) * (kQk + kV); };
+    auto q_at = [&](int c) { return L::kStages * (kQk + kV) + (L::kQStages == 2 ? (c & 1) : 0) * kQk; };
+    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
+    auto bring = [&](int c) {
+        dma_pieces<WAVES, kQk>(qk_buf(c), 0, lds0 + k_at(c), wave, lane);
+        dma_pieces<WAVES, kV>(buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * kV, kV), 0, lds0 + k_at(c) + kQk, wave, lane);
+    };
+    auto bring_q = [&](int c) { dma_pieces<WAVES, kQk>(qk_buf(c), kQk, lds0 + q_at(c), wave, lane); };
+    // V of this lane's column, tokens 16 it + 4 hh + r
+    typename Raw<T>::type raw[4][4];
+    const uint32_t ldv = (uint32_t)p.ld * sz, ldo = (uint32_t)p.ld_out * sz;
+    const uint32_t v0 = on ? (uint32_t)(4 * hh) * ldv + (uint32_t)(c0 + (lane & 15)) * sz : kOffOutOfRange;
+    const uint32_t o0 = (uint32_t)(4 * hh) * ldo + (uint32_t)(c0 + (lane & 15)) * sz;
+    auto bring_v = [&](int c) {
+        const int nq = min(rows - c * kC, kC);
+        const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
+                                                     (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[it][k] = Raw<T>::load(r, v0 + (uint32_t)(16 * it + k) * ldv);
+    };
+    if (n > 0) {
+        bring(0);
+        bring_q(0);
+        bring_v(0);
+    }
     float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
     f32x4 S[NT];
     const bool carry = ok && p.has_init[seq];
@@ -464,94 +548,142 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
     }
     float unit = 1.0f;                                 // S times this power of two is the state
     for (int c = 0; c < n; ++c) {
-        const char* qk = a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk);
-        const char* vs = a.w.v + ((int64_t)(base + c) * p.Hv + h) * kV;
-        __syncthreads();
-        for (int u = tid; u < 2 * kQk / 16; u += 64 * WAVES) *(u32x4*)(s_qk + u * 16) = *(const u32x4*)(qk + u * 16);
-        for (int u = tid; u < kV / 16; u += 64 * WAVES) *(u32x4*)(s_v + u * 16) = *(const u32x4*)(vs + u * 16);
-        const int64_t t0 = (int64_t)sr.lo + (int64_t)c * kC;
-        const int nq = min(sr.n - c * kC, kC);
-        // V of this lane's column, tokens 16 it + 4 hh + r
+        // the outputs' 16 stores are the youngest where everything of this chunk was asked for in front of them
+        if (L::kQStages == 2 && on && c > 0) wait_vm<16>();
+        else wait_vm<0>();
+        wait_lgkm0();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
         float v[4][4];
 #pragma unroll
         for (int it = 0; it < 4; ++it)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 16 * it + 4 * hh + r;
-                v[it][r] = on && t < nq ? to_f32(((const T*)p.qkv)[(t0 + t) * p.ld + 2 * p.Hk * p.dk + h * p.dv + c0 + (lane & 15)]) : 0.0f;
+            for (int k = 0; k < 4; ++k) {
+                v[it][k] = Raw<T>::value(raw[it][k]);
+                asm volatile("" : "+v"(v[it][k]));     // taken here, in front of the loads for the next chunk
             }
-        __syncthreads();
-        if (!on) continue;
-        const float* fac = (const float*)(s_v + kFrags * (2 + PA) * 1024);
-        auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
-        auto tri = [&](int part, int it, int s) { return *(const f16x8*)(s_v + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16); };
+        if (L::kStages == 2 && c + 1 < n) {
+            bring(c + 1);
+            if (L::kQStages == 2) bring_q(c + 1);
+            bring_v(c + 1);
+        }
+        const char* s_k = lds + k_at(c);
+        const char* s_v = s_k + kQk;
+        const char* s_q = lds + q_at(c);
+        if (on) {
+            const int nq = min(rows - c * kC, kC);
+            const float* fac = (const float*)(s_v + kFrags * (2 + PA) * 1024);
+            auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
+            auto tri = [&](int part, int it, int s) { return *(const f16x8*)(s_v + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16); };
 
-        // K S
-        f16x8 Sh[NS], Sl[NS];
-        const float ms = column_max(largest(S));
-        const int es = scale_exp(ms);
+            // K S, and Q S for the outputs, whose products run while R is formed
+            f16x8 Sh[NS], Sl[NS];
+            const float ms = column_max(largest(S));
+            const int es = scale_exp(ms);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) split2(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
-        const float fs = unit * pow2(-es);
-        f32x4 R[4];
+            for (int s = 0; s < NS; ++s) split2<true>(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
+            const float fs = unit * pow2(-es);
+            f32x4 R[4], O[4];
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            R[it] = f32x4{};
+            for (int it = 0; it < 4; ++it) {
+                R[it] = f32x4{};
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const f16x8 k = qk_piece<NS>(s_qk, 0, it, s, lane);
-                R[it] = mma(k, Sh[s], R[it]);
-                R[it] = mma(k, Sl[s], R[it]);
-                if constexpr (PA == 2) R[it] = mma(qk_piece<NS>(s_qk, 1, it, s, lane), Sh[s], R[it]);
+                for (int s = 0; s < NS; ++s) {
+                    const f16x8 k = qk_piece<NS>(s_k, 0, it, s, lane);
+                    R[it] = mma(k, Sh[s], R[it]);
+                    R[it] = mma(k, Sl[s], R[it]);
+                    if constexpr (PA == 2) R[it] = mma(qk_piece<NS>(s_k, 1, it, s, lane), Sh[s], R[it]);
+                }
             }
-            const f32x4 be = tok4(0, it), bk = tok4(1, it);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) R[it][r] = be[r] * v[it][r] - bk[r] * (R[it][r] * fs);
-        }
-        // U = T R
-        const int er = scale_exp(column_max(largest(R)));
-        f16x8 Rh[2], Rl[2];
+            for (int it = 0; it < 4; ++it) {
+                O[it] = f32x4{};
 #pragma unroll
-        for (int s = 0; s < 2; ++s) split2(R[2 * s], R[2 * s + 1], pow2(er), Rh[s], Rl[s]);
-        f32x4 U[4], W[4];
-        const float fr = pow2(-er) * pow2(-12);
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            f32x4 x{};
-#pragma unroll
-            for (int s = 0; s <= it / 2; ++s) {
-                const f16x8 th = tri(0, it, s), tl = tri(1, it, s);
-                x = mma(th, Rh[s], x);
-                x = mma(th, Rl[s], x);
-                x = mma(tl, Rh[s], x);
+                for (int s = 0; s < NS; ++s) {
+                    const f16x8 q = qk_piece<NS>(s_q, 0, it, s, lane);
+                    O[it] = mma(q, Sh[s], O[it]);
+                    if constexpr (PA == 2) {
+                        O[it] = mma(q, Sl[s], O[it]);
+                        O[it] = mma(qk_piece<NS>(s_q, 1, it, s, lane), Sh[s], O[it]);
+                    }
+                }
             }
-            const f32x4 ka = tok4(2, it), kw = tok4(3, it);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float u = x[r] * fr;
-                U[it][r] = u * ka[r];
-                W[it][r] = u * kw[r];
+            for (int it = 0; it < 4; ++it) {
+                const f32x4 be = tok4(0, it), bk = tok4(1, it);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) R[it][r] = be[r] * v[it][r] - bk[r] * (R[it][r] * fs);
             }
-        }
-        // O = Q S + P U
-        {
+            // U = T R
+            const int er = scale_exp(column_max(largest(R)));
+            f16x8 Rh[2], Rl[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], pow2(er), Rh[s], Rl[s]);
+            f32x4 U[4], W[4];
+            const float fr = pow2(-er) * pow2(-12);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                f32x4 x{};
+#pragma unroll
+                for (int s = 0; s <= it / 2; ++s) {
+                    const f16x8 th = tri(0, it, s), tl = tri(1, it, s);
+                    x = mma(th, Rh[s], x);
+                    x = mma(th, Rl[s], x);
+                    x = mma(tl, Rh[s], x);
+                }
+                const f32x4 ka = tok4(2, it), kw = tok4(3, it);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float u = x[r] * fr;
+                    U[it][r] = u * ka[r];
+                    W[it][r] = u * kw[r];
+                }
+            }
+            // S <- decay S + K^T W, in the units of W's scale; a state far above W keeps the scale in range
+            const float decay = fac[6 * kC];
+            const float mw = column_max(largest(W));
+            const int ew = scale_exp(fmaxf(mw, ms * unit * decay * pow2(-10)));
+            f16x8 Wh[2], Wl[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) split2<true>(W[2 * s], W[2 * s + 1], pow2(ew), Wh[s], Wl[s]);
+            const float keep = decay * unit * pow2(ew);
+            unit = pow2(-ew);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[t][r] *= keep;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of
+                    // 16 values of k, transposed as they are read
+                    typedef short s16x4 __attribute__((ext_vector_type(4)));
+                    typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+                    for (int part = 0; part < PA; ++part) {
+                        s16x4 k2[2];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const char* at = s_k + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 +
+                                                    qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
+                            k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+                        }
+                        const f16x8 k = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                        S[t] = mma(k, Wh[s], S[t]);
+                        if (part == 0) S[t] = mma(k, Wl[s], S[t]);
+                    }
+                }
+            }
+            // O = Q S + P U
             const int eu = scale_exp(column_max(largest(U)));
             f16x8 Uh[2], Ul[2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) split2(U[2 * s], U[2 * s + 1], pow2(eu), Uh[s], Ul[s]);
-            T* out = (T*)p.out + t0 * p.ld_out + h * p.dv + c0 + (lane & 15);
+            for (int s = 0; s < 2; ++s) split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), Uh[s], Ul[s]);
+            const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)c * kC) * p.ld_out + h * p.dv,
+                                                          (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                f32x4 x{}, y{};
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const f16x8 q = qk_piece<NS>(s_qk + kQk, 0, it, s, lane);
-                    x = mma(q, Sh[s], x);
-                    if constexpr (PA == 2) {
-                        x = mma(q, Sl[s], x);
-                        x = mma(qk_piece<NS>(s_qk + kQk, 1, it, s, lane), Sh[s], x);
-                    }
-                }
+                f32x4 y{};
 #pragma unroll
                 for (int s = 0; s <= it / 2; ++s) {
                     const f16x8 q = tri(2, it, s);
@@ -563,44 +695,19 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
                 }
                 const f32x4 ce = tok4(4, it), cc = tok4(5, it);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int t = 16 * it + 4 * hh + r;
-                    if (t < nq) out[t * p.ld_out] = from_f32<T>(ce[r] * (x[r] * fs) + cc[r] * (y[r] * pow2(-eu)));
-                }
+                for (int r = 0; r < 4; ++r)
+                    Raw<T>::store(ro, o0 + (uint32_t)(16 * it + r) * ldo, ce[r] * (O[it][r] * fs) + cc[r] * (y[r] * pow2(-eu)));
             }
         }
-        // S <- decay S + K^T W, in the units of W's scale; a state far above W keeps the scale in range
-        const float decay = fac[6 * kC];
-        const float mw = column_max(largest(W));
-        const int ew = scale_exp(fmaxf(mw, ms * unit * decay * pow2(-10)));
-        f16x8 Wh[2], Wl[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) split2(W[2 * s], W[2 * s + 1], pow2(ew), Wh[s], Wl[s]);
-        const float keep = decay * unit * pow2(ew);
-        unit = pow2(-ew);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= keep;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of 16
-                // values of k, transposed as they are read
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) s16x4* lds4;
-#pragma unroll
-                for (int part = 0; part < PA; ++part) {
-                    s16x4 k2[2];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const char* at = s_qk + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 +
-                                                 qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
-                        k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-                    }
-                    const f16x8 k = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    S[t] = mma(k, Wh[s], S[t]);
-                    if (part == 0) S[t] = mma(k, Wl[s], S[t]);
-                }
+        if (L::kQStages < 2 && c + 1 < n) {            // q (and, with one stage, everything) is read by now
+            wait_lgkm0();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            bring_q(c + 1);
+            if (L::kStages == 1) {
+                bring(c + 1);
+                bring_v(c + 1);
             }
         }
     }
@@ -637,8 +744,11 @@ DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, 
     return w;
 }
 
+template <typename T, int NS, int WAVES> void main_launch(const Args& a, hipStream_t s) {
+    const unsigned blocks = (unsigned)((a.d.dv + 16 * WAVES - 1) / (16 * WAVES));
+    SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), dim3(a.d.Hv * blocks, (unsigned)a.d.nseq), dim3(64 * WAVES), 0, s, a);
+}
 template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream_t s) {
-    constexpr int WAVES = 4;
     const DeltaArgs& p = a.d;
     if (p.nseq > kFindSeqs) {
         KernelTimer kt("delta.plan", s);
@@ -648,9 +758,10 @@ template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream
         KernelTimer kt("delta.chunk", s);
         SSM_LAUNCH((delta_chunk_kernel<T, NS>), dim3((unsigned)a.w.slots, (unsigned)p.Hv), dim3(256), 0, s, a);
     }
-    const unsigned blocks = (unsigned)((p.dv + 16 * WAVES - 1) / (16 * WAVES));
     KernelTimer kt("delta.main", s);
-    SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), dim3(p.Hv * blocks, (unsigned)p.nseq), dim3(64 * WAVES), 0, s, a);
+    const int64_t pairs = (int64_t)p.nseq * p.Hv, n2 = pairs * ((p.dv + 31) / 32), n4 = pairs * ((p.dv + 63) / 64);
+    if (n4 < 256 && n2 > n4) main_launch<T, NS, 2>(a, s);
+    else main_launch<T, NS, 4>(a, s);
     return hipGetLastError();
 }
 template <typename T> hipError_t prefill_steps(const Args& a, hipStream_t s) {

@@ -135,7 +135,7 @@ def _call(kind="prefill", desc=None, rows=100, **kw):
 
 BAD = [(dict(qkv=None), -1), (dict(qkv=16 * M + 8), -2), (dict(ld_qkv=508), -1), (dict(ld_qkv=(1 << 22) + 8), -1), (dict(ld_qkv=516), -2), (dict(a=None), -1),
        (dict(b=None), -1), (dict(a=32 * M + 1), -2), (dict(ld_ab=3), -1), (dict(pool=None), -1), (dict(pool=64 * M + 4), -2),
-       (dict(slots=0), -1), (dict(out=None), -1), (dict(out=48 * M + 2), -2), (dict(ld_out=248), -1), (dict(ld_out=260), -2),
+       (dict(slots=0), -1), (dict(out=None), -1), (dict(out=48 * M + 2), -2), (dict(ld_out=248), -1), (dict(ld_out=260), -2), (dict(ld_out=(1 << 22) + 8), -1),
        (dict(ws=None), -1), (dict(ws=128 * M + 8), -2), (dict(ws_bytes=255), -3), (dict(A_log=None), -1), (dict(dt_bias=M + 4), -2),
        (dict(out=16 * M), -1), (dict(out=16 * M + 512), -1), (dict(a=48 * M, b=48 * M + 8), -1), (dict(b=48 * M + 2), -1),
        (dict(pool=48 * M), -1), (dict(pool=16 * M), -1), (dict(out=64 * M + 8 * 65536 - 16), -1)]
