@@ -25,7 +25,9 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;           // tokens per chunk
 constexpr int kFrags = 6;        // 16 x 32 pieces of a lower triangular 64 x 64 matrix
-constexpr size_t kScalBytes = 2048;   // beta, beta e^G kappa, kappa, kappa e^(G_C - G), c e^G, c 2^20, e^(G_C), each by token
+// factors for the state, by token: e^G kappa, e^(G_C - G); then e^(G_C), the scale of T, the largest of the first
+constexpr int kFacDecay = 2 * kC, kFacT = 2 * kC + 1, kFacMax = 2 * kC + 2;
+constexpr size_t kFacBytes = 1024, kOutFacBytes = 1024;   // and for the outputs: c e^G, c 2^20
 constexpr int kFindSeqs = 256;   // more sequences are laid out by a launch of its own
 
 // the parts of a stored q, k or product: float32 activations take two f16 values
@@ -38,10 +40,12 @@ __host__ __device__ constexpr int frag_of(int it, int s) { return it < 2 ? it : 
 // have their rows rotated by 4 hh, so that the transposing reads of k meet every bank once.
 __device__ __forceinline__ int qk_unit(int row, int hh) { return 16 * hh + ((row + 4 * hh) & 15); }
 
-// Sizes of the workspace. Per chunk and q/k head: pieces of k, then of q; per chunk and value head: T (two parts), the
-// products of queries and keys, the tokens' factors.
+// Sizes of the workspace. Per chunk and q/k head: pieces of k, then of q; per chunk and value head: kappa T beta (two
+// parts) and the state's factors, then the products of queries and keys and the outputs' factors.
 constexpr size_t qk_bytes(int NS, int parts) { return (size_t)4 * NS * parts * 1024; }   // k or q
-constexpr size_t v_bytes(int parts) { return (size_t)kFrags * (2 + parts) * 1024 + kScalBytes; }
+constexpr size_t t_bytes() { return (size_t)kFrags * 2 * 1024 + kFacBytes; }                            // for the state
+constexpr size_t p_bytes(int parts) { return (size_t)kFrags * parts * 1024 + kOutFacBytes; }           // for the outputs
+constexpr size_t v_bytes(int parts) { return t_bytes() + p_bytes(parts); }
 
 struct DeltaWs {
     int32_t* base;     // [nseq] first chunk of every sequence
@@ -192,7 +196,8 @@ template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk
     constexpr int PA = kParts<T>;
     __shared__ __attribute__((aligned(16))) char s_k[qk_bytes(NS, PA)], s_q[qk_bytes(NS, PA)];
     __shared__ __attribute__((aligned(16))) float s_t[kC * kLdA];
-    __shared__ float s_gh[kC], s_gl[kC], s_beta[kC], s_kap[kC], s_c[kC];
+    __shared__ __attribute__((aligned(16))) float s_gh[kC], s_gl[kC], s_beta[kC], s_kap[kC], s_c[kC];
+    __shared__ float s_max[4];
     __shared__ int s_find[8];
     const DeltaArgs& p = a.d;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, slot = blockIdx.x, h = blockIdx.y;
@@ -302,7 +307,7 @@ template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk
 #pragma unroll
                 for (int part = 0; part < PA; ++part) {
                     const f16x8 o = pair_f16(x, 0);
-                    *(f16x8*)(vout + (size_t)((2 + part) * kFrags + frag_of(wave, jt >> 1)) * 1024 + lane * 16) = o;
+                    *(f16x8*)(vout + t_bytes() + (size_t)(part * kFrags + frag_of(wave, jt >> 1)) * 1024 + lane * 16) = o;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] -= (float)o[e];
                 }
@@ -318,17 +323,22 @@ template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk
         }
     }
     // the tokens' factors
+    float* fac = (float*)(vout + t_bytes() - kFacBytes);
     if (tid < kC) {
-        float* f = (float*)(vout + (size_t)kFrags * (2 + PA) * 1024);
+        float* f = (float*)(vout + v_bytes(PA) - kOutFacBytes);
         const float gh = s_gh[tid], gl = s_gl[tid], ch = s_gh[kC - 1], cl = s_gl[kC - 1];
-        const float eg = fast_exp2(gh + gl), kap = s_kap[tid];
-        f[tid] = s_beta[tid];
-        f[kC + tid] = s_beta[tid] * eg * kap;
-        f[2 * kC + tid] = kap;
-        f[3 * kC + tid] = kap * fast_exp2((ch - gh) + (cl - gl));
-        f[4 * kC + tid] = s_c[tid] * eg;
-        f[5 * kC + tid] = s_c[tid] * pow2(20);
-        f[6 * kC + tid] = fast_exp2(ch + cl);
+        const float eg = fast_exp2(gh + gl), bg = eg * s_kap[tid];
+        fac[tid] = bg;
+        fac[kC + tid] = fast_exp2((ch - gh) + (cl - gl));
+        float m = bg;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        if (tid == 0) {
+            fac[kFacDecay] = fast_exp2(ch + cl);
+            fac[kFacMax] = m;
+        }
+        f[tid] = s_c[tid] * eg;
+        f[kC + tid] = s_c[tid] * pow2(20);
     }
     __syncthreads();
 
@@ -393,22 +403,42 @@ template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk
         put(32 + 16 * r2, c0, y);
     }
     __syncthreads();
-    for (int f = wave; f < kFrags; f += 4) {
+    // kappa T beta, scaled by the power of two that takes its largest value to 2^12
+    float x[2][8], m = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int f = wave + 4 * n;
+        if (f >= kFrags) continue;
         const int it = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) & 1;
         const f32x4 v0 = row4(16 * it, 32 * s);
         const f32x4 v1 = 2 * s + 1 <= it ? row4(16 * it, 32 * s + 16) : f32x4{};
-        float x[8];
+        const f32x4 b0 = *(const f32x4*)&s_beta[32 * s + 4 * hh], b1 = *(const f32x4*)&s_beta[32 * s + 16 + 4 * hh];
+        const float ka = s_kap[16 * it + col];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            x[e] = v0[e] * pow2(12);
-            x[4 + e] = v1[e] * pow2(12);
+            x[n][e] = v0[e] * b0[e] * ka;
+            x[n][4 + e] = v1[e] * b1[e] * ka;
+            m = fmaxf(m, fmaxf(fabsf(x[n][e]), fabsf(x[n][4 + e])));
         }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if (lane == 0) s_max[wave] = m;
+    __syncthreads();
+    const int et = scale_exp(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])));
+    if (tid == 0) fac[kFacT] = pow2(-et);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int f = wave + 4 * n;
+        if (f >= kFrags) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[n][e] *= pow2(et);
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            const f16x8 o = pair_f16(x, 0);
+            const f16x8 o = pair_f16(x[n], 0);
             *(f16x8*)(vout + (size_t)(part * kFrags + f) * 1024 + lane * 16) = o;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] -= (float)o[e];
+            for (int e = 0; e < 8; ++e) x[n][e] -= (float)o[e];
         }
     }
 }
@@ -573,9 +603,9 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
         const char* s_q = lds + q_at(c);
         if (on) {
             const int nq = min(rows - c * kC, kC);
-            const float* fac = (const float*)(s_v + kFrags * (2 + PA) * 1024);
-            auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
-            auto tri = [&](int part, int it, int s) { return *(const f16x8*)(s_v + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16); };
+            const float *fac = (const float*)(s_v + t_bytes() - kFacBytes), *ofac = (const float*)(s_v + v_bytes(PA) - kOutFacBytes);
+            auto tok4 = [&](const float* f, int k, int it) { return *(const f32x4*)&f[k * kC + 16 * it + 4 * hh]; };
+            auto tri = [&](const char* m, int part, int it, int s) { return *(const f16x8*)(m + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16); };
 
             // K S, and Q S for the outputs, whose products run while R is formed
             f16x8 Sh[NS], Sl[NS];
@@ -611,9 +641,9 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
             }
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                const f32x4 be = tok4(0, it), bk = tok4(1, it);
+                const f32x4 bg = tok4(fac, 0, it);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) R[it][r] = be[r] * v[it][r] - bk[r] * (R[it][r] * fs);
+                for (int r = 0; r < 4; ++r) R[it][r] = v[it][r] - bg[r] * (R[it][r] * fs);
             }
             // U = T R
             const int er = scale_exp(column_max(largest(R)));
@@ -621,27 +651,26 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
 #pragma unroll
             for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], pow2(er), Rh[s], Rl[s]);
             f32x4 U[4], W[4];
-            const float fr = pow2(-er) * pow2(-12);
+            const float fr = pow2(-er) * fac[kFacT];
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
                 f32x4 x{};
 #pragma unroll
                 for (int s = 0; s <= it / 2; ++s) {
-                    const f16x8 th = tri(0, it, s), tl = tri(1, it, s);
+                    const f16x8 th = tri(s_v, 0, it, s), tl = tri(s_v, 1, it, s);
                     x = mma(th, Rh[s], x);
                     x = mma(th, Rl[s], x);
                     x = mma(tl, Rh[s], x);
                 }
-                const f32x4 ka = tok4(2, it), kw = tok4(3, it);
+                const f32x4 w = tok4(fac, 1, it);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float u = x[r] * fr;
-                    U[it][r] = u * ka[r];
-                    W[it][r] = u * kw[r];
+                    U[it][r] = x[r] * fr;
+                    W[it][r] = U[it][r] * w[r];
                 }
             }
             // S <- decay S + K^T W, in the units of W's scale; a state far above W keeps the scale in range
-            const float decay = fac[6 * kC];
+            const float decay = fac[kFacDecay];
             const float mw = column_max(largest(W));
             const int ew = scale_exp(fmaxf(mw, ms * unit * decay * pow2(-10)));
             f16x8 Wh[2], Wl[2];
@@ -686,14 +715,14 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
                 f32x4 y{};
 #pragma unroll
                 for (int s = 0; s <= it / 2; ++s) {
-                    const f16x8 q = tri(2, it, s);
+                    const f16x8 q = tri(s_v + t_bytes(), 0, it, s);
                     y = mma(q, Uh[s], y);
                     if constexpr (PA == 2) {
                         y = mma(q, Ul[s], y);
-                        y = mma(tri(3, it, s), Uh[s], y);
+                        y = mma(tri(s_v + t_bytes(), 1, it, s), Uh[s], y);
                     }
                 }
-                const f32x4 ce = tok4(4, it), cc = tok4(5, it);
+                const f32x4 ce = tok4(ofac, 0, it), cc = tok4(ofac, 1, it);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     Raw<T>::store(ro, o0 + (uint32_t)(16 * it + r) * ldo, ce[r] * (O[it][r] * fs) + cc[r] * (y[r] * pow2(-eu)));
@@ -709,6 +738,293 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
                 bring(c + 1);
                 bring_v(c + 1);
             }
+        }
+    }
+    if (ok && on) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (16 * t >= p.dk) break;
+            f32x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = S[t][r] * unit;
+            *(f32x4*)(state + 16 * t) = o;
+        }
+    }
+}
+
+// As delta_main_kernel, with the outputs by waves of their own: W waves carry the state, W more form the outputs of the
+// chunk before from the operands that the first left in LDS. The chain from chunk to chunk is that much shorter, and
+// both kinds run beside each other. Scales that need not be exact are bounds, known before what they scale:
+// a bound loses headroom (f16 pairs hold 39 bits, 22 are used), not precision.
+template <typename T, int NS, int W> struct SplitLds {
+    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes(), kP = (int)p_bytes(kParts<T>);
+    static constexpr int kHand = (NS + 2) * kParts<T> * 1024 + 256;     // S, U and their scales of 16 columns
+    static constexpr int kBytes = 2 * (2 * kQk + kT + kP + W * kHand);
+    static constexpr bool kFits = kBytes <= (int)kLds;
+};
+
+template <typename T, int NS, int W>
+__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void delta_split_kernel(Args a) {
+    constexpr int PA = kParts<T>, NT = 2 * NS;
+    using L = SplitLds<T, NS, W>;
+    constexpr int kQk = L::kQk, kT = L::kT, kP = L::kP, kHand = L::kHand, kStage = 2 * kQk + kT + kP;
+    constexpr uint32_t sz = sizeof(T);
+    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
+    const DeltaArgs& p = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int blocks = (p.dv + 16 * W - 1) / (16 * W), h = blockIdx.x / blocks, seq = blockIdx.y, hk = h / p.rep;
+    const bool carries = wave < W;
+    const int wc = carries ? wave : wave - W;
+    const int c0 = ((int)(blockIdx.x % blocks) * W + wc) * 16;           // this wave's columns
+    const bool on = c0 < p.dv;
+    const SeqRows sr = seq_rows(p, seq);
+    const int lo = __builtin_amdgcn_readfirstlane(sr.lo), rows = __builtin_amdgcn_readfirstlane(sr.n);
+    const int slot = p.slot[seq], n = chunks_of(rows), base = rows > 0 ? __builtin_amdgcn_readfirstlane(a.w.base[seq]) : 0;
+    const bool fits = sr.ok && base + n <= a.w.slots, ok = slot >= 0 && slot < p.S;
+    if (blockIdx.x == 0 && tid == 0 && (!fits || !ok))
+        atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
+    if (!fits) return;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
+    // a stage: k, T and the state's factors; q, the products and the outputs' factors; what the waves hand over
+    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
+    auto v_buf = [&](int c) { return buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * (kT + kP), kT + kP); };
+    auto bring_state = [&](int c) {
+        const uint32_t to = lds0 + (c & 1) * kStage;
+        dma_pieces<2 * W, kQk>(qk_buf(c), 0, to, wave, lane);
+        dma_pieces<2 * W, kT>(v_buf(c), 0, to + kQk, wave, lane);
+    };
+    auto bring_out = [&](int c) {
+        const uint32_t to = lds0 + (c & 1) * kStage + kQk + kT;
+        dma_pieces<2 * W, kQk>(qk_buf(c), kQk, to, wave, lane);
+        dma_pieces<2 * W, kP>(v_buf(c), kT, to + kQk, wave, lane);
+    };
+    auto hand = [&](int c) { return lds + 2 * kStage + ((c & 1) * W + wc) * kHand; };
+    auto meet = [&] {
+        wait_lgkm0();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (n > 0) bring_state(0);
+
+    if (!carries) {
+        // O^T of 16 columns: rows are columns of the state, a lane's token is its column of the product
+        const uint32_t ldo = (uint32_t)p.ld_out * sz;
+        const uint32_t o0 = (uint32_t)(lane & 15) * ldo + (uint32_t)(c0 + 4 * hh) * sz;
+        for (int c = 0; c <= n; ++c) {
+            if (on && c > 1) wait_vm<4>();             // but for the stores of the outputs
+            else wait_vm<0>();
+            if (n == 0) break;
+            meet();
+            if (c + 1 < n) bring_state(c + 1);
+            if (c < n) bring_out(c);
+            if (c == 0 || !on) continue;
+            const int d = c - 1, nq = min(rows - d * kC, kC);
+            const char *s_q = lds + (d & 1) * kStage + kQk + kT, *s_p = s_q + kQk, *from = hand(d);
+            const float *fac = (const float*)(s_p + kP - kOutFacBytes), *sc = (const float*)(from + (NS + 2) * PA * 1024);
+            f16x8 S[PA][NS], U[PA][2];
+#pragma unroll
+            for (int part = 0; part < PA; ++part) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) S[part][s] = *(const f16x8*)(from + (part * NS + s) * 1024 + lane * 16);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) U[part][s] = *(const f16x8*)(from + (PA * NS + part * 2 + s) * 1024 + lane * 16);
+            }
+            const f32x4 fs = *(const f32x4*)&sc[4 * hh], fu = *(const f32x4*)&sc[16 + 4 * hh];
+            const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)d * kC) * p.ld_out + h * p.dv,
+                                                          (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                f32x4 x{}, y{};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const f16x8 q = qk_piece<NS>(s_q, 0, it, s, lane);
+                    x = mma(S[0][s], q, x);
+                    if constexpr (PA == 2) {
+                        x = mma(S[1][s], q, x);
+                        x = mma(S[0][s], qk_piece<NS>(s_q, 1, it, s, lane), x);
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s <= it / 2; ++s) {
+                    const f16x8 q = *(const f16x8*)(s_p + frag_of(it, s) * 1024 + lane * 16);
+                    y = mma(U[0][s], q, y);
+                    if constexpr (PA == 2) {
+                        y = mma(U[1][s], q, y);
+                        y = mma(U[0][s], *(const f16x8*)(s_p + (kFrags + frag_of(it, s)) * 1024 + lane * 16), y);
+                    }
+                }
+                const float ce = fac[16 * it + (lane & 15)], cc = fac[kC + 16 * it + (lane & 15)];
+                T o[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(ce * (x[r] * fs[r]) + cc * (y[r] * fu[r]));
+                if constexpr (PA == 2) {
+                    u32x4 w;
+                    __builtin_memcpy(&w, o, 16);
+                    __builtin_amdgcn_raw_buffer_store_b128(w, ro, (int)(o0 + (uint32_t)(16 * it) * ldo), 0, 0);
+                } else {
+                    u32x2 w;
+                    __builtin_memcpy(&w, o, 8);
+                    __builtin_amdgcn_raw_buffer_store_b64(w, ro, (int)(o0 + (uint32_t)(16 * it) * ldo), 0, 0);
+                }
+            }
+        }
+        return;
+    }
+
+    // V of this lane's column, tokens 16 it + 4 hh + r
+    typename Raw<T>::type raw[4][4];
+    const uint32_t ldv = (uint32_t)p.ld * sz;
+    const uint32_t v0 = on ? (uint32_t)(4 * hh) * ldv + (uint32_t)(c0 + (lane & 15)) * sz : kOffOutOfRange;
+    auto bring_v = [&](int c) {
+        const int nq = min(rows - c * kC, kC);
+        const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
+                                                     (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) raw[it][k] = Raw<T>::load(r, v0 + (uint32_t)(16 * it + k) * ldv);
+    };
+    if (n > 0) bring_v(0);
+    float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
+    f32x4 S[NT];
+    const bool carry = ok && p.has_init[seq];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        S[t] = f32x4{};
+        if (carry && on && 16 * t < p.dk) S[t] = *(const f32x4*)(state + 16 * t);
+    }
+    // S times unit (a power of two) is the state; its operand is S 2^es, |S| <= bound
+    float unit = 1.0f, bound = column_max(largest(S));
+    int es = scale_exp(bound);
+    f16x8 Sh[NS], Sl[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) split2<true>(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
+    for (int c = 0; c <= n; ++c) {
+        wait_vm<0>();
+        if (n == 0) break;
+        meet();
+        float v[4][4], vmax = 0.0f;
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[it][k] = Raw<T>::value(raw[it][k]);
+                asm volatile("" : "+v"(v[it][k]));     // taken here, in front of the loads for the next chunk
+            }
+        if (c + 1 < n) bring_state(c + 1);
+        if (c < n) bring_out(c);
+        if (c + 1 < n) bring_v(c + 1);
+        if (c == n || !on) continue;
+        const char *s_k = lds + (c & 1) * kStage, *s_t = s_k + kQk;
+        const float* fac = (const float*)(s_t + kT - kFacBytes);
+        char* to = hand(c);
+        auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
+
+        // R = V - e^G K S
+        f32x4 R[4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            R[it] = f32x4{};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const f16x8 k = qk_piece<NS>(s_k, 0, it, s, lane);
+                R[it] = mma(k, Sh[s], R[it]);
+                R[it] = mma(k, Sl[s], R[it]);
+                if constexpr (PA == 2) R[it] = mma(qk_piece<NS>(s_k, 1, it, s, lane), Sh[s], R[it]);
+            }
+        }
+        const float fs = unit * pow2(-es);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            *(f16x8*)(to + s * 1024 + lane * 16) = Sh[s];
+            if constexpr (PA == 2) *(f16x8*)(to + (NS + s) * 1024 + lane * 16) = Sl[s];
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) vmax = fmaxf(vmax, fabsf(v[it][k]));
+        const float ms = column_max(largest(S));
+        // values of k are below 2^13
+        const int er = scale_exp(column_max(vmax) + fac[kFacMax] * pow2(13) * (float)(32 * NS) * (ms * unit));
+        const float gr = pow2(er);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const f32x4 bg = tok4(0, it);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(-(bg[r] * fs), R[it][r], v[it][r]);
+        }
+        f16x8 Rh[2], Rl[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], gr, Rh[s], Rl[s]);
+        // U = kappa T beta R, W = e^(G_C - G) U; both times 1 / fu
+        f32x4 U[4], X[4];
+        const float fu = pow2(-er) * fac[kFacT];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            U[it] = f32x4{};
+#pragma unroll
+            for (int s = 0; s <= it / 2; ++s) {
+                const f16x8 th = *(const f16x8*)(s_t + frag_of(it, s) * 1024 + lane * 16),
+                            tl = *(const f16x8*)(s_t + (kFrags + frag_of(it, s)) * 1024 + lane * 16);
+                U[it] = mma(th, Rh[s], U[it]);
+                U[it] = mma(th, Rl[s], U[it]);
+                U[it] = mma(tl, Rh[s], U[it]);
+            }
+            const f32x4 w = tok4(1, it);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * w[r];
+        }
+        // S <- decay S + K^T W in the units of W's scale; a state far above W keeps the scale in range
+        const float decay = fac[kFacDecay], mw = column_max(largest(X)) * fu;
+        const int ew = scale_exp(fmaxf(mw, bound * unit * decay * pow2(-10)));
+        f16x8 Wh[2], Wl[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) split2<true>(X[2 * s], X[2 * s + 1], fu * pow2(ew), Wh[s], Wl[s]);
+        const float keep = decay * unit * pow2(ew);
+        // 64 products of values below 2^13
+        bound = keep * ms + mw * pow2(ew) * pow2(19);
+        unit = pow2(-ew);
+        es = scale_exp(bound);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] *= keep;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of
+                // 16 values of k, transposed as they are read
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+                for (int part = 0; part < PA; ++part) {
+                    s16x4 k2[2];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const char* at = s_k + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 +
+                                                qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
+                        k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+                    }
+                    const f16x8 k = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    S[t] = mma(k, Wh[s], S[t]);
+                    if (part == 0) S[t] = mma(k, Wl[s], S[t]);
+                }
+            }
+            if (t & 1) split2<true>(S[t - 1], S[t], pow2(es), Sh[t / 2], Sl[t / 2]);
+        }
+        // U for the outputs
+        const int eu = scale_exp(column_max(largest(U)));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            f16x8 uh, ul;
+            split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), uh, ul);
+            *(f16x8*)(to + (PA * NS + s) * 1024 + lane * 16) = uh;
+            if constexpr (PA == 2) *(f16x8*)(to + (PA * NS + 2 + s) * 1024 + lane * 16) = ul;
+        }
+        if (hh == 0) {
+            float* sc = (float*)(to + (NS + 2) * PA * 1024);
+            sc[lane] = fs;
+            sc[16 + lane] = fu * pow2(-eu);
         }
     }
     if (ok && on) {
@@ -746,7 +1062,9 @@ DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, 
 
 template <typename T, int NS, int WAVES> void main_launch(const Args& a, hipStream_t s) {
     const unsigned blocks = (unsigned)((a.d.dv + 16 * WAVES - 1) / (16 * WAVES));
-    SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), dim3(a.d.Hv * blocks, (unsigned)a.d.nseq), dim3(64 * WAVES), 0, s, a);
+    const dim3 grid(a.d.Hv * blocks, (unsigned)a.d.nseq);
+    if constexpr (SplitLds<T, NS, WAVES>::kFits) SSM_LAUNCH((delta_split_kernel<T, NS, WAVES>), grid, dim3(128 * WAVES), 0, s, a);
+    else SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), grid, dim3(64 * WAVES), 0, s, a);
 }
 template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream_t s) {
     const DeltaArgs& p = a.d;
