@@ -471,9 +471,8 @@ template <bool LO> __device__ __forceinline__ void split2(const f32x4& x0, const
         hi[r] = h[0];
         hi[r + 1] = h[1];
         if constexpr (LO) {
-            const f16x2 l = __builtin_convertvector((f32x2){__builtin_fmaf(a, f, -(float)h[0]), __builtin_fmaf(b, f, -(float)h[1])}, f16x2);
-            lo[r] = l[0];
-            lo[r + 1] = l[1];
+            lo[r] = (_Float16)__builtin_fmaf(a, f, -(float)h[0]);
+            lo[r + 1] = (_Float16)__builtin_fmaf(b, f, -(float)h[1]);
         }
     }
 }
@@ -519,6 +518,21 @@ template <> struct Raw<bf16> {
     static __device__ __forceinline__ float value(type v) { return (float)__builtin_bit_cast(bf16, v); }
 };
 
+// Workgroups are dealt out to the XCDs in turn: item (sequence, q/k head) u runs on XCD u % 8, whose L2 then holds the
+// pieces that its value heads and column blocks share. Grid: 8 rep blocks by every eighth item, in rows of kGridRow.
+constexpr int kGridRow = 1 << 15;
+struct WorkItem {
+    int seq, head, block;   // seq may be past the last
+};
+__device__ __forceinline__ WorkItem work_item(const DeltaArgs& p, int blocks) {
+    const int u = ((int)blockIdx.z * kGridRow + (int)blockIdx.y) * 8 + (int)(blockIdx.x & 7), in = (int)(blockIdx.x >> 3);
+    return WorkItem{u / p.Hk, u % p.Hk * p.rep + in / blocks, in % blocks};
+}
+dim3 work_grid(const DeltaArgs& p, int blocks) {
+    const unsigned rows = (unsigned)(((int64_t)p.nseq * p.Hk + 7) / 8);
+    return dim3((unsigned)(8 * p.rep * blocks), std::min<unsigned>(rows, kGridRow), (rows + kGridRow - 1) / kGridRow);
+}
+
 // While a chunk is computed the next one's pieces and values are on their way, and the stores of its outputs stay out
 // at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'.
 template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES) void delta_main_kernel(Args a) {
@@ -529,14 +543,15 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
     __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
     const DeltaArgs& p = a.d;
     const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int blocks = (p.dv + 16 * WAVES - 1) / (16 * WAVES), h = blockIdx.x / blocks, seq = blockIdx.y, hk = h / p.rep;
-    const int c0 = ((int)(blockIdx.x % blocks) * WAVES + wave) * 16;     // this wave's columns
+    const WorkItem it0 = work_item(p, (p.dv + 16 * WAVES - 1) / (16 * WAVES));
+    if (it0.seq >= p.nseq) return;
+    const int seq = it0.seq, h = it0.head, hk = h / p.rep, c0 = (it0.block * WAVES + wave) * 16;   // this wave's columns
     const bool on = c0 < p.dv;
     const SeqRows sr = seq_rows(p, seq);
     const int lo = __builtin_amdgcn_readfirstlane(sr.lo), rows = __builtin_amdgcn_readfirstlane(sr.n);
     const int slot = p.slot[seq], n = chunks_of(rows), base = rows > 0 ? __builtin_amdgcn_readfirstlane(a.w.base[seq]) : 0;
     const bool fits = sr.ok && base + n <= a.w.slots, ok = slot >= 0 && slot < p.S;
-    if (blockIdx.x == 0 && tid == 0 && (!fits || !ok))
+    if (h == 0 && it0.block == 0 && tid == 0 && (!fits || !ok))
         atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
     if (!fits) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
@@ -758,45 +773,60 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
 // a bound loses headroom (f16 pairs hold 39 bits, 22 are used), not precision.
 template <typename T, int NS, int W> struct SplitLds {
     static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes(), kP = (int)p_bytes(kParts<T>);
-    static constexpr int kHand = (NS + 2) * kParts<T> * 1024 + 256;     // S, U and their scales of 16 columns
-    static constexpr int kBytes = 2 * (2 * kQk + kT + kP + W * kHand);
+    static constexpr int kRow = 16 * W * (int)sizeof(T), kRows = kC * kRow;   // the workgroup's values of a token, of a chunk
+    static constexpr int kHand = (NS + 2) * kParts<T> * 1024 + 256;           // S, U and their scales of 16 columns
+    static constexpr int kStage = 2 * kQk + kT + kRows + (int)kOutFacBytes, kBytes = 2 * (kStage + W * kHand);
     static constexpr bool kFits = kBytes <= (int)kLds;
 };
 
 template <typename T, int NS, int W>
-__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void delta_split_kernel(Args a) {
+__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) void delta_split_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = SplitLds<T, NS, W>;
-    constexpr int kQk = L::kQk, kT = L::kT, kP = L::kP, kHand = L::kHand, kStage = 2 * kQk + kT + kP;
+    constexpr int kQk = L::kQk, kT = L::kT, kP = L::kP, kRow = L::kRow, kRows = L::kRows, kHand = L::kHand, kStage = L::kStage;
     constexpr uint32_t sz = sizeof(T);
-    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
     const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int blocks = (p.dv + 16 * W - 1) / (16 * W), h = blockIdx.x / blocks, seq = blockIdx.y, hk = h / p.rep;
+    const WorkItem it0 = work_item(p, (p.dv + 16 * W - 1) / (16 * W));
+    if (it0.seq >= p.nseq) return;
+    const int seq = it0.seq, h = it0.head, hk = h / p.rep;
     const bool carries = wave < W;
     const int wc = carries ? wave : wave - W;
-    const int c0 = ((int)(blockIdx.x % blocks) * W + wc) * 16;           // this wave's columns
+    const int c0 = (it0.block * W + wc) * 16;          // this wave's columns
     const bool on = c0 < p.dv;
     const SeqRows sr = seq_rows(p, seq);
     const int lo = __builtin_amdgcn_readfirstlane(sr.lo), rows = __builtin_amdgcn_readfirstlane(sr.n);
     const int slot = p.slot[seq], n = chunks_of(rows), base = rows > 0 ? __builtin_amdgcn_readfirstlane(a.w.base[seq]) : 0;
     const bool fits = sr.ok && base + n <= a.w.slots, ok = slot >= 0 && slot < p.S;
-    if (blockIdx.x == 0 && tid == 0 && (!fits || !ok))
+    if (h == 0 && it0.block == 0 && tid == 0 && (!fits || !ok))
         atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
     if (!fits) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    // a stage: k, T and the state's factors; q, the products and the outputs' factors; what the waves hand over
+    // a stage: k, T and the state's factors, values; q and the outputs' factors; then what the waves hand over
     auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
-    auto v_buf = [&](int c) { return buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * (kT + kP), kT + kP); };
+    auto v_at = [&](int c) { return a.w.v + ((int64_t)(base + c) * p.Hv + h) * (kT + kP); };
+    const uint32_t ldv = (uint32_t)p.ld * sz;
+    // All that comes by DMA is asked for by the waves of the outputs: beside a burst of it a wave waits long to issue a load
     auto bring_state = [&](int c) {
         const uint32_t to = lds0 + (c & 1) * kStage;
-        dma_pieces<2 * W, kQk>(qk_buf(c), 0, to, wave, lane);
-        dma_pieces<2 * W, kT>(v_buf(c), 0, to + kQk, wave, lane);
+        dma_pieces<W, kQk>(qk_buf(c), 0, to, wc, lane);
+        dma_pieces<W, kT>(buffer_rsrc(v_at(c), kT), 0, to + kQk, wc, lane);
+        const int nq = min(rows - c * kC, kC);
+        const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
+                                                     (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
+        constexpr int kPer = 1024 / kRow;              // rows in 1 KB
+        const uint32_t off = (uint32_t)(lane / (kRow / 16)) * ldv + (uint32_t)(it0.block * kRow + lane % (kRow / 16) * 16);
+#pragma unroll
+        for (int i = 0; i < kRows / 1024 / W; ++i) {
+            const uint32_t q = (uint32_t)(wc + W * i);
+            dma16(r, off + q * kPer * ldv, 0, __builtin_amdgcn_readfirstlane(to + kQk + kT + q * 1024));
+        }
     };
     auto bring_out = [&](int c) {
-        const uint32_t to = lds0 + (c & 1) * kStage + kQk + kT;
-        dma_pieces<2 * W, kQk>(qk_buf(c), kQk, to, wave, lane);
-        dma_pieces<2 * W, kP>(v_buf(c), kT, to + kQk, wave, lane);
+        const uint32_t to = lds0 + (c & 1) * kStage + kQk + kT + kRows;
+        dma_pieces<W, kQk>(qk_buf(c), kQk, to, wc, lane);
+        dma_pieces<W, (int)kOutFacBytes>(buffer_rsrc(v_at(c) + kT + kP - kOutFacBytes, kOutFacBytes), 0, to + kQk, wc, lane);
     };
     auto hand = [&](int c) { return lds + 2 * kStage + ((c & 1) * W + wc) * kHand; };
     auto meet = [&] {
@@ -805,23 +835,34 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    if (n > 0) bring_state(0);
-
     if (!carries) {
+        if (n > 0) bring_state(0);
         // O^T of 16 columns: rows are columns of the state, a lane's token is its column of the product
         const uint32_t ldo = (uint32_t)p.ld_out * sz;
         const uint32_t o0 = (uint32_t)(lane & 15) * ldo + (uint32_t)(c0 + 4 * hh) * sz;
-        for (int c = 0; c <= n; ++c) {
+        f16x8 Pn[PA][kFrags];                          // the next products of queries and keys
+        for (int c = 0; c <= n && n > 0; ++c) {
             if (on && c > 1) wait_vm<4>();             // but for the stores of the outputs
             else wait_vm<0>();
-            if (n == 0) break;
+            f16x8 P[PA][kFrags];
+#pragma unroll
+            for (int part = 0; part < PA; ++part)
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f) P[part][f] = Pn[part][f];
             meet();
             if (c + 1 < n) bring_state(c + 1);
-            if (c < n) bring_out(c);
+            if (c < n) {
+                bring_out(c);
+                const char* from = v_at(c) + kT;
+#pragma unroll
+                for (int part = 0; part < PA; ++part)
+#pragma unroll
+                    for (int f = 0; f < kFrags; ++f) Pn[part][f] = *(const f16x8*)(from + (part * kFrags + f) * 1024 + lane * 16);
+            }
             if (c == 0 || !on) continue;
             const int d = c - 1, nq = min(rows - d * kC, kC);
-            const char *s_q = lds + (d & 1) * kStage + kQk + kT, *s_p = s_q + kQk, *from = hand(d);
-            const float *fac = (const float*)(s_p + kP - kOutFacBytes), *sc = (const float*)(from + (NS + 2) * PA * 1024);
+            const char *s_q = lds + (d & 1) * kStage + kQk + kT + kRows, *from = hand(d);
+            const float *fac = (const float*)(s_q + kQk), *sc = (const float*)(from + (NS + 2) * PA * 1024);
             f16x8 S[PA][NS], U[PA][2];
 #pragma unroll
             for (int part = 0; part < PA; ++part) {
@@ -833,31 +874,41 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void
             const f32x4 fs = *(const f32x4*)&sc[4 * hh], fu = *(const f32x4*)&sc[16 + 4 * hh];
             const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)d * kC) * p.ld_out + h * p.dv,
                                                           (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
+            f32x4 O[4], Y[4];
+#pragma unroll
+            for (int it = 0; it < 4; ++it) O[it] = Y[it] = f32x4{};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                f16x8 q[PA][4];
+#pragma unroll
+                for (int part = 0; part < PA; ++part)
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) q[part][it] = qk_piece<NS>(s_q, part, it, s, lane);
+#pragma unroll
+                for (int it = 0; it < 4; ++it) O[it] = mma(S[0][s], q[0][it], O[it]);
+                if constexpr (PA == 2) {
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) O[it] = mma(S[PA - 1][s], q[0][it], O[it]);
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) O[it] = mma(S[0][s], q[PA - 1][it], O[it]);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int it = 2 * s; it < 4; ++it) {
+                    Y[it] = mma(U[0][s], P[0][frag_of(it, s)], Y[it]);
+                    if constexpr (PA == 2) {
+                        Y[it] = mma(U[PA - 1][s], P[0][frag_of(it, s)], Y[it]);
+                        Y[it] = mma(U[0][s], P[PA - 1][frag_of(it, s)], Y[it]);
+                    }
+                }
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                f32x4 x{}, y{};
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const f16x8 q = qk_piece<NS>(s_q, 0, it, s, lane);
-                    x = mma(S[0][s], q, x);
-                    if constexpr (PA == 2) {
-                        x = mma(S[1][s], q, x);
-                        x = mma(S[0][s], qk_piece<NS>(s_q, 1, it, s, lane), x);
-                    }
-                }
-#pragma unroll
-                for (int s = 0; s <= it / 2; ++s) {
-                    const f16x8 q = *(const f16x8*)(s_p + frag_of(it, s) * 1024 + lane * 16);
-                    y = mma(U[0][s], q, y);
-                    if constexpr (PA == 2) {
-                        y = mma(U[1][s], q, y);
-                        y = mma(U[0][s], *(const f16x8*)(s_p + (kFrags + frag_of(it, s)) * 1024 + lane * 16), y);
-                    }
-                }
                 const float ce = fac[16 * it + (lane & 15)], cc = fac[kC + 16 * it + (lane & 15)];
                 T o[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(ce * (x[r] * fs[r]) + cc * (y[r] * fu[r]));
+                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(ce * (O[it][r] * fs[r]) + cc * (Y[it][r] * fu[r]));
                 if constexpr (PA == 2) {
                     u32x4 w;
                     __builtin_memcpy(&w, o, 16);
@@ -872,20 +923,6 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void
         return;
     }
 
-    // V of this lane's column, tokens 16 it + 4 hh + r
-    typename Raw<T>::type raw[4][4];
-    const uint32_t ldv = (uint32_t)p.ld * sz;
-    const uint32_t v0 = on ? (uint32_t)(4 * hh) * ldv + (uint32_t)(c0 + (lane & 15)) * sz : kOffOutOfRange;
-    auto bring_v = [&](int c) {
-        const int nq = min(rows - c * kC, kC);
-        const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
-                                                     (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) raw[it][k] = Raw<T>::load(r, v0 + (uint32_t)(16 * it + k) * ldv);
-    };
-    if (n > 0) bring_v(0);
     float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
     f32x4 S[NT];
     const bool carry = ok && p.has_init[seq];
@@ -900,102 +937,123 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void
     f16x8 Sh[NS], Sl[NS];
 #pragma unroll
     for (int s = 0; s < NS; ++s) split2<true>(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
-    for (int c = 0; c <= n; ++c) {
-        wait_vm<0>();
-        if (n == 0) break;
+    for (int c = 0; c <= n && n > 0; ++c) {
         meet();
-        float v[4][4], vmax = 0.0f;
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[it][k] = Raw<T>::value(raw[it][k]);
-                asm volatile("" : "+v"(v[it][k]));     // taken here, in front of the loads for the next chunk
-            }
-        if (c + 1 < n) bring_state(c + 1);
-        if (c < n) bring_out(c);
-        if (c + 1 < n) bring_v(c + 1);
         if (c == n || !on) continue;
         const char *s_k = lds + (c & 1) * kStage, *s_t = s_k + kQk;
         const float* fac = (const float*)(s_t + kT - kFacBytes);
         char* to = hand(c);
-        auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
+        // What is read from LDS is asked for well in front of its use, as nothing else hides its way: two k steps of k
+        // ahead of their products, T behind the last of them, k transposed in front of the products with T
+        f16x8 K[2][PA][4], Tr[2][kFrags];
+        f32x4 bg[4], wg[4];
+        auto read_k = [&](int s) {
+#pragma unroll
+            for (int part = 0; part < PA; ++part)
+#pragma unroll
+                for (int it = 0; it < 4; ++it) K[s & 1][part][it] = qk_piece<NS>(s_k, part, it, s, lane);
+        };
+        read_k(0);
+        if (NS > 1) read_k(1);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            bg[it] = *(const f32x4*)&fac[16 * it + 4 * hh];
+            wg[it] = *(const f32x4*)&fac[kC + 16 * it + 4 * hh];
+        }
+        const float decay = fac[kFacDecay], tscale = fac[kFacT], gmax = fac[kFacMax];
+        // V of this lane's column, tokens 16 it + 4 hh + r
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        const char* s_v = s_t + kT + wc * 16 * (int)sizeof(T);
+        float v[4][4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            if constexpr (PA == 1) {
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds4)(s_v + (16 * it + 4 * hh + ((lane & 15) >> 2)) * kRow + (lane & 3) * 8));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[it][r] = (float)__builtin_bit_cast(bf16, (short)x[r]);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[it][r] = *(const float*)(s_v + (16 * it + 4 * hh + r) * kRow + (lane & 15) * 4);
+            }
+        }
+        if (c == n - 1) {                              // what lies behind the sequence is no value of it
+#pragma unroll
+            for (int it = 0; it < 4; ++it)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * it + 4 * hh + r >= rows - c * kC) v[it][r] = 0.0f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
 
-        // R = V - e^G K S
+        // K S beside all that does not wait for it
         f32x4 R[4];
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            R[it] = f32x4{};
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const f16x8 k = qk_piece<NS>(s_k, 0, it, s, lane);
-                R[it] = mma(k, Sh[s], R[it]);
-                R[it] = mma(k, Sl[s], R[it]);
-                if constexpr (PA == 2) R[it] = mma(qk_piece<NS>(s_k, 1, it, s, lane), Sh[s], R[it]);
-            }
-        }
+        for (int it = 0; it < 4; ++it) R[it] = f32x4{};
         const float fs = unit * pow2(-es);
+        float ms, fu, wc2, keep;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][0][it], Sh[s], R[it]);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][0][it], Sl[s], R[it]);
+            if constexpr (PA == 2) {
+#pragma unroll
+                for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][PA - 1][it], Sh[s], R[it]);
+            }
+            if (s + 2 < NS) read_k(s + 2);
+            if (s >= NS - 2) {
+                const int part = s - (NS - 2);
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f) Tr[part][f] = *(const f16x8*)(s_t + (part * kFrags + f) * 1024 + lane * 16);
+            }
             *(f16x8*)(to + s * 1024 + lane * 16) = Sh[s];
             if constexpr (PA == 2) *(f16x8*)(to + (NS + s) * 1024 + lane * 16) = Sl[s];
-        }
+            if (s == 0) {
+                float vmax = 0.0f;
 #pragma unroll
-        for (int it = 0; it < 4; ++it)
+                for (int it = 0; it < 4; ++it)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) vmax = fmaxf(vmax, fabsf(v[it][k]));
-        const float ms = column_max(largest(S));
-        // values of k are below 2^13
-        const int er = scale_exp(column_max(vmax) + fac[kFacMax] * pow2(13) * (float)(32 * NS) * (ms * unit));
-        const float gr = pow2(er);
+                    for (int k = 0; k < 4; ++k) vmax = fmaxf(vmax, fabsf(v[it][k]));
+                ms = column_max(largest(S));
+                // R = V - e^G K S is below this, as values of k are below 2^13; U and W then are below 2^32 fu
+                const int er = scale_exp(column_max(vmax) + gmax * pow2(13) * (float)(32 * NS) * (ms * unit));
+                fu = pow2(-er) * tscale;
+                // the units of the state are those of W's operand; a state far above W keeps them in range
+                const int ew = scale_exp(fmaxf(fu * pow2(32), bound * unit * decay * pow2(-20)));
+                const float gr = pow2(er), cr = fs * gr;
+                wc2 = fu * pow2(ew);
+                keep = decay * unit * pow2(ew);
+                unit = pow2(-ew);
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const f32x4 bg = tok4(0, it);
+                for (int it = 0; it < 4; ++it)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(-(bg[r] * fs), R[it][r], v[it][r]);
-        }
-        f16x8 Rh[2], Rl[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], gr, Rh[s], Rl[s]);
-        // U = kappa T beta R, W = e^(G_C - G) U; both times 1 / fu
-        f32x4 U[4], X[4];
-        const float fu = pow2(-er) * fac[kFacT];
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            U[it] = f32x4{};
-#pragma unroll
-            for (int s = 0; s <= it / 2; ++s) {
-                const f16x8 th = *(const f16x8*)(s_t + frag_of(it, s) * 1024 + lane * 16),
-                            tl = *(const f16x8*)(s_t + (kFrags + frag_of(it, s)) * 1024 + lane * 16);
-                U[it] = mma(th, Rh[s], U[it]);
-                U[it] = mma(th, Rl[s], U[it]);
-                U[it] = mma(tl, Rh[s], U[it]);
+                    for (int r = 0; r < 4; ++r) {
+                        v[it][r] *= gr;
+                        bg[it][r] *= -cr;
+                    }
             }
-            const f32x4 w = tok4(1, it);
+            if (s == 1) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * w[r];
+                for (int it = 0; it < 4; ++it)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) wg[it][r] *= wc2;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[t][r] *= keep;
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        // S <- decay S + K^T W in the units of W's scale; a state far above W keeps the scale in range
-        const float decay = fac[kFacDecay], mw = column_max(largest(X)) * fu;
-        const int ew = scale_exp(fmaxf(mw, bound * unit * decay * pow2(-10)));
-        f16x8 Wh[2], Wl[2];
+        // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of 16 values of k,
+        // transposed as they are read
+        f16x8 Kt[PA][2][NT];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) split2<true>(X[2 * s], X[2 * s + 1], fu * pow2(ew), Wh[s], Wl[s]);
-        const float keep = decay * unit * pow2(ew);
-        // 64 products of values below 2^13
-        bound = keep * ms + mw * pow2(ew) * pow2(19);
-        unit = pow2(-ew);
-        es = scale_exp(bound);
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= keep;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of
-                // 16 values of k, transposed as they are read
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) s16x4* lds4;
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int part = 0; part < PA; ++part) {
                     s16x4 k2[2];
@@ -1005,27 +1063,80 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_num_vgpr(256))) void
                                                 qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
                         k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
                     }
-                    const f16x8 k = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    S[t] = mma(k, Wh[s], S[t]);
-                    if (part == 0) S[t] = mma(k, Wl[s], S[t]);
+                    Kt[part][s][t] = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
                 }
-            }
-            if (t & 1) split2<true>(S[t - 1], S[t], pow2(es), Sh[t / 2], Sl[t / 2]);
-        }
-        // U for the outputs
-        const int eu = scale_exp(column_max(largest(U)));
+        __builtin_amdgcn_sched_barrier(0);
+        float one = 1.0f;
+        asm volatile("" : "+s"(one));
+        f16x8 Rh[2], Rl[2];
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(bg[it][r], R[it][r], v[it][r]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], one, Rh[s], Rl[s]);
+        // U = kappa T beta R times 1 / fu
+        f32x4 U[4], X[4];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) U[it] = f32x4{};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            f16x8 uh, ul;
-            split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), uh, ul);
-            *(f16x8*)(to + (PA * NS + s) * 1024 + lane * 16) = uh;
-            if constexpr (PA == 2) *(f16x8*)(to + (PA * NS + 2 + s) * 1024 + lane * 16) = ul;
+#pragma unroll
+            for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[0][frag_of(it, s)], Rh[s], U[it]);
+#pragma unroll
+            for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[0][frag_of(it, s)], Rl[s], U[it]);
+#pragma unroll
+            for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[1][frag_of(it, s)], Rh[s], U[it]);
         }
-        if (hh == 0) {
-            float* sc = (float*)(to + (NS + 2) * PA * 1024);
-            sc[lane] = fs;
-            sc[16 + lane] = fu * pow2(-eu);
+        // W = e^(G_C - G) U, the state's update
+        f16x8 Wh[2], Wl[2];
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * wg[it][r];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) split2<true>(X[2 * s], X[2 * s + 1], one, Wh[s], Wl[s]);
+        __builtin_amdgcn_sched_barrier(0);
+        // S <- decay S + K^T W: four tiles' products, then their operands beside the next four's
+#pragma unroll
+        for (int t0 = 0; t0 < NT; t0 += 4) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int t = t0; t < t0 + 4 && t < NT; ++t) S[t] = mma(Kt[0][s][t], Wh[s], S[t]);
+#pragma unroll
+                for (int t = t0; t < t0 + 4 && t < NT; ++t) S[t] = mma(Kt[0][s][t], Wl[s], S[t]);
+                if constexpr (PA == 2) {
+#pragma unroll
+                    for (int t = t0; t < t0 + 4 && t < NT; ++t) S[t] = mma(Kt[PA - 1][s][t], Wh[s], S[t]);
+                }
+            }
+            if (t0 == 0) {
+                // 64 products of values of k below 2^13
+                bound = keep * ms + column_max(largest(X)) * pow2(19);
+                es = scale_exp(bound);
+                // U for the outputs
+                const int eu = scale_exp(column_max(largest(U)));
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    f16x8 uh, ul;
+                    split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), uh, ul);
+                    *(f16x8*)(to + (PA * NS + s) * 1024 + lane * 16) = uh;
+                    if constexpr (PA == 2) *(f16x8*)(to + (PA * NS + 2 + s) * 1024 + lane * 16) = ul;
+                }
+                if (hh == 0) {
+                    float* sc = (float*)(to + (NS + 2) * PA * 1024);
+                    sc[lane] = fs;
+                    sc[16 + lane] = fu * pow2(-eu);
+                }
+            }
+            if (t0 > 0) {
+#pragma unroll
+                for (int t = t0 - 4; t < t0; t += 2) split2<true>(S[t], S[t + 1], pow2(es), Sh[t / 2], Sl[t / 2]);
+            }
         }
+#pragma unroll
+        for (int t = (NT - 1) / 4 * 4; t < NT; t += 2) split2<true>(S[t], S[t + 1], pow2(es), Sh[t / 2], Sl[t / 2]);
     }
     if (ok && on) {
 #pragma unroll
@@ -1061,9 +1172,9 @@ DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, 
 }
 
 template <typename T, int NS, int WAVES> void main_launch(const Args& a, hipStream_t s) {
-    const unsigned blocks = (unsigned)((a.d.dv + 16 * WAVES - 1) / (16 * WAVES));
-    const dim3 grid(a.d.Hv * blocks, (unsigned)a.d.nseq);
-    if constexpr (SplitLds<T, NS, WAVES>::kFits) SSM_LAUNCH((delta_split_kernel<T, NS, WAVES>), grid, dim3(128 * WAVES), 0, s, a);
+    const dim3 grid = work_grid(a.d, (a.d.dv + 16 * WAVES - 1) / (16 * WAVES));
+    constexpr int bytes = SplitLds<T, NS, WAVES>::kBytes;
+    if constexpr (SplitLds<T, NS, WAVES>::kFits) SSM_LAUNCH((delta_split_kernel<T, NS, WAVES>), grid, dim3(128 * WAVES), bytes, s, a);
     else SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), grid, dim3(64 * WAVES), 0, s, a);
 }
 template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream_t s) {
