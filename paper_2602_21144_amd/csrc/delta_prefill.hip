@@ -3,8 +3,8 @@
 //   A_ij = beta_i e^(Gi - Gj) k_i . k_j (j < i),  T = (I + A)^-1                         no state in it
 //   R = beta V - beta e^G (K S),  U = T R,  O = e^G (Q S) + (e^(Gi - Gj) q_i . k_j)_{j <= i} U
 //   S <- e^(G_C) S + K^T (e^(G_C - Gj) U)
-// Pass 1 (delta_chunk_kernel) has a workgroup per chunk and value head: T and the masked products of queries
-// and keys. Pass 2 (delta_main_kernel) walks a sequence's chunks with the state in accumulators: columns of S
+// Pass 1 (delta_chunk_kernel) has a workgroup per chunk and q/k head: T and the masked products of queries and keys
+// of its value heads. Pass 2 (delta_main_kernel) walks a sequence's chunks with the state in accumulators: columns of S
 // need nothing of each other, so a wave owns 16 of them and talks to no other wave.
 //
 // Operands are f16, sums float32. A row of q or k is scaled by the power of two that takes its largest value to
@@ -71,15 +71,54 @@ __device__ __forceinline__ SeqRows seq_rows(const DeltaArgs& p, int i) {
 }
 __device__ __forceinline__ int chunks_of(int rows) { return (rows + kC - 1) / kC; }
 
+// Inclusive running sums over the wave's lanes, in the vector unit: from the lanes 1, 2, 4 and 8 before in a row of 16,
+// then the row before's last lane to rows 1 and 3, then row 1's to rows 2 and 3
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ int64_t dpp64(int64_t v) {
+    return (int64_t)(((uint64_t)(uint32_t)dpp<CTRL, ROWS>((int)(v >> 32)) << 32) | (uint32_t)dpp<CTRL, ROWS>((int)v));
+}
+__device__ __forceinline__ int wave_scan32(int c) {
+    c += dpp<0x111, 0xF>(c);
+    c += dpp<0x112, 0xF>(c);
+    c += dpp<0x114, 0xF>(c);
+    c += dpp<0x118, 0xF>(c);
+    c += dpp<0x142, 0xA>(c);
+    return c + dpp<0x143, 0xC>(c);
+}
+__device__ __forceinline__ int64_t wave_scan64(int64_t c) {
+    c += dpp64<0x111, 0xF>(c);
+    c += dpp64<0x112, 0xF>(c);
+    c += dpp64<0x114, 0xF>(c);
+    c += dpp64<0x118, 0xF>(c);
+    c += dpp64<0x142, 0xA>(c);
+    return c + dpp64<0x143, 0xC>(c);
+}
+
+// The largest of the wave's values, none of them negative (their bits compare like they do)
+__device__ __forceinline__ float wave_max(float v) {
+    int c = __builtin_bit_cast(int, v);
+    c = max(c, dpp<0x111, 0xF>(c));
+    c = max(c, dpp<0x112, 0xF>(c));
+    c = max(c, dpp<0x114, 0xF>(c));
+    c = max(c, dpp<0x118, 0xF>(c));
+    c = max(c, dpp<0x142, 0xA>(c));
+    c = max(c, dpp<0x143, 0xC>(c));
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(c, 63));
+}
+// over four neighbouring lanes
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __builtin_bit_cast(float, dpp<0xB1, 0xF>(__builtin_bit_cast(int, v)));
+    return v + __builtin_bit_cast(float, dpp<0x4E, 0xF>(__builtin_bit_cast(int, v)));
+}
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __builtin_bit_cast(float, dpp<0xB1, 0xF>(__builtin_bit_cast(int, v))));
+    return fmaxf(v, __builtin_bit_cast(float, dpp<0x4E, 0xF>(__builtin_bit_cast(int, v))));
+}
+
 // exclusive running sum of v over the 256 threads; total: the whole sum
 __device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
     const int tid = threadIdx.x;
-    int c = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_up(c, off, 64);
-        if ((tid & 63) >= off) c += o;
-    }
+    const int c = wave_scan32(v);
     if ((tid & 63) == 63) lds[tid >> 6] = c;
     __syncthreads();
     int before = 0;
@@ -133,56 +172,58 @@ __device__ __forceinline__ f32x4 mma4(float a, float b, const f32x4& c) {
 // ---------------------------------------------------------------- pass 1
 constexpr int kLdA = kC + 4;   // row stride of the 64 x 64 float32 matrix
 
-// This thread's 8-value pieces of a row of q or k: scaled to f16 parts in operand layout. Returns the sum of squares
-// of the row; e: the exponent of its scale.
+template <typename T> struct Piece {   // eight values of a row
+    u32x4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t& r, uint32_t off) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = buffer_load16(r, off + 16 * i);
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        T x[8];
+        __builtin_memcpy(x, w, sizeof x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = to_f32(x[k]);
+    }
+};
+
+// The pieces of a row of q or k that this thread (c4 of four) holds: scaled to f16 parts in operand layout, to LDS. Returns
+// the sum of squares of the row; e: the exponent of its scale.
 template <typename T, int NS>
-__device__ __forceinline__ float stage_row(const __amdgpu_buffer_rsrc_t& r, uint32_t off, int dk, int row, int c4, char* lds, int* e) {
-    float v[NS][8], ss = 0.0f, m = 0.0f;
+__device__ __forceinline__ float stage_row(const Piece<T> (&x)[NS], int row, int c4, char* lds, int* e) {
+    float ss = 0.0f, m = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const int n = 32 * s + 8 * c4;
-        const uint32_t at = n < dk ? off + n * (uint32_t)sizeof(T) : kOffOutOfRange;
-        T x[8];
-        u32x4 raw[sizeof(T) / 2];
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = buffer_load16(r, n < dk ? at + 16 * i : at);
-        __builtin_memcpy(x, raw, sizeof x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[s][k] = to_f32(x[k]);
-    }
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
+        float v[8];
+        x[s].values(v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            ss = __builtin_fmaf(v[s][k], v[s][k], ss);
-            m = fmaxf(m, fabsf(v[s][k]));
+            ss = __builtin_fmaf(v[k], v[k], ss);
+            m = fmaxf(m, fabsf(v[k]));
         }
-    ss += __shfl_xor(ss, 1, 64);
-    ss += __shfl_xor(ss, 2, 64);
-    m = fmaxf(m, __shfl_xor(m, 1, 64));
-    m = fmaxf(m, __shfl_xor(m, 2, 64));
-    *e = scale_exp(m);
+    }
+    ss = quad_sum(ss);
+    *e = scale_exp(quad_max(m));
     const float f = pow2(*e);
-    const int it = row >> 4;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        float x[8];
+        float v[8];
+        x[s].values(v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = v[s][k] * f;
+        for (int k = 0; k < 8; ++k) v[k] *= f;
 #pragma unroll
         for (int part = 0; part < kParts<T>; ++part) {
-            const f16x8 h = pair_f16(x, 0);
+            const f16x8 h = pair_f16(v, 0);
             // values 0..3 of the piece are (hh, half) = (2 (c4 & 1), c4 / 2), values 4..7 the next hh
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 f16x4 o;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[k] = h[4 * q + k];
-                char* unit = lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(row & 15, 2 * (c4 & 1) + q)) * 16 + (c4 >> 1) * 8;
-                *(f16x4*)unit = o;
+                const int at = (((part * 4 + (row >> 4)) * NS + s) * 64 + qk_unit(row & 15, 2 * (c4 & 1) + q)) * 16 + (c4 >> 1) * 8;
+                *(f16x4*)(lds + at) = o;
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] -= (float)h[k];
+            for (int k = 0; k < 8; ++k) v[k] -= (float)h[k];
         }
     }
     return ss;
@@ -192,26 +233,32 @@ template <int NS> __device__ __forceinline__ f16x8 qk_piece(const char* lds, int
     return *(const f16x8*)(lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(lane & 15, lane >> 4)) * 16);
 }
 
-template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk_kernel(Args a) {
-    constexpr int PA = kParts<T>;
-    __shared__ __attribute__((aligned(16))) char s_k[qk_bytes(NS, PA)], s_q[qk_bytes(NS, PA)];
-    __shared__ __attribute__((aligned(16))) float s_t[kC * kLdA];
-    __shared__ __attribute__((aligned(16))) float s_gh[kC], s_gl[kC], s_beta[kC], s_kap[kC], s_c[kC];
-    __shared__ float s_max[4];
+// One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves.
+// HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
+// is not stored.
+template <typename T, int NS, int HB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void delta_chunk_kernel(Args a) {
+    constexpr int PA = kParts<T>, kQk = (int)qk_bytes(NS, PA);
+    // q's pieces, and once they are used the heads' matrices in their place
+    constexpr int kMat = HB * kC * kLdA * 4;
+    __shared__ __attribute__((aligned(16))) char s_k[kQk], s_q[kQk > kMat ? kQk : kMat];
+    float(*s_t)[kC * kLdA] = (float(*)[kC * kLdA])s_q;
+    __shared__ __attribute__((aligned(16))) float s_gh[HB][kC], s_gl[HB][kC], s_beta[HB][kC], s_kap[kC], s_c[kC];
+    __shared__ float s_max[HB][4];
     __shared__ int s_find[8];
     const DeltaArgs& p = a.d;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, slot = blockIdx.x, h = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = blockIdx.x, hk = blockIdx.y;
     int seq = -1, chunk = 0;
     if (p.nseq <= kFindSeqs) {
         int n = 0, total;
         if (tid < p.nseq) {
             const SeqRows r = seq_rows(p, tid);
             n = chunks_of(r.n);
-            if (!r.ok && slot == 0 && h == 0) atomicOr(p.status, SSM_STATUS_BAD_SEQLENS);
+            if (!r.ok && slot == 0 && hk == 0) atomicOr(p.status, SSM_STATUS_BAD_SEQLENS);
         }
         if (tid == 0) s_find[4] = -1;
         const int at = block_scan(n, s_find, &total);
-        if (slot == 0 && h == 0 && tid < p.nseq) a.w.base[tid] = at;
+        if (slot == 0 && hk == 0 && tid < p.nseq) a.w.base[tid] = at;
         if (slot >= at && slot < at + n) {
             s_find[4] = tid;
             s_find[5] = slot - at;
@@ -230,215 +277,290 @@ template <typename T, int NS> __global__ __launch_bounds__(256) void delta_chunk
     const SeqRows sr = seq_rows(p, seq);
     const int64_t t0 = (int64_t)__builtin_amdgcn_readfirstlane(sr.lo) + (int64_t)chunk * kC;
     const int nq = min(__builtin_amdgcn_readfirstlane(sr.n) - chunk * kC, kC);
-    const int hk = h / p.rep;
 
     // rows of q and k: four threads to a row
     const __amdgpu_buffer_rsrc_t rx = buffer_rsrc((const T*)p.qkv + t0 * p.ld, (uint32_t)((nq - 1) * p.ld + 2 * p.Hk * p.dk) * sizeof(T));
     const int row = tid >> 2, c4 = tid & 3;
-    const uint32_t off = row < nq ? (uint32_t)(row * p.ld + hk * p.dk) * (uint32_t)sizeof(T) : kOffOutOfRange;
-    float av = 0.0f, bv = 0.0f;
-    if (tid < nq) {
-        av = to_f32(((const T*)p.a)[(t0 + tid) * p.ld_ab + h]);
-        bv = to_f32(((const T*)p.b)[(t0 + tid) * p.ld_ab + h]);
+    Piece<T> xq[NS], xk[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const int n = 32 * s + 8 * c4;
+        const uint32_t off = row < nq && n < p.dk ? (uint32_t)(row * p.ld + hk * p.dk + n) * (uint32_t)sizeof(T) : kOffOutOfRange;
+        xk[s].load(rx, off + (uint32_t)(p.Hk * p.dk) * (uint32_t)sizeof(T));
+        xq[s].load(rx, off);
     }
+    // the gates of a value head by wave 2 or 3, a token a lane; into place b
+    float av = 0.0f, bv = 0.0f;
+    auto gate_loads = [&](int h) {
+        if (lane < nq) {
+            av = to_f32(((const T*)p.a)[(t0 + lane) * p.ld_ab + h]);
+            bv = to_f32(((const T*)p.b)[(t0 + lane) * p.ld_ab + h]);
+        }
+    };
+    if (wave >= 2 && wave - 2 < HB) gate_loads(hk * p.rep + wave - 2);
+    auto gates = [&](int h, int b) {
+        // log2 of alpha; below -1000 it is 0 in float32 either way, and the sums of what follows stay exact. The running
+        // sum in 64 bits of 2^-40 (its absolute error is what counts), kept as two float32 values: what comes
+        // after a reset is as exact as without one
+        float g = -fast_exp2(p.A_log[h] * kLog2e) * kLog2e * softplus_f(av + p.dt_bias[h]);
+        const bool nan = g != g;
+        g = lane < nq ? (g < -1000.0f ? -1000.0f : g) : 0.0f;
+        const int64_t c = wave_scan64(nan ? 0 : (int64_t)((double)g * 1099511627776.0));
+        const double d = (double)c * (1.0 / 1099511627776.0);
+        // a decay that is no number leaves none from its token on
+        const bool bad = (__ballot(nan && lane < nq) & (~0ull >> (63 - lane))) != 0;
+        s_gh[b][lane] = bad ? __builtin_nanf("") : (float)d;
+        s_gl[b][lane] = (float)(d - (double)(float)d);
+        s_beta[b][lane] = lane < nq ? p.beta_max * sigmoid_f(bv) : 0.0f;
+    };
     int eq, ek;
-    const float sq = stage_row<T, NS>(rx, off, row < nq ? p.dk : 0, row, c4, s_q, &eq);
-    const float sk = stage_row<T, NS>(rx, off + (uint32_t)(p.Hk * p.dk) * (uint32_t)sizeof(T), row < nq ? p.dk : 0, row, c4, s_k, &ek);
+    const float sk = stage_row<T, NS>(xk, row, c4, s_k, &ek);
+    const float sq = stage_row<T, NS>(xq, row, c4, s_q, &eq);
     if (c4 == 0) {
         s_c[row] = p.scale * (p.qk_norm ? 1.0f / sqrtf(fmaxf(sq + p.eps, 1.2e-38f)) : 1.0f) * pow2(-eq);
         s_kap[row] = (p.qk_norm ? 1.0f / sqrtf(fmaxf(sk + p.eps, 1.2e-38f)) : 1.0f) * pow2(-ek);
     }
-    if (tid < kC) {
-        // log2 of alpha; below -1000 it is 0 in float32 either way, and the sums of what follows stay exact. The running
-        // sum in 64 bits, kept as two float32 values: what comes after a reset is as exact as without one
-        float g = -fast_exp2(p.A_log[h] * kLog2e) * kLog2e * softplus_f(av + p.dt_bias[h]);
-        g = tid < nq ? (g < -1000.0f ? -1000.0f : g) : 0.0f;
-        double c = (double)g;
+    if (wave >= 2 && wave - 2 < HB) gates(hk * p.rep + wave - 2, wave - 2);
+    __syncthreads();
+
+    // K K^T and K Q^T: wave w has columns i = 16 w + lane % 16, pieces n of rows j = 32 n + 16 q + 4 hh + r up to the
+    // diagonal: one piece for waves 0 and 1, two for the others
+    const int hh = lane >> 4, col = lane & 15, it = wave, i = 16 * it + col, pieces = 1 + it / 2;
+    const bool odd = (it & 1) != 0;                    // the second tile of the last piece reaches the diagonal
+    const float kap = s_kap[i];
+    f32x4 kk[2][2], kq[2][2];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const double up = __shfl_up(c, o, 64);
-            if (tid >= o) c += up;
+    for (int n = 0; n < 2; ++n) {
+        if (n >= pieces) break;
+        kk[n][0] = kk[n][1] = kq[n][0] = kq[n][1] = f32x4{};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const f16x8 y = qk_piece<NS>(s_k, 0, it, s, lane), z = qk_piece<NS>(s_q, 0, it, s, lane);
+            f16x8 yl{}, zl{};
+            if constexpr (PA == 2) {
+                yl = qk_piece<NS>(s_k, 1, it, s, lane);
+                zl = qk_piece<NS>(s_q, 1, it, s, lane);
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (q == 1 && n + 1 == pieces && !odd) break;
+                const f16x8 x = qk_piece<NS>(s_k, 0, 2 * n + q, s, lane);
+                kk[n][q] = mma(x, y, kk[n][q]);
+                kq[n][q] = mma(x, z, kq[n][q]);
+                if constexpr (PA == 2) {
+                    const f16x8 xl = qk_piece<NS>(s_k, 1, 2 * n + q, s, lane);
+                    kk[n][q] = mma(xl, y, kk[n][q]);
+                    kq[n][q] = mma(xl, z, kq[n][q]);
+                    kk[n][q] = mma(x, yl, kk[n][q]);
+                    kq[n][q] = mma(x, zl, kq[n][q]);
+                }
+            }
         }
-        s_gh[tid] = (float)c;
-        s_gl[tid] = (float)(c - (double)(float)c);
-        s_beta[tid] = tid < nq ? p.beta_max * sigmoid_f(bv) : 0.0f;
+    }
+    char* qk = a.w.qk + ((int64_t)slot * p.Hk + hk) * (2 * kQk);
+#pragma unroll
+    for (int n = 0; n < kQk / 4096; ++n) {
+        const int u = (n * 256 + tid) * 16;
+        *(u32x4*)(qk + u) = *(const u32x4*)(s_k + u);
+        *(u32x4*)(qk + kQk + u) = *(const u32x4*)(s_q + u);
     }
     __syncthreads();
 
-    // wave w: columns i = 16 w + lane % 16 of K K^T and K Q^T, rows j = 16 jt + 4 hh + r
-    const int hh = lane >> 4, i = 16 * wave + (lane & 15);
-    char* vout = a.w.v + ((int64_t)slot * p.Hv + h) * v_bytes(PA);
-    {
-        const float gh = s_gh[i], gl = s_gl[i], bk = s_beta[i] * s_kap[i];
-        float pv[2][4];
+    for (int r0 = 0; r0 < p.rep; r0 += HB) {
+        const int heads = min(HB, p.rep - r0);
+        auto vout = [&](int b) { return a.w.v + ((int64_t)slot * p.Hv + hk * p.rep + r0 + b) * v_bytes(PA); };
+        if (r0 > 0) {
+            __syncthreads();
+            if (wave >= 2 && wave - 2 < heads) {
+                gate_loads(hk * p.rep + r0 + wave - 2);
+                gates(hk * p.rep + r0 + wave - 2, wave - 2);
+            }
+            __syncthreads();
+        }
+        float gh[HB], gl[HB], bk[HB];
 #pragma unroll
-        for (int jt = 0; jt < 4; ++jt) {
-            if (jt > wave && jt % 2 == 0) break;
-            f32x4 kk{}, kq{};
-            if (jt <= wave) {
+        for (int b = 0; b < HB; ++b) {
+            gh[b] = s_gh[b][i];
+            gl[b] = s_gl[b][i];
+            bk[b] = s_beta[b][i] * kap;
+        }
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const f16x8 x = qk_piece<NS>(s_k, 0, jt, s, lane), y = qk_piece<NS>(s_k, 0, wave, s, lane),
-                                z = qk_piece<NS>(s_q, 0, wave, s, lane);
-                    kk = mma(x, y, kk);
-                    kq = mma(x, z, kq);
-                    if constexpr (PA == 2) {
-                        const f16x8 xl = qk_piece<NS>(s_k, 1, jt, s, lane);
-                        kk = mma(xl, y, kk);
-                        kq = mma(xl, z, kq);
-                        kk = mma(x, qk_piece<NS>(s_k, 1, wave, s, lane), kk);
-                        kq = mma(x, qk_piece<NS>(s_q, 1, wave, s, lane), kq);
-                    }
+        for (int n = 0; n < 2; ++n) {
+            if (n >= pieces) break;
+            float x[HB][8];
+            f32x4 jh[HB][2], jl[HB][2], jk[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int j = 32 * n + 16 * q + 4 * hh;
+                jk[q] = *(const f32x4*)&s_kap[j];
+#pragma unroll
+                for (int b = 0; b < HB; ++b) {
+                    jh[b][q] = *(const f32x4*)&s_gh[b][j];
+                    jl[b][q] = *(const f32x4*)&s_gl[b][j];
                 }
             }
-            const int j0 = 16 * jt + 4 * hh;
-            const float4 jh = *(const float4*)&s_gh[j0], jl = *(const float4*)&s_gl[j0], jk = *(const float4*)&s_kap[j0];
-            const float jhv[4] = {jh.x, jh.y, jh.z, jh.w}, jlv[4] = {jl.x, jl.y, jl.z, jl.w}, jkv[4] = {jk.x, jk.y, jk.z, jk.w};
-            f32x4 av4;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float ex = fast_exp2((gh - jhv[r]) + (gl - jlv[r]));
-                av4[r] = j0 + r < i ? kk[r] * ex * (bk * jkv[r]) : 0.0f;
-                pv[jt & 1][r] = j0 + r <= i ? kq[r] * ex * pow2(-20) : 0.0f;
-            }
-            if (jt <= wave) *(f32x4*)&s_t[i * kLdA + j0] = av4;
-            if (jt & 1) {
-                float x[8] = {pv[0][0], pv[0][1], pv[0][2], pv[0][3], pv[1][0], pv[1][1], pv[1][2], pv[1][3]};
+            for (int b = 0; b < HB; ++b)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int j = 32 * n + 16 * q + 4 * hh;
+                    f32x4 m;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float ex = fast_exp2((gh[b] - jh[b][q][r]) + (gl[b] - jl[b][q][r]));
+                        m[r] = j + r < i ? kk[n][q][r] * ex * (bk[b] * jk[q][r]) : 0.0f;
+                        x[b][4 * q + r] = j + r <= i ? kq[n][q][r] * ex * pow2(-20) : 0.0f;
+                    }
+                    *(f32x4*)&s_t[b][i * kLdA + j] = m;   // zeros above the diagonal, where this piece has them
+                }
+#pragma unroll
+            for (int b = 0; b < HB; ++b) {
+                if (b >= heads) break;
+                char* to = vout(b) + t_bytes() + (frag_of(it, n) * 1024 + lane * 16);
 #pragma unroll
                 for (int part = 0; part < PA; ++part) {
-                    const f16x8 o = pair_f16(x, 0);
-                    *(f16x8*)(vout + t_bytes() + (size_t)(part * kFrags + frag_of(wave, jt >> 1)) * 1024 + lane * 16) = o;
+                    const f16x8 o = pair_f16(x[b], 0);
+                    *(f16x8*)(to + part * kFrags * 1024) = o;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] -= (float)o[e];
+                    for (int e = 0; e < 8; ++e) x[b][e] -= (float)o[e];
                 }
             }
         }
-    }
-    // q and k for pass 2, once per q/k head
-    if (h % p.rep == 0) {
-        char* qk = a.w.qk + ((int64_t)slot * p.Hk + hk) * (2 * qk_bytes(NS, PA));
-        for (int u = tid; u < (int)qk_bytes(NS, PA) / 16; u += 256) {
-            *(u32x4*)(qk + u * 16) = *(const u32x4*)(s_k + u * 16);
-            *(u32x4*)(qk + qk_bytes(NS, PA) + u * 16) = *(const u32x4*)(s_q + u * 16);
-        }
-    }
-    // the tokens' factors
-    float* fac = (float*)(vout + t_bytes() - kFacBytes);
-    if (tid < kC) {
-        float* f = (float*)(vout + v_bytes(PA) - kOutFacBytes);
-        const float gh = s_gh[tid], gl = s_gl[tid], ch = s_gh[kC - 1], cl = s_gl[kC - 1];
-        const float eg = fast_exp2(gh + gl), bg = eg * s_kap[tid];
-        fac[tid] = bg;
-        fac[kC + tid] = fast_exp2((ch - gh) + (cl - gl));
-        float m = bg;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        if (tid == 0) {
-            fac[kFacDecay] = fast_exp2(ch + cl);
-            fac[kFacMax] = m;
-        }
-        f[tid] = s_c[tid] * eg;
-        f[kC + tid] = s_c[tid] * pow2(20);
-    }
-    __syncthreads();
-
-    // T = (I + A)^-1 in place, in float32: the diagonal 16 x 16 blocks by substitution (lane: block and column), then
-    // [T1 0; -T2 A21 T1 T2] for blocks of 16 and of 32
-    if (wave == 0) {
-        const int b0 = 16 * hh, c = lane & 15;
-        float x[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            float s = r == c ? 1.0f : 0.0f;
-#pragma unroll
-            for (int j4 = 0; j4 < 16; j4 += 4) {
-                if (j4 >= r) break;
-                const f32x4 m = *(const f32x4*)&s_t[(b0 + r) * kLdA + b0 + j4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j4 + e < r) s = __builtin_fmaf(-m[e], x[j4 + e], s);
-            }
-            x[r] = s;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s_t[(b0 + r) * kLdA + b0 + c] = x[r];
-    }
-    __syncthreads();
-    const int col = lane & 15;
-    // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column
-    auto row4 = [&](int r0, int c0) { return *(const f32x4*)&s_t[(r0 + col) * kLdA + c0 + 4 * hh]; };
-    auto times = [&](f32x4 m, const f32x4& x, f32x4 acc) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc = mma4(m[r], x[r], acc);
-        return acc;
-    };
-    auto col4 = [&](int r0, int c0) {
-        f32x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = s_t[(r0 + 4 * hh + r) * kLdA + c0 + col];
-        return v;
-    };
-    auto put = [&](int r0, int c0, const f32x4& v) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s_t[(r0 + 4 * hh + r) * kLdA + c0 + col] = -v[r];
-    };
-    if (wave < 2) {
-        const int c0 = 32 * wave, r0 = c0 + 16;
-        const f32x4 x = times(row4(r0, c0), col4(c0, c0), f32x4{});
-        put(r0, c0, times(row4(r0, r0), x, f32x4{}));
-    }
-    __syncthreads();
-    {
-        const int r2 = wave >> 1, c0 = 16 * (wave & 1);
-        f32x4 x[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            x[k] = f32x4{};
-            if ((wave & 1) == 0) x[k] = times(row4(32 + 16 * k, 0), col4(0, c0), x[k]);
-            x[k] = times(row4(32 + 16 * k, 16), col4(16, c0), x[k]);
-        }
-        f32x4 y = times(row4(32 + 16 * r2, 32), x[0], f32x4{});
-        if (r2 == 1) y = times(row4(48, 48), x[1], y);
         __syncthreads();
-        put(32 + 16 * r2, c0, y);
-    }
-    __syncthreads();
-    // kappa T beta, scaled by the power of two that takes its largest value to 2^12
-    float x[2][8], m = 0.0f;
+        // T = (I + A)^-1 in place, in float32: the diagonal 16 x 16 blocks by substitution (lane: block and column), then
+        // [T1 0; -T2 A21 T1 T2] for blocks of 16 and of 32. One wave per head, then two, then all for each
+        if (wave < HB) {
+            float* t = s_t[wave] + 16 * hh * kLdA + 16 * hh;
+            // row r in pieces of four, asked for in two lots in front of their use
+            constexpr int kCut = 12;
+            f32x4 m[16][4];
+            float x[16];
+            auto ask = [&](int r0, int r1) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        const int f = wave + 4 * n;
-        if (f >= kFrags) continue;
-        const int it = f < 2 ? f : 2 + (f - 2) / 2, s = f < 2 ? 0 : (f - 2) & 1;
-        const f32x4 v0 = row4(16 * it, 32 * s);
-        const f32x4 v1 = 2 * s + 1 <= it ? row4(16 * it, 32 * s + 16) : f32x4{};
-        const f32x4 b0 = *(const f32x4*)&s_beta[32 * s + 4 * hh], b1 = *(const f32x4*)&s_beta[32 * s + 16 + 4 * hh];
-        const float ka = s_kap[16 * it + col];
+                for (int r = r0; r < r1; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[n][e] = v0[e] * b0[e] * ka;
-            x[n][4 + e] = v1[e] * b1[e] * ka;
-            m = fmaxf(m, fmaxf(fabsf(x[n][e]), fabsf(x[n][4 + e])));
+                    for (int j = 0; 4 * j < r; ++j) m[r][j] = *(const f32x4*)&t[r * kLdA + 4 * j];
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto solve = [&](int r0, int r1) {
+#pragma unroll
+                for (int r = r0; r < r1; ++r) {
+                    float s = r == col ? 1.0f : 0.0f;
+#pragma unroll
+                    for (int j = 0; j < r; ++j) s = __builtin_fmaf(-m[r][j / 4][j % 4], x[j], s);
+                    x[r] = s;
+                }
+            };
+            ask(1, kCut);
+            solve(0, kCut);
+            ask(kCut, 16);
+            solve(kCut, 16);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) t[r * kLdA + col] = x[r];
         }
-    }
+        // the tokens' factors, by waves 2 and 3
+        if (wave >= 2 && wave - 2 < heads) {
+            const int b = wave - 2;
+            float *fac = (float*)(vout(b) + t_bytes() - kFacBytes), *f = (float*)(vout(b) + v_bytes(PA) - kOutFacBytes);
+            const float gh = s_gh[b][lane], gl = s_gl[b][lane], ch = s_gh[b][kC - 1], cl = s_gl[b][kC - 1];
+            const float eg = fast_exp2(gh + gl), bg = eg * s_kap[lane];
+            fac[lane] = bg;
+            fac[kC + lane] = fast_exp2((ch - gh) + (cl - gl));
+            const float m = wave_max(bg);
+            if (lane == 0) {
+                fac[kFacDecay] = fast_exp2(ch + cl);
+                fac[kFacMax] = m;
+            }
+            f[lane] = s_c[lane] * eg;
+            f[kC + lane] = s_c[lane] * pow2(20);
+        }
+        __syncthreads();
+        // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column
+        auto row4 = [&](const float* t, int y, int x) { return *(const f32x4*)&t[(y + col) * kLdA + x + 4 * hh]; };
+        auto col4 = [&](const float* t, int y, int x) {
+            f32x4 v;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if (lane == 0) s_max[wave] = m;
-    __syncthreads();
-    const int et = scale_exp(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])));
-    if (tid == 0) fac[kFacT] = pow2(-et);
+            for (int r = 0; r < 4; ++r) v[r] = t[(y + 4 * hh + r) * kLdA + x + col];
+            return v;
+        };
+        auto times = [&](const f32x4& m, const f32x4& x, f32x4 acc) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        const int f = wave + 4 * n;
-        if (f >= kFrags) continue;
+            for (int r = 0; r < 4; ++r) acc = mma4(m[r], x[r], acc);
+            return acc;
+        };
+        auto put = [&](float* t, int y, int x, const f32x4& v) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[n][e] *= pow2(et);
+            for (int r = 0; r < 4; ++r) t[(y + 4 * hh + r) * kLdA + x + col] = -v[r];
+        };
+        if (wave < 2 * HB) {
+            float* t = s_t[wave >> 1];
+            const int c0 = 32 * (wave & 1), y0 = c0 + 16;
+            const f32x4 x = times(row4(t, y0, c0), col4(t, c0, c0), f32x4{});
+            put(t, y0, c0, times(row4(t, y0, y0), x, f32x4{}));
+        }
+        __syncthreads();
+        {
+            const int r2 = wave >> 1, c0 = 16 * (wave & 1);
+            // [T1 0; T21 T2] again, in 16 x 16 blocks; what lies above the diagonal is not stored and counts as zero
+            f32x4 y[HB];
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const f16x8 o = pair_f16(x[n], 0);
-            *(f16x8*)(vout + (size_t)(part * kFrags + f) * 1024 + lane * 16) = o;
+            for (int b = 0; b < HB; ++b) {
+                const float* t = s_t[b];
+                const f32x4 zero{}, t0 = col4(t, 0, 0), t1 = col4(t, 16, c0);
+                const f32x4 u0 = (wave & 1) == 0 ? t0 : zero;
+                f32x4 x[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[n][e] -= (float)o[e];
+                for (int k = 0; k < 2; ++k) x[k] = times(row4(t, 32 + 16 * k, 16), t1, times(row4(t, 32 + 16 * k, 0), u0, zero));
+                const f32x4 m1 = r2 == 1 ? row4(t, 48, 48) : zero;
+                y[b] = times(m1, x[1], times(row4(t, 32 + 16 * r2, 32), x[0], zero));
+            }
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < HB; ++b) put(s_t[b], 32 + 16 * r2, c0, y[b]);
+        }
+        __syncthreads();
+        // kappa T beta, scaled by the power of two that takes its largest value to 2^12; wave w has row tile w
+        float x[HB][2][8];
+#pragma unroll
+        for (int b = 0; b < HB; ++b) {
+            float m = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                if (n >= pieces) break;
+                const f32x4 v0 = row4(s_t[b], 16 * it, 32 * n), v1 = row4(s_t[b], 16 * it, 32 * n + 16);
+                const f32x4 b0 = *(const f32x4*)&s_beta[b][32 * n + 4 * hh], b1 = *(const f32x4*)&s_beta[b][32 * n + 16 + 4 * hh];
+                const bool two = odd || n + 1 < pieces;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[b][n][e] = v0[e] * b0[e] * kap;
+                    x[b][n][4 + e] = two ? v1[e] * b1[e] * kap : 0.0f;
+                    m = fmaxf(m, fmaxf(fabsf(x[b][n][e]), fabsf(x[b][n][4 + e])));
+                }
+            }
+            m = wave_max(m);
+            if (lane == 0) s_max[b][wave] = m;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < HB; ++b) {
+            if (b >= heads) break;
+            const int et = scale_exp(fmaxf(fmaxf(s_max[b][0], s_max[b][1]), fmaxf(s_max[b][2], s_max[b][3])));
+            const float f = pow2(et);
+            if (tid == 0) ((float*)(vout(b) + t_bytes() - kFacBytes))[kFacT] = pow2(-et);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                if (n >= pieces) break;
+                char* to = vout(b) + (frag_of(it, n) * 1024 + lane * 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[b][n][e] *= f;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const f16x8 o = pair_f16(x[b][n], 0);
+                    *(f16x8*)(to + part * kFrags * 1024) = o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[b][n][e] -= (float)o[e];
+                }
+            }
         }
     }
 }
@@ -1185,7 +1307,9 @@ template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream
     }
     {
         KernelTimer kt("delta.chunk", s);
-        SSM_LAUNCH((delta_chunk_kernel<T, NS>), dim3((unsigned)a.w.slots, (unsigned)p.Hv), dim3(256), 0, s, a);
+        const dim3 grid((unsigned)a.w.slots, (unsigned)p.Hk);
+        if (p.rep == 1) SSM_LAUNCH((delta_chunk_kernel<T, NS, 1>), grid, dim3(256), 0, s, a);
+        else SSM_LAUNCH((delta_chunk_kernel<T, NS, 2>), grid, dim3(256), 0, s, a);
     }
     KernelTimer kt("delta.main", s);
     const int64_t pairs = (int64_t)p.nseq * p.Hv, n2 = pairs * ((p.dv + 31) / 32), n4 = pairs * ((p.dv + 63) / 64);
