@@ -24,14 +24,18 @@ __device__ __forceinline__ float dot4(const f32x4& x, const f32x4& y, float s) {
     for (int e = 0; e < 4; ++e) s = __builtin_fmaf(x[e], y[e], s);
     return s;
 }
+// over eight neighbouring lanes, complete in each: by DPP within four, then from the mirrored lane of the eight
+template <int CTRL> __device__ __forceinline__ float dpp_f32(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
 __device__ __forceinline__ float sum8(float v) {
-    v += __shfl_xor(v, 1, 64);
-    v += __shfl_xor(v, 2, 64);
-    return v + __shfl_xor(v, 4, 64);
+    v += dpp_f32<0xB1>(v);    // quad_perm: lane ^ 1
+    v += dpp_f32<0x4E>(v);    // lane ^ 2
+    return v + dpp_f32<0x141>(v);   // row_half_mirror: lane ^ 7, whose quad holds the other sum
 }
 
 // one token's q and k of a head (q scaled, both normalised where the descriptor says so) and its
-// decay and write strength
+// decay and write strength: asked for, then worked out
 template <typename T, int NJ> struct Token {
     f32x4 q[NJ], k[NJ];
     float alpha, beta;
@@ -42,9 +46,12 @@ template <typename T, int NJ> struct Token {
             q[j] = head4(pq, 32 * j + 4 * lane8, p.dk);
             k[j] = head4(pq + p.Hk * p.dk, 32 * j + 4 * lane8, p.dk);
         }
-        const float av = to_f32(((const T*)p.a)[t * p.ld_ab + h]), bv = to_f32(((const T*)p.b)[t * p.ld_ab + h]);
-        alpha = fast_exp2(-fast_exp2(p.A_log[h] * kLog2e) * kLog2e * softplus_f(av + p.dt_bias[h]));
-        beta = p.beta_max * sigmoid_f(bv);
+        alpha = to_f32(((const T*)p.a)[t * p.ld_ab + h]) + p.dt_bias[h];
+        beta = to_f32(((const T*)p.b)[t * p.ld_ab + h]);
+    }
+    __device__ __forceinline__ void form(const DeltaArgs& p, float a_log) {
+        alpha = fast_exp2(-fast_exp2(a_log * kLog2e) * kLog2e * softplus_f(alpha));
+        beta = p.beta_max * sigmoid_f(beta);
         float rq = p.scale, rk = 1.0f;
         if (p.qk_norm) {
             float sq = 0.0f, sk = 0.0f;
@@ -81,23 +88,38 @@ __device__ __forceinline__ float row_step(f32x4 (&S)[NJ], const Token<T, NJ>& x,
     return sum8(o);
 }
 
-template <int NJ> __device__ __forceinline__ void row_load(f32x4 (&S)[NJ], const float* row, int lane8, int dk) {
+// PAST: past the caches, for states that they would not keep until the next step
+template <bool PAST, int NJ> __device__ __forceinline__ void row_load(f32x4 (&S)[NJ], const float* row, int lane8, int dk) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) S[j] = head4(row, 32 * j + 4 * lane8, dk);
+    for (int j = 0; j < NJ; ++j) {
+        const f32x4* at = (const f32x4*)(row + 32 * j + 4 * lane8);
+        S[j] = f32x4{};
+        if (32 * j + 4 * lane8 < dk) S[j] = PAST ? __builtin_nontemporal_load(at) : *at;
+    }
 }
-template <int NJ> __device__ __forceinline__ void row_store(const f32x4 (&S)[NJ], float* row, int lane8, int dk) {
+template <bool PAST, int NJ> __device__ __forceinline__ void row_store(const f32x4 (&S)[NJ], float* row, int lane8, int dk) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-        if (32 * j + 4 * lane8 < dk) *(f32x4*)(row + 32 * j + 4 * lane8) = S[j];
+    for (int j = 0; j < NJ; ++j) {
+        f32x4* at = (f32x4*)(row + 32 * j + 4 * lane8);
+        if (32 * j + 4 * lane8 >= dk) continue;
+        if constexpr (PAST) __builtin_nontemporal_store(S[j], at);
+        else *at = S[j];
+    }
 }
 
 // ---------------------------------------------------------------- single tokens
-// One workgroup per (head, sequence): 32 rows a pass, NP passes' rows in flight together.
-template <typename T, int NJ, int NP> __global__ __launch_bounds__(256) void delta_decode_kernel(DeltaArgs p) {
+// One workgroup per (head, sequence): 32 rows a pass, NP passes' rows in flight together, what needs no state worked out
+// meanwhile. Bound by the states' traffic: 256 sequences of 16 heads of 128 x 128 (537 MB) 104 us, 5.2 TB/s; one sequence
+// 5.5 us, a launch and two round trips (slot, then state).
+template <typename T, int NJ, int NP, bool PAST> __global__ __launch_bounds__(256) void delta_decode_kernel(DeltaArgs p) {
     __shared__ float s_o[512], s_sum[4];
     const int h = blockIdx.x, tid = threadIdx.x, lane8 = tid & 7;
     const int64_t i = blockIdx.y;
     const int slot = p.slot[i];
+    const T* x = (const T*)p.qkv + i * p.ld;
+    Token<T, NJ> tok;
+    tok.load(p, x, i, h, lane8);
+    const float a_log = p.A_log[h];
     const bool ok = slot >= 0 && slot < p.S;
     T* out = (T*)p.out + i * p.ld_out + h * p.dv;
     if (!ok) {
@@ -106,25 +128,24 @@ template <typename T, int NJ, int NP> __global__ __launch_bounds__(256) void del
         return;
     }
     float* head = p.pool + ((int64_t)slot * p.Hv + h) * p.dv * p.dk;
-    const T* x = (const T*)p.qkv + i * p.ld;
-    Token<T, NJ> tok;
-    tok.load(p, x, i, h, lane8);
+    bool formed = false;
     for (int r0 = 0; r0 < p.dv; r0 += 32 * NP) {
         f32x4 S[NP][NJ];
         float v[NP];
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
-            const int r = r0 + 32 * n + (tid >> 3);
-            if (r >= p.dv) continue;
-            row_load(S[n], head + (int64_t)r * p.dk, lane8, p.dk);
+            const int r = min(r0 + 32 * n + (tid >> 3), p.dv - 1);
+            row_load<PAST>(S[n], head + (int64_t)r * p.dk, lane8, p.dk);
             v[n] = to_f32(x[2 * p.Hk * p.dk + h * p.dv + r]);
         }
+        if (!formed) tok.form(p, a_log);
+        formed = true;
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
             const int r = r0 + 32 * n + (tid >> 3);
-            if (r >= p.dv) continue;   // whole groups of 8 lanes
             const float o = row_step(S[n], tok, v[n]);
-            row_store(S[n], head + (int64_t)r * p.dk, lane8, p.dk);
+            if (r >= p.dv) continue;   // whole groups of 8 lanes
+            row_store<PAST>(S[n], head + (int64_t)r * p.dk, lane8, p.dk);
             if (lane8 == 0) s_o[r] = o;
         }
     }
@@ -157,12 +178,18 @@ template <typename T, int NJ, int NP> __global__ __launch_bounds__(256) void del
         if (tid + 256 * e < p.dv) out[tid + 256 * e] = from_f32<T>(y[e]);
 }
 
-template <typename T> hipError_t decode_launch(const DeltaArgs& p, hipStream_t s) {
+template <typename T, bool PAST> hipError_t decode_launch(const DeltaArgs& p, hipStream_t s) {
     const dim3 grid((unsigned)p.Hv, (unsigned)p.nseq);
-    if (p.dk <= 64) SSM_LAUNCH((delta_decode_kernel<T, 2, 4>), grid, dim3(256), 0, s, p);
-    else if (p.dk <= 128) SSM_LAUNCH((delta_decode_kernel<T, 4, 4>), grid, dim3(256), 0, s, p);
-    else SSM_LAUNCH((delta_decode_kernel<T, 8, 2>), grid, dim3(256), 0, s, p);
+    if (p.dk <= 64) SSM_LAUNCH((delta_decode_kernel<T, 2, 4, PAST>), grid, dim3(256), 0, s, p);
+    else if (p.dk <= 128) SSM_LAUNCH((delta_decode_kernel<T, 4, 4, PAST>), grid, dim3(256), 0, s, p);
+    else SSM_LAUNCH((delta_decode_kernel<T, 8, 2, PAST>), grid, dim3(256), 0, s, p);
     return hipGetLastError();
+}
+// States of more than 96 MB are read and written past the caches: 128 sequences of 1 MB 60 -> 54 us, 256 112 -> 104; below
+// that the 256 MB cache can keep them from step to step (64 sequences 22.9, past the caches 26.8)
+template <typename T> hipError_t decode_launch(const DeltaArgs& p, hipStream_t s) {
+    const bool past = (int64_t)p.nseq * p.Hv * p.dv * p.dk * 4 > (96ll << 20);
+    return past ? decode_launch<T, true>(p, s) : decode_launch<T, false>(p, s);
 }
 
 }  // namespace

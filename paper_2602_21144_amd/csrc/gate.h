@@ -27,5 +27,10 @@ template <typename T> __device__ __forceinline__ void write8(T* p, const float (
     for (int e = 0; e < 8; ++e) x[e] = from_f32<T>(v[e]);
     store16(p, x);
 }
+// the same past the caches
+__device__ __forceinline__ void write8_past(float* p, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) __builtin_nontemporal_store(f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]}, (f32x4*)p + i);
+}
 
 }  // namespace ssm
