@@ -7,9 +7,9 @@
 // of its value heads. Pass 2 (delta_main_kernel) walks a sequence's chunks with the state in accumulators: columns of S
 // need nothing of each other, so a wave owns 16 of them and talks to no other wave.
 //
-// Operands are f16, sums float32. A row of q or k is scaled by the power of two that takes its largest value to
-// 2^12, which holds bf16 values exactly (down to 2^-26 of the row's largest; smaller ones to 2^-37 of it); float32
-// ones are two f16 values, 22 bits. What is computed (S, R, U) is scaled by column in the same way and
+// Operands are f16, sums float32. A row of q or k is scaled by the power of two that takes its largest value to 2^12
+// or to 1, which holds bf16 values exactly (those of k down to 2^-14 of the row's largest, smaller ones to 2^-25 of it);
+// float32 ones are two f16 values, 22 bits or 2^-25 of the largest. What is computed (S, R, U) is scaled by column in the same way and
 // split in two where it carries the state on; a product of two splits is three MFMAs, off by 2^-22. Where only an
 // output that will be rounded to bf16 depends on it, the first f16 value alone (2^-11) stands for S, U and the
 // products of queries and keys.
@@ -25,9 +25,9 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;           // tokens per chunk
 constexpr int kFrags = 6;        // 16 x 32 pieces of a lower triangular 64 x 64 matrix
-// factors for the state, by token: e^G kappa, e^(G_C - G); then e^(G_C), the scale of T, the largest of the first
+// factors for the state, by token: e^G kappa, e^(G_C - G); then e^(G_C), the scale of T, a bound of e^G |k|
 constexpr int kFacDecay = 2 * kC, kFacT = 2 * kC + 1, kFacMax = 2 * kC + 2;
-constexpr size_t kFacBytes = 1024, kOutFacBytes = 1024;   // and for the outputs: c e^G, c 2^20
+constexpr size_t kFacBytes = 1024, kOutFacBytes = 1024;   // and for the outputs: c e^G, c 2^8
 constexpr int kFindSeqs = 256;   // more sequences are laid out by a launch of its own
 
 // the parts of a stored q, k or product: float32 activations take two f16 values
@@ -186,10 +186,10 @@ template <typename T> struct Piece {   // eight values of a row
     }
 };
 
-// The pieces of a row of q or k that this thread (c4 of four) holds: scaled to f16 parts in operand layout, to LDS. Returns
-// the sum of squares of the row; e: the exponent of its scale.
+// The pieces of a row of q or k that this thread (c4 of four) holds: scaled to f16 parts in operand layout, to LDS. The
+// row's largest value comes to 2^top. Returns the sum of squares of the row; e: the exponent of its scale.
 template <typename T, int NS>
-__device__ __forceinline__ float stage_row(const Piece<T> (&x)[NS], int row, int c4, char* lds, int* e) {
+__device__ __forceinline__ float stage_row(const Piece<T> (&x)[NS], int row, int c4, int top, char* lds, int* e) {
     float ss = 0.0f, m = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -202,7 +202,7 @@ __device__ __forceinline__ float stage_row(const Piece<T> (&x)[NS], int row, int
         }
     }
     ss = quad_sum(ss);
-    *e = scale_exp(quad_max(m));
+    *e = scale_exp(quad_max(m)) - 12 + top;
     const float f = pow2(*e);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
     constexpr int kMat = HB * kC * kLdA * 4;
     __shared__ __attribute__((aligned(16))) char s_k[kQk], s_q[kQk > kMat ? kQk : kMat];
     float(*s_t)[kC * kLdA] = (float(*)[kC * kLdA])s_q;
-    __shared__ __attribute__((aligned(16))) float s_gh[HB][kC], s_gl[HB][kC], s_beta[HB][kC], s_kap[kC], s_c[kC];
+    __shared__ __attribute__((aligned(16))) float s_gh[HB][kC], s_gl[HB][kC], s_beta[HB][kC], s_kap[kC], s_c[kC], s_len[kC];
     __shared__ float s_max[HB][4];
     __shared__ int s_find[8];
     const DeltaArgs& p = a.d;
@@ -314,9 +314,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
         s_beta[b][lane] = lane < nq ? p.beta_max * sigmoid_f(bv) : 0.0f;
     };
     int eq, ek;
-    const float sk = stage_row<T, NS>(xk, row, c4, s_k, &ek);
-    const float sq = stage_row<T, NS>(xq, row, c4, s_q, &eq);
+    const float sk = stage_row<T, NS>(xk, row, c4, 0, s_k, &ek);
+    const float sq = stage_row<T, NS>(xq, row, c4, 12, s_q, &eq);
     if (c4 == 0) {
+        s_len[row] = sqrtf(sk) * pow2(ek);
         s_c[row] = p.scale * (p.qk_norm ? 1.0f / sqrtf(fmaxf(sq + p.eps, 1.2e-38f)) : 1.0f) * pow2(-eq);
         s_kap[row] = (p.qk_norm ? 1.0f / sqrtf(fmaxf(sk + p.eps, 1.2e-38f)) : 1.0f) * pow2(-ek);
     }
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
                     for (int r = 0; r < 4; ++r) {
                         const float ex = fast_exp2((gh[b] - jh[b][q][r]) + (gl[b] - jl[b][q][r]));
                         m[r] = j + r < i ? kk[n][q][r] * ex * (bk[b] * jk[q][r]) : 0.0f;
-                        x[b][4 * q + r] = j + r <= i ? kq[n][q][r] * ex * pow2(-20) : 0.0f;
+                        x[b][4 * q + r] = j + r <= i ? kq[n][q][r] * ex * pow2(-8) : 0.0f;
                     }
                     *(f32x4*)&s_t[b][i * kLdA + j] = m;   // zeros above the diagonal, where this piece has them
                 }
@@ -466,13 +467,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
             const float eg = fast_exp2(gh + gl), bg = eg * s_kap[lane];
             fac[lane] = bg;
             fac[kC + lane] = fast_exp2((ch - gh) + (cl - gl));
-            const float m = wave_max(bg);
+            const float m = wave_max(bg * s_len[lane] * 1.001f);
             if (lane == 0) {
                 fac[kFacDecay] = fast_exp2(ch + cl);
                 fac[kFacMax] = m;
             }
             f[lane] = s_c[lane] * eg;
-            f[kC + lane] = s_c[lane] * pow2(20);
+            f[kC + lane] = s_c[lane] * pow2(8);
         }
         __syncthreads();
         // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column
@@ -1053,12 +1054,27 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
         S[t] = f32x4{};
         if (carry && on && 16 * t < p.dk) S[t] = *(const f32x4*)(state + 16 * t);
     }
-    // S times unit (a power of two) is the state; its operand is S 2^es, |S| <= bound
-    float unit = 1.0f, bound = column_max(largest(S));
-    int es = scale_exp(bound);
-    f16x8 Sh[NS], Sl[NS];
+    // S times unit (a power of two) is the state; |S| stays below 2^15, so that S itself is the pair of operands.
+    // Tiles of which these are formed beside the products of the others; the others' behind the barrier, beside the first
+    // reads
+    constexpr int kEarly = NT / 4 * 2;
+    float one = 1.0f;
+    asm volatile("" : "+s"(one));
+    float unit;
+    {
+        const int e = scale_exp(column_max(largest(S))) + 2;
+        unit = pow2(-e);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) split2<true>(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] *= pow2(e);
+    }
+    f16x8 Sh[NS], Sl[NS];
+    auto form = [&](int t0, int t1) {
+#pragma unroll
+        for (int t = t0; t < t1; t += 2) split2<true>(S[t], S[t + 1], one, Sh[t / 2], Sl[t / 2]);
+    };
+    form(0, kEarly);
     for (int c = 0; c <= n && n > 0; ++c) {
         meet();
         if (c == n || !on) continue;
@@ -1108,13 +1124,15 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
                     if (16 * it + 4 * hh + r >= rows - c * kC) v[it][r] = 0.0f;
         }
         __builtin_amdgcn_sched_barrier(0);
+        form(kEarly, NT);
 
         // K S beside all that does not wait for it
         f32x4 R[4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) R[it] = f32x4{};
-        const float fs = unit * pow2(-es);
-        float ms, fu, wc2, keep;
+        const float fs = unit;
+        constexpr float kRoot = NS <= 2 ? 8.0f : NS <= 4 ? 11.4f : 16.0f;   // of 32 NS, or above it
+        float ms, fu;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
 #pragma unroll
@@ -1140,15 +1158,10 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
                     for (int k = 0; k < 4; ++k) vmax = fmaxf(vmax, fabsf(v[it][k]));
                 ms = column_max(largest(S));
-                // R = V - e^G K S is below this, as values of k are below 2^13; U and W then are below 2^32 fu
-                const int er = scale_exp(column_max(vmax) + gmax * pow2(13) * (float)(32 * NS) * (ms * unit));
-                fu = pow2(-er) * tscale;
-                // the units of the state are those of W's operand; a state far above W keeps them in range
-                const int ew = scale_exp(fmaxf(fu * pow2(32), bound * unit * decay * pow2(-20)));
+                // a bound of R = V - e^G K S: |k . S| <= |k| sqrt(dk) max |S|
+                const int er = scale_exp(column_max(vmax) + gmax * kRoot * (ms * unit));
                 const float gr = pow2(er), cr = fs * gr;
-                wc2 = fu * pow2(ew);
-                keep = decay * unit * pow2(ew);
-                unit = pow2(-ew);
+                fu = pow2(-er) * tscale;
 #pragma unroll
                 for (int it = 0; it < 4; ++it)
 #pragma unroll
@@ -1156,16 +1169,6 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
                         v[it][r] *= gr;
                         bg[it][r] *= -cr;
                     }
-            }
-            if (s == 1) {
-#pragma unroll
-                for (int it = 0; it < 4; ++it)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) wg[it][r] *= wc2;
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) S[t][r] *= keep;
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -1188,21 +1191,19 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
                     Kt[part][s][t] = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
                 }
         __builtin_amdgcn_sched_barrier(0);
-        float one = 1.0f;
-        asm volatile("" : "+s"(one));
-        f16x8 Rh[2], Rl[2];
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(bg[it][r], R[it][r], v[it][r]);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], one, Rh[s], Rl[s]);
-        // U = kappa T beta R times 1 / fu
+        // From here tokens 0 .. 31 run ahead of the others: while the one half is in the matrix cores the other is formed.
+        // U = kappa T beta R times 1 / fu, W = e^(G_C - G) U
+        f16x8 Rh[2], Rl[2], Wh[2], Wl[2];
         f32x4 U[4], X[4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) U[it] = f32x4{};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int it = 2 * s; it < 2 * s + 2; ++it)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(bg[it][r], R[it][r], v[it][r]);
+            split2<true>(R[2 * s], R[2 * s + 1], one, Rh[s], Rl[s]);
 #pragma unroll
             for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[0][frag_of(it, s)], Rh[s], U[it]);
 #pragma unroll
@@ -1210,55 +1211,84 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
             for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[1][frag_of(it, s)], Rh[s], U[it]);
         }
-        // W = e^(G_C - G) U, the state's update
-        f16x8 Wh[2], Wl[2];
+        // The state's units: what is left of it and 64 products of W with values of k below 2 come to 2^15 at most. In bf16
+        // W's largest value follows from R's (times the 64 of a row of T below 2^13) while the products run; in
+        // float32, where a token's own precision is asked for, it is W's own
+        float keep;
+        auto units = [&](float most) {                 // of W
+            const int ew = scale_exp(__builtin_fmaf(decay * ms, unit, most * pow2(7))) + 2;
+            keep = decay * unit * pow2(ew);
+            unit = pow2(-ew);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[t][r] *= keep;
+            return pow2(ew);
+        };
+        float wc = fu;
+        if constexpr (PA == 1) wc *= units(fu * pow2(19) * column_max(largest(R)));
 #pragma unroll
         for (int it = 0; it < 4; ++it)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * wg[it][r];
+            for (int r = 0; r < 4; ++r) wg[it][r] *= wc;
+        auto weigh = [&](int s) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) split2<true>(X[2 * s], X[2 * s + 1], one, Wh[s], Wl[s]);
-        __builtin_amdgcn_sched_barrier(0);
-        // S <- decay S + K^T W: four tiles' products, then their operands beside the next four's
+            for (int it = 2 * s; it < 2 * s + 2; ++it)
 #pragma unroll
-        for (int t0 = 0; t0 < NT; t0 += 4) {
+                for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * wg[it][r];
+        };
+        if constexpr (PA == 2) {
+            weigh(0);
+            weigh(1);
+            const float f = units(column_max(largest(X)));
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
+            for (int it = 0; it < 4; ++it)
 #pragma unroll
-                for (int t = t0; t < t0 + 4 && t < NT; ++t) S[t] = mma(Kt[0][s][t], Wh[s], S[t]);
-#pragma unroll
-                for (int t = t0; t < t0 + 4 && t < NT; ++t) S[t] = mma(Kt[0][s][t], Wl[s], S[t]);
-                if constexpr (PA == 2) {
-#pragma unroll
-                    for (int t = t0; t < t0 + 4 && t < NT; ++t) S[t] = mma(Kt[PA - 1][s][t], Wh[s], S[t]);
-                }
-            }
-            if (t0 == 0) {
-                // 64 products of values of k below 2^13
-                bound = keep * ms + column_max(largest(X)) * pow2(19);
-                es = scale_exp(bound);
-                // U for the outputs
-                const int eu = scale_exp(column_max(largest(U)));
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    f16x8 uh, ul;
-                    split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), uh, ul);
-                    *(f16x8*)(to + (PA * NS + s) * 1024 + lane * 16) = uh;
-                    if constexpr (PA == 2) *(f16x8*)(to + (PA * NS + 2 + s) * 1024 + lane * 16) = ul;
-                }
-                if (hh == 0) {
-                    float* sc = (float*)(to + (NS + 2) * PA * 1024);
-                    sc[lane] = fs;
-                    sc[16 + lane] = fu * pow2(-eu);
-                }
-            }
-            if (t0 > 0) {
-#pragma unroll
-                for (int t = t0 - 4; t < t0; t += 2) split2<true>(S[t], S[t + 1], pow2(es), Sh[t / 2], Sl[t / 2]);
-            }
+                for (int r = 0; r < 4; ++r) X[it][r] *= f;
         }
 #pragma unroll
-        for (int t = (NT - 1) / 4 * 4; t < NT; t += 2) split2<true>(S[t], S[t + 1], pow2(es), Sh[t / 2], Sl[t / 2]);
+        for (int s = 0; s < 2; ++s) {
+            if constexpr (PA == 1) weigh(s);
+            split2<true>(X[2 * s], X[2 * s + 1], one, Wh[s], Wl[s]);
+            if (s == 0) {
+                // S <- decay S + K^T W, the first half's products
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t] = mma(Kt[0][0][t], Wh[0], S[t]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t] = mma(Kt[0][0][t], Wl[0], S[t]);
+                if constexpr (PA == 2) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) S[t] = mma(Kt[PA - 1][0][t], Wh[0], S[t]);
+                }
+            }
+        }
+        auto second = [&](int t0, int t1) {
+#pragma unroll
+            for (int t = t0; t < t1; ++t) S[t] = mma(Kt[0][1][t], Wh[1], S[t]);
+#pragma unroll
+            for (int t = t0; t < t1; ++t) S[t] = mma(Kt[0][1][t], Wl[1], S[t]);
+            if constexpr (PA == 2) {
+#pragma unroll
+                for (int t = t0; t < t1; ++t) S[t] = mma(Kt[PA - 1][1][t], Wh[1], S[t]);
+            }
+        };
+        second(0, kEarly);
+        second(kEarly, NT);
+        // U for the outputs
+        const int eu = scale_exp(column_max(largest(U)));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            f16x8 uh, ul;
+            split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), uh, ul);
+            *(f16x8*)(to + (PA * NS + s) * 1024 + lane * 16) = uh;
+            if constexpr (PA == 2) *(f16x8*)(to + (PA * NS + 2 + s) * 1024 + lane * 16) = ul;
+        }
+        if (hh == 0) {
+            float* sc = (float*)(to + (NS + 2) * PA * 1024);
+            sc[lane] = fs;
+            sc[16 + lane] = fu * pow2(-eu);
+        }
+        form(0, kEarly);
     }
     if (ok && on) {
 #pragma unroll
