@@ -1341,9 +1341,13 @@ template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream
         if (p.rep == 1) SSM_LAUNCH((delta_chunk_kernel<T, NS, 1>), grid, dim3(256), 0, s, a);
         else SSM_LAUNCH((delta_chunk_kernel<T, NS, 2>), grid, dim3(256), 0, s, a);
     }
+    // Two waves of columns to a workgroup where all of these run at once, a compute unit each; else four, which share what
+    // they read. 16 heads of 128 x 128 over prompts of 1024 tokens, whole call: 4 prompts (256 workgroups of two) 53.5 us
+    // by twos and 61 by fours, 6 prompts (384) 92 and 72, 24 prompts 285 and 232; float32 4 prompts 103 and 108, 6
+    // 190 and 123
     KernelTimer kt("delta.main", s);
-    const int64_t pairs = (int64_t)p.nseq * p.Hv, n2 = pairs * ((p.dv + 31) / 32), n4 = pairs * ((p.dv + 63) / 64);
-    if (n4 < 256 && n2 > n4) main_launch<T, NS, 2>(a, s);
+    const int64_t pairs = (int64_t)p.nseq * p.Hv, by_two = pairs * ((p.dv + 31) / 32);
+    if (by_two <= 256 || p.dv <= 32) main_launch<T, NS, 2>(a, s);
     else main_launch<T, NS, 4>(a, s);
     return hipGetLastError();
 }

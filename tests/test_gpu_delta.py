@@ -152,6 +152,32 @@ def test_a_workspace_for_more_serves_fewer():
     _check(L, out, pool)
 
 
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,lens", [((16, 32, 128, 128), [70, 1, 65]), ((32, 64, 64, 80), [66, 40]), ((20, 60, 96, 64), [3, 130, 1, 0, 64]),
+                                        ((4, 12, 192, 192), [64, 100, 1, 70]), ((8, 8, 256, 512), [65, 3, 90]), ((64, 64, 32, 48), [20, 3, 65])],
+                         ids=str)
+def test_prefill_of_many_heads(heads, lens, act):
+    """More pairs of a head and a sequence than run at once, by workgroups of four waves of columns; head counts that
+    the eight XCDs do not divide, three value heads to a q/k head, columns that leave waves without any."""
+    L = Layer(torch, heads, lens, act, seed=sum(heads), init=[i % 2 for i in range(len(lens))])
+    out, pool, status, behind = _prefill(L, rows_behind=1)
+    assert status == 0 and torch.isnan(behind).all()
+    _check(L, out, pool)
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [2.0 ** -40, 1.0, 2.0 ** 30])
+def test_prefill_far_scales(size, act):
+    """Values and states far from one, and keys of the program's own lengths from 2^-12 to 1: what is scaled inside
+    comes back."""
+    L = Layer(torch, (1, 2, 64, 64), [150], act, seed=19, init=[1], qk_norm=False)
+    L.qkv[:, 128:] *= size
+    L.pool *= np.float32(size)
+    L.qkv[:, 64:128] = L.stored(L.qkv[:, 64:128] * 2.0 ** -np.random.default_rng(1).integers(0, 13, (150, 1)))
+    out, pool, _, _ = _prefill(L)
+    _check(L, out, pool)
+
+
 def test_runs_give_the_same_bits():
     L = Layer(torch, (2, 4, 128, 128), [257, 64, 500], "bf16", seed=11)
     a, b = _prefill(L), _prefill(L)
@@ -294,6 +320,17 @@ def test_decode_with_the_head_norm(heads, per_head, with_z, kw, act):
     y = od.head_norm(o, wf, z, kw.get("eps", 1e-5), kw.get("gate", "silu"), kw.get("gate_first", False))
     near(f64(out).reshape(o.shape), y, _norm_bound(o, sizes, y, wf, z, act, kw), "out")
     near(f64(pool)[L.slots], want[L.slots], state_bound(want[L.slots], act), "state")
+
+
+def test_decode_of_states_that_no_cache_keeps():
+    """More than 96 MB of states, which go past the caches."""
+    n, heads = 50, (16, 32, 128, 128)
+    L = Layer(torch, heads, [1] * n, "bf16", seed=24, init=[1] * n)
+    out, pool, status = _decode(L)
+    assert status == 0
+    o, want, sizes = L.oracle()
+    near(f64(out).reshape(o.shape), o, 2.0 ** -8 * np.abs(o) + 64 * 2.0 ** -24 * sizes + 1e-30, "out")
+    near(f64(pool)[L.slots], want[L.slots], state_bound(want[L.slots], "bf16"), "state")
 
 
 def test_decode_bad_slots():
