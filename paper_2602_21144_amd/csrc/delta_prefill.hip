@@ -326,9 +326,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
 
     // K K^T and K Q^T: wave w has columns i = 16 w + lane % 16, pieces n of rows j = 32 n + 16 q + 4 hh + r up to the
     // diagonal: one piece for waves 0 and 1, two for the others
-    const int hh = lane >> 4, col = lane & 15, it = wave, i = 16 * it + col, pieces = 1 + it / 2;
+    const int it = wave, pieces = 1 + it / 2;
+    // The lane's place in a tile, worked out anew in every phase: addresses kept from one to the next cost a third of the
+    // registers and with them a workgroup per compute unit
+    auto place = [&] {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
     const bool odd = (it & 1) != 0;                    // the second tile of the last piece reaches the diagonal
-    const float kap = s_kap[i];
+    const float kap = s_kap[16 * it + (lane & 15)];
     f32x4 kk[2][2], kq[2][2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -378,6 +385,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
             }
             __syncthreads();
         }
+        {
+        const int l = place(), hh = l >> 4, i = 16 * it + (l & 15);
         float gh[HB], gl[HB], bk[HB];
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
@@ -417,7 +426,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
 #pragma unroll
             for (int b = 0; b < HB; ++b) {
                 if (b >= heads) break;
-                char* to = vout(b) + t_bytes() + (frag_of(it, n) * 1024 + lane * 16);
+                char* to = vout(b) + t_bytes() + (frag_of(it, n) * 1024 + l * 16);
 #pragma unroll
                 for (int part = 0; part < PA; ++part) {
                     const f16x8 o = pair_f16(x[b], 0);
@@ -427,13 +436,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
                 }
             }
         }
+        }
         __syncthreads();
         // T = (I + A)^-1 in place, in float32: the diagonal 16 x 16 blocks by substitution (lane: block and column), then
         // [T1 0; -T2 A21 T1 T2] for blocks of 16 and of 32. One wave per head, then two, then all for each
         if (wave < HB) {
+            const int l = place(), hh = l >> 4, col = l & 15;
             float* t = s_t[wave] + 16 * hh * kLdA + 16 * hh;
-            // row r in pieces of four, asked for in two lots in front of their use
-            constexpr int kCut = 12;
+            // row r in pieces of four, asked for in three lots in front of their use
             f32x4 m[16][4];
             float x[16];
             auto ask = [&](int r0, int r1) {
@@ -452,10 +462,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
                     x[r] = s;
                 }
             };
-            ask(1, kCut);
-            solve(0, kCut);
-            ask(kCut, 16);
-            solve(kCut, 16);
+            ask(1, 8);
+            solve(0, 8);
+            ask(8, 12);
+            solve(8, 12);
+            ask(12, 16);
+            solve(12, 16);
 #pragma unroll
             for (int r = 0; r < 16; ++r) t[r * kLdA + col] = x[r];
         }
@@ -476,12 +488,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
             f[kC + lane] = s_c[lane] * pow2(8);
         }
         __syncthreads();
-        // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column
-        auto row4 = [&](const float* t, int y, int x) { return *(const f32x4*)&t[(y + col) * kLdA + x + 4 * hh]; };
-        auto col4 = [&](const float* t, int y, int x) {
+        // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column;
+        // l: the lane
+        auto row4 = [&](const float* t, int y, int x, int l) { return *(const f32x4*)&t[(y + (l & 15)) * kLdA + x + 4 * (l >> 4)]; };
+        auto col4 = [&](const float* t, int y, int x, int l) {
             f32x4 v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = t[(y + 4 * hh + r) * kLdA + x + col];
+            for (int r = 0; r < 4; ++r) v[r] = t[(y + 4 * (l >> 4) + r) * kLdA + x + (l & 15)];
             return v;
         };
         auto times = [&](const f32x4& m, const f32x4& x, f32x4 acc) {
@@ -489,46 +502,47 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
             for (int r = 0; r < 4; ++r) acc = mma4(m[r], x[r], acc);
             return acc;
         };
-        auto put = [&](float* t, int y, int x, const f32x4& v) {
+        auto put = [&](float* t, int y, int x, const f32x4& v, int l) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) t[(y + 4 * hh + r) * kLdA + x + col] = -v[r];
+            for (int r = 0; r < 4; ++r) t[(y + 4 * (l >> 4) + r) * kLdA + x + (l & 15)] = -v[r];
         };
         if (wave < 2 * HB) {
             float* t = s_t[wave >> 1];
-            const int c0 = 32 * (wave & 1), y0 = c0 + 16;
-            const f32x4 x = times(row4(t, y0, c0), col4(t, c0, c0), f32x4{});
-            put(t, y0, c0, times(row4(t, y0, y0), x, f32x4{}));
+            const int c0 = 32 * (wave & 1), y0 = c0 + 16, l = place();
+            const f32x4 x = times(row4(t, y0, c0, l), col4(t, c0, c0, l), f32x4{});
+            put(t, y0, c0, times(row4(t, y0, y0, l), x, f32x4{}), l);
         }
         __syncthreads();
         {
-            const int r2 = wave >> 1, c0 = 16 * (wave & 1);
+            const int r2 = wave >> 1, c0 = 16 * (wave & 1), l = place();
             // [T1 0; T21 T2] again, in 16 x 16 blocks; what lies above the diagonal is not stored and counts as zero
             f32x4 y[HB];
 #pragma unroll
             for (int b = 0; b < HB; ++b) {
                 const float* t = s_t[b];
-                const f32x4 zero{}, t0 = col4(t, 0, 0), t1 = col4(t, 16, c0);
+                const f32x4 zero{}, t0 = col4(t, 0, 0, l), t1 = col4(t, 16, c0, l);
                 const f32x4 u0 = (wave & 1) == 0 ? t0 : zero;
                 f32x4 x[2];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) x[k] = times(row4(t, 32 + 16 * k, 16), t1, times(row4(t, 32 + 16 * k, 0), u0, zero));
-                const f32x4 m1 = r2 == 1 ? row4(t, 48, 48) : zero;
-                y[b] = times(m1, x[1], times(row4(t, 32 + 16 * r2, 32), x[0], zero));
+                for (int k = 0; k < 2; ++k) x[k] = times(row4(t, 32 + 16 * k, 16, l), t1, times(row4(t, 32 + 16 * k, 0, l), u0, zero));
+                const f32x4 m1 = r2 == 1 ? row4(t, 48, 48, l) : zero;
+                y[b] = times(m1, x[1], times(row4(t, 32 + 16 * r2, 32, l), x[0], zero));
             }
             __syncthreads();
 #pragma unroll
-            for (int b = 0; b < HB; ++b) put(s_t[b], 32 + 16 * r2, c0, y[b]);
+            for (int b = 0; b < HB; ++b) put(s_t[b], 32 + 16 * r2, c0, y[b], l);
         }
         __syncthreads();
         // kappa T beta, scaled by the power of two that takes its largest value to 2^12; wave w has row tile w
         float x[HB][2][8];
+        const int l = place(), hh = l >> 4;
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
             float m = 0.0f;
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 if (n >= pieces) break;
-                const f32x4 v0 = row4(s_t[b], 16 * it, 32 * n), v1 = row4(s_t[b], 16 * it, 32 * n + 16);
+                const f32x4 v0 = row4(s_t[b], 16 * it, 32 * n, l), v1 = row4(s_t[b], 16 * it, 32 * n + 16, l);
                 const f32x4 b0 = *(const f32x4*)&s_beta[b][32 * n + 4 * hh], b1 = *(const f32x4*)&s_beta[b][32 * n + 16 + 4 * hh];
                 const bool two = odd || n + 1 < pieces;
 #pragma unroll
@@ -551,7 +565,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 if (n >= pieces) break;
-                char* to = vout(b) + (frag_of(it, n) * 1024 + lane * 16);
+                char* to = vout(b) + (frag_of(it, n) * 1024 + l * 16);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[b][n][e] *= f;
 #pragma unroll
