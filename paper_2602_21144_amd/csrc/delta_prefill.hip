@@ -597,18 +597,24 @@ template <int N> __device__ __forceinline__ float largest(const f32x4 (&v)[N]) {
         for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(v[t][r]));
     return m;
 }
-// two stacked tiles, times f (a power of two), as an operand: its first f16 values, and what they leave
+// Two stacked tiles, times f (a power of two), as an operand: its first f16 values, and what they leave. SCALED false: f is
+// one, though the compiler does not know it. Of two values that are left the first goes through an empty statement, which
+// makes one instruction of each (a product, a difference and a rounding), where their conversion as a pair would
+// take three
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-template <bool LO> __device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, float f, f16x8& hi, f16x8& lo) {
+template <bool LO, bool SCALED = true>
+__device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, float f, f16x8& hi, f16x8& lo) {
 #pragma unroll
     for (int r = 0; r < 8; r += 2) {
         const float a = r < 4 ? x0[r] : x1[r - 4], b = r < 4 ? x0[r + 1] : x1[r - 3];
-        const f16x2 h = __builtin_convertvector((f32x2){a * f, b * f}, f16x2);
+        const f16x2 h = __builtin_convertvector((f32x2){SCALED ? a * f : a, SCALED ? b * f : b}, f16x2);
         hi[r] = h[0];
         hi[r + 1] = h[1];
         if constexpr (LO) {
-            lo[r] = (_Float16)__builtin_fmaf(a, f, -(float)h[0]);
+            _Float16 l = (_Float16)__builtin_fmaf(a, f, -(float)h[0]);
+            asm("" : "+v"(l));
+            lo[r] = l;
             lo[r + 1] = (_Float16)__builtin_fmaf(b, f, -(float)h[1]);
         }
     }
@@ -672,12 +678,13 @@ dim3 work_grid(const DeltaArgs& p, int blocks) {
 
 // While a chunk is computed the next one's pieces and values are on their way, and the stores of its outputs stay out
 // at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'.
-template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES) void delta_main_kernel(Args a) {
+template <typename T, int NS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <= 4 ? 2 : 1))) void delta_main_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = MainLds<T, NS>;
     constexpr int kQk = L::kQk, kV = L::kV;
     constexpr uint32_t sz = sizeof(T);
-    __shared__ __attribute__((aligned(1024))) char lds[L::kBytes];
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
     const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const WorkItem it0 = work_item(p, (p.dv + 16 * WAVES - 1) / (16 * WAVES));
@@ -768,27 +775,37 @@ template <typename T, int NS, int WAVES> __global__ __launch_bounds__(64 * WAVES
             const float fs = unit * pow2(-es);
             f32x4 R[4], O[4];
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                R[it] = f32x4{};
+            for (int it = 0; it < 4; ++it) R[it] = O[it] = f32x4{};
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const f16x8 k = qk_piece<NS>(s_k, 0, it, s, lane);
-                    R[it] = mma(k, Sh[s], R[it]);
-                    R[it] = mma(k, Sl[s], R[it]);
-                    if constexpr (PA == 2) R[it] = mma(qk_piece<NS>(s_k, 1, it, s, lane), Sh[s], R[it]);
+            for (int s = 0; s < NS; ++s) {
+                f16x8 k[PA][4];
+#pragma unroll
+                for (int part = 0; part < PA; ++part)
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) k[part][it] = qk_piece<NS>(s_k, part, it, s, lane);
+#pragma unroll
+                for (int it = 0; it < 4; ++it) R[it] = mma(k[0][it], Sh[s], R[it]);
+#pragma unroll
+                for (int it = 0; it < 4; ++it) R[it] = mma(k[0][it], Sl[s], R[it]);
+                if constexpr (PA == 2) {
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) R[it] = mma(k[PA - 1][it], Sh[s], R[it]);
                 }
             }
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                O[it] = f32x4{};
+            for (int s = 0; s < NS; ++s) {
+                f16x8 q[PA][4];
 #pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const f16x8 q = qk_piece<NS>(s_q, 0, it, s, lane);
-                    O[it] = mma(q, Sh[s], O[it]);
-                    if constexpr (PA == 2) {
-                        O[it] = mma(q, Sl[s], O[it]);
-                        O[it] = mma(qk_piece<NS>(s_q, 1, it, s, lane), Sh[s], O[it]);
-                    }
+                for (int part = 0; part < PA; ++part)
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) q[part][it] = qk_piece<NS>(s_q, part, it, s, lane);
+#pragma unroll
+                for (int it = 0; it < 4; ++it) O[it] = mma(q[0][it], Sh[s], O[it]);
+                if constexpr (PA == 2) {
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) O[it] = mma(q[0][it], Sl[s], O[it]);
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) O[it] = mma(q[PA - 1][it], Sh[s], O[it]);
                 }
             }
 #pragma unroll
@@ -1086,7 +1103,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
     f16x8 Sh[NS], Sl[NS];
     auto form = [&](int t0, int t1) {
 #pragma unroll
-        for (int t = t0; t < t1; t += 2) split2<true>(S[t], S[t + 1], one, Sh[t / 2], Sl[t / 2]);
+        for (int t = t0; t < t1; t += 2) split2<true, false>(S[t], S[t + 1], one, Sh[t / 2], Sl[t / 2]);
     };
     form(0, kEarly);
     for (int c = 0; c <= n && n > 0; ++c) {
@@ -1217,7 +1234,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
             for (int it = 2 * s; it < 2 * s + 2; ++it)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(bg[it][r], R[it][r], v[it][r]);
-            split2<true>(R[2 * s], R[2 * s + 1], one, Rh[s], Rl[s]);
+            split2<true, false>(R[2 * s], R[2 * s + 1], one, Rh[s], Rl[s]);
 #pragma unroll
             for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[0][frag_of(it, s)], Rh[s], U[it]);
 #pragma unroll
@@ -1263,7 +1280,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             if constexpr (PA == 1) weigh(s);
-            split2<true>(X[2 * s], X[2 * s + 1], one, Wh[s], Wl[s]);
+            split2<true, false>(X[2 * s], X[2 * s + 1], one, Wh[s], Wl[s]);
             if (s == 0) {
                 // S <- decay S + K^T W, the first half's products
 #pragma unroll
@@ -1339,9 +1356,12 @@ DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, 
 
 template <typename T, int NS, int WAVES> void main_launch(const Args& a, hipStream_t s) {
     const dim3 grid = work_grid(a.d, (a.d.dv + 16 * WAVES - 1) / (16 * WAVES));
-    constexpr int bytes = SplitLds<T, NS, WAVES>::kBytes;
-    if constexpr (SplitLds<T, NS, WAVES>::kFits) SSM_LAUNCH((delta_split_kernel<T, NS, WAVES>), grid, dim3(128 * WAVES), bytes, s, a);
-    else SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), grid, dim3(64 * WAVES), 0, s, a);
+    // LDS is asked for at the launch: a kernel that the compiler sees to fill it alone has half of its registers where only
+    // MFMAs reach them, and a move for every value that goes between the two
+    constexpr bool split = SplitLds<T, NS, WAVES>::kFits;
+    constexpr int bytes = split ? SplitLds<T, NS, WAVES>::kBytes : MainLds<T, NS>::kBytes;
+    if constexpr (split) SSM_LAUNCH((delta_split_kernel<T, NS, WAVES>), grid, dim3(128 * WAVES), bytes, s, a);
+    else SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), grid, dim3(64 * WAVES), bytes, s, a);
 }
 template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream_t s) {
     const DeltaArgs& p = a.d;
