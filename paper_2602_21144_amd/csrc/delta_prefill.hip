@@ -1,18 +1,22 @@
 // Prompts of the gated delta rule, in chunks of 64 tokens on the matrix cores. Per value head, with the state S
-// (dk x dv here), G the running sum of log alpha in the chunk and kappa k~ = the key's unit vector:
-//   A_ij = beta_i e^(Gi - Gj) k_i . k_j (j < i),  T = (I + A)^-1                         no state in it
-//   R = beta V - beta e^G (K S),  U = T R,  O = e^G (Q S) + (e^(Gi - Gj) q_i . k_j)_{j <= i} U
+// (dk x dv here), G the running sum of log alpha in the chunk, K the keys as they are staged and kappa_i what makes row i
+// of them the token's key:
+//   A_ij = beta_i e^(Gi - Gj) kappa_i kappa_j k_i . k_j (j < i),  T = kappa (I + A)^-1 beta        no state in it
+//   R = V - kappa e^G (K S),  U = T R,  O = c e^G (Q S) + (c_i e^(Gi - Gj) q_i . k_j)_{j <= i} U
 //   S <- e^(G_C) S + K^T (e^(G_C - Gj) U)
-// Pass 1 (delta_chunk_kernel) has a workgroup per chunk and q/k head: T and the masked products of queries and keys
-// of its value heads. Pass 2 (delta_main_kernel) walks a sequence's chunks with the state in accumulators: columns of S
-// need nothing of each other, so a wave owns 16 of them and talks to no other wave.
+// (c: the queries' lengths and the output's scale.) Pass 1 (delta_chunk_kernel) has a workgroup per chunk and q/k head:
+// T and the masked products of queries and keys of its value heads. Pass 2 walks a sequence's chunks with the state in
+// accumulators: columns of S need nothing of each other, so a wave owns 16 of them and waits for no sum of another.
+// delta_split_kernel gives the outputs waves of their own where its LDS suffices, delta_main_kernel has one kind of wave.
+// Longer chunks than 64 tokens would have fewer steps in the chain, but more work in the inversion and in the products
+// with T; shorter ones more steps, each with the same waits.
 //
-// Operands are f16, sums float32. A row of q or k is scaled by the power of two that takes its largest value to 2^12
-// or to 1, which holds bf16 values exactly (those of k down to 2^-14 of the row's largest, smaller ones to 2^-25 of it);
-// float32 ones are two f16 values, 22 bits or 2^-25 of the largest. What is computed (S, R, U) is scaled by column in the same way and
-// split in two where it carries the state on; a product of two splits is three MFMAs, off by 2^-22. Where only an
-// output that will be rounded to bf16 depends on it, the first f16 value alone (2^-11) stands for S, U and the
-// products of queries and keys.
+// Operands are f16, sums float32. A row of k or q is scaled by the power of two that takes its largest value to 1
+// or to 2^12, which holds bf16 values exactly (those of k down to 2^-14 of the row's largest, smaller ones to 2^-25 of
+// it); float32 ones are two f16 values, 22 bits or 2^-25 of the largest. What is computed (S, R, U) is scaled by column
+// in the same way and split in two where it carries the state on; a product of two splits is three MFMAs, off by 2^-22.
+// Where only an output that will be rounded to bf16 depends on it, the first f16 value alone (2^-11) stands for S, U and
+// the products of queries and keys.
 #include <algorithm>
 
 #include "gate.h"
@@ -233,7 +237,11 @@ template <int NS> __device__ __forceinline__ f16x8 qk_piece(const char* lds, int
     return *(const f16x8*)(lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(lane & 15, lane >> 4)) * 16);
 }
 
-// One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves.
+// One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves. What bounds it is the
+// chain of its phases (rows to LDS, products, inversion by blocks, output), half of whose time is waits: 8 prompts of
+// 2048 tokens, 16 bf16 value heads of 128 over 8, 54 us for 147 MB written, the matrix pipe 12% busy, LDS 18%; three
+// workgroups to a compute unit for two took 63 us to that. A chunk of its own per value head read and multiplied the
+// rows twice (4 x 16384 tokens: 274 us for 222).
 // HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
 // is not stored.
 template <typename T, int NS, int HB>
@@ -678,6 +686,9 @@ dim3 work_grid(const DeltaArgs& p, int blocks) {
 
 // While a chunk is computed the next one's pieces and values are on their way, and the stores of its outputs stay out
 // at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'.
+// Bound by a chunk's chain of products and of the vector instructions that scale and split between them: 317, 1130 and
+// 601 float32 tokens, 16 heads of 128 x 128, 73 us, 4.0 us a chunk of the longest; with staging in front of each
+// chunk instead of beside it bf16 took 185 us for 62.
 template <typename T, int NS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <= 4 ? 2 : 1))) void delta_main_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
@@ -925,6 +936,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <
 // chunk before from the operands that the first left in LDS. The chain from chunk to chunk is that much shorter, and
 // both kinds run beside each other. Scales that need not be exact are bounds, known before what they scale:
 // a bound loses headroom (f16 pairs hold 39 bits, 22 are used), not precision.
+// 317, 1130 and 601 bf16 tokens, 16 heads of 128 x 128: 37.5 us, 2.1 us a chunk of the longest sequence (51
+// when it was built, 62 by delta_main_kernel then); 8 x 2048 tokens 98 us for 294 MB. Bound by the instructions of a chunk's chain (480 vector ones
+// and 82 MFMAs of a wave that carries the state) with the next chunk's 55 KB on their way; matrix pipe 24% busy, LDS
+// 34%. Touching the chunk after next for L2, loads by the waves that carry the state and other orders of the products
+// gave nothing or cost time.
 template <typename T, int NS, int W> struct SplitLds {
     static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes(), kP = (int)p_bytes(kParts<T>);
     static constexpr int kRow = 16 * W * (int)sizeof(T), kRows = kC * kRow;   // the workgroup's values of a token, of a chunk

@@ -235,6 +235,18 @@ def test_empty_sequences():
     assert (f64(pool)[L.slots[0]] == 0).all() and np.array_equal(f64(pool)[L.slots[2]], L.pool[L.slots[2]])
 
 
+@pytest.mark.parametrize("n", [2, 300])
+@pytest.mark.parametrize("rows", [0, 5])
+def test_call_without_tokens(n, rows):
+    """Nothing but the states of fresh sequences is written, which become zeros."""
+    L = Layer(torch, (1, 2, 64, 64), [0] * n, "f32", seed=16, init=[0, 1] * (n // 2))
+    out, pool, status, behind = _prefill(L, rows_behind=rows)
+    assert status == 0 and out.shape[0] == rows and torch.isnan(behind).all()
+    want = L.pool.copy()
+    want[L.slots[::2]] = 0
+    assert np.array_equal(f64(pool), want, equal_nan=True)
+
+
 @pytest.mark.parametrize("act", ["bf16", "f32"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
 def test_values_that_are_not_finite(act, value):
