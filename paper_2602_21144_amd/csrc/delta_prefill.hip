@@ -286,6 +286,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
     const int64_t t0 = (int64_t)__builtin_amdgcn_readfirstlane(sr.lo) + (int64_t)chunk * kC;
     const int nq = min(__builtin_amdgcn_readfirstlane(sr.n) - chunk * kC, kC);
 
+    // the gates of a value head by wave 2 or 3, a token a lane; into place b. Asked for in front of the rows and worked out
+    // while these are on their way
+    T av{}, bv{};
+    float la = 0.0f, db = 0.0f;
+    auto gate_loads = [&](int h) {
+        if (lane < nq) {
+            av = ((const T*)p.a)[(t0 + lane) * p.ld_ab + h];
+            bv = ((const T*)p.b)[(t0 + lane) * p.ld_ab + h];
+        }
+        la = p.A_log[h];
+        db = p.dt_bias[h];
+    };
+    if (wave >= 2 && wave - 2 < HB) gate_loads(hk * p.rep + wave - 2);
+
     // rows of q and k: four threads to a row
     const __amdgpu_buffer_rsrc_t rx = buffer_rsrc((const T*)p.qkv + t0 * p.ld, (uint32_t)((nq - 1) * p.ld + 2 * p.Hk * p.dk) * sizeof(T));
     const int row = tid >> 2, c4 = tid & 3;
@@ -297,20 +311,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
         xk[s].load(rx, off + (uint32_t)(p.Hk * p.dk) * (uint32_t)sizeof(T));
         xq[s].load(rx, off);
     }
-    // the gates of a value head by wave 2 or 3, a token a lane; into place b
-    float av = 0.0f, bv = 0.0f;
-    auto gate_loads = [&](int h) {
-        if (lane < nq) {
-            av = to_f32(((const T*)p.a)[(t0 + lane) * p.ld_ab + h]);
-            bv = to_f32(((const T*)p.b)[(t0 + lane) * p.ld_ab + h]);
-        }
-    };
-    if (wave >= 2 && wave - 2 < HB) gate_loads(hk * p.rep + wave - 2);
-    auto gates = [&](int h, int b) {
+    auto gates = [&](int b) {
         // log2 of alpha; below -1000 it is 0 in float32 either way, and the sums of what follows stay exact. The running
         // sum in 64 bits of 2^-40 (its absolute error is what counts), kept as two float32 values: what comes
         // after a reset is as exact as without one
-        float g = -fast_exp2(p.A_log[h] * kLog2e) * kLog2e * softplus_f(av + p.dt_bias[h]);
+        float g = -fast_exp2(la * kLog2e) * kLog2e * softplus_f(to_f32(av) + db);
         const bool nan = g != g;
         g = lane < nq ? (g < -1000.0f ? -1000.0f : g) : 0.0f;
         const int64_t c = wave_scan64(nan ? 0 : (int64_t)((double)g * 1099511627776.0));
@@ -319,8 +324,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
         const bool bad = (__ballot(nan && lane < nq) & (~0ull >> (63 - lane))) != 0;
         s_gh[b][lane] = bad ? __builtin_nanf("") : (float)d;
         s_gl[b][lane] = (float)(d - (double)(float)d);
-        s_beta[b][lane] = lane < nq ? p.beta_max * sigmoid_f(bv) : 0.0f;
+        s_beta[b][lane] = lane < nq ? p.beta_max * sigmoid_f(to_f32(bv)) : 0.0f;
     };
+    if (wave >= 2 && wave - 2 < HB) gates(wave - 2);
     int eq, ek;
     const float sk = stage_row<T, NS>(xk, row, c4, 0, s_k, &ek);
     const float sq = stage_row<T, NS>(xq, row, c4, 12, s_q, &eq);
@@ -329,7 +335,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
         s_c[row] = p.scale * (p.qk_norm ? 1.0f / sqrtf(fmaxf(sq + p.eps, 1.2e-38f)) : 1.0f) * pow2(-eq);
         s_kap[row] = (p.qk_norm ? 1.0f / sqrtf(fmaxf(sk + p.eps, 1.2e-38f)) : 1.0f) * pow2(-ek);
     }
-    if (wave >= 2 && wave - 2 < HB) gates(hk * p.rep + wave - 2, wave - 2);
     __syncthreads();
 
     // K K^T and K Q^T: wave w has columns i = 16 w + lane % 16, pieces n of rows j = 32 n + 16 q + 4 hh + r up to the
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void d
             __syncthreads();
             if (wave >= 2 && wave - 2 < heads) {
                 gate_loads(hk * p.rep + r0 + wave - 2);
-                gates(hk * p.rep + r0 + wave - 2, wave - 2);
+                gates(wave - 2);
             }
             __syncthreads();
         }
@@ -936,11 +941,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <
 // chunk before from the operands that the first left in LDS. The chain from chunk to chunk is that much shorter, and
 // both kinds run beside each other. Scales that need not be exact are bounds, known before what they scale:
 // a bound loses headroom (f16 pairs hold 39 bits, 22 are used), not precision.
-// 317, 1130 and 601 bf16 tokens, 16 heads of 128 x 128: 37.5 us, 2.1 us a chunk of the longest sequence (51
-// when it was built, 62 by delta_main_kernel then); 8 x 2048 tokens 98 us for 294 MB. Bound by the instructions of a chunk's chain (480 vector ones
-// and 82 MFMAs of a wave that carries the state) with the next chunk's 55 KB on their way; matrix pipe 24% busy, LDS
-// 34%. Touching the chunk after next for L2, loads by the waves that carry the state and other orders of the products
-// gave nothing or cost time.
+// 317, 1130 and 601 bf16 tokens, 16 heads of 128 x 128: 37.5 us, 2.1 us a chunk of the longest sequence (51 when it was
+// built, 62 by delta_main_kernel then); 8 x 2048 tokens 98 us for 294 MB. Bound by the instructions of a chunk's chain
+// (480 vector ones and 82 MFMAs of a wave that carries the state) with the next chunk's 55 KB on their way; matrix pipe
+// 24% busy, LDS 34%. Touching the chunk after next for L2, loads by the waves that carry the state and other orders of
+// the products gave nothing or cost time.
 template <typename T, int NS, int W> struct SplitLds {
     static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes(), kP = (int)p_bytes(kParts<T>);
     static constexpr int kRow = 16 * W * (int)sizeof(T), kRows = kC * kRow;   // the workgroup's values of a token, of a chunk
