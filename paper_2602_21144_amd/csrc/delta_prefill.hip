@@ -239,8 +239,8 @@ template <int NS> __device__ __forceinline__ f16x8 qk_piece(const char* lds, int
 
 // One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves. What bounds it is the
 // chain of its phases (rows to LDS, products, inversion by blocks, output), half of whose time is waits: 8 prompts of
-// 2048 tokens, 16 bf16 value heads of 128 over 8, 54 us for 147 MB written, the matrix pipe 12% busy, LDS 18%; three
-// workgroups to a compute unit for two took 63 us to that. A chunk of its own per value head read and multiplied the
+// 2048 tokens, 16 bf16 value heads of 128 over 8, 53 us for 147 MB written, the matrix pipe 12% busy, LDS 18%; three
+// workgroups to a compute unit for two took 63 us to 55. 4 x 16384 tokens, 924 MB, 180 us: HBM. A chunk of its own per value head read and multiplied the
 // rows twice (4 x 16384 tokens: 274 us for 222).
 // HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
 // is not stored.
