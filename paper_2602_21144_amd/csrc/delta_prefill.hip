@@ -245,7 +245,7 @@ template <int NS> __device__ __forceinline__ f16x8 qk_piece(const char* lds, int
 // HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
 // is not stored.
 template <typename T, int NS, int HB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void delta_chunk_kernel(Args a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> * NS <= 8 ? 2 : 1))) void delta_chunk_kernel(Args a) {
     constexpr int PA = kParts<T>, kQk = (int)qk_bytes(NS, PA);
     // q's pieces, and once they are used the heads' matrices in their place
     constexpr int kMat = HB * kC * kLdA * 4;
