@@ -11,12 +11,12 @@
 // Longer chunks than 64 tokens would have fewer steps in the chain, but more work in the inversion and in the products
 // with T; shorter ones more steps, each with the same waits.
 //
-// Operands are f16, sums float32. A row of k or q is scaled by the power of two that takes its largest value to 1
-// or to 2^12, which holds bf16 values exactly (those of k down to 2^-14 of the row's largest, smaller ones to 2^-25 of
-// it); float32 ones are two f16 values, 22 bits or 2^-25 of the largest. What is computed (S, R, U) is scaled by column
-// in the same way and split in two where it carries the state on; a product of two splits is three MFMAs, off by 2^-22.
-// Where only an output that will be rounded to bf16 depends on it, the first f16 value alone (2^-11) stands for S, U and
-// the products of queries and keys.
+// Operands are bf16, sums float32. A float32 value is the sum of three bf16 ones, each the rounding of what those in front
+// of it leave: 8 bits and a sign each, float32's range, so nothing has a scale that another value could set. Of
+// the products of two such values the six largest are formed; the others are below 2^-26 of the whole. q, k and v in
+// bf16 are one value. f16 pairs with a scale by row or column were faster (a product of two is three MFMAs, and
+// T and the products with queries take two thirds of the bytes), but what lay far below the largest value of a
+// scale lost its bits: tokens whose write gate is nearly closed, all that follows a reset.
 #include <algorithm>
 
 #include "gate.h"
@@ -24,18 +24,19 @@
 namespace ssm {
 namespace {
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kC = 64;           // tokens per chunk
 constexpr int kFrags = 6;        // 16 x 32 pieces of a lower triangular 64 x 64 matrix
-// factors for the state, by token: e^G kappa, e^(G_C - G); then e^(G_C), the scale of T, a bound of e^G |k|
-constexpr int kFacDecay = 2 * kC, kFacT = 2 * kC + 1, kFacMax = 2 * kC + 2;
-constexpr size_t kFacBytes = 1024, kOutFacBytes = 1024;   // and for the outputs: c e^G, c 2^8
+// factors by token: e^G kappa, e^(G_C - G), e^G, c; e^(G_C) is the last token's e^G (behind a sequence G stays)
+constexpr int kFacDecay = 3 * kC - 1;
+constexpr size_t kFacBytes = 4 * kC * 4;
 constexpr int kFindSeqs = 256;   // more sequences are laid out by a launch of its own
 
-// the parts of a stored q, k or product: float32 activations take two f16 values
-template <typename T> constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+constexpr int kSplit = 3;        // bf16 values that hold a float32 one
+// the parts of a stored q or k
+template <typename T> constexpr int kParts = sizeof(T) == 4 ? kSplit : 1;
 
 // Piece (row tile it, k step s) of a lower triangle: rows 16 it .., columns 32 s ..
 __host__ __device__ constexpr int frag_of(int it, int s) { return it < 2 ? it : 2 * it - 2 + s; }
@@ -44,12 +45,12 @@ __host__ __device__ constexpr int frag_of(int it, int s) { return it < 2 ? it : 
 // have their rows rotated by 4 hh, so that the transposing reads of k meet every bank once.
 __device__ __forceinline__ int qk_unit(int row, int hh) { return 16 * hh + ((row + 4 * hh) & 15); }
 
-// Sizes of the workspace. Per chunk and q/k head: pieces of k, then of q; per chunk and value head: kappa T beta (two
-// parts) and the state's factors, then the products of queries and keys and the outputs' factors.
+// Sizes of the workspace. Per chunk and q/k head: pieces of k, then of q; per chunk and value head: kappa T beta and the
+// factors, then the products of queries and keys.
 constexpr size_t qk_bytes(int NS, int parts) { return (size_t)4 * NS * parts * 1024; }   // k or q
-constexpr size_t t_bytes() { return (size_t)kFrags * 2 * 1024 + kFacBytes; }                            // for the state
-constexpr size_t p_bytes(int parts) { return (size_t)kFrags * parts * 1024 + kOutFacBytes; }           // for the outputs
-constexpr size_t v_bytes(int parts) { return t_bytes() + p_bytes(parts); }
+constexpr size_t t_bytes() { return (size_t)kFrags * kSplit * 1024 + kFacBytes; }        // for the state
+constexpr size_t p_bytes() { return (size_t)kFrags * kSplit * 1024; }                    // for the outputs
+constexpr size_t v_bytes() { return t_bytes() + p_bytes(); }
 
 struct DeltaWs {
     int32_t* base;     // [nseq] first chunk of every sequence
@@ -98,17 +99,6 @@ __device__ __forceinline__ int64_t wave_scan64(int64_t c) {
     return c + dpp64<0x143, 0xC>(c);
 }
 
-// The largest of the wave's values, none of them negative (their bits compare like they do)
-__device__ __forceinline__ float wave_max(float v) {
-    int c = __builtin_bit_cast(int, v);
-    c = max(c, dpp<0x111, 0xF>(c));
-    c = max(c, dpp<0x112, 0xF>(c));
-    c = max(c, dpp<0x114, 0xF>(c));
-    c = max(c, dpp<0x118, 0xF>(c));
-    c = max(c, dpp<0x142, 0xA>(c));
-    c = max(c, dpp<0x143, 0xC>(c));
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(c, 63));
-}
 // over four neighbouring lanes
 __device__ __forceinline__ float quad_sum(float v) {
     v += __builtin_bit_cast(float, dpp<0xB1, 0xF>(__builtin_bit_cast(int, v)));
@@ -152,23 +142,38 @@ __global__ __launch_bounds__(256) void delta_plan_kernel(Args a) {
 }
 
 __device__ __forceinline__ float pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(127 + e) << 23); }
-// The exponent of m's scale: m pow2(scale_exp(m)) lies in [2^12, 2^13); 0 and what is too small or not finite get one
-// that keeps all factors finite
-__device__ __forceinline__ int scale_exp(float m) {
+// The exponent that takes a row's largest value m to [1, 2); 0 and what is too small or not finite get one that keeps all
+// factors finite
+__device__ __forceinline__ int row_exp(float m) {
     const int e = (int)((__builtin_bit_cast(uint32_t, m) >> 23) & 255u);
-    return 12 + 127 - min(max(e, 40), 230);
+    return 127 - min(max(e, 40), 230);
 }
 
-template <int N> __device__ __forceinline__ f16x8 pair_f16(const float (&v)[N], int at) {
-    f16x8 o;
+// The next bf16 values of eight that are left, rounded to nearest; v: what they leave
+__device__ __forceinline__ bf16x8 take8(float (&v)[8]) {
+    bf16x8 o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = (_Float16)v[at + e];
+    for (int e = 0; e < 8; e += 2) {
+        const bf16x2 h = __builtin_convertvector((f32x2){v[e], v[e + 1]}, bf16x2);
+        o[e] = h[0];
+        o[e + 1] = h[1];
+        v[e] -= (float)h[0];
+        v[e + 1] -= (float)h[1];
+    }
     return o;
 }
-
-__device__ __forceinline__ f32x4 mma(const f16x8& a, const f16x8& b, const f32x4& c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+template <int N> __device__ __forceinline__ void split8(float (&v)[8], bf16x8 (&o)[N]) {
+#pragma unroll
+    for (int part = 0; part < N; ++part) o[part] = take8(v);
 }
+
+__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// The products of two values in parts, the largest first: part first(n) of the one and second(n) of the other
+constexpr int kProducts = 6;
+constexpr int first(int n) { return n == 2 || n == 4 ? 1 : n == 5 ? 2 : 0; }
+constexpr int second(int n) { return n == 1 || n == 4 ? 1 : n == 3 ? 2 : 0; }
 __device__ __forceinline__ f32x4 mma4(float a, float b, const f32x4& c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
@@ -190,10 +195,8 @@ template <typename T> struct Piece {   // eight values of a row
     }
 };
 
-// The pieces of a row of q or k that this thread (c4 of four) holds: scaled to f16 parts in operand layout, to LDS. The
-// row's largest value comes to 2^top. Returns the sum of squares of the row; e: the exponent of its scale.
-template <typename T, int NS>
-__device__ __forceinline__ float stage_row(const Piece<T> (&x)[NS], int row, int c4, int top, char* lds, int* e) {
+// Of a row of q or k that four threads hold: the sum of squares, and the exponent of its scale
+template <typename T, int NS> __device__ __forceinline__ float row_sizes(const Piece<T> (&x)[NS], int* e) {
     float ss = 0.0f, m = 0.0f;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -205,54 +208,53 @@ __device__ __forceinline__ float stage_row(const Piece<T> (&x)[NS], int row, int
             m = fmaxf(m, fabsf(v[k]));
         }
     }
-    ss = quad_sum(ss);
-    *e = scale_exp(quad_max(m)) - 12 + top;
-    const float f = pow2(*e);
+    *e = row_exp(quad_max(m));
+    return quad_sum(ss);
+}
+// N pieces of the row that this thread (c4 of four) holds, from s0 on, times f: in operand layout, to LDS
+template <typename T, int N, int NS>
+__device__ __forceinline__ void stage_row(const Piece<T> (&x)[NS], int s0, int row, int c4, float f, char* lds) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
+    for (int s = 0; s < N; ++s) {
         float v[8];
-        x[s].values(v);
+        x[s0 + s].values(v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= f;
 #pragma unroll
         for (int part = 0; part < kParts<T>; ++part) {
-            const f16x8 h = pair_f16(v, 0);
+            const bf16x8 h = take8(v);
             // values 0..3 of the piece are (hh, half) = (2 (c4 & 1), c4 / 2), values 4..7 the next hh
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                f16x4 o;
+                bf16x4 o;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[k] = h[4 * q + k];
-                const int at = (((part * 4 + (row >> 4)) * NS + s) * 64 + qk_unit(row & 15, 2 * (c4 & 1) + q)) * 16 + (c4 >> 1) * 8;
-                *(f16x4*)(lds + at) = o;
+                const int at = (((part * 4 + (row >> 4)) * N + s) * 64 + qk_unit(row & 15, 2 * (c4 & 1) + q)) * 16 + (c4 >> 1) * 8;
+                *(bf16x4*)(lds + at) = o;
             }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] -= (float)h[k];
         }
     }
-    return ss;
 }
 
-template <int NS> __device__ __forceinline__ f16x8 qk_piece(const char* lds, int part, int it, int s, int lane) {
-    return *(const f16x8*)(lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(lane & 15, lane >> 4)) * 16);
+template <int NS> __device__ __forceinline__ bf16x8 qk_piece(const char* lds, int part, int it, int s, int lane) {
+    return *(const bf16x8*)(lds + (((part * 4 + it) * NS + s) * 64 + qk_unit(lane & 15, lane >> 4)) * 16);
 }
 
 // One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves. What bounds it is the
-// chain of its phases (rows to LDS, products, inversion by blocks, output), half of whose time is waits: 8 prompts of
-// 2048 tokens, 16 bf16 value heads of 128 over 8, 53 us for 147 MB written, the matrix pipe 12% busy, LDS 18%; three
-// workgroups to a compute unit for two took 63 us to 55. 4 x 16384 tokens, 924 MB, 180 us: HBM. A chunk of its own per value head read and multiplied the
-// rows twice (4 x 16384 tokens: 274 us for 222).
+// chain of its phases (rows to LDS, products, inversion by blocks, output), half of whose time is waits, and with many
+// chunks HBM. A chunk of its own per value head read and multiplied the rows twice.
 // HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
 // is not stored.
 template <typename T, int NS, int HB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> * NS <= 8 ? 2 : 1))) void delta_chunk_kernel(Args a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> * NS <= 12 ? 2 : 1))) void delta_chunk_kernel(Args a) {
     constexpr int PA = kParts<T>, kQk = (int)qk_bytes(NS, PA);
+    // pieces in LDS at a time: float32 rows come in two halves
+    constexpr int kTurns = PA > 1 && NS >= 4 ? 2 : 1, NH = NS / kTurns, kTurn = kQk / kTurns;
     // q's pieces, and once they are used the heads' matrices in their place
     constexpr int kMat = HB * kC * kLdA * 4;
-    __shared__ __attribute__((aligned(16))) char s_k[kQk], s_q[kQk > kMat ? kQk : kMat];
+    __shared__ __attribute__((aligned(16))) char s_k[kTurn], s_q[kTurn > kMat ? kTurn : kMat];
     float(*s_t)[kC * kLdA] = (float(*)[kC * kLdA])s_q;
-    __shared__ __attribute__((aligned(16))) float s_gh[HB][kC], s_gl[HB][kC], s_beta[HB][kC], s_kap[kC], s_c[kC], s_len[kC];
-    __shared__ float s_max[HB][4];
+    __shared__ __attribute__((aligned(16))) float s_gh[HB][kC], s_gl[HB][kC], s_beta[HB][kC], s_kap[kC], s_c[kC];
     __shared__ int s_find[8];
     const DeltaArgs& p = a.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slot = blockIdx.x, hk = blockIdx.y;
@@ -328,14 +330,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> *
     };
     if (wave >= 2 && wave - 2 < HB) gates(wave - 2);
     int eq, ek;
-    const float sk = stage_row<T, NS>(xk, row, c4, 0, s_k, &ek);
-    const float sq = stage_row<T, NS>(xq, row, c4, 12, s_q, &eq);
+    const float sk = row_sizes<T, NS>(xk, &ek), sq = row_sizes<T, NS>(xq, &eq);
     if (c4 == 0) {
-        s_len[row] = sqrtf(sk) * pow2(ek);
         s_c[row] = p.scale * (p.qk_norm ? 1.0f / sqrtf(fmaxf(sq + p.eps, 1.2e-38f)) : 1.0f) * pow2(-eq);
         s_kap[row] = (p.qk_norm ? 1.0f / sqrtf(fmaxf(sk + p.eps, 1.2e-38f)) : 1.0f) * pow2(-ek);
     }
-    __syncthreads();
 
     // K K^T and K Q^T: wave w has columns i = 16 w + lane % 16, pieces n of rows j = 32 n + 16 q + 4 hh + r up to the
     // diagonal: one piece for waves 0 and 1, two for the others
@@ -348,48 +347,55 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> *
         return l;
     };
     const bool odd = (it & 1) != 0;                    // the second tile of the last piece reaches the diagonal
-    const float kap = s_kap[16 * it + (lane & 15)];
     f32x4 kk[2][2], kq[2][2];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        if (n >= pieces) break;
-        kk[n][0] = kk[n][1] = kq[n][0] = kq[n][1] = f32x4{};
+    for (int n = 0; n < 2; ++n) kk[n][0] = kk[n][1] = kq[n][0] = kq[n][1] = f32x4{};
+    char* qk = a.w.qk + ((int64_t)slot * p.Hk + hk) * (2 * kQk);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const f16x8 y = qk_piece<NS>(s_k, 0, it, s, lane), z = qk_piece<NS>(s_q, 0, it, s, lane);
-            f16x8 yl{}, zl{};
-            if constexpr (PA == 2) {
-                yl = qk_piece<NS>(s_k, 1, it, s, lane);
-                zl = qk_piece<NS>(s_q, 1, it, s, lane);
-            }
+    for (int turn = 0; turn < kTurns; ++turn) {
+        if (turn > 0) __syncthreads();
+        stage_row<T, NH, NS>(xk, NH * turn, row, c4, pow2(ek), s_k);
+        stage_row<T, NH, NS>(xq, NH * turn, row, c4, pow2(eq), s_q);
+        __syncthreads();
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                if (q == 1 && n + 1 == pieces && !odd) break;
-                const f16x8 x = qk_piece<NS>(s_k, 0, 2 * n + q, s, lane);
-                kk[n][q] = mma(x, y, kk[n][q]);
-                kq[n][q] = mma(x, z, kq[n][q]);
-                if constexpr (PA == 2) {
-                    const f16x8 xl = qk_piece<NS>(s_k, 1, 2 * n + q, s, lane);
-                    kk[n][q] = mma(xl, y, kk[n][q]);
-                    kq[n][q] = mma(xl, z, kq[n][q]);
-                    kk[n][q] = mma(x, yl, kk[n][q]);
-                    kq[n][q] = mma(x, zl, kq[n][q]);
+        for (int n = 0; n < 2; ++n) {
+            if (n >= pieces) break;
+#pragma unroll
+            for (int s = 0; s < NH; ++s) {
+                bf16x8 y[PA], z[PA];
+#pragma unroll
+                for (int part = 0; part < PA; ++part) {
+                    y[part] = qk_piece<NH>(s_k, part, it, s, lane);
+                    z[part] = qk_piece<NH>(s_q, part, it, s, lane);
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    if (q == 1 && n + 1 == pieces && !odd) break;
+                    bf16x8 x[PA];
+#pragma unroll
+                    for (int part = 0; part < PA; ++part) x[part] = qk_piece<NH>(s_k, part, 2 * n + q, s, lane);
+#pragma unroll
+                    for (int m = 0; m < kProducts; ++m) {
+                        if (first(m) >= PA || second(m) >= PA) continue;
+                        kk[n][q] = mma(x[first(m)], y[second(m)], kk[n][q]);
+                        kq[n][q] = mma(x[first(m)], z[second(m)], kq[n][q]);
+                    }
                 }
             }
         }
-    }
-    char* qk = a.w.qk + ((int64_t)slot * p.Hk + hk) * (2 * kQk);
 #pragma unroll
-    for (int n = 0; n < kQk / 4096; ++n) {
-        const int u = (n * 256 + tid) * 16;
-        *(u32x4*)(qk + u) = *(const u32x4*)(s_k + u);
-        *(u32x4*)(qk + kQk + u) = *(const u32x4*)(s_q + u);
+        for (int n = 0; n < kTurn / 4096; ++n) {
+            const int b = n * 4 + wave, from = (b * 64 + lane) * 16, to = ((b / NH * NS + turn * NH + b % NH) * 64 + lane) * 16;
+            *(u32x4*)(qk + to) = *(const u32x4*)(s_k + from);
+            *(u32x4*)(qk + kQk + to) = *(const u32x4*)(s_q + from);
+        }
     }
+    const float kap = s_kap[16 * it + (lane & 15)];
     __syncthreads();
 
     for (int r0 = 0; r0 < p.rep; r0 += HB) {
         const int heads = min(HB, p.rep - r0);
-        auto vout = [&](int b) { return a.w.v + ((int64_t)slot * p.Hv + hk * p.rep + r0 + b) * v_bytes(PA); };
+        auto vout = [&](int b) { return a.w.v + ((int64_t)slot * p.Hv + hk * p.rep + r0 + b) * v_bytes(); };
         if (r0 > 0) {
             __syncthreads();
             if (wave >= 2 && wave - 2 < heads) {
@@ -432,7 +438,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> *
                     for (int r = 0; r < 4; ++r) {
                         const float ex = fast_exp2((gh[b] - jh[b][q][r]) + (gl[b] - jl[b][q][r]));
                         m[r] = j + r < i ? kk[n][q][r] * ex * (bk[b] * jk[q][r]) : 0.0f;
-                        x[b][4 * q + r] = j + r <= i ? kq[n][q][r] * ex * pow2(-8) : 0.0f;
+                        x[b][4 * q + r] = j + r <= i ? kq[n][q][r] * ex : 0.0f;
                     }
                     *(f32x4*)&s_t[b][i * kLdA + j] = m;   // zeros above the diagonal, where this piece has them
                 }
@@ -441,12 +447,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> *
                 if (b >= heads) break;
                 char* to = vout(b) + t_bytes() + (frag_of(it, n) * 1024 + l * 16);
 #pragma unroll
-                for (int part = 0; part < PA; ++part) {
-                    const f16x8 o = pair_f16(x[b], 0);
-                    *(f16x8*)(to + part * kFrags * 1024) = o;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[b][e] -= (float)o[e];
-                }
+                for (int part = 0; part < kSplit; ++part) *(bf16x8*)(to + part * kFrags * 1024) = take8(x[b]);
             }
         }
         }
@@ -487,18 +488,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> *
         // the tokens' factors, by waves 2 and 3
         if (wave >= 2 && wave - 2 < heads) {
             const int b = wave - 2;
-            float *fac = (float*)(vout(b) + t_bytes() - kFacBytes), *f = (float*)(vout(b) + v_bytes(PA) - kOutFacBytes);
+            float* fac = (float*)(vout(b) + t_bytes() - kFacBytes);
             const float gh = s_gh[b][lane], gl = s_gl[b][lane], ch = s_gh[b][kC - 1], cl = s_gl[b][kC - 1];
-            const float eg = fast_exp2(gh + gl), bg = eg * s_kap[lane];
-            fac[lane] = bg;
+            const float eg = fast_exp2(gh + gl);
+            fac[lane] = eg * s_kap[lane];
             fac[kC + lane] = fast_exp2((ch - gh) + (cl - gl));
-            const float m = wave_max(bg * s_len[lane] * 1.001f);
-            if (lane == 0) {
-                fac[kFacDecay] = fast_exp2(ch + cl);
-                fac[kFacMax] = m;
-            }
-            f[lane] = s_c[lane] * eg;
-            f[kC + lane] = s_c[lane] * pow2(8);
+            fac[2 * kC + lane] = eg;
+            fac[3 * kC + lane] = s_c[lane];
         }
         __syncthreads();
         // a row piece (this lane's row, columns 4 hh ..) of a block, and its column entries 4 hh + r of this lane's column;
@@ -546,101 +542,48 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kParts<T> *
             for (int b = 0; b < HB; ++b) put(s_t[b], 32 + 16 * r2, c0, y[b], l);
         }
         __syncthreads();
-        // kappa T beta, scaled by the power of two that takes its largest value to 2^12; wave w has row tile w
-        float x[HB][2][8];
+        // kappa T beta: wave w has row tile w
         const int l = place(), hh = l >> 4;
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
-            float m = 0.0f;
+            if (b >= heads) break;
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 if (n >= pieces) break;
                 const f32x4 v0 = row4(s_t[b], 16 * it, 32 * n, l), v1 = row4(s_t[b], 16 * it, 32 * n + 16, l);
                 const f32x4 b0 = *(const f32x4*)&s_beta[b][32 * n + 4 * hh], b1 = *(const f32x4*)&s_beta[b][32 * n + 16 + 4 * hh];
                 const bool two = odd || n + 1 < pieces;
+                float x[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    x[b][n][e] = v0[e] * b0[e] * kap;
-                    x[b][n][4 + e] = two ? v1[e] * b1[e] * kap : 0.0f;
-                    m = fmaxf(m, fmaxf(fabsf(x[b][n][e]), fabsf(x[b][n][4 + e])));
+                    x[e] = v0[e] * b0[e] * kap;
+                    x[4 + e] = two ? v1[e] * b1[e] * kap : 0.0f;
                 }
-            }
-            m = wave_max(m);
-            if (lane == 0) s_max[b][wave] = m;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int b = 0; b < HB; ++b) {
-            if (b >= heads) break;
-            const int et = scale_exp(fmaxf(fmaxf(s_max[b][0], s_max[b][1]), fmaxf(s_max[b][2], s_max[b][3])));
-            const float f = pow2(et);
-            if (tid == 0) ((float*)(vout(b) + t_bytes() - kFacBytes))[kFacT] = pow2(-et);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                if (n >= pieces) break;
                 char* to = vout(b) + (frag_of(it, n) * 1024 + l * 16);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[b][n][e] *= f;
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const f16x8 o = pair_f16(x[b][n], 0);
-                    *(f16x8*)(to + part * kFrags * 1024) = o;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[b][n][e] -= (float)o[e];
-                }
+                for (int part = 0; part < kSplit; ++part) *(bf16x8*)(to + part * kFrags * 1024) = take8(x);
             }
         }
     }
 }
 
 // ---------------------------------------------------------------- pass 2
-// Values of this lane's column: their largest magnitude over the column's four lanes
-__device__ __forceinline__ float column_max(float m) {
-    const uint32_t v = __builtin_bit_cast(uint32_t, m);
-    const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    const uint32_t w = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])));
-    const auto y = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)y[0]), __builtin_bit_cast(float, (uint32_t)y[1]));
-}
-template <int N> __device__ __forceinline__ float largest(const f32x4 (&v)[N]) {
-    float m = 0.0f;
+// Two stacked tiles as an operand: the bf16 values of each
+template <int N> __device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, bf16x8 (&o)[N]) {
+    float v[8];
 #pragma unroll
-    for (int t = 0; t < N; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(v[t][r]));
-    return m;
-}
-// Two stacked tiles, times f (a power of two), as an operand: its first f16 values, and what they leave. SCALED false: f is
-// one, though the compiler does not know it. Of two values that are left the first goes through an empty statement, which
-// makes one instruction of each (a product, a difference and a rounding), where their conversion as a pair would
-// take three
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-template <bool LO, bool SCALED = true>
-__device__ __forceinline__ void split2(const f32x4& x0, const f32x4& x1, float f, f16x8& hi, f16x8& lo) {
-#pragma unroll
-    for (int r = 0; r < 8; r += 2) {
-        const float a = r < 4 ? x0[r] : x1[r - 4], b = r < 4 ? x0[r + 1] : x1[r - 3];
-        const f16x2 h = __builtin_convertvector((f32x2){SCALED ? a * f : a, SCALED ? b * f : b}, f16x2);
-        hi[r] = h[0];
-        hi[r + 1] = h[1];
-        if constexpr (LO) {
-            _Float16 l = (_Float16)__builtin_fmaf(a, f, -(float)h[0]);
-            asm("" : "+v"(l));
-            lo[r] = l;
-            lo[r + 1] = (_Float16)__builtin_fmaf(b, f, -(float)h[1]);
-        }
+    for (int r = 0; r < 4; ++r) {
+        v[r] = x0[r];
+        v[4 + r] = x1[r];
     }
+    split8(v, o);
 }
 
-// What pass 2 holds in LDS: two stages of a chunk's k, masked products and factors, and of its q where they fit
-// (kQStages 2); else one of q (1); else a single stage of everything, waited for in full (0).
+// What delta_main_kernel holds in LDS: a chunk's k, T and factors, in two stages or, where these do not fit, one
 constexpr size_t kLds = 160 * 1024;
 template <typename T, int NS> struct MainLds {
-    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kV = (int)v_bytes(kParts<T>);
-    static constexpr int kQStages = 2 * (2 * kQk + kV) <= (int)kLds ? 2 : 2 * (kQk + kV) + kQk <= (int)kLds ? 1 : 0;
-    static constexpr int kStages = kQStages > 0 ? 2 : 1;
-    static constexpr int kBytes = kStages * (kQk + kV) + (kQStages == 2 ? 2 : 1) * kQk;
+    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes();
+    static constexpr int kStages = 2 * (kQk + kT) <= (int)kLds ? 2 : 1, kBytes = kStages * (kQk + kT);
     static_assert(kBytes <= (int)kLds, "pass 2 does not fit into LDS");
 };
 
@@ -653,6 +596,32 @@ template <int WAVES, int BYTES> __device__ __forceinline__ void dma_pieces(const
         if (N % WAVES == 0 || j < N)
             dma16(r, (uint32_t)lane * 16, from + (uint32_t)j * 1024, __builtin_amdgcn_readfirstlane(lds + (uint32_t)j * 1024));
     }
+}
+// Pieces that a wave holds in registers: of q, k step s, and the products of queries and keys
+template <int NS, int PA> __device__ __forceinline__ void load_q(bf16x8 (&q)[PA][4], const char* from, int s, int lane) {
+#pragma unroll
+    for (int part = 0; part < PA; ++part)
+#pragma unroll
+        for (int it = 0; it < 4; ++it) q[part][it] = qk_piece<NS>(from, part, it, s, lane);
+}
+__device__ __forceinline__ void load_p(bf16x8 (&x)[kSplit][kFrags], const char* from, int lane) {
+#pragma unroll
+    for (int part = 0; part < kSplit; ++part)
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) x[part][f] = *(const bf16x8*)(from + (part * kFrags + f) * 1024 + lane * 16);
+}
+// Rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of 16 values of k, transposed
+// as they are read
+template <int NS> __device__ __forceinline__ bf16x8 kt_piece(const char* s_k, int part, int s, int t, int lane) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds4;
+    s16x4 k2[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const char* at = s_k + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 + qk_unit(4 * (lane >> 4) + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
+        k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
+    }
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // One value of a row of T, zero (and nothing stored) behind the buffer's end
@@ -690,15 +659,14 @@ dim3 work_grid(const DeltaArgs& p, int blocks) {
 }
 
 // While a chunk is computed the next one's pieces and values are on their way, and the stores of its outputs stay out
-// at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'.
-// Bound by a chunk's chain of products and of the vector instructions that scale and split between them: 317, 1130 and
-// 601 float32 tokens, 16 heads of 128 x 128, 73 us, 4.0 us a chunk of the longest; with staging in front of each
-// chunk instead of beside it bf16 took 185 us for 62.
+// at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'. q, in a
+// wave's registers, is asked for again once it is used where all of it fits there (kHold).
 template <typename T, int NS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <= 4 ? 2 : 1))) void delta_main_kernel(Args a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1))) void delta_main_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
+    constexpr bool kHold = NS * PA <= 12;
     using L = MainLds<T, NS>;
-    constexpr int kQk = L::kQk, kV = L::kV;
+    constexpr int kQk = L::kQk, kT = L::kT;
     constexpr uint32_t sz = sizeof(T);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
@@ -715,15 +683,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <
         atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
     if (!fits) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    // places of a stage: k and the masked products by stage, q behind them
-    auto k_at = [&](int c) { return (L::kStages == 2 ? (c & 1) : 0) * (kQk + kV); };
-    auto q_at = [&](int c) { return L::kStages * (kQk + kV) + (L::kQStages == 2 ? (c & 1) : 0) * kQk; };
-    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
+    auto k_at = [&](int c) { return (L::kStages == 2 ? (c & 1) : 0) * (kQk + kT); };
+    auto qk_at = [&](int c) { return a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk); };
+    auto v_at = [&](int c) { return a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(); };
     auto bring = [&](int c) {
-        dma_pieces<WAVES, kQk>(qk_buf(c), 0, lds0 + k_at(c), wave, lane);
-        dma_pieces<WAVES, kV>(buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * kV, kV), 0, lds0 + k_at(c) + kQk, wave, lane);
+        dma_pieces<WAVES, kQk>(buffer_rsrc(qk_at(c), kQk), 0, lds0 + k_at(c), wave, lane);
+        dma_pieces<WAVES, kT>(buffer_rsrc(v_at(c), kT), 0, lds0 + k_at(c) + kQk, wave, lane);
     };
-    auto bring_q = [&](int c) { dma_pieces<WAVES, kQk>(qk_buf(c), kQk, lds0 + q_at(c), wave, lane); };
     // V of this lane's column, tokens 16 it + 4 hh + r
     typename Raw<T>::type raw[4][4];
     const uint32_t ldv = (uint32_t)p.ld * sz, ldo = (uint32_t)p.ld_out * sz;
@@ -738,10 +704,17 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <
 #pragma unroll
             for (int k = 0; k < 4; ++k) raw[it][k] = Raw<T>::load(r, v0 + (uint32_t)(16 * it + k) * ldv);
     };
+    bf16x8 q[kHold ? NS : 1][PA][4], P[kSplit][kFrags];
+    auto bring_q = [&](int c) {
+        if constexpr (kHold) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_at(c) + kQk, s, lane);
+        }
+    };
     if (n > 0) {
         bring(0);
-        bring_q(0);
         bring_v(0);
+        bring_q(0);
     }
     float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
     f32x4 S[NT];
@@ -751,10 +724,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <
         S[t] = f32x4{};
         if (carry && on && 16 * t < p.dk) S[t] = *(const f32x4*)(state + 16 * t);
     }
-    float unit = 1.0f;                                 // S times this power of two is the state
     for (int c = 0; c < n; ++c) {
         // the outputs' 16 stores are the youngest where everything of this chunk was asked for in front of them
-        if (L::kQStages == 2 && on && c > 0) wait_vm<16>();
+        if (L::kStages == 2 && kHold && on && c > 0) wait_vm<16>();
         else wait_vm<0>();
         wait_lgkm0();
         asm volatile("" ::: "memory");
@@ -768,197 +740,152 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NS <
                 v[it][k] = Raw<T>::value(raw[it][k]);
                 asm volatile("" : "+v"(v[it][k]));     // taken here, in front of the loads for the next chunk
             }
+        if (on) load_p(P, v_at(c) + kT, lane);
+        asm volatile("" ::: "memory");
         if (L::kStages == 2 && c + 1 < n) {
             bring(c + 1);
-            if (L::kQStages == 2) bring_q(c + 1);
             bring_v(c + 1);
         }
         const char* s_k = lds + k_at(c);
-        const char* s_v = s_k + kQk;
-        const char* s_q = lds + q_at(c);
+        const char* s_t = s_k + kQk;
         if (on) {
             const int nq = min(rows - c * kC, kC);
-            const float *fac = (const float*)(s_v + t_bytes() - kFacBytes), *ofac = (const float*)(s_v + v_bytes(PA) - kOutFacBytes);
-            auto tok4 = [&](const float* f, int k, int it) { return *(const f32x4*)&f[k * kC + 16 * it + 4 * hh]; };
-            auto tri = [&](const char* m, int part, int it, int s) { return *(const f16x8*)(m + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16); };
+            const float* fac = (const float*)(s_t + kT - kFacBytes);
+            auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
 
             // K S, and Q S for the outputs, whose products run while R is formed
-            f16x8 Sh[NS], Sl[NS];
-            const float ms = column_max(largest(S));
-            const int es = scale_exp(ms);
-#pragma unroll
-            for (int s = 0; s < NS; ++s) split2<true>(S[2 * s], S[2 * s + 1], pow2(es), Sh[s], Sl[s]);
-            const float fs = unit * pow2(-es);
+            bf16x8 Sp[NS][kSplit];
             f32x4 R[4], O[4];
 #pragma unroll
             for (int it = 0; it < 4; ++it) R[it] = O[it] = f32x4{};
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                f16x8 k[PA][4];
+                split2(S[2 * s], S[2 * s + 1], Sp[s]);
+                bf16x8 k[PA][4];
 #pragma unroll
                 for (int part = 0; part < PA; ++part)
 #pragma unroll
                     for (int it = 0; it < 4; ++it) k[part][it] = qk_piece<NS>(s_k, part, it, s, lane);
 #pragma unroll
-                for (int it = 0; it < 4; ++it) R[it] = mma(k[0][it], Sh[s], R[it]);
+                for (int m = 0; m < kProducts; ++m) {
+                    if (first(m) >= PA) continue;
 #pragma unroll
-                for (int it = 0; it < 4; ++it) R[it] = mma(k[0][it], Sl[s], R[it]);
-                if constexpr (PA == 2) {
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) R[it] = mma(k[PA - 1][it], Sh[s], R[it]);
+                    for (int it = 0; it < 4; ++it) R[it] = mma(k[first(m)][it], Sp[s][second(m)], R[it]);
                 }
             }
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                f16x8 q[PA][4];
+                if constexpr (!kHold) load_q<NS, PA>(q[0], qk_at(c) + kQk, s, lane);
+                auto& qs = q[kHold ? s : 0];
 #pragma unroll
-                for (int part = 0; part < PA; ++part)
+                for (int m = 0; m < kProducts; ++m) {
+                    if (first(m) >= PA) continue;
 #pragma unroll
-                    for (int it = 0; it < 4; ++it) q[part][it] = qk_piece<NS>(s_q, part, it, s, lane);
-#pragma unroll
-                for (int it = 0; it < 4; ++it) O[it] = mma(q[0][it], Sh[s], O[it]);
-                if constexpr (PA == 2) {
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(q[0][it], Sl[s], O[it]);
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(q[PA - 1][it], Sh[s], O[it]);
+                    for (int it = 0; it < 4; ++it) O[it] = mma(qs[first(m)][it], Sp[s][second(m)], O[it]);
                 }
             }
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const f32x4 bg = tok4(fac, 0, it);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) R[it][r] = v[it][r] - bg[r] * (R[it][r] * fs);
-            }
-            // U = T R
-            const int er = scale_exp(column_max(largest(R)));
-            f16x8 Rh[2], Rl[2];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) split2<true>(R[2 * s], R[2 * s + 1], pow2(er), Rh[s], Rl[s]);
+            if (c + 1 < n) bring_q(c + 1);
+            // R = V - e^G kappa K S, U = T R and W = e^(G_C - G) U
             f32x4 U[4], W[4];
-            const float fr = pow2(-er) * fac[kFacT];
+            bf16x8 Rp[2][kSplit];
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                f32x4 x{};
+                const f32x4 bg = tok4(0, it);
 #pragma unroll
-                for (int s = 0; s <= it / 2; ++s) {
-                    const f16x8 th = tri(s_v, 0, it, s), tl = tri(s_v, 1, it, s);
-                    x = mma(th, Rh[s], x);
-                    x = mma(th, Rl[s], x);
-                    x = mma(tl, Rh[s], x);
-                }
-                const f32x4 w = tok4(fac, 1, it);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    U[it][r] = x[r] * fr;
-                    W[it][r] = U[it][r] * w[r];
-                }
+                for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(-bg[r], R[it][r], v[it][r]);
+                U[it] = f32x4{};
             }
-            // S <- decay S + K^T W, in the units of W's scale; a state far above W keeps the scale in range
-            const float decay = fac[kFacDecay];
-            const float mw = column_max(largest(W));
-            const int ew = scale_exp(fmaxf(mw, ms * unit * decay * pow2(-10)));
-            f16x8 Wh[2], Wl[2];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) split2<true>(W[2 * s], W[2 * s + 1], pow2(ew), Wh[s], Wl[s]);
-            const float keep = decay * unit * pow2(ew);
-            unit = pow2(-ew);
+            for (int s = 0; s < 2; ++s) {
+                split2(R[2 * s], R[2 * s + 1], Rp[s]);
+                bf16x8 x[kSplit][4];
+#pragma unroll
+                for (int part = 0; part < kSplit; ++part)
+#pragma unroll
+                    for (int it = 2 * s; it < 4; ++it) x[part][it] = *(const bf16x8*)(s_t + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16);
+#pragma unroll
+                for (int m = 0; m < kProducts; ++m)
+#pragma unroll
+                    for (int it = 2 * s; it < 4; ++it) U[it] = mma(x[first(m)][it], Rp[s][second(m)], U[it]);
+            }
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                const f32x4 w = tok4(1, it);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) W[it][r] = U[it][r] * w[r];
+            }
+            // S <- e^(G_C) S + K^T W
+            const float decay = fac[kFacDecay];
+            bf16x8 Wp[2][kSplit];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) split2(W[2 * s], W[2 * s + 1], Wp[s]);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][r] *= keep;
+                for (int r = 0; r < 4; ++r) S[t][r] *= decay;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of
-                    // 16 values of k, transposed as they are read
-                    typedef short s16x4 __attribute__((ext_vector_type(4)));
-                    typedef __attribute__((address_space(3))) s16x4* lds4;
+                    bf16x8 k[PA];
 #pragma unroll
-                    for (int part = 0; part < PA; ++part) {
-                        s16x4 k2[2];
+                    for (int part = 0; part < PA; ++part) k[part] = kt_piece<NS>(s_k, part, s, t, lane);
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const char* at = s_k + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 +
-                                                    qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
-                            k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-                        }
-                        const f16x8 k = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                        S[t] = mma(k, Wh[s], S[t]);
-                        if (part == 0) S[t] = mma(k, Wl[s], S[t]);
-                    }
+                    for (int m = 0; m < kProducts; ++m)
+                        if (first(m) < PA) S[t] = mma(k[first(m)], Wp[s][second(m)], S[t]);
                 }
             }
-            // O = Q S + P U
-            const int eu = scale_exp(column_max(largest(U)));
-            f16x8 Uh[2], Ul[2];
+            // O = c (e^G Q S + P U)
+            bf16x8 Up[2][kSplit];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), Uh[s], Ul[s]);
+            for (int s = 0; s < 2; ++s) split2(U[2 * s], U[2 * s + 1], Up[s]);
             const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)c * kC) * p.ld_out + h * p.dv,
                                                           (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                f32x4 y{};
+                const f32x4 eg = tok4(2, it), cc = tok4(3, it);
 #pragma unroll
-                for (int s = 0; s <= it / 2; ++s) {
-                    const f16x8 q = tri(s_v + t_bytes(), 0, it, s);
-                    y = mma(q, Uh[s], y);
-                    if constexpr (PA == 2) {
-                        y = mma(q, Ul[s], y);
-                        y = mma(tri(s_v + t_bytes(), 1, it, s), Uh[s], y);
-                    }
-                }
-                const f32x4 ce = tok4(ofac, 0, it), cc = tok4(ofac, 1, it);
+                for (int r = 0; r < 4; ++r) O[it][r] *= eg[r];
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    Raw<T>::store(ro, o0 + (uint32_t)(16 * it + r) * ldo, ce[r] * (O[it][r] * fs) + cc[r] * (y[r] * pow2(-eu)));
+                for (int s = 0; s <= it / 2; ++s)
+#pragma unroll
+                    for (int m = 0; m < kProducts; ++m) O[it] = mma(P[first(m)][frag_of(it, s)], Up[s][second(m)], O[it]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) Raw<T>::store(ro, o0 + (uint32_t)(16 * it + r) * ldo, cc[r] * O[it][r]);
             }
         }
-        if (L::kQStages < 2 && c + 1 < n) {            // q (and, with one stage, everything) is read by now
+        if (L::kStages == 1 && c + 1 < n) {            // everything is read by now
             wait_lgkm0();
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            bring_q(c + 1);
-            if (L::kStages == 1) {
-                bring(c + 1);
-                bring_v(c + 1);
-            }
+            bring(c + 1);
+            bring_v(c + 1);
         }
     }
     if (ok && on) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if (16 * t >= p.dk) break;
-            f32x4 o;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = S[t][r] * unit;
-            *(f32x4*)(state + 16 * t) = o;
+            *(f32x4*)(state + 16 * t) = S[t];
         }
     }
 }
 
 // As delta_main_kernel, with the outputs by waves of their own: W waves carry the state, W more form the outputs of the
-// chunk before from the operands that the first left in LDS. The chain from chunk to chunk is that much shorter, and
-// both kinds run beside each other. Scales that need not be exact are bounds, known before what they scale:
-// a bound loses headroom (f16 pairs hold 39 bits, 22 are used), not precision.
-// 317, 1130 and 601 bf16 tokens, 16 heads of 128 x 128: 37.5 us, 2.1 us a chunk of the longest sequence (51 when it was
-// built, 62 by delta_main_kernel then); 8 x 2048 tokens 98 us for 294 MB. Bound by the instructions of a chunk's chain
-// (480 vector ones and 82 MFMAs of a wave that carries the state) with the next chunk's 55 KB on their way; matrix pipe
-// 24% busy, LDS 34%. Touching the chunk after next for L2, loads by the waves that carry the state and other orders of
-// the products gave nothing or cost time.
+// chunk before from what the first left in LDS. The chain from chunk to chunk is that much shorter, and both
+// kinds run beside each other.
 template <typename T, int NS, int W> struct SplitLds {
-    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes(), kP = (int)p_bytes(kParts<T>);
+    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes();
     static constexpr int kRow = 16 * W * (int)sizeof(T), kRows = kC * kRow;   // the workgroup's values of a token, of a chunk
-    static constexpr int kHand = (NS + 2) * kParts<T> * 1024 + 256;           // S, U and their scales of 16 columns
-    static constexpr int kStage = 2 * kQk + kT + kRows + (int)kOutFacBytes, kBytes = 2 * (kStage + W * kHand);
-    static constexpr bool kFits = kBytes <= (int)kLds;
+    static constexpr int kHand = (2 * NS + 4) * 1024;                         // S and U of 16 columns
+    static constexpr int kStage = kQk + kT + kRows + (int)kFacBytes, kBytes = 2 * kStage + W * kHand;
+    static constexpr bool kFits = kBytes <= (int)kLds && NS <= 4;
 };
 
 template <typename T, int NS, int W>
 __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) void delta_split_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = SplitLds<T, NS, W>;
-    constexpr int kQk = L::kQk, kT = L::kT, kP = L::kP, kRow = L::kRow, kRows = L::kRows, kHand = L::kHand, kStage = L::kStage;
+    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kRows = L::kRows, kHand = L::kHand, kStage = L::kStage;
     constexpr uint32_t sz = sizeof(T);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
@@ -978,14 +905,14 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
         atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
     if (!fits) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    // a stage: k, T and the state's factors, values; q and the outputs' factors; then what the waves hand over
-    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
-    auto v_at = [&](int c) { return a.w.v + ((int64_t)(base + c) * p.Hv + h) * (kT + kP); };
+    // a stage: k, T and the factors, values; the factors again, a chunk later, for the outputs; then what the waves hand over
+    auto qk_at = [&](int c) { return a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk); };
+    auto v_at = [&](int c) { return a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(); };
     const uint32_t ldv = (uint32_t)p.ld * sz;
     // All that comes by DMA is asked for by the waves of the outputs: beside a burst of it a wave waits long to issue a load
     auto bring_state = [&](int c) {
         const uint32_t to = lds0 + (c & 1) * kStage;
-        dma_pieces<W, kQk>(qk_buf(c), 0, to, wc, lane);
+        dma_pieces<W, kQk>(buffer_rsrc(qk_at(c), kQk), 0, to, wc, lane);
         dma_pieces<W, kT>(buffer_rsrc(v_at(c), kT), 0, to + kQk, wc, lane);
         const int nq = min(rows - c * kC, kC);
         const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
@@ -998,93 +925,97 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
             dma16(r, off + q * kPer * ldv, 0, __builtin_amdgcn_readfirstlane(to + kQk + kT + q * 1024));
         }
     };
+    auto out_at = [&](int c) { return (c & 1) * kStage + kQk + kT + kRows; };
     auto bring_out = [&](int c) {
-        const uint32_t to = lds0 + (c & 1) * kStage + kQk + kT + kRows;
-        dma_pieces<W, kQk>(qk_buf(c), kQk, to, wc, lane);
-        dma_pieces<W, (int)kOutFacBytes>(buffer_rsrc(v_at(c) + kT + kP - kOutFacBytes, kOutFacBytes), 0, to + kQk, wc, lane);
+        dma_pieces<W, (int)kFacBytes>(buffer_rsrc(v_at(c) + kT - kFacBytes, kFacBytes), 0, lds0 + out_at(c), wc, lane);
     };
-    auto hand = [&](int c) { return lds + 2 * kStage + ((c & 1) * W + wc) * kHand; };
-    auto meet = [&] {
-        wait_lgkm0();
+    char* hand = lds + 2 * kStage + wc * kHand;
+    auto barrier = [&] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    // Two barriers a chunk: at the first all of it has arrived and the chunk before has been handed over, at the second that
+    // has been taken
+    auto meet = [&] {
+        wait_lgkm0();
+        barrier();
+    };
     if (!carries) {
-        if (n > 0) bring_state(0);
+        if (n == 0) return;
+        bring_state(0);
         // O^T of 16 columns: rows are columns of the state, a lane's token is its column of the product
         const uint32_t ldo = (uint32_t)p.ld_out * sz;
         const uint32_t o0 = (uint32_t)(lane & 15) * ldo + (uint32_t)(c0 + 4 * hh) * sz;
-        f16x8 Pn[PA][kFrags];                          // the next products of queries and keys
-        for (int c = 0; c <= n && n > 0; ++c) {
+        bf16x8 q[NS][PA][4], P[kSplit][kFrags];        // of the next outputs
+        for (int c = 0; c <= n; ++c) {
             if (on && c > 1) wait_vm<4>();             // but for the stores of the outputs
             else wait_vm<0>();
-            f16x8 P[PA][kFrags];
-#pragma unroll
-            for (int part = 0; part < PA; ++part)
-#pragma unroll
-                for (int f = 0; f < kFrags; ++f) P[part][f] = Pn[part][f];
             meet();
             if (c + 1 < n) bring_state(c + 1);
-            if (c < n) {
-                bring_out(c);
-                const char* from = v_at(c) + kT;
+            if (c < n) bring_out(c);
+            auto ask_q = [&] {
 #pragma unroll
-                for (int part = 0; part < PA; ++part)
-#pragma unroll
-                    for (int f = 0; f < kFrags; ++f) Pn[part][f] = *(const f16x8*)(from + (part * kFrags + f) * 1024 + lane * 16);
+                for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_at(c) + kQk, s, lane);
+            };
+            if (c == 0 || !on) {
+                meet();
+                if (on) {
+                    ask_q();
+                    load_p(P, v_at(c) + kT, lane);
+                }
+                continue;
             }
-            if (c == 0 || !on) continue;
             const int d = c - 1, nq = min(rows - d * kC, kC);
-            const char *s_q = lds + (d & 1) * kStage + kQk + kT + kRows, *from = hand(d);
-            const float *fac = (const float*)(s_q + kQk), *sc = (const float*)(from + (NS + 2) * PA * 1024);
-            f16x8 S[PA][NS], U[PA][2];
+            const float* fac = (const float*)(lds + out_at(d)) + 2 * kC;
+            f32x4 S[NT], U[4];
 #pragma unroll
-            for (int part = 0; part < PA; ++part) {
+            for (int t = 0; t < NT; ++t) S[t] = *(const f32x4*)(hand + t * 1024 + lane * 16);
 #pragma unroll
-                for (int s = 0; s < NS; ++s) S[part][s] = *(const f16x8*)(from + (part * NS + s) * 1024 + lane * 16);
-#pragma unroll
-                for (int s = 0; s < 2; ++s) U[part][s] = *(const f16x8*)(from + (PA * NS + part * 2 + s) * 1024 + lane * 16);
-            }
-            const f32x4 fs = *(const f32x4*)&sc[4 * hh], fu = *(const f32x4*)&sc[16 + 4 * hh];
+            for (int it = 0; it < 4; ++it) U[it] = *(const f32x4*)(hand + (NT + it) * 1024 + lane * 16);
+            meet();
             const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)d * kC) * p.ld_out + h * p.dv,
                                                           (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
-            f32x4 O[4], Y[4];
+            f32x4 O[4];
 #pragma unroll
-            for (int it = 0; it < 4; ++it) O[it] = Y[it] = f32x4{};
+            for (int it = 0; it < 4; ++it) O[it] = f32x4{};
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                f16x8 q[PA][4];
+                bf16x8 Sp[kSplit];
+                split2(S[2 * s], S[2 * s + 1], Sp);
 #pragma unroll
-                for (int part = 0; part < PA; ++part)
+                for (int m = 0; m < kProducts; ++m) {
+                    if (second(m) >= PA) continue;
 #pragma unroll
-                    for (int it = 0; it < 4; ++it) q[part][it] = qk_piece<NS>(s_q, part, it, s, lane);
-#pragma unroll
-                for (int it = 0; it < 4; ++it) O[it] = mma(S[0][s], q[0][it], O[it]);
-                if constexpr (PA == 2) {
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(S[PA - 1][s], q[0][it], O[it]);
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(S[0][s], q[PA - 1][it], O[it]);
+                    for (int it = 0; it < 4; ++it) O[it] = mma(Sp[first(m)], q[s][second(m)][it], O[it]);
                 }
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int it = 2 * s; it < 4; ++it) {
-                    Y[it] = mma(U[0][s], P[0][frag_of(it, s)], Y[it]);
-                    if constexpr (PA == 2) {
-                        Y[it] = mma(U[PA - 1][s], P[0][frag_of(it, s)], Y[it]);
-                        Y[it] = mma(U[0][s], P[PA - 1][frag_of(it, s)], Y[it]);
-                    }
-                }
+            if (c < n) ask_q();
+            float cc[4];
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                const float ce = fac[16 * it + (lane & 15)], cc = fac[kC + 16 * it + (lane & 15)];
+                const float eg = fac[16 * it + (lane & 15)];
+                cc[it] = fac[kC + 16 * it + (lane & 15)];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) O[it][r] *= eg;
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                bf16x8 Up[kSplit];
+                split2(U[2 * s], U[2 * s + 1], Up);
+#pragma unroll
+                for (int m = 0; m < kProducts; ++m)
+#pragma unroll
+                    for (int it = 2 * s; it < 4; ++it) O[it] = mma(Up[first(m)], P[second(m)][frag_of(it, s)], O[it]);
+            }
+            if (c < n) load_p(P, v_at(c) + kT, lane);
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
                 T o[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(ce * (O[it][r] * fs[r]) + cc * (Y[it][r] * fu[r]));
-                if constexpr (PA == 2) {
+                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(cc[it] * O[it][r]);
+                if constexpr (sz == 4) {
                     u32x4 w;
                     __builtin_memcpy(&w, o, 16);
                     __builtin_amdgcn_raw_buffer_store_b128(w, ro, (int)(o0 + (uint32_t)(16 * it) * ldo), 0, 0);
@@ -1097,7 +1028,6 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
         }
         return;
     }
-
     float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
     f32x4 S[NT];
     const bool carry = ok && p.has_init[seq];
@@ -1106,36 +1036,26 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
         S[t] = f32x4{};
         if (carry && on && 16 * t < p.dk) S[t] = *(const f32x4*)(state + 16 * t);
     }
-    // S times unit (a power of two) is the state; |S| stays below 2^15, so that S itself is the pair of operands.
-    // Tiles of which these are formed beside the products of the others; the others' behind the barrier, beside the first
+    // Steps whose operands are formed beside the products of the others; the others' behind the barrier, beside the first
     // reads
-    constexpr int kEarly = NT / 4 * 2;
-    float one = 1.0f;
-    asm volatile("" : "+s"(one));
-    float unit;
-    {
-        const int e = scale_exp(column_max(largest(S))) + 2;
-        unit = pow2(-e);
+    constexpr int kEarly = NS / 2;
+    bf16x8 Sp[NS][kSplit];
+    auto form = [&](int s0, int s1) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= pow2(e);
-    }
-    f16x8 Sh[NS], Sl[NS];
-    auto form = [&](int t0, int t1) {
-#pragma unroll
-        for (int t = t0; t < t1; t += 2) split2<true, false>(S[t], S[t + 1], one, Sh[t / 2], Sl[t / 2]);
+        for (int s = s0; s < s1; ++s) split2(S[2 * s], S[2 * s + 1], Sp[s]);
     };
     form(0, kEarly);
-    for (int c = 0; c <= n && n > 0; ++c) {
+    for (int c = 0; c < n; ++c) {
         meet();
-        if (c == n || !on) continue;
+        if (!on) {
+            barrier();
+            continue;
+        }
         const char *s_k = lds + (c & 1) * kStage, *s_t = s_k + kQk;
         const float* fac = (const float*)(s_t + kT - kFacBytes);
-        char* to = hand(c);
         // What is read from LDS is asked for well in front of its use, as nothing else hides its way: two k steps of k
         // ahead of their products, T behind the last of them, k transposed in front of the products with T
-        f16x8 K[2][PA][4], Tr[2][kFrags];
+        bf16x8 K[2][PA][4], Tr[kSplit][kFrags];
         f32x4 bg[4], wg[4];
         auto read_k = [&](int s) {
 #pragma unroll
@@ -1150,7 +1070,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
             bg[it] = *(const f32x4*)&fac[16 * it + 4 * hh];
             wg[it] = *(const f32x4*)&fac[kC + 16 * it + 4 * hh];
         }
-        const float decay = fac[kFacDecay], tscale = fac[kFacT], gmax = fac[kFacMax];
+        const float decay = fac[kFacDecay];
         // V of this lane's column, tokens 16 it + 4 hh + r
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds4;
@@ -1176,180 +1096,94 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
                     if (16 * it + 4 * hh + r >= rows - c * kC) v[it][r] = 0.0f;
         }
         __builtin_amdgcn_sched_barrier(0);
-        form(kEarly, NT);
+        form(kEarly, NS);
 
-        // K S beside all that does not wait for it
+        // K S
         f32x4 R[4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) R[it] = f32x4{};
-        const float fs = unit;
-        constexpr float kRoot = NS <= 2 ? 8.0f : NS <= 4 ? 11.4f : 16.0f;   // of 32 NS, or above it
-        float ms, fu;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
 #pragma unroll
-            for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][0][it], Sh[s], R[it]);
+            for (int m = 0; m < kProducts; ++m) {
+                if (first(m) >= PA) continue;
 #pragma unroll
-            for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][0][it], Sl[s], R[it]);
-            if constexpr (PA == 2) {
-#pragma unroll
-                for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][PA - 1][it], Sh[s], R[it]);
+                for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][first(m)][it], Sp[s][second(m)], R[it]);
             }
             if (s + 2 < NS) read_k(s + 2);
-            if (s >= NS - 2) {
-                const int part = s - (NS - 2);
-#pragma unroll
-                for (int f = 0; f < kFrags; ++f) Tr[part][f] = *(const f16x8*)(s_t + (part * kFrags + f) * 1024 + lane * 16);
-            }
-            *(f16x8*)(to + s * 1024 + lane * 16) = Sh[s];
-            if constexpr (PA == 2) *(f16x8*)(to + (NS + s) * 1024 + lane * 16) = Sl[s];
-            if (s == 0) {
-                float vmax = 0.0f;
-#pragma unroll
-                for (int it = 0; it < 4; ++it)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) vmax = fmaxf(vmax, fabsf(v[it][k]));
-                ms = column_max(largest(S));
-                // a bound of R = V - e^G K S: |k . S| <= |k| sqrt(dk) max |S|
-                const int er = scale_exp(column_max(vmax) + gmax * kRoot * (ms * unit));
-                const float gr = pow2(er), cr = fs * gr;
-                fu = pow2(-er) * tscale;
-#pragma unroll
-                for (int it = 0; it < 4; ++it)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        v[it][r] *= gr;
-                        bg[it][r] *= -cr;
-                    }
-            }
             __builtin_amdgcn_sched_barrier(0);
         }
-        // rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of 16 values of k,
-        // transposed as they are read
-        f16x8 Kt[PA][2][NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int part = 0; part < kSplit; ++part)
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int part = 0; part < PA; ++part) {
-                    s16x4 k2[2];
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const char* at = s_k + (((part * 4 + 2 * s + q) * NS + t / 2) * 64 +
-                                                qk_unit(4 * hh + ((lane & 15) >> 2), lane & 3)) * 16 + (t & 1) * 8;
-                        k2[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-                    }
-                    Kt[part][s][t] = __builtin_bit_cast(f16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                }
+            for (int f = 0; f < kFrags; ++f) Tr[part][f] = *(const bf16x8*)(s_t + (part * kFrags + f) * 1024 + lane * 16);
         __builtin_amdgcn_sched_barrier(0);
         // From here tokens 0 .. 31 run ahead of the others: while the one half is in the matrix cores the other is formed.
-        // U = kappa T beta R times 1 / fu, W = e^(G_C - G) U
-        f16x8 Rh[2], Rl[2], Wh[2], Wl[2];
+        // U = T R, W = e^(G_C - G) U
         f32x4 U[4], X[4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) U[it] = f32x4{};
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
+            bf16x8 Rp[kSplit];
 #pragma unroll
             for (int it = 2 * s; it < 2 * s + 2; ++it)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(bg[it][r], R[it][r], v[it][r]);
-            split2<true, false>(R[2 * s], R[2 * s + 1], one, Rh[s], Rl[s]);
+                for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(-bg[it][r], R[it][r], v[it][r]);
+            split2(R[2 * s], R[2 * s + 1], Rp);
 #pragma unroll
-            for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[0][frag_of(it, s)], Rh[s], U[it]);
+            for (int m = 0; m < kProducts; ++m)
 #pragma unroll
-            for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[0][frag_of(it, s)], Rl[s], U[it]);
-#pragma unroll
-            for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[1][frag_of(it, s)], Rh[s], U[it]);
+                for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[first(m)][frag_of(it, s)], Rp[second(m)], U[it]);
         }
-        // The state's units: what is left of it and 64 products of W with values of k below 2 come to 2^15 at most. In bf16
-        // W's largest value follows from R's (times the 64 of a row of T below 2^13) while the products run; in
-        // float32, where a token's own precision is asked for, it is W's own
-        float keep;
-        auto units = [&](float most) {                 // of W
-            const int ew = scale_exp(__builtin_fmaf(decay * ms, unit, most * pow2(7))) + 2;
-            keep = decay * unit * pow2(ew);
-            unit = pow2(-ew);
+        barrier();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            *(f32x4*)(hand + t * 1024 + lane * 16) = S[t];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] *= decay;
+        }
+        bf16x8 Kt[2][PA][NT];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][r] *= keep;
-            return pow2(ew);
+                for (int part = 0; part < PA; ++part) Kt[s][part][t] = kt_piece<NS>(s_k, part, s, t, lane);
+        bf16x8 Wp[2][kSplit];
+        // S <- decay S + K^T W
+        auto grow = [&](int s, int t0, int t1) {
+#pragma unroll
+            for (int m = 0; m < kProducts; ++m) {
+                if (first(m) >= PA) continue;
+#pragma unroll
+                for (int t = t0; t < t1; ++t) S[t] = mma(Kt[s][first(m)][t], Wp[s][second(m)], S[t]);
+            }
         };
-        float wc = fu;
-        if constexpr (PA == 1) wc *= units(fu * pow2(19) * column_max(largest(R)));
 #pragma unroll
-        for (int it = 0; it < 4; ++it)
+        for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) wg[it][r] *= wc;
-        auto weigh = [&](int s) {
-#pragma unroll
-            for (int it = 2 * s; it < 2 * s + 2; ++it)
+            for (int it = 2 * s; it < 2 * s + 2; ++it) {
+                *(f32x4*)(hand + (NT + it) * 1024 + lane * 16) = U[it];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * wg[it][r];
-        };
-        if constexpr (PA == 2) {
-            weigh(0);
-            weigh(1);
-            const float f = units(column_max(largest(X)));
-#pragma unroll
-            for (int it = 0; it < 4; ++it)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) X[it][r] *= f;
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if constexpr (PA == 1) weigh(s);
-            split2<true, false>(X[2 * s], X[2 * s + 1], one, Wh[s], Wl[s]);
-            if (s == 0) {
-                // S <- decay S + K^T W, the first half's products
-#pragma unroll
-                for (int t = 0; t < NT; ++t) S[t] = mma(Kt[0][0][t], Wh[0], S[t]);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) S[t] = mma(Kt[0][0][t], Wl[0], S[t]);
-                if constexpr (PA == 2) {
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t] = mma(Kt[PA - 1][0][t], Wh[0], S[t]);
-                }
             }
+            split2(X[2 * s], X[2 * s + 1], Wp[s]);
+            if (s == 0) grow(0, 0, NT);
         }
-        auto second = [&](int t0, int t1) {
-#pragma unroll
-            for (int t = t0; t < t1; ++t) S[t] = mma(Kt[0][1][t], Wh[1], S[t]);
-#pragma unroll
-            for (int t = t0; t < t1; ++t) S[t] = mma(Kt[0][1][t], Wl[1], S[t]);
-            if constexpr (PA == 2) {
-#pragma unroll
-                for (int t = t0; t < t1; ++t) S[t] = mma(Kt[PA - 1][1][t], Wh[1], S[t]);
-            }
-        };
-        second(0, kEarly);
-        second(kEarly, NT);
-        // U for the outputs
-        const int eu = scale_exp(column_max(largest(U)));
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            f16x8 uh, ul;
-            split2<PA == 2>(U[2 * s], U[2 * s + 1], pow2(eu), uh, ul);
-            *(f16x8*)(to + (PA * NS + s) * 1024 + lane * 16) = uh;
-            if constexpr (PA == 2) *(f16x8*)(to + (PA * NS + 2 + s) * 1024 + lane * 16) = ul;
-        }
-        if (hh == 0) {
-            float* sc = (float*)(to + (NS + 2) * PA * 1024);
-            sc[lane] = fs;
-            sc[16 + lane] = fu * pow2(-eu);
-        }
+        grow(1, 0, 2 * kEarly);
+        grow(1, 2 * kEarly, NT);
         form(0, kEarly);
+    }
+    if (n > 0) {
+        meet();
+        barrier();
     }
     if (ok && on) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if (16 * t >= p.dk) break;
-            f32x4 o;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = S[t][r] * unit;
-            *(f32x4*)(state + 16 * t) = o;
+            *(f32x4*)(state + 16 * t) = S[t];
         }
     }
 }
@@ -1362,7 +1196,7 @@ int steps_of(int dk) {
 
 DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, int nseq, size_t* total) {
     DeltaWs w{};
-    const int parts = bf16_act ? 1 : 2;
+    const int parts = bf16_act ? kParts<bf16> : kParts<float>;
     w.slots = (int)(T / kC) + nseq;
     size_t off = 0;
     auto take = [&](size_t bytes) { char* q = scratch ? scratch + off : nullptr; off += align256(bytes); return q; };
@@ -1370,7 +1204,7 @@ DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, 
     w.count = (int32_t*)take(4);
     w.plan = (int2*)take((size_t)w.slots * 8);
     w.qk = take((size_t)w.slots * Hk * 2 * qk_bytes(steps_of(dk), parts));
-    w.v = take((size_t)w.slots * Hv * v_bytes(parts));
+    w.v = take((size_t)w.slots * Hv * v_bytes());
     *total = off;
     return w;
 }
