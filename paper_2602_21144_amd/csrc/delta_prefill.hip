@@ -149,7 +149,7 @@ __device__ __forceinline__ int row_exp(float m) {
     return 127 - min(max(e, 40), 230);
 }
 
-// The next bf16 values of eight that are left, rounded to nearest; v: what they leave
+// The next bf16 values of eight that are left, rounded to nearest; v: what they leave.
 __device__ __forceinline__ bf16x8 take8(float (&v)[8]) {
     bf16x8 o;
 #pragma unroll
@@ -579,6 +579,16 @@ template <int N> __device__ __forceinline__ void split2(const f32x4& x0, const f
     split8(v, o);
 }
 
+// Asks for an order of what lies between two sched_barriers: M times an MFMA and V vector instructions
+template <int M, int V> __device__ __forceinline__ void interleave() {
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // What delta_main_kernel holds in LDS: a chunk's k, T and factors, in two stages or, where these do not fit, one
 constexpr size_t kLds = 160 * 1024;
 template <typename T, int NS> struct MainLds {
@@ -598,17 +608,21 @@ template <int WAVES, int BYTES> __device__ __forceinline__ void dma_pieces(const
     }
 }
 // Pieces that a wave holds in registers: of q, k step s, and the products of queries and keys
-template <int NS, int PA> __device__ __forceinline__ void load_q(bf16x8 (&q)[PA][4], const char* from, int s, int lane) {
+template <int NS, int PA>
+__device__ __forceinline__ void load_q(bf16x8 (&q)[PA][4], const __amdgpu_buffer_rsrc_t& r, uint32_t from, int s, int lane) {
+    const int off = qk_unit(lane & 15, lane >> 4) * 16;
 #pragma unroll
     for (int part = 0; part < PA; ++part)
 #pragma unroll
-        for (int it = 0; it < 4; ++it) q[part][it] = qk_piece<NS>(from, part, it, s, lane);
+        for (int it = 0; it < 4; ++it)
+            q[part][it] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, (int)from + ((part * 4 + it) * NS + s) * 1024, 0));
 }
-__device__ __forceinline__ void load_p(bf16x8 (&x)[kSplit][kFrags], const char* from, int lane) {
+__device__ __forceinline__ void load_p(bf16x8 (&x)[kSplit][kFrags], const __amdgpu_buffer_rsrc_t& r, uint32_t from, int lane) {
 #pragma unroll
     for (int part = 0; part < kSplit; ++part)
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f) x[part][f] = *(const bf16x8*)(from + (part * kFrags + f) * 1024 + lane * 16);
+        for (int f = 0; f < kFrags; ++f)
+            x[part][f] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, (int)from + (part * kFrags + f) * 1024, 0));
 }
 // Rows dk = 16 t + lane % 16 of K^T, tokens 32 s + 4 hh .. and 32 s + 16 + 4 hh ..: four rows of 16 values of k, transposed
 // as they are read
@@ -684,11 +698,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
     if (!fits) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
     auto k_at = [&](int c) { return (L::kStages == 2 ? (c & 1) : 0) * (kQk + kT); };
-    auto qk_at = [&](int c) { return a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk); };
-    auto v_at = [&](int c) { return a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(); };
+    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
+    auto v_buf = [&](int c) { return buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(), (uint32_t)v_bytes()); };
     auto bring = [&](int c) {
-        dma_pieces<WAVES, kQk>(buffer_rsrc(qk_at(c), kQk), 0, lds0 + k_at(c), wave, lane);
-        dma_pieces<WAVES, kT>(buffer_rsrc(v_at(c), kT), 0, lds0 + k_at(c) + kQk, wave, lane);
+        dma_pieces<WAVES, kQk>(qk_buf(c), 0, lds0 + k_at(c), wave, lane);
+        dma_pieces<WAVES, kT>(v_buf(c), 0, lds0 + k_at(c) + kQk, wave, lane);
     };
     // V of this lane's column, tokens 16 it + 4 hh + r
     typename Raw<T>::type raw[4][4];
@@ -708,7 +722,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
     auto bring_q = [&](int c) {
         if constexpr (kHold) {
 #pragma unroll
-            for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_at(c) + kQk, s, lane);
+            for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_buf(c), kQk, s, lane);
         }
     };
     if (n > 0) {
@@ -740,7 +754,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
                 v[it][k] = Raw<T>::value(raw[it][k]);
                 asm volatile("" : "+v"(v[it][k]));     // taken here, in front of the loads for the next chunk
             }
-        if (on) load_p(P, v_at(c) + kT, lane);
+        if (on) load_p(P, v_buf(c), kT, lane);
         asm volatile("" ::: "memory");
         if (L::kStages == 2 && c + 1 < n) {
             bring(c + 1);
@@ -775,7 +789,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
             }
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                if constexpr (!kHold) load_q<NS, PA>(q[0], qk_at(c) + kQk, s, lane);
+                if constexpr (!kHold) load_q<NS, PA>(q[0], qk_buf(c), kQk, s, lane);
                 auto& qs = q[kHold ? s : 0];
 #pragma unroll
                 for (int m = 0; m < kProducts; ++m) {
@@ -873,19 +887,30 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1)))
 // As delta_main_kernel, with the outputs by waves of their own: W waves carry the state, W more form the outputs of the
 // chunk before from what the first left in LDS. The chain from chunk to chunk is that much shorter, and both
 // kinds run beside each other.
+// What a workgroup has in LDS. Two barriers a chunk, at its begin and in its middle, tell what is free: in two stages k, which
+// the state needs all the time; in one T (arriving in a chunk's first half, read in its second), the factors and values
+// (read in the first), what is handed over (read in the first, written in the second). Four waves of columns share
+// q (arriving in the first half, read in the second) and the products of queries and keys (read in the first) there too;
+// with two each has them in registers, where there is room for longer rows.
 template <typename T, int NS, int W> struct SplitLds {
-    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes();
+    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)(t_bytes() - kFacBytes), kFac = (int)kFacBytes, kP = (int)p_bytes();
     static constexpr int kRow = 16 * W * (int)sizeof(T), kRows = kC * kRow;   // the workgroup's values of a token, of a chunk
     static constexpr int kHand = (2 * NS + 4) * 1024;                         // S and U of 16 columns
-    static constexpr int kStage = kQk + kT + kRows + (int)kFacBytes, kBytes = 2 * kStage + W * kHand;
-    static constexpr bool kFits = kBytes <= (int)kLds && NS <= 4;
+    // where there is room T has two stages as well
+    static constexpr int kState = 2 * kQk + kT + kFac + kRows + W * kHand;
+    static constexpr bool kDirect = kState + kQk + kFac + kP > (int)kLds;
+    static constexpr int kOne = kState + (kDirect ? 0 : kQk + kFac + kP);
+    static constexpr int kTStages = kOne + kT <= (int)kLds ? 2 : 1, kBytes = kOne + (kTStages - 1) * kT;
+    static constexpr int kTAt = 2 * kQk, kFacAt = kTAt + kTStages * kT, kRowsAt = kFacAt + kFac, kHandAt = kRowsAt + kRows;
+    static constexpr int kQAt = kHandAt + W * kHand, kOutFacAt = kQAt + kQk, kPAt = kOutFacAt + kFac;
+    static constexpr bool kFits = kBytes <= (int)kLds && !(kDirect && W > 2);
 };
 
 template <typename T, int NS, int W>
-__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) void delta_split_kernel(Args a) {
+__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kParts<T> <= 4 ? 2 : 1))) void delta_split_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = SplitLds<T, NS, W>;
-    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kRows = L::kRows, kHand = L::kHand, kStage = L::kStage;
+    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kRows = L::kRows, kHand = L::kHand, kP = L::kP;
     constexpr uint32_t sz = sizeof(T);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
@@ -905,15 +930,14 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
         atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
     if (!fits) return;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    // a stage: k, T and the factors, values; the factors again, a chunk later, for the outputs; then what the waves hand over
-    auto qk_at = [&](int c) { return a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk); };
-    auto v_at = [&](int c) { return a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(); };
+    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
+    auto v_buf = [&](int c) { return buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(), (uint32_t)v_bytes()); };
     const uint32_t ldv = (uint32_t)p.ld * sz;
     // All that comes by DMA is asked for by the waves of the outputs: beside a burst of it a wave waits long to issue a load
+    // In front of a chunk: k, its values and factors
     auto bring_state = [&](int c) {
-        const uint32_t to = lds0 + (c & 1) * kStage;
-        dma_pieces<W, kQk>(buffer_rsrc(qk_at(c), kQk), 0, to, wc, lane);
-        dma_pieces<W, kT>(buffer_rsrc(v_at(c), kT), 0, to + kQk, wc, lane);
+        dma_pieces<W, kQk>(qk_buf(c), 0, lds0 + (c & 1) * kQk, wc, lane);
+        dma_pieces<W, L::kFac>(v_buf(c), kT, lds0 + L::kFacAt, wc, lane);
         const int nq = min(rows - c * kC, kC);
         const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
                                                      (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
@@ -922,21 +946,28 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
         for (int i = 0; i < kRows / 1024 / W; ++i) {
             const uint32_t q = (uint32_t)(wc + W * i);
-            dma16(r, off + q * kPer * ldv, 0, __builtin_amdgcn_readfirstlane(to + kQk + kT + q * 1024));
+            dma16(r, off + q * kPer * ldv, 0, __builtin_amdgcn_readfirstlane(lds0 + L::kRowsAt + q * 1024));
         }
     };
-    auto out_at = [&](int c) { return (c & 1) * kStage + kQk + kT + kRows; };
-    auto bring_out = [&](int c) {
-        dma_pieces<W, (int)kFacBytes>(buffer_rsrc(v_at(c) + kT - kFacBytes, kFacBytes), 0, lds0 + out_at(c), wc, lane);
+    // At its begin or, in two stages, in front of it: T
+    auto t_at = [&](int c) { return L::kTAt + (L::kTStages == 2 ? (c & 1) * kT : 0); };
+    auto bring_t = [&](int c) { dma_pieces<W, kT>(v_buf(c), 0, lds0 + t_at(c), wc, lane); };
+    // At its begin: for the outputs of the chunk before, q and the factors
+    auto bring_q = [&](int c) {
+        if (L::kDirect) return;
+        dma_pieces<W, kQk>(qk_buf(c), kQk, lds0 + L::kQAt, wc, lane);
+        dma_pieces<W, L::kFac>(v_buf(c), kT, lds0 + L::kOutFacAt, wc, lane);
     };
-    char* hand = lds + 2 * kStage + wc * kHand;
+    // In its middle: what its outputs have of queries and keys
+    auto bring_p = [&](int c) {
+        if (!L::kDirect) dma_pieces<W, kP>(v_buf(c), kT + L::kFac, lds0 + L::kPAt, wc, lane);
+    };
+    char* hand = lds + L::kHandAt + wc * kHand;
     auto barrier = [&] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // Two barriers a chunk: at the first all of it has arrived and the chunk before has been handed over, at the second that
-    // has been taken
     auto meet = [&] {
         wait_lgkm0();
         barrier();
@@ -944,77 +975,145 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
     if (!carries) {
         if (n == 0) return;
         bring_state(0);
+        bring_t(0);
+        wait_vm<0>();
+        meet();
+        barrier();
+        if (!on) {
+            for (int c = 1; c <= n; ++c) {
+                if (c < n) bring_state(c);
+                if (L::kTStages == 2 && c < n) bring_t(c);
+                bring_p(c - 1);
+                wait_vm<0>();
+                meet();
+                if (L::kTStages == 1 && c < n) bring_t(c);
+                bring_q(c - 1);
+                wait_vm<0>();
+                barrier();
+            }
+            return;
+        }
         // O^T of 16 columns: rows are columns of the state, a lane's token is its column of the product
         const uint32_t ldo = (uint32_t)p.ld_out * sz;
         const uint32_t o0 = (uint32_t)(lane & 15) * ldo + (uint32_t)(c0 + 4 * hh) * sz;
-        bf16x8 q[NS][PA][4], P[kSplit][kFrags];        // of the next outputs
-        for (int c = 0; c <= n; ++c) {
-            if (on && c > 1) wait_vm<4>();             // but for the stores of the outputs
-            else wait_vm<0>();
-            meet();
-            if (c + 1 < n) bring_state(c + 1);
-            if (c < n) bring_out(c);
-            auto ask_q = [&] {
+        const char *s_q = lds + L::kQAt, *s_p = lds + L::kPAt;
+        const float* s_fac = (const float*)(lds + L::kOutFacAt) + 2 * kC + (lane & 15);
+        constexpr bool kDirect = L::kDirect;
+        constexpr int kAskQ = kDirect ? NS * PA * 4 : 0, kAskP = kDirect ? kSplit * kFrags + 8 : 0;   // loads of them
+        bf16x8 q[kDirect ? NS : 2][PA][4], P[kSplit][kFrags];
+        float eg[4], cc[4];
+        auto ask_q = [&](int c) {
+            if constexpr (kDirect) {
 #pragma unroll
-                for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_at(c) + kQk, s, lane);
-            };
-            if (c == 0 || !on) {
-                meet();
-                if (on) {
-                    ask_q();
-                    load_p(P, v_at(c) + kT, lane);
-                }
-                continue;
+                for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_buf(c), kQk, s, lane);
             }
-            const int d = c - 1, nq = min(rows - d * kC, kC);
-            const float* fac = (const float*)(lds + out_at(d)) + 2 * kC;
-            f32x4 S[NT], U[4];
+        };
+        auto ask_p = [&](int c) {
+            if constexpr (kDirect) {
+                load_p(P, v_buf(c), kT + L::kFac, lane);
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const int at = kT + (2 * kC + 16 * it) * 4;
+                    eg[it] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(v_buf(c), (lane & 15) * 4, at, 0));
+                    cc[it] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(v_buf(c), (lane & 15) * 4, at + kC * 4, 0));
+                }
+            }
+        };
+        ask_p(0);
+        if (n > 1) bring_state(1);
+        if (L::kTStages == 2 && n > 1) bring_t(1);
+        bring_p(0);
+        ask_q(0);
+        wait_vm<kAskQ>();
+        for (int c = 1; c <= n; ++c) {
+            wait_vm<kAskQ + 4>();                      // the next q, and the stores of the outputs, may be out
+            meet();
+            const int d = c - 1, nq = min(rows - d * kC, kC), next = min(c, n - 1);
+            if (L::kTStages == 1 && c < n) bring_t(c);
+            bring_q(d);
+            f32x4 S[NT], U[4], Y[4], O[4];
+#pragma unroll
+            for (int it = 0; it < 4; ++it) U[it] = *(const f32x4*)(hand + (NT + it) * 1024 + lane * 16);
+            if constexpr (!kDirect) {
+#pragma unroll
+                for (int part = 0; part < kSplit; ++part)
+#pragma unroll
+                    for (int f = 0; f < kFrags; ++f) P[part][f] = *(const bf16x8*)(s_p + (part * kFrags + f) * 1024 + lane * 16);
+            }
 #pragma unroll
             for (int t = 0; t < NT; ++t) S[t] = *(const f32x4*)(hand + t * 1024 + lane * 16);
 #pragma unroll
-            for (int it = 0; it < 4; ++it) U[it] = *(const f32x4*)(hand + (NT + it) * 1024 + lane * 16);
+            for (int it = 0; it < 4; ++it) Y[it] = O[it] = f32x4{};
+            // P U, and beside it the first operands of Q S
+            bf16x8 Up[2][kSplit], Sp[2][kSplit];
+            split2(U[0], U[1], Up[0]);
+            __builtin_amdgcn_sched_barrier(0);
+            auto times_p = [&](int s) {
+#pragma unroll
+                for (int m = 0; m < kProducts; ++m)
+#pragma unroll
+                    for (int it = 2 * s; it < 4; ++it) Y[it] = mma(Up[s][first(m)], P[second(m)][frag_of(it, s)], Y[it]);
+            };
+            split2(U[2], U[3], Up[1]);
+            times_p(0);
+            interleave<kProducts * 4, 2>();
+            split2(S[0], S[1], Sp[0]);
+            times_p(1);
+            interleave<kProducts * 2, 4>();
+            float ce[4], co[4];
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                ce[it] = eg[it];
+                co[it] = cc[it];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            ask_p(next);
+            if (!kDirect || L::kTStages == 1) wait_vm<kAskP>();
             meet();
+            __builtin_amdgcn_sched_barrier(0);
+            if (c + 1 < n) bring_state(c + 1);
+            if (L::kTStages == 2 && c + 1 < n) bring_t(c + 1);
+            if (c < n) bring_p(c);
             const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)d * kC) * p.ld_out + h * p.dv,
                                                           (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
-            f32x4 O[4];
+            if constexpr (!kDirect) {
 #pragma unroll
-            for (int it = 0; it < 4; ++it) O[it] = f32x4{};
+                for (int part = 0; part < PA; ++part)
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) q[0][part][it] = qk_piece<NS>(s_q, part, it, 0, lane);
+            }
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
-                bf16x8 Sp[kSplit];
-                split2(S[2 * s], S[2 * s + 1], Sp);
+                if (!kDirect && s + 1 < NS) {
+#pragma unroll
+                    for (int part = 0; part < PA; ++part)
+#pragma unroll
+                        for (int it = 0; it < 4; ++it) q[(s + 1) & (kDirect ? 0 : 1)][part][it] = qk_piece<NS>(s_q, part, it, s + 1, lane);
+                }
+                if (s + 1 < NS) split2(S[2 * (s + 1 < NS ? s + 1 : s)], S[2 * (s + 1 < NS ? s + 1 : s) + 1], Sp[(s + 1) & 1]);
+                auto& qs = q[kDirect ? s : s & 1];
 #pragma unroll
                 for (int m = 0; m < kProducts; ++m) {
                     if (second(m) >= PA) continue;
 #pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(Sp[first(m)], q[s][second(m)][it], O[it]);
+                    for (int it = 0; it < 4; ++it) O[it] = mma(Sp[s & 1][first(m)], qs[second(m)][it], O[it]);
+                }
+                interleave<(PA == 1 ? 12 : 24), (PA == 1 ? 4 : 2)>();
+            }
+            ask_q(next);
+            asm volatile("" ::: "memory");
+            if constexpr (!kDirect) {
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    ce[it] = s_fac[16 * it];
+                    co[it] = s_fac[kC + 16 * it];
                 }
             }
-            if (c < n) ask_q();
-            float cc[4];
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const float eg = fac[16 * it + (lane & 15)];
-                cc[it] = fac[kC + 16 * it + (lane & 15)];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) O[it][r] *= eg;
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                bf16x8 Up[kSplit];
-                split2(U[2 * s], U[2 * s + 1], Up);
-#pragma unroll
-                for (int m = 0; m < kProducts; ++m)
-#pragma unroll
-                    for (int it = 2 * s; it < 4; ++it) O[it] = mma(Up[first(m)], P[second(m)][frag_of(it, s)], O[it]);
-            }
-            if (c < n) load_p(P, v_at(c) + kT, lane);
-            asm volatile("" ::: "memory");
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
                 T o[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(cc[it] * O[it][r]);
+                for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(co[it] * __builtin_fmaf(ce[it], O[it][r], Y[it][r]));
                 if constexpr (sz == 4) {
                     u32x4 w;
                     __builtin_memcpy(&w, o, 16);
@@ -1038,7 +1137,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
     }
     // Steps whose operands are formed beside the products of the others; the others' behind the barrier, beside the first
     // reads
-    constexpr int kEarly = NS / 2;
+    constexpr int kEarly = 1;
     bf16x8 Sp[NS][kSplit];
     auto form = [&](int s0, int s1) {
 #pragma unroll
@@ -1051,8 +1150,8 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
             barrier();
             continue;
         }
-        const char *s_k = lds + (c & 1) * kStage, *s_t = s_k + kQk;
-        const float* fac = (const float*)(s_t + kT - kFacBytes);
+        const char *s_k = lds + (c & 1) * kQk, *s_t = lds + t_at(c);
+        const float* fac = (const float*)(lds + L::kFacAt);
         // What is read from LDS is asked for well in front of its use, as nothing else hides its way: two k steps of k
         // ahead of their products, T behind the last of them, k transposed in front of the products with T
         bf16x8 K[2][PA][4], Tr[kSplit][kFrags];
@@ -1074,7 +1173,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
         // V of this lane's column, tokens 16 it + 4 hh + r
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const char* s_v = s_t + kT + wc * 16 * (int)sizeof(T);
+        const char* s_v = lds + L::kRowsAt + wc * 16 * (int)sizeof(T);
         float v[4][4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
@@ -1096,62 +1195,83 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
                     if (16 * it + 4 * hh + r >= rows - c * kC) v[it][r] = 0.0f;
         }
         __builtin_amdgcn_sched_barrier(0);
-        form(kEarly, NS);
 
-        // K S
+        // K S, and beside it the operands of the next step, at last of the first half of R
         f32x4 R[4];
+        bf16x8 Rp[2][kSplit];
+        constexpr int kN = PA == 1 ? 3 : kProducts;    // products of a value of k and one in parts
 #pragma unroll
         for (int it = 0; it < 4; ++it) R[it] = f32x4{};
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
+        auto times_s = [&](int s, int i0, int i1) {
 #pragma unroll
             for (int m = 0; m < kProducts; ++m) {
                 if (first(m) >= PA) continue;
 #pragma unroll
-                for (int it = 0; it < 4; ++it) R[it] = mma(K[s & 1][first(m)][it], Sp[s][second(m)], R[it]);
+                for (int it = i0; it < i1; ++it) R[it] = mma(K[s & 1][first(m)][it], Sp[s][second(m)], R[it]);
             }
-            if (s + 2 < NS) read_k(s + 2);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int part = 0; part < kSplit; ++part)
-#pragma unroll
-            for (int f = 0; f < kFrags; ++f) Tr[part][f] = *(const bf16x8*)(s_t + (part * kFrags + f) * 1024 + lane * 16);
-        __builtin_amdgcn_sched_barrier(0);
-        // From here tokens 0 .. 31 run ahead of the others: while the one half is in the matrix cores the other is formed.
-        // U = T R, W = e^(G_C - G) U
-        f32x4 U[4], X[4];
-#pragma unroll
-        for (int it = 0; it < 4; ++it) U[it] = f32x4{};
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            bf16x8 Rp[kSplit];
+        };
+        auto part_r = [&](int s) {
 #pragma unroll
             for (int it = 2 * s; it < 2 * s + 2; ++it)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(-bg[it][r], R[it][r], v[it][r]);
-            split2(R[2 * s], R[2 * s + 1], Rp);
+            split2(R[2 * s], R[2 * s + 1], Rp[s]);
+        };
+#pragma unroll
+        for (int s = 0; s + 1 < NS; ++s) {
+            form(s + 1, s + 2);
+            times_s(s, 0, 4);
+            interleave<4 * kN, (PA == 1 ? 4 : 2)>();
+            if (s + 2 < NS) read_k(s + 2);
+        }
+        auto read_t = [&] {
+#pragma unroll
+            for (int part = 0; part < kSplit; ++part)
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f) Tr[part][f] = *(const bf16x8*)(s_t + (part * kFrags + f) * 1024 + lane * 16);
+        };
+        if constexpr (L::kTStages == 2) read_t();
+        times_s(NS - 1, 0, 2);
+        __builtin_amdgcn_sched_barrier(0);
+        times_s(NS - 1, 2, 4);
+        part_r(0);
+        interleave<2 * kN, (PA == 1 ? 8 : 4)>();
+        barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (L::kTStages == 1) read_t();
+        bf16x8 Kt[2][PA][NT];
+        auto read_kt = [&](int s) {
+#pragma unroll
+            for (int part = 0; part < PA; ++part)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) Kt[s][part][t] = kt_piece<NS>(s_k, part, s, t, lane);
+        };
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *(f32x4*)(hand + t * 1024 + lane * 16) = S[t];
+        read_kt(0);
+        __builtin_amdgcn_sched_barrier(0);
+        // U = T R, W = e^(G_C - G) U. Tokens 0 .. 31 run ahead of the others
+        f32x4 U[4];
+        bf16x8 Wp[2][kSplit];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) U[it] = f32x4{};
+        auto times_r = [&](int s) {
 #pragma unroll
             for (int m = 0; m < kProducts; ++m)
 #pragma unroll
-                for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[first(m)][frag_of(it, s)], Rp[second(m)], U[it]);
-        }
-        barrier();
+                for (int it = 2 * s; it < 4; ++it) U[it] = mma(Tr[first(m)][frag_of(it, s)], Rp[s][second(m)], U[it]);
+        };
+        auto part_w = [&](int s) {
+            f32x4 x[2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            *(f32x4*)(hand + t * 1024 + lane * 16) = S[t];
+            for (int i = 0; i < 2; ++i) {
+                *(f32x4*)(hand + (NT + 2 * s + i) * 1024 + lane * 16) = U[2 * s + i];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][r] *= decay;
-        }
-        bf16x8 Kt[2][PA][NT];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int part = 0; part < PA; ++part) Kt[s][part][t] = kt_piece<NS>(s_k, part, s, t, lane);
-        bf16x8 Wp[2][kSplit];
-        // S <- decay S + K^T W
+                for (int r = 0; r < 4; ++r) x[i][r] = U[2 * s + i][r] * wg[2 * s + i][r];
+            }
+            split2(x[0], x[1], Wp[s]);
+        };
+        // S <- e^(G_C) S + K^T W
         auto grow = [&](int s, int t0, int t1) {
 #pragma unroll
             for (int m = 0; m < kProducts; ++m) {
@@ -1160,20 +1280,25 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(2))) vo
                 for (int t = t0; t < t1; ++t) S[t] = mma(Kt[s][first(m)][t], Wp[s][second(m)], S[t]);
             }
         };
+        part_r(1);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int it = 2 * s; it < 2 * s + 2; ++it) {
-                *(f32x4*)(hand + (NT + it) * 1024 + lane * 16) = U[it];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) X[it][r] = U[it][r] * wg[it][r];
-            }
-            split2(X[2 * s], X[2 * s + 1], Wp[s]);
-            if (s == 0) grow(0, 0, NT);
-        }
-        grow(1, 0, 2 * kEarly);
-        grow(1, 2 * kEarly, NT);
-        form(0, kEarly);
+            for (int r = 0; r < 4; ++r) S[t][r] *= decay;
+        times_r(0);
+        interleave<4 * kProducts, 4>();
+        part_w(0);
+        times_r(1);
+        interleave<2 * kProducts, 4>();
+        read_kt(1);
+        part_w(1);
+        grow(0, 0, NT);
+        interleave<NT * kN, (60 + NT * kN - 1) / (NT * kN)>();
+        grow(1, 0, 2);
+        __builtin_amdgcn_sched_barrier(0);
+        grow(1, 2, NT);
+        form(0, 1);
+        interleave<(NT - 2) * kN, (50 + (NT - 2) * kN - 1) / ((NT - 2) * kN)>();
     }
     if (n > 0) {
         meet();
