@@ -589,13 +589,7 @@ template <int M, int V> __device__ __forceinline__ void interleave() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// What delta_main_kernel holds in LDS: a chunk's k, T and factors, in two stages or, where these do not fit, one
 constexpr size_t kLds = 160 * 1024;
-template <typename T, int NS> struct MainLds {
-    static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)t_bytes();
-    static constexpr int kStages = 2 * (kQk + kT) <= (int)kLds ? 2 : 1, kBytes = kStages * (kQk + kT);
-    static_assert(kBytes <= (int)kLds, "pass 2 does not fit into LDS");
-};
 
 // `bytes` (a multiple of 1 KB) from a buffer to LDS, dealt out over the workgroup's waves
 template <int WAVES, int BYTES> __device__ __forceinline__ void dma_pieces(const __amdgpu_buffer_rsrc_t& r, uint32_t from, uint32_t lds, int wave, int lane) {
@@ -638,25 +632,6 @@ template <int NS> __device__ __forceinline__ bf16x8 kt_piece(const char* s_k, in
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(k2[0], k2[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// One value of a row of T, zero (and nothing stored) behind the buffer's end
-template <typename T> struct Raw;
-template <> struct Raw<float> {
-    typedef uint32_t type;
-    static __device__ __forceinline__ type load(const __amdgpu_buffer_rsrc_t& r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0); }
-    static __device__ __forceinline__ void store(const __amdgpu_buffer_rsrc_t& r, uint32_t off, float v) {
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, (int)off, 0, 0);
-    }
-    static __device__ __forceinline__ float value(type v) { return __builtin_bit_cast(float, v); }
-};
-template <> struct Raw<bf16> {
-    typedef uint16_t type;
-    static __device__ __forceinline__ type load(const __amdgpu_buffer_rsrc_t& r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b16(r, (int)off, 0, 0); }
-    static __device__ __forceinline__ void store(const __amdgpu_buffer_rsrc_t& r, uint32_t off, float v) {
-        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (bf16)v), r, (int)off, 0, 0);
-    }
-    static __device__ __forceinline__ float value(type v) { return (float)__builtin_bit_cast(bf16, v); }
-};
-
 // Workgroups are dealt out to the XCDs in turn: item (sequence, q/k head) u runs on XCD u % 8, whose L2 then holds the
 // pieces that its value heads and column blocks share. Grid: 8 rep blocks by every eighth item, in rows of kGridRow.
 constexpr int kGridRow = 1 << 15;
@@ -672,245 +647,37 @@ dim3 work_grid(const DeltaArgs& p, int blocks) {
     return dim3((unsigned)(8 * p.rep * blocks), std::min<unsigned>(rows, kGridRow), (rows + kGridRow - 1) / kGridRow);
 }
 
-// While a chunk is computed the next one's pieces and values are on their way, and the stores of its outputs stay out
-// at the wait in front of the next: every wave waits for its own share, then the barrier stands for the others'. q, in a
-// wave's registers, is asked for again once it is used where all of it fits there (kHold).
-template <typename T, int NS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(1))) void delta_main_kernel(Args a) {
-    constexpr int PA = kParts<T>, NT = 2 * NS;
-    constexpr bool kHold = NS * PA <= 12;
-    using L = MainLds<T, NS>;
-    constexpr int kQk = L::kQk, kT = L::kT;
-    constexpr uint32_t sz = sizeof(T);
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const DeltaArgs& p = a.d;
-    const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const WorkItem it0 = work_item(p, (p.dv + 16 * WAVES - 1) / (16 * WAVES));
-    if (it0.seq >= p.nseq) return;
-    const int seq = it0.seq, h = it0.head, hk = h / p.rep, c0 = (it0.block * WAVES + wave) * 16;   // this wave's columns
-    const bool on = c0 < p.dv;
-    const SeqRows sr = seq_rows(p, seq);
-    const int lo = __builtin_amdgcn_readfirstlane(sr.lo), rows = __builtin_amdgcn_readfirstlane(sr.n);
-    const int slot = p.slot[seq], n = chunks_of(rows), base = rows > 0 ? __builtin_amdgcn_readfirstlane(a.w.base[seq]) : 0;
-    const bool fits = sr.ok && base + n <= a.w.slots, ok = slot >= 0 && slot < p.S;
-    if (h == 0 && it0.block == 0 && tid == 0 && (!fits || !ok))
-        atomicOr(p.status, (fits ? 0 : SSM_STATUS_BAD_SEQLENS) | (ok ? 0 : SSM_STATUS_BAD_SLOT));
-    if (!fits) return;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    auto k_at = [&](int c) { return (L::kStages == 2 ? (c & 1) : 0) * (kQk + kT); };
-    auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
-    auto v_buf = [&](int c) { return buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(), (uint32_t)v_bytes()); };
-    auto bring = [&](int c) {
-        dma_pieces<WAVES, kQk>(qk_buf(c), 0, lds0 + k_at(c), wave, lane);
-        dma_pieces<WAVES, kT>(v_buf(c), 0, lds0 + k_at(c) + kQk, wave, lane);
-    };
-    // V of this lane's column, tokens 16 it + 4 hh + r
-    typename Raw<T>::type raw[4][4];
-    const uint32_t ldv = (uint32_t)p.ld * sz, ldo = (uint32_t)p.ld_out * sz;
-    const uint32_t v0 = on ? (uint32_t)(4 * hh) * ldv + (uint32_t)(c0 + (lane & 15)) * sz : kOffOutOfRange;
-    const uint32_t o0 = (uint32_t)(4 * hh) * ldo + (uint32_t)(c0 + (lane & 15)) * sz;
-    auto bring_v = [&](int c) {
-        const int nq = min(rows - c * kC, kC);
-        const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
-                                                     (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) raw[it][k] = Raw<T>::load(r, v0 + (uint32_t)(16 * it + k) * ldv);
-    };
-    bf16x8 q[kHold ? NS : 1][PA][4], P[kSplit][kFrags];
-    auto bring_q = [&](int c) {
-        if constexpr (kHold) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_buf(c), kQk, s, lane);
-        }
-    };
-    if (n > 0) {
-        bring(0);
-        bring_v(0);
-        bring_q(0);
-    }
-    float* state = p.pool + (((int64_t)(ok ? slot : 0) * p.Hv + h) * p.dv + (on ? c0 + (lane & 15) : 0)) * p.dk + 4 * hh;
-    f32x4 S[NT];
-    const bool carry = ok && p.has_init[seq];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        S[t] = f32x4{};
-        if (carry && on && 16 * t < p.dk) S[t] = *(const f32x4*)(state + 16 * t);
-    }
-    for (int c = 0; c < n; ++c) {
-        // the outputs' 16 stores are the youngest where everything of this chunk was asked for in front of them
-        if (L::kStages == 2 && kHold && on && c > 0) wait_vm<16>();
-        else wait_vm<0>();
-        wait_lgkm0();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        float v[4][4];
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[it][k] = Raw<T>::value(raw[it][k]);
-                asm volatile("" : "+v"(v[it][k]));     // taken here, in front of the loads for the next chunk
-            }
-        if (on) load_p(P, v_buf(c), kT, lane);
-        asm volatile("" ::: "memory");
-        if (L::kStages == 2 && c + 1 < n) {
-            bring(c + 1);
-            bring_v(c + 1);
-        }
-        const char* s_k = lds + k_at(c);
-        const char* s_t = s_k + kQk;
-        if (on) {
-            const int nq = min(rows - c * kC, kC);
-            const float* fac = (const float*)(s_t + kT - kFacBytes);
-            auto tok4 = [&](int k, int it) { return *(const f32x4*)&fac[k * kC + 16 * it + 4 * hh]; };
-
-            // K S, and Q S for the outputs, whose products run while R is formed
-            bf16x8 Sp[NS][kSplit];
-            f32x4 R[4], O[4];
-#pragma unroll
-            for (int it = 0; it < 4; ++it) R[it] = O[it] = f32x4{};
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                split2(S[2 * s], S[2 * s + 1], Sp[s]);
-                bf16x8 k[PA][4];
-#pragma unroll
-                for (int part = 0; part < PA; ++part)
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) k[part][it] = qk_piece<NS>(s_k, part, it, s, lane);
-#pragma unroll
-                for (int m = 0; m < kProducts; ++m) {
-                    if (first(m) >= PA) continue;
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) R[it] = mma(k[first(m)][it], Sp[s][second(m)], R[it]);
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                if constexpr (!kHold) load_q<NS, PA>(q[0], qk_buf(c), kQk, s, lane);
-                auto& qs = q[kHold ? s : 0];
-#pragma unroll
-                for (int m = 0; m < kProducts; ++m) {
-                    if (first(m) >= PA) continue;
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(qs[first(m)][it], Sp[s][second(m)], O[it]);
-                }
-            }
-            if (c + 1 < n) bring_q(c + 1);
-            // R = V - e^G kappa K S, U = T R and W = e^(G_C - G) U
-            f32x4 U[4], W[4];
-            bf16x8 Rp[2][kSplit];
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const f32x4 bg = tok4(0, it);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) R[it][r] = __builtin_fmaf(-bg[r], R[it][r], v[it][r]);
-                U[it] = f32x4{};
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                split2(R[2 * s], R[2 * s + 1], Rp[s]);
-                bf16x8 x[kSplit][4];
-#pragma unroll
-                for (int part = 0; part < kSplit; ++part)
-#pragma unroll
-                    for (int it = 2 * s; it < 4; ++it) x[part][it] = *(const bf16x8*)(s_t + (part * kFrags + frag_of(it, s)) * 1024 + lane * 16);
-#pragma unroll
-                for (int m = 0; m < kProducts; ++m)
-#pragma unroll
-                    for (int it = 2 * s; it < 4; ++it) U[it] = mma(x[first(m)][it], Rp[s][second(m)], U[it]);
-            }
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const f32x4 w = tok4(1, it);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) W[it][r] = U[it][r] * w[r];
-            }
-            // S <- e^(G_C) S + K^T W
-            const float decay = fac[kFacDecay];
-            bf16x8 Wp[2][kSplit];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) split2(W[2 * s], W[2 * s + 1], Wp[s]);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[t][r] *= decay;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    bf16x8 k[PA];
-#pragma unroll
-                    for (int part = 0; part < PA; ++part) k[part] = kt_piece<NS>(s_k, part, s, t, lane);
-#pragma unroll
-                    for (int m = 0; m < kProducts; ++m)
-                        if (first(m) < PA) S[t] = mma(k[first(m)], Wp[s][second(m)], S[t]);
-                }
-            }
-            // O = c (e^G Q S + P U)
-            bf16x8 Up[2][kSplit];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) split2(U[2 * s], U[2 * s + 1], Up[s]);
-            const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)c * kC) * p.ld_out + h * p.dv,
-                                                          (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
-#pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const f32x4 eg = tok4(2, it), cc = tok4(3, it);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) O[it][r] *= eg[r];
-#pragma unroll
-                for (int s = 0; s <= it / 2; ++s)
-#pragma unroll
-                    for (int m = 0; m < kProducts; ++m) O[it] = mma(P[first(m)][frag_of(it, s)], Up[s][second(m)], O[it]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) Raw<T>::store(ro, o0 + (uint32_t)(16 * it + r) * ldo, cc[r] * O[it][r]);
-            }
-        }
-        if (L::kStages == 1 && c + 1 < n) {            // everything is read by now
-            wait_lgkm0();
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            bring(c + 1);
-            bring_v(c + 1);
-        }
-    }
-    if (ok && on) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (16 * t >= p.dk) break;
-            *(f32x4*)(state + 16 * t) = S[t];
-        }
-    }
-}
-
-// As delta_main_kernel, with the outputs by waves of their own: W waves carry the state, W more form the outputs of the
-// chunk before from what the first left in LDS. The chain from chunk to chunk is that much shorter, and both
-// kinds run beside each other.
-// What a workgroup has in LDS. Two barriers a chunk, at its begin and in its middle, tell what is free: in two stages k, which
-// the state needs all the time; in one T (arriving in a chunk's first half, read in its second), the factors and values
-// (read in the first), what is handed over (read in the first, written in the second). Four waves of columns share
-// q (arriving in the first half, read in the second) and the products of queries and keys (read in the first) there too;
-// with two each has them in registers, where there is room for longer rows.
+// A workgroup has W waves that carry the state, 16 columns each, and W that form the outputs of the chunk before from what
+// the first left in LDS: the chain from chunk to chunk is that much shorter, and both kinds run beside each other.
+//
+// What it has in LDS. Two barriers a chunk, at its begin and in its middle, tell what is free. Read by the middle: the
+// factors and values of the chunk, and what is handed over; k and T are needed until the end and have two stages where
+// there is room (else they arrive by the middle). For the outputs, q arrives by the middle and is read behind it, and
+// the products of queries and keys are read by it; where these do not fit, each wave has its own in registers (kDirect). Where
+// values do not fit, so has each wave that carries the state.
 template <typename T, int NS, int W> struct SplitLds {
     static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)(t_bytes() - kFacBytes), kFac = (int)kFacBytes, kP = (int)p_bytes();
-    static constexpr int kRow = 16 * W * (int)sizeof(T), kRows = kC * kRow;   // the workgroup's values of a token, of a chunk
+    static constexpr int kRow = 16 * W * (int)sizeof(T);                      // the workgroup's values of a token
     static constexpr int kHand = (2 * NS + 4) * 1024;                         // S and U of 16 columns
-    // where there is room T has two stages as well
-    static constexpr int kState = 2 * kQk + kT + kFac + kRows + W * kHand;
-    static constexpr bool kDirect = kState + kQk + kFac + kP > (int)kLds;
-    static constexpr int kOne = kState + (kDirect ? 0 : kQk + kFac + kP);
-    static constexpr int kTStages = kOne + kT <= (int)kLds ? 2 : 1, kBytes = kOne + (kTStages - 1) * kT;
-    static constexpr int kTAt = 2 * kQk, kFacAt = kTAt + kTStages * kT, kRowsAt = kFacAt + kFac, kHandAt = kRowsAt + kRows;
+    static constexpr int k_stages(int mode) { return mode < 4 ? 2 : 1; }
+    static constexpr int t_stages(int mode) { return mode == 0 || mode == 2 ? 2 : 1; }
+    static constexpr int row_bytes(int mode) { return mode < 5 ? kC * kRow : 0; }
+    static constexpr int bytes(int mode) {
+        return k_stages(mode) * kQk + t_stages(mode) * kT + kFac + row_bytes(mode) + W * kHand + (mode < 2 ? kQk + kFac + kP : 0);
+    }
+    static constexpr int pick(int mode) { return mode == 6 || bytes(mode) <= (int)kLds ? mode : pick(mode + 1); }
+    static constexpr int kMode = pick(0), kBytes = bytes(kMode), kKStages = k_stages(kMode), kTStages = t_stages(kMode);
+    static constexpr bool kDirect = kMode >= 2, kOwnRows = kMode >= 5;
+    static constexpr int kTAt = kKStages * kQk, kFacAt = kTAt + kTStages * kT, kRowsAt = kFacAt + kFac, kHandAt = kRowsAt + row_bytes(kMode);
     static constexpr int kQAt = kHandAt + W * kHand, kOutFacAt = kQAt + kQk, kPAt = kOutFacAt + kFac;
-    static constexpr bool kFits = kBytes <= (int)kLds && !(kDirect && W > 2);
 };
 
 template <typename T, int NS, int W>
 __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kParts<T> <= 4 ? 2 : 1))) void delta_split_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = SplitLds<T, NS, W>;
-    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kRows = L::kRows, kHand = L::kHand, kP = L::kP;
+    static_assert(L::kMode < 6, "pass 2 does not fit into LDS");
+    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kHand = L::kHand, kP = L::kP;
     constexpr uint32_t sz = sizeof(T);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
@@ -933,32 +700,37 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
     auto qk_buf = [&](int c) { return buffer_rsrc(a.w.qk + ((int64_t)(base + c) * p.Hk + hk) * (2 * kQk), 2 * kQk); };
     auto v_buf = [&](int c) { return buffer_rsrc(a.w.v + ((int64_t)(base + c) * p.Hv + h) * (int64_t)v_bytes(), (uint32_t)v_bytes()); };
     const uint32_t ldv = (uint32_t)p.ld * sz;
-    // All that comes by DMA is asked for by the waves of the outputs: beside a burst of it a wave waits long to issue a load
-    // In front of a chunk: k, its values and factors
-    auto bring_state = [&](int c) {
-        dma_pieces<W, kQk>(qk_buf(c), 0, lds0 + (c & 1) * kQk, wc, lane);
-        dma_pieces<W, L::kFac>(v_buf(c), kT, lds0 + L::kFacAt, wc, lane);
+    auto rows_buf = [&](int c) {                       // this head's values
         const int nq = min(rows - c * kC, kC);
-        const __amdgpu_buffer_rsrc_t r = buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
-                                                     (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
-        constexpr int kPer = 1024 / kRow;              // rows in 1 KB
-        const uint32_t off = (uint32_t)(lane / (kRow / 16)) * ldv + (uint32_t)(it0.block * kRow + lane % (kRow / 16) * 16);
+        return buffer_rsrc((const T*)p.qkv + ((int64_t)lo + (int64_t)c * kC) * p.ld + 2 * p.Hk * p.dk + h * p.dv,
+                           (uint32_t)(nq - 1) * ldv + (uint32_t)p.dv * sz);
+    };
+    // What comes by DMA, a wave's share: k; the factors and values; T. A wave waits long at a burst of these: T in two
+    // stages is asked for by the waves that carry the state, the rest by those of the outputs
+    auto k_at = [&](int c) { return L::kKStages == 2 ? (c & 1) * kQk : 0; };
+    auto bring_k = [&](int c) { dma_pieces<W, kQk>(qk_buf(c), 0, lds0 + k_at(c), wc, lane); };
+    auto bring_state = [&](int c) {
+        dma_pieces<W, L::kFac>(v_buf(c), kT, lds0 + L::kFacAt, wc, lane);
+        if constexpr (!L::kOwnRows) {
+            constexpr int kPer = 1024 / kRow;          // rows in 1 KB
+            const __amdgpu_buffer_rsrc_t r = rows_buf(c);
+            const uint32_t off = (uint32_t)(lane / (kRow / 16)) * ldv + (uint32_t)(it0.block * kRow + lane % (kRow / 16) * 16);
 #pragma unroll
-        for (int i = 0; i < kRows / 1024 / W; ++i) {
-            const uint32_t q = (uint32_t)(wc + W * i);
-            dma16(r, off + q * kPer * ldv, 0, __builtin_amdgcn_readfirstlane(lds0 + L::kRowsAt + q * 1024));
+            for (int i = 0; i < kC / kPer / W; ++i) {
+                const uint32_t q = (uint32_t)(wc + W * i);
+                dma16(r, off + q * kPer * ldv, 0, __builtin_amdgcn_readfirstlane(lds0 + L::kRowsAt + q * 1024));
+            }
         }
     };
-    // At its begin or, in two stages, in front of it: T
     auto t_at = [&](int c) { return L::kTAt + (L::kTStages == 2 ? (c & 1) * kT : 0); };
     auto bring_t = [&](int c) { dma_pieces<W, kT>(v_buf(c), 0, lds0 + t_at(c), wc, lane); };
-    // At its begin: for the outputs of the chunk before, q and the factors
+    // For the outputs, q and the factors again
     auto bring_q = [&](int c) {
         if (L::kDirect) return;
         dma_pieces<W, kQk>(qk_buf(c), kQk, lds0 + L::kQAt, wc, lane);
         dma_pieces<W, L::kFac>(v_buf(c), kT, lds0 + L::kOutFacAt, wc, lane);
     };
-    // In its middle: what its outputs have of queries and keys
+    // and the products of queries and keys
     auto bring_p = [&](int c) {
         if (!L::kDirect) dma_pieces<W, kP>(v_buf(c), kT + L::kFac, lds0 + L::kPAt, wc, lane);
     };
@@ -974,6 +746,23 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
     };
     if (!carries) {
         if (n == 0) return;
+        // behind the middle of chunk c, for the next one and c's outputs; behind the begin of c, for itself and the outputs of
+        // the one before
+        auto bring_next = [&](int c) {
+            if (c + 1 < n) {
+                if (L::kKStages == 2) bring_k(c + 1);
+                bring_state(c + 1);
+            }
+            if (c < n) bring_p(c);
+        };
+        auto bring_now = [&](int c) {
+            if (c < n) {
+                if (L::kKStages == 1) bring_k(c);
+                if (L::kTStages == 1) bring_t(c);
+            }
+            bring_q(c - 1);
+        };
+        bring_k(0);
         bring_state(0);
         bring_t(0);
         wait_vm<0>();
@@ -981,13 +770,10 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
         barrier();
         if (!on) {
             for (int c = 1; c <= n; ++c) {
-                if (c < n) bring_state(c);
-                if (L::kTStages == 2 && c < n) bring_t(c);
-                bring_p(c - 1);
+                bring_next(c - 1);
                 wait_vm<0>();
                 meet();
-                if (L::kTStages == 1 && c < n) bring_t(c);
-                bring_q(c - 1);
+                bring_now(c);
                 wait_vm<0>();
                 barrier();
             }
@@ -999,14 +785,14 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
         const char *s_q = lds + L::kQAt, *s_p = lds + L::kPAt;
         const float* s_fac = (const float*)(lds + L::kOutFacAt) + 2 * kC + (lane & 15);
         constexpr bool kDirect = L::kDirect;
-        constexpr int kAskQ = kDirect ? NS * PA * 4 : 0, kAskP = kDirect ? kSplit * kFrags + 8 : 0;   // loads of them
-        bf16x8 q[kDirect ? NS : 2][PA][4], P[kSplit][kFrags];
+        // steps of q that a wave holds from one chunk to the next, the others two steps in front of their use
+        constexpr int kHold = !kDirect ? 0 : NS * PA <= 12 ? NS : 2, kRing = !kDirect ? 2 : kHold == NS ? NS : 3;
+        constexpr int kAskQ = kHold * PA * 4, kAskP = kDirect ? kSplit * kFrags + 8 : 0;   // loads of them
+        bf16x8 q[kRing][PA][4], P[kSplit][kFrags];
         float eg[4], cc[4];
         auto ask_q = [&](int c) {
-            if constexpr (kDirect) {
 #pragma unroll
-                for (int s = 0; s < NS; ++s) load_q<NS, PA>(q[s], qk_buf(c), kQk, s, lane);
-            }
+            for (int s = 0; s < kHold; ++s) load_q<NS, PA>(q[s], qk_buf(c), kQk, s, lane);
         };
         auto ask_p = [&](int c) {
             if constexpr (kDirect) {
@@ -1020,17 +806,14 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
             }
         };
         ask_p(0);
-        if (n > 1) bring_state(1);
-        if (L::kTStages == 2 && n > 1) bring_t(1);
-        bring_p(0);
+        bring_next(0);
         ask_q(0);
         wait_vm<kAskQ>();
         for (int c = 1; c <= n; ++c) {
             wait_vm<kAskQ + 4>();                      // the next q, and the stores of the outputs, may be out
             meet();
             const int d = c - 1, nq = min(rows - d * kC, kC), next = min(c, n - 1);
-            if (L::kTStages == 1 && c < n) bring_t(c);
-            bring_q(d);
+            bring_now(c);
             f32x4 S[NT], U[4], Y[4], O[4];
 #pragma unroll
             for (int it = 0; it < 4; ++it) U[it] = *(const f32x4*)(hand + (NT + it) * 1024 + lane * 16);
@@ -1071,9 +854,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
             if (!kDirect || L::kTStages == 1) wait_vm<kAskP>();
             meet();
             __builtin_amdgcn_sched_barrier(0);
-            if (c + 1 < n) bring_state(c + 1);
-            if (L::kTStages == 2 && c + 1 < n) bring_t(c + 1);
-            if (c < n) bring_p(c);
+            bring_next(c);
             const __amdgpu_buffer_rsrc_t ro = buffer_rsrc((T*)p.out + ((int64_t)lo + (int64_t)d * kC) * p.ld_out + h * p.dv,
                                                           (uint32_t)(nq - 1) * ldo + (uint32_t)p.dv * sz);
             if constexpr (!kDirect) {
@@ -1088,10 +869,11 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
 #pragma unroll
                     for (int part = 0; part < PA; ++part)
 #pragma unroll
-                        for (int it = 0; it < 4; ++it) q[(s + 1) & (kDirect ? 0 : 1)][part][it] = qk_piece<NS>(s_q, part, it, s + 1, lane);
+                        for (int it = 0; it < 4; ++it) q[(s + 1) % kRing][part][it] = qk_piece<NS>(s_q, part, it, s + 1, lane);
                 }
+                if (kDirect && s + 2 >= kHold && s + 2 < NS) load_q<NS, PA>(q[(s + 2) % kRing], qk_buf(d), kQk, s + 2, lane);
                 if (s + 1 < NS) split2(S[2 * (s + 1 < NS ? s + 1 : s)], S[2 * (s + 1 < NS ? s + 1 : s) + 1], Sp[(s + 1) & 1]);
-                auto& qs = q[kDirect ? s : s & 1];
+                auto& qs = q[s % kRing];
 #pragma unroll
                 for (int m = 0; m < kProducts; ++m) {
                     if (second(m) >= PA) continue;
@@ -1144,13 +926,28 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
         for (int s = s0; s < s1; ++s) split2(S[2 * s], S[2 * s + 1], Sp[s]);
     };
     form(0, kEarly);
+    // the values of this lane's column, where they are not in LDS
+    float own[4][4];
+    auto ask_own = [&](int c) {
+        if constexpr (L::kOwnRows) {
+            static_assert(sz == 4, "float32 rows");
+            const uint32_t at = (uint32_t)(4 * hh) * ldv + (uint32_t)(c0 + (lane & 15)) * sz;
+#pragma unroll
+            for (int it = 0; it < 4; ++it)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) own[it][r] = buffer_load_f32(rows_buf(c), at + (uint32_t)(16 * it + r) * ldv);
+        }
+    };
+    if (n > 0 && on) ask_own(0);
     for (int c = 0; c < n; ++c) {
+        wait_vm<0>();
         meet();
         if (!on) {
             barrier();
+            if (L::kTStages == 2 && c + 1 < n) bring_t(c + 1);
             continue;
         }
-        const char *s_k = lds + (c & 1) * kQk, *s_t = lds + t_at(c);
+        const char *s_k = lds + k_at(c), *s_t = lds + t_at(c);
         const float* fac = (const float*)(lds + L::kFacAt);
         // What is read from LDS is asked for well in front of its use, as nothing else hides its way: two k steps of k
         // ahead of their products, T behind the last of them, k transposed in front of the products with T
@@ -1162,8 +959,11 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
 #pragma unroll
                 for (int it = 0; it < 4; ++it) K[s & 1][part][it] = qk_piece<NS>(s_k, part, it, s, lane);
         };
-        read_k(0);
-        if (NS > 1) read_k(1);
+        auto first_k = [&] {
+            read_k(0);
+            read_k(1);
+        };
+        if constexpr (L::kKStages == 2) first_k();
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
             bg[it] = *(const f32x4*)&fac[16 * it + 4 * hh];
@@ -1177,7 +977,10 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
         float v[4][4];
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
-            if constexpr (PA == 1) {
+            if constexpr (L::kOwnRows) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[it][r] = own[it][r];
+            } else if constexpr (PA == 1) {
                 const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (lds4)(s_v + (16 * it + 4 * hh + ((lane & 15) >> 2)) * kRow + (lane & 3) * 8));
 #pragma unroll
@@ -1195,6 +998,11 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
                     if (16 * it + 4 * hh + r >= rows - c * kC) v[it][r] = 0.0f;
         }
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (L::kKStages == 1) {              // k arrives by now
+            meet();
+            __builtin_amdgcn_sched_barrier(0);
+            first_k();
+        }
 
         // K S, and beside it the operands of the next step, at last of the first half of R
         f32x4 R[4];
@@ -1236,15 +1044,17 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
         times_s(NS - 1, 2, 4);
         part_r(0);
         interleave<2 * kN, (PA == 1 ? 8 : 4)>();
-        barrier();
+        if constexpr (L::kKStages == 2) barrier();
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (L::kTStages == 1) read_t();
-        bf16x8 Kt[2][PA][NT];
-        auto read_kt = [&](int s) {
+        // k transposed, in groups of tiles, for tokens 0 .. 31 and then the others
+        constexpr int kG = PA == 1 ? NT : NT % 4 == 0 ? 4 : 2, kGroups = NT / kG;
+        bf16x8 Kt[2][PA][kG];
+        auto read_kt = [&](int i) {
 #pragma unroll
             for (int part = 0; part < PA; ++part)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) Kt[s][part][t] = kt_piece<NS>(s_k, part, s, t, lane);
+                for (int t = 0; t < kG; ++t) Kt[i & 1][part][t] = kt_piece<NS>(s_k, part, i / kGroups, i % kGroups * kG + t, lane);
         };
 #pragma unroll
         for (int t = 0; t < NT; ++t) *(f32x4*)(hand + t * 1024 + lane * 16) = S[t];
@@ -1271,16 +1081,18 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
             }
             split2(x[0], x[1], Wp[s]);
         };
-        // S <- e^(G_C) S + K^T W
-        auto grow = [&](int s, int t0, int t1) {
+        // S <- e^(G_C) S + K^T W, tiles t0 .. t1 of a group
+        auto grow = [&](int i, int t0, int t1) {
 #pragma unroll
             for (int m = 0; m < kProducts; ++m) {
                 if (first(m) >= PA) continue;
 #pragma unroll
-                for (int t = t0; t < t1; ++t) S[t] = mma(Kt[s][first(m)][t], Wp[s][second(m)], S[t]);
+                for (int t = t0; t < t1; ++t)
+                    S[i % kGroups * kG + t] = mma(Kt[i & 1][first(m)][t], Wp[i / kGroups][second(m)], S[i % kGroups * kG + t]);
             }
         };
         part_r(1);
+        if (c + 1 < n) ask_own(c + 1);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -1290,15 +1102,25 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
         part_w(0);
         times_r(1);
         interleave<2 * kProducts, 4>();
-        read_kt(1);
-        part_w(1);
-        grow(0, 0, NT);
-        interleave<NT * kN, (60 + NT * kN - 1) / (NT * kN)>();
-        grow(1, 0, 2);
+        if (L::kTStages == 2 && c + 1 < n) bring_t(c + 1);
         __builtin_amdgcn_sched_barrier(0);
-        grow(1, 2, NT);
-        form(0, 1);
-        interleave<(NT - 2) * kN, (50 + (NT - 2) * kN - 1) / ((NT - 2) * kN)>();
+#pragma unroll
+        for (int i = 0; i < 2 * kGroups; ++i) {
+            constexpr int kM = kG * kN, kRest = kG > 2 ? kM - 2 * kN : 1;
+            if (i + 1 < 2 * kGroups) read_kt(i + 1);
+            if (i == 0) part_w(1);
+            if (kGroups == 1 && i == 1) {              // the first operands of the next chunk beside the last products
+                grow(1, 0, 2);
+                __builtin_amdgcn_sched_barrier(0);
+                form(0, 1);
+                grow(1, 2, kG);
+                interleave<kRest, (50 + kRest - 1) / kRest>();
+            } else {
+                if (i == kGroups + 1) form(0, 1);
+                grow(i, 0, kG);
+                interleave<kM, (60 + kM - 1) / kM>();
+            }
+        }
     }
     if (n > 0) {
         meet();
@@ -1334,14 +1156,11 @@ DeltaWs layout(char* scratch, bool bf16_act, int Hk, int Hv, int dk, int64_t T, 
     return w;
 }
 
-template <typename T, int NS, int WAVES> void main_launch(const Args& a, hipStream_t s) {
-    const dim3 grid = work_grid(a.d, (a.d.dv + 16 * WAVES - 1) / (16 * WAVES));
+template <typename T, int NS, int W> void split_launch(const Args& a, hipStream_t s) {
+    const dim3 grid = work_grid(a.d, (a.d.dv + 16 * W - 1) / (16 * W));
     // LDS is asked for at the launch: a kernel that the compiler sees to fill it alone has half of its registers where only
     // MFMAs reach them, and a move for every value that goes between the two
-    constexpr bool split = SplitLds<T, NS, WAVES>::kFits;
-    constexpr int bytes = split ? SplitLds<T, NS, WAVES>::kBytes : MainLds<T, NS>::kBytes;
-    if constexpr (split) SSM_LAUNCH((delta_split_kernel<T, NS, WAVES>), grid, dim3(128 * WAVES), bytes, s, a);
-    else SSM_LAUNCH((delta_main_kernel<T, NS, WAVES>), grid, dim3(64 * WAVES), bytes, s, a);
+    SSM_LAUNCH((delta_split_kernel<T, NS, W>), grid, dim3(128 * W), (SplitLds<T, NS, W>::kBytes), s, a);
 }
 template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream_t s) {
     const DeltaArgs& p = a.d;
@@ -1361,8 +1180,14 @@ template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream
     // 190 and 123
     KernelTimer kt("delta.main", s);
     const int64_t pairs = (int64_t)p.nseq * p.Hv, by_two = pairs * ((p.dv + 31) / 32);
-    if (by_two <= 256 || p.dv <= 32) main_launch<T, NS, 2>(a, s);
-    else main_launch<T, NS, 4>(a, s);
+    constexpr bool by_four = sizeof(T) == 2 && SplitLds<T, NS, 4>::kMode < 2;
+    if constexpr (by_four) {
+        if (by_two > 256 && p.dv > 32) {
+            split_launch<T, NS, 4>(a, s);
+            return hipGetLastError();
+        }
+    }
+    split_launch<T, NS, 2>(a, s);
     return hipGetLastError();
 }
 template <typename T> hipError_t prefill_steps(const Args& a, hipStream_t s) {
