@@ -146,3 +146,68 @@ def test_resets_in_many_heads(act, heads):
         b[min(lo + 2, hi - 1):hi] = -10.0
     _hold(L)
 
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("what", ["q", "k", "a", "b", "state"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_value_that_is_not_finite_stays_in_its_sequence(value, what, act):
+    """In a sequence between two others: those and what lies more than 63 rows in front keep their values; for the gates
+    and a state so do the other value heads of the same keys."""
+    L, b, a = _layer(act, (1, 2, 64, 64), [90, 200, 64], init=[1, 1, 1])
+    o, want, sizes = L.oracle()
+    at, pool = 90 + 150, L.pool.copy()
+    if what == "q":
+        L.qkv[at, 7] = value
+    elif what == "k":
+        L.qkv[at, 64 + 7] = value
+    elif what == "state":
+        L.pool[L.slots[1], 1, 5, 9] = value
+        at = 90
+    else:
+        # an infinite decay forgets everything and an infinite write strength is 1: both are ordinary
+        (a if what == "a" else b)[at, 1] = float("nan")
+    out, got_pool, status, _ = _prefill(L)
+    assert status == 0
+    got, tol = f64(out).reshape(o.shape), once_bound(o, sizes, act)
+    rows = np.r_[0:max(at - 63, 90), 290:354]
+    near(got[rows], o[rows], tol[rows], "rows of others")
+    if what in ("a", "b", "state"):
+        near(got[:, 0], o[:, 0], tol[:, 0], "the other head")
+        assert not np.isfinite(got[at, 1]).all()
+    else:
+        assert not np.isfinite(got[at]).any()
+    st, bound = f64(got_pool), state_bound(want, act)
+    others = [L.slots[0], L.slots[2]]
+    near(st[others], want[others], bound[others], "states of others")
+    assert np.isfinite(st[L.slots[1]]).all() == (what == "q")
+    spare = [s for s in range(L.S) if s not in L.slots]
+    assert np.array_equal(st[spare], pool[spare].astype(np.float64))
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("n,overlap", [(3, False), (64, True), (300, True), (300, False)])
+def test_nothing_is_written_behind_the_workspace(n, overlap, act):
+    """A workspace of the exact size in front of a filled region. Where every second sequence names all rows of the call
+    there are far more chunks than a call of that many rows has, laid out by the first launch (up to 256 sequences) or
+    by one of its own."""
+    from paper_2602_21144_amd import binding as B
+    T = 640
+    L = Layer(torch, (1, 2, 32, 16), [T] + [0] * (n - 1) if overlap else [T // n] * n, act, seed=13)
+    dd = L.desc(B)
+    meta = B.SeqMeta(L.cu, L.slots, L.init, L.S)
+    if overlap:
+        meta.cu.copy_(torch.tensor([0, T] * (n // 2) + [0], dtype=torch.int32))
+    need = B.delta_workspace_bytes(dd, L.T, n)
+    buf = torch.full((need + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda")
+    ws = buf[:need]
+    ws.zero_()
+    proj, pool = L.dev(L.proj), L.dev(L.pool, False)
+    _, b, a = L.columns(proj)
+    out = torch.empty(L.T, L.wide, dtype=L.tdt, device="cuda")
+    B.ssm_delta_prefill(dd, L.gates(B, dd), L.dev(L.qkv), a, b, meta, pool, out, ws)
+    torch.cuda.synchronize()
+    assert (buf[need:] == 0xA5).all()
+    assert bool(B.take_status(ws) & B.SSM_STATUS_BAD_SEQLENS) == overlap
+    others = [s for s in range(L.S) if s not in L.slots]
+    assert np.array_equal(f64(pool)[others], L.pool[others].astype(np.float64))
