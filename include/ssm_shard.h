@@ -539,7 +539,8 @@ int ssm_attn_decode(const ssm_attn_desc_t* desc, const void* q, int64_t ld_q, co
  * Requirements: qk_heads divides v_heads, v_heads at most 128; qk_dim a multiple of 16 up to 256,
  * v_dim a multiple of 16 up to 512; scale finite and positive; norm_eps positive; beta_max in (0, 2];
  * a call has up to 2^22 rows and 2^15 sequences. The rule is stable for keys of length up to
- * sqrt(2 / beta): with qk_norm 0 that is the caller's. Squares of q and k have to stay in float32.
+ * sqrt(2 / beta): with qk_norm 0 that is the caller's. Squares of q and k have to stay in float32,
+ * values of v and of the states below 2^108 in magnitude.
  * State cache: ssm_pool [num_slots][v_heads][v_dim][qk_dim] float32.
  * A value that is not finite reaches what the formulas say; in prompts also up to 63 rows of its
  * sequence in front of its own, in the heads that read it. */
@@ -574,7 +575,11 @@ typedef struct ssm_gated_norm {
 } ssm_gated_norm_t;
 int ssm_delta_check_desc(const ssm_delta_desc_t* desc);
 /* One workspace serves both operators for calls of up to max_tokens rows and max_seqs sequences.
- * Initialise it and read its status as for the mixer's; calls that share it must not overlap in time. */
+ * Initialise it and read its status as for the mixer's; calls that share it must not overlap in time.
+ * It holds the operands of all chunks of a call: for every 64 tokens or part of them that a sequence has, 37 KB a value
+ * head and, with qk_dim up to 64, 96, 128, 192 or 256, 16, 24, 32, 48 or 64 KB a query/key head (three times that in
+ * float32): 13 KB a token for 16 bf16 heads of 128 over 8. A long prompt can come in several calls, each from
+ * the state that the one before stored. */
 int ssm_delta_workspace_bytes(const ssm_delta_desc_t* desc, int64_t max_tokens, int32_t max_seqs, size_t* bytes);
 /* Packed prompts: qkv [T][ld_qkv] act, columns [q heads | k heads | v heads]; a and b [T][ld_ab] act, v_heads
  * columns each (any stride of at least v_heads, aligned to their type: columns of the projection); out [T][ld_out]

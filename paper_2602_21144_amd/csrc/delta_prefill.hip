@@ -5,18 +5,18 @@
 //   R = V - kappa e^G (K S),  U = T R,  O = c e^G (Q S) + (c_i e^(Gi - Gj) q_i . k_j)_{j <= i} U
 //   S <- e^(G_C) S + K^T (e^(G_C - Gj) U)
 // (c: the queries' lengths and the output's scale.) Pass 1 (delta_chunk_kernel) has a workgroup per chunk and q/k head:
-// T and the masked products of queries and keys of its value heads. Pass 2 walks a sequence's chunks with the state in
-// accumulators: columns of S need nothing of each other, so a wave owns 16 of them and waits for no sum of another.
-// delta_split_kernel gives the outputs waves of their own where its LDS suffices, delta_main_kernel has one kind of wave.
-// Longer chunks than 64 tokens would have fewer steps in the chain, but more work in the inversion and in the products
-// with T; shorter ones more steps, each with the same waits.
+// T and the masked products of queries and keys of its value heads. Pass 2 (delta_split_kernel) walks a sequence's chunks with
+// the state in accumulators: columns of S need nothing of each other, so a wave owns 16 of them and waits for no sum of
+// another; the outputs are formed by waves of their own. Longer chunks than 64 tokens would have fewer steps in the
+// chain, but more work in the inversion and in the products with T; shorter ones more steps, each with the same waits.
 //
 // Operands are bf16, sums float32. A float32 value is the sum of three bf16 ones, each the rounding of what those in front
-// of it leave: 8 bits and a sign each, float32's range, so nothing has a scale that another value could set. Of
+// of it leave: 8 bits and a sign each, in float32's range, so nothing has a scale that another value could set. Of
 // the products of two such values the six largest are formed; the others are below 2^-26 of the whole. q, k and v in
-// bf16 are one value. f16 pairs with a scale by row or column were faster (a product of two is three MFMAs, and
-// T and the products with queries take two thirds of the bytes), but what lay far below the largest value of a
-// scale lost its bits: tokens whose write gate is nearly closed, all that follows a reset.
+// bf16 are one value. f16 pairs with a scale by row or column are faster (three MFMAs for a product of two, three vector
+// instructions to split a pair of values for eleven, a third less to write and read: prompts of 16 bf16 heads of 128 x 128
+// took 53 us for 59, 142 for 185 and 643 for 860), but what lies far below the largest value of its scale loses its bits:
+// tokens whose write gate is nearly closed, all that follows a reset.
 #include <algorithm>
 
 #include "gate.h"
@@ -242,7 +242,9 @@ template <int NS> __device__ __forceinline__ bf16x8 qk_piece(const char* lds, in
 
 // One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves. What bounds it is the
 // chain of its phases (rows to LDS, products, inversion by blocks, output), half of whose time is waits, and with many
-// chunks HBM. A chunk of its own per value head read and multiplied the rows twice.
+// chunks HBM: 8 prompts of 2048 tokens, 16 bf16 value heads of 128 over 8, 64 us for 217 MB written, 4 of 16384 tokens,
+// 868 MB, 219 us; three workgroups to a compute unit for two took the first from 63 to 55 when it wrote 147 MB. A chunk of
+// its own per value head read and multiplied the rows twice (then 274 us for 222 of the second).
 // HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
 // is not stored.
 template <typename T, int NS, int HB>
@@ -649,6 +651,14 @@ dim3 work_grid(const DeltaArgs& p, int blocks) {
 
 // A workgroup has W waves that carry the state, 16 columns each, and W that form the outputs of the chunk before from what
 // the first left in LDS: the chain from chunk to chunk is that much shorter, and both kinds run beside each other.
+// 317, 1130 and 601 tokens, 16 heads of 128 x 128: 45.6 us in bf16 (2.5 a chunk of the longest), 68 in float32 (3.8). Bound
+// by a chunk's chain: a wave that carries the state has 132 MFMAs and 420 vector instructions, which share its issue port (8
+// and 4 cycles each), and waits for what it reads from LDS in between; with four waves of columns by those of the outputs
+// beside them on the same SIMD: 8 prompts of 2048 tokens 140 us (4.4 a chunk), the matrix pipe 36% busy, vector
+// instructions 40%, LDS 32%. Each stretch of a chunk asks the compiler for vector instructions between its MFMAs that are
+// for those of the next. Tried: taking a half of a pair off by a dot product with (-1, 0), one instruction for two, which is
+// exact too, but runs in the matrix pipe (float32 76 us for 68); DMA spread over the products instead of in bursts (173 us
+// for 158 of the 8 prompts); a higher priority for either kind of wave (nothing).
 //
 // What it has in LDS. Two barriers a chunk, at its begin and in its middle, tell what is free. Read by the middle: the
 // factors and values of the chunk, and what is handed over; k and T are needed until the end and have two stages where
@@ -1174,10 +1184,9 @@ template <typename T, int NS> hipError_t prefill_launch(const Args& a, hipStream
         if (p.rep == 1) SSM_LAUNCH((delta_chunk_kernel<T, NS, 1>), grid, dim3(256), 0, s, a);
         else SSM_LAUNCH((delta_chunk_kernel<T, NS, 2>), grid, dim3(256), 0, s, a);
     }
-    // Two waves of columns to a workgroup where all of these run at once, a compute unit each; else four, which share what
-    // they read. 16 heads of 128 x 128 over prompts of 1024 tokens, whole call: 4 prompts (256 workgroups of two) 53.5 us
-    // by twos and 61 by fours, 6 prompts (384) 92 and 72, 24 prompts 285 and 232; float32 4 prompts 103 and 108, 6
-    // 190 and 123
+    // Two waves of columns to a workgroup where all of these run at once, a compute unit each; else in bf16 four, which share
+    // what they read (float32 stages leave no LDS for four). 16 heads of 128 x 128 over prompts of 1024 tokens, whole call:
+    // 4 prompts (256 workgroups of two) 63 us by twos and 80 by fours, 6 prompts 96 and 81, 24 prompts 360 and 285
     KernelTimer kt("delta.main", s);
     const int64_t pairs = (int64_t)p.nseq * p.Hv, by_two = pairs * ((p.dv + 31) / 32);
     constexpr bool by_four = sizeof(T) == 2 && SplitLds<T, NS, 4>::kMode < 2;
