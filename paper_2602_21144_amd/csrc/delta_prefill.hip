@@ -668,7 +668,10 @@ dim3 work_grid(const DeltaArgs& p, int blocks) {
 template <typename T, int NS, int W> struct SplitLds {
     static constexpr int kQk = (int)qk_bytes(NS, kParts<T>), kT = (int)(t_bytes() - kFacBytes), kFac = (int)kFacBytes, kP = (int)p_bytes();
     static constexpr int kRow = 16 * W * (int)sizeof(T);                      // the workgroup's values of a token
-    static constexpr int kHand = (2 * NS + 4) * 1024;                         // S and U of 16 columns
+    // S and U of 16 columns; with four waves of columns, where the waves of the outputs are late, S as operands, which they
+    // then need not form (8 prompts of 2048 tokens 177 us for 184; two waves of columns lose by it, 62.4 us for 59.5)
+    static constexpr bool kFormed = W == 4;
+    static constexpr int kHandS = (kFormed ? kSplit * NS : 2 * NS) * 1024, kHand = kHandS + 4 * 1024;
     static constexpr int k_stages(int mode) { return mode < 4 ? 2 : 1; }
     static constexpr int t_stages(int mode) { return mode == 0 || mode == 2 ? 2 : 1; }
     static constexpr int row_bytes(int mode) { return mode < 5 ? kC * kRow : 0; }
@@ -687,7 +690,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = SplitLds<T, NS, W>;
     static_assert(L::kMode < 6, "pass 2 does not fit into LDS");
-    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kHand = L::kHand, kP = L::kP;
+    constexpr int kQk = L::kQk, kT = L::kT, kRow = L::kRow, kHandS = L::kHandS, kHand = L::kHand, kP = L::kP;
     constexpr uint32_t sz = sizeof(T);
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const DeltaArgs& p = a.d;
@@ -825,8 +828,9 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
             const int d = c - 1, nq = min(rows - d * kC, kC), next = min(c, n - 1);
             bring_now(c);
             f32x4 S[NT], U[4], Y[4], O[4];
+            bf16x8 Sp[L::kFormed ? NS : 2][kSplit];
 #pragma unroll
-            for (int it = 0; it < 4; ++it) U[it] = *(const f32x4*)(hand + (NT + it) * 1024 + lane * 16);
+            for (int it = 0; it < 4; ++it) U[it] = *(const f32x4*)(hand + kHandS + it * 1024 + lane * 16);
             if constexpr (!kDirect) {
 #pragma unroll
                 for (int part = 0; part < kSplit; ++part)
@@ -834,11 +838,14 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
                     for (int f = 0; f < kFrags; ++f) P[part][f] = *(const bf16x8*)(s_p + (part * kFrags + f) * 1024 + lane * 16);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t] = *(const f32x4*)(hand + t * 1024 + lane * 16);
+            for (int i = 0; i < kHandS / 1024; ++i) {
+                if constexpr (L::kFormed) Sp[i / kSplit][i % kSplit] = *(const bf16x8*)(hand + i * 1024 + lane * 16);
+                else S[i] = *(const f32x4*)(hand + i * 1024 + lane * 16);
+            }
 #pragma unroll
             for (int it = 0; it < 4; ++it) Y[it] = O[it] = f32x4{};
             // P U, and beside it the first operands of Q S
-            bf16x8 Up[2][kSplit], Sp[2][kSplit];
+            bf16x8 Up[2][kSplit];
             split2(U[0], U[1], Up[0]);
             __builtin_amdgcn_sched_barrier(0);
             auto times_p = [&](int s) {
@@ -850,7 +857,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
             split2(U[2], U[3], Up[1]);
             times_p(0);
             interleave<kProducts * 4, 2>();
-            split2(S[0], S[1], Sp[0]);
+            if constexpr (!L::kFormed) split2(S[0], S[1], Sp[0]);
             times_p(1);
             interleave<kProducts * 2, 4>();
             float ce[4], co[4];
@@ -882,13 +889,16 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
                         for (int it = 0; it < 4; ++it) q[(s + 1) % kRing][part][it] = qk_piece<NS>(s_q, part, it, s + 1, lane);
                 }
                 if (kDirect && s + 2 >= kHold && s + 2 < NS) load_q<NS, PA>(q[(s + 2) % kRing], qk_buf(d), kQk, s + 2, lane);
-                if (s + 1 < NS) split2(S[2 * (s + 1 < NS ? s + 1 : s)], S[2 * (s + 1 < NS ? s + 1 : s) + 1], Sp[(s + 1) & 1]);
+                constexpr int kS = L::kFormed ? NS : 2;   // steps of S that there is room for
+                if constexpr (!L::kFormed) {
+                    if (s + 1 < NS) split2(S[2 * (s + 1 < NS ? s + 1 : s)], S[2 * (s + 1 < NS ? s + 1 : s) + 1], Sp[(s + 1) % kS]);
+                }
                 auto& qs = q[s % kRing];
 #pragma unroll
                 for (int m = 0; m < kProducts; ++m) {
                     if (second(m) >= PA) continue;
 #pragma unroll
-                    for (int it = 0; it < 4; ++it) O[it] = mma(Sp[s & 1][first(m)], qs[second(m)][it], O[it]);
+                    for (int it = 0; it < 4; ++it) O[it] = mma(Sp[s % kS][first(m)], qs[second(m)][it], O[it]);
                 }
                 interleave<(PA == 1 ? 12 : 24), (PA == 1 ? 4 : 2)>();
             }
@@ -1067,7 +1077,10 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
                 for (int t = 0; t < kG; ++t) Kt[i & 1][part][t] = kt_piece<NS>(s_k, part, i / kGroups, i % kGroups * kG + t, lane);
         };
 #pragma unroll
-        for (int t = 0; t < NT; ++t) *(f32x4*)(hand + t * 1024 + lane * 16) = S[t];
+        for (int i = 0; i < kHandS / 1024; ++i) {
+            if constexpr (L::kFormed) *(bf16x8*)(hand + i * 1024 + lane * 16) = Sp[i / kSplit][i % kSplit];
+            else *(f32x4*)(hand + i * 1024 + lane * 16) = S[i];
+        }
         read_kt(0);
         __builtin_amdgcn_sched_barrier(0);
         // U = T R, W = e^(G_C - G) U. Tokens 0 .. 31 run ahead of the others
@@ -1085,7 +1098,7 @@ __global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kP
             f32x4 x[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                *(f32x4*)(hand + (NT + 2 * s + i) * 1024 + lane * 16) = U[2 * s + i];
+                *(f32x4*)(hand + kHandS + (2 * s + i) * 1024 + lane * 16) = U[2 * s + i];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[i][r] = U[2 * s + i][r] * wg[2 * s + i][r];
             }
