@@ -242,8 +242,8 @@ template <int NS> __device__ __forceinline__ bf16x8 qk_piece(const char* lds, in
 
 // One workgroup per chunk and q/k head; its value heads two at a time, each inverted by two waves. What bounds it is the
 // chain of its phases (rows to LDS, products, inversion by blocks, output), half of whose time is waits, and with many
-// chunks HBM: 8 prompts of 2048 tokens, 16 bf16 value heads of 128 over 8, 64 us for 217 MB written, 4 of 16384 tokens,
-// 868 MB, 219 us; three workgroups to a compute unit for two took the first from 63 to 55 when it wrote 147 MB. A chunk of
+// chunks HBM: 8 prompts of 2048 tokens, 16 bf16 value heads of 128 over 8, 60 us for 222 MB written, 4 of 16384 tokens,
+// 889 MB, 222 us; three workgroups to a compute unit for two took the first from 63 to 55 when it wrote 147 MB. A chunk of
 // its own per value head read and multiplied the rows twice (then 274 us for 222 of the second).
 // HB: value heads a pass, 1 where a q/k head has one. What a pass of two computes for a second head that is not there
 // is not stored.
@@ -685,8 +685,10 @@ template <typename T, int NS, int W> struct SplitLds {
     static constexpr int kQAt = kHandAt + W * kHand, kOutFacAt = kQAt + kQk, kPAt = kOutFacAt + kFac;
 };
 
+// Where 256 registers are enough the kernel is held to them: beyond, the compiler keeps half where only MFMAs reach them (391
+// float32 tokens, heads of 64: 30.7 us for 32.4, bf16 heads of 192: 72.8 for 77.7)
 template <typename T, int NS, int W>
-__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kParts<T> <= 4 ? 2 : 1))) void delta_split_kernel(Args a) {
+__global__ __launch_bounds__(128 * W) __attribute__((amdgpu_waves_per_eu(NS * kParts<T> <= 6 ? 2 : 1))) void delta_split_kernel(Args a) {
     constexpr int PA = kParts<T>, NT = 2 * NS;
     using L = SplitLds<T, NS, W>;
     static_assert(L::kMode < 6, "pass 2 does not fit into LDS");

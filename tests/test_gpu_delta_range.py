@@ -23,7 +23,8 @@ SHAPES = [("bf16", (1, 2, 64, 64)), ("bf16", (2, 2, 128, 128)), ("bf16", (1, 1, 
 
 def once_bound(want, sizes, act):
     """What out_bound gives float32 outputs, for both types: sums, states and their operands have float32's precision
-    (128 times 2^-24 of what is summed, see there), and one rounding of the value to its type stands behind them."""
+    (128 times 2^-24 of what is summed, see there), and one rounding of the value to its type stands behind them. What
+    out_bound leaves bf16 beyond that, for operands of 11 bits, none of them needs."""
     return (2.0 ** -8 if act == "bf16" else 2.0 ** -24) * np.abs(want) + 128 * 2.0 ** -24 * sizes + 1e-30
 
 
